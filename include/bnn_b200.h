@@ -48,7 +48,8 @@ enum {
     BNN_ERR_TOO_LARGE = -6      /* bnn_mlp_forward_noalloc: the problem does not fit the built-in scratch */
 };
 
-enum { BNN_F32 = 0, BNN_F16 = 1, BNN_I8 = 2 }; /* element type of bnn_pack_signs' source */
+enum { BNN_F32 = 0, BNN_F16 = 1, BNN_I8 = 2, /* element types of bnn_pack_signs' source */
+       BNN_BF16 = 3 };                        /* real-valued operators only */
 
 typedef struct bnn_ctx bnn_ctx;
 
@@ -362,6 +363,124 @@ BNN_API int bnn_mlp_forward_noalloc(bnn_ctx *ctx, const bnn_mlp_desc *m, const u
  */
 BNN_API int bnn_fold_batchnorm(const float *gamma, const float *beta, const float *mean, const float *var, double eps,
                        int64_t n, int64_t x_max, int32_t *thr, uint32_t *flip);
+
+/* ---------------------------------------------------------------------------------------------
+ * Real-valued feed-forward sublayer: what stays in 16 (or 32) bits around the binary products of a deep network --
+ * dense layers, gated projections, the norms and gates that tie a block to its residual stream, and dropout.
+ *
+ * Conventions of these calls, beyond the ones at the top
+ *  - Matrices are row-major with a leading dimension in ELEMENTS (ld >= columns; any value, odd ones too); base pointers
+ *    are aligned to their element (BNN_ERR_ALIGNMENT otherwise).  Vectors are contiguous.
+ *  - `dtype` is the type of every matrix and vector of a call unless it says float: BNN_BF16 or BNN_F16 for the products,
+ *    also BNN_F32 for norms and dropout.  Sums, statistics and activations are computed in float32 and every result is
+ *    rounded once to `dtype`.
+ *  - Where a call needs scratch, bnn_*_workspace_bytes says how much of the context's workspace it takes
+ *    (BNN_ERR_WORKSPACE if less is lent).  Matrix products read their operands in 16-byte groups: an operand whose base
+ *    or leading dimension is not a multiple of 16 bytes is first copied to the workspace, so `aligned` = 0 asks for room
+ *    for those copies; `aligned` = 1 promises that x, dy (dh) and the weights all satisfy the rule.
+ *  - An output may be the very matrix that a call adds to it (y = residual, dx = dy: same pointer, same ld) but must not
+ *    overlap any other input.  */
+
+/* Activations.  htanh(z) = max(-1, min(1, z)); its slope 1 for |z| <= 1, else 0, is the straight-through estimator of Sign
+ * (Section 1.3, Eq. 4-5). */
+enum { BNN_ACT_NONE = 0, BNN_ACT_RELU = 1, BNN_ACT_GELU = 2 /* z Phi(z) */, BNN_ACT_GELU_TANH = 3 /* its tanh form */,
+       BNN_ACT_SILU = 4, BNN_ACT_SIGMOID = 5, BNN_ACT_HTANH = 6 };
+
+/* Dense layer  z = x W^T + bias,  y = residual + act(z):  W is N x K (one row per output), bias N values or NULL. */
+typedef struct {
+    int32_t dtype;  /* BNN_BF16 or BNN_F16 */
+    int32_t act;
+    int64_t K, N;
+    const void *W;  /* N x K (device) */
+    int64_t ldw;
+    const void *bias; /* N or NULL (device) */
+} bnn_linear_desc;
+
+/* x M x K, residual M x N or NULL, y M x N.  pre: NULL, or M x N float32 (leading dimension ldp) that receives z for
+ * bnn_linear_backward.  K = 0 gives z = bias. */
+BNN_API size_t bnn_linear_workspace_bytes(const bnn_linear_desc *layer, int64_t M, int backward, int aligned);
+BNN_API int bnn_linear(bnn_ctx *ctx, const bnn_linear_desc *layer, const void *x, int64_t ldx, int64_t M, const void *residual,
+                       int64_t ldr, void *y, int64_t ldy, float *pre, int64_t ldp);
+/* Gradients of bnn_linear from dy (M x N, the gradient of y; the residual's gradient is dy itself):
+ *   dz = dy * act'(z) (rounded to dtype, the operand of both products);  dx = dz W,  dW = dz^T x,  dbias = column sums of dz.
+ * pre: z as bnn_linear left it, or NULL: z is computed again (one more product, no M x N float32 kept).  dx (M x K),
+ * dW (N x K, ld lddw) and dbias (N) may each be NULL if not wanted.  M = 0 gives zero dW and dbias. */
+BNN_API int bnn_linear_backward(bnn_ctx *ctx, const bnn_linear_desc *layer, const void *dy, int64_t lddy, const void *x, int64_t ldx,
+                                int64_t M, const float *pre, int64_t ldp, void *dx, int64_t lddx, void *dW, int64_t lddw,
+                                void *dbias);
+
+/* Gated projections  h = act(x Wg^T) * (x Wu^T):  both products, the activation and the product in one kernel. */
+typedef struct {
+    int32_t dtype; /* BNN_BF16 or BNN_F16 */
+    int32_t act;
+    int64_t K, N;  /* inputs, hidden units */
+    const void *Wg; /* N x K (device): the activated half */
+    int64_t ldg;
+    const void *Wu; /* N x K (device) */
+    int64_t ldu;
+} bnn_gated_desc;
+
+/* x M x K, h M x N.  pre: NULL, or float32 [2][M][ldp]: receives g = x Wg^T and u = x Wu^T for bnn_gated_backward. */
+BNN_API size_t bnn_gated_workspace_bytes(const bnn_gated_desc *layer, int64_t M, int backward, int aligned);
+BNN_API int bnn_gated(bnn_ctx *ctx, const bnn_gated_desc *layer, const void *x, int64_t ldx, int64_t M, void *h, int64_t ldh,
+                      float *pre, int64_t ldp);
+/* Gradients from dh (M x N):  dg = dh * u * act'(g), du = dh * act(g) (rounded to dtype);  dx = dg Wg + du Wu,
+ * dWg = dg^T x, dWu = du^T x.  pre: as bnn_gated left it, or NULL: g and u are computed again.  dx, dWg, dWu may be NULL. */
+BNN_API int bnn_gated_backward(bnn_ctx *ctx, const bnn_gated_desc *layer, const void *dh, int64_t lddh, const void *x, int64_t ldx,
+                               int64_t M, const float *pre, int64_t ldp, void *dx, int64_t lddx, void *dWg, int64_t lddg,
+                               void *dWu, int64_t lddu);
+
+/* Norms around a block, with its gate and the residual scale, in one pass over the rows:
+ *   p      = post ? Norm(block; post_weight, post_shift) : block
+ *   stream = alpha * x + gate * p
+ *   normed = pre ? Norm(stream; pre_weight, pre_shift) : not computed    (the next block's input, from the unrounded stream)
+ *   Norm(v; w, c) = (v - mean) / sqrt(variance + eps) * w + c  (BNN_NORM_LAYER),   v / sqrt(mean square + eps) * w + c
+ *   (BNN_NORM_RMS);  w NULL stands for 1, c NULL for 0.
+ * gate: NULL (1), or ceil(M / rows_per_gate) x D: row m of the stream uses gate row m / rows_per_gate (one gate row for all
+ * rows: rows_per_gate >= M).  1 <= D <= 32768. */
+enum { BNN_NORM_RMS = 0, BNN_NORM_LAYER = 1 };
+typedef struct {
+    int32_t dtype; /* BNN_BF16, BNN_F16 or BNN_F32 */
+    int32_t kind;
+    int64_t D;
+    float eps, alpha;
+    int32_t post, pre; /* which norms are applied: 0 or 1 */
+    const void *post_weight, *post_shift, *pre_weight, *pre_shift; /* D values each or NULL (device) */
+    const void *gate;                                              /* device or NULL */
+    int64_t ld_gate, rows_per_gate;
+} bnn_block_norm_desc;
+
+/* block NULL: no block has run yet, stream = alpha * x (post must be 0 and gate NULL).  stream and normed may be NULL if not
+ * wanted (normed must be NULL when pre is 0).  stats: NULL, or M x 4 float32 (mean and reciprocal deviation of the block's row,
+ * then of the stream's) for the backward call. */
+BNN_API int bnn_block_norm(bnn_ctx *ctx, const bnn_block_norm_desc *norm, const void *x, int64_t ldx, const void *block, int64_t ldb,
+                           int64_t M, void *stream, int64_t lds, void *normed, int64_t ldn, float *stats);
+
+/* What bnn_block_norm_backward writes; any pointer may be NULL if not wanted.  dpost_*, dpre_* hold D values, dgate as many rows
+ * as the gate.  Sums over rows are taken in float32 in a fixed order: the same call gives the same bits. */
+typedef struct {
+    void *dx;
+    int64_t lddx;
+    void *dblock;
+    int64_t lddb;
+    void *dpost_weight, *dpost_shift, *dpre_weight, *dpre_shift;
+    void *dgate;
+    int64_t ld_dgate;
+} bnn_block_norm_grads;
+/* dstream (gradient of the stream from later in the network) and dnormed may each be NULL (zero); x, block and stats as given to
+ * and left by bnn_block_norm.  M = 0 gives zero sums. */
+BNN_API size_t bnn_block_norm_workspace_bytes(const bnn_block_norm_desc *norm, int64_t M);
+BNN_API int bnn_block_norm_backward(bnn_ctx *ctx, const bnn_block_norm_desc *norm, const void *dstream, int64_t ldds, const void *dnormed,
+                                    int64_t lddn, const void *x, int64_t ldx, const void *block, int64_t ldb, const float *stats,
+                                    int64_t M, const bnn_block_norm_grads *grads);
+
+/* Dropout whose mask is never stored:  y = residual + (kept ? x / (1 - p) : 0).  Element e = row * cols + col is kept when word
+ * e % 4 of Philox4x32-10 (Salmon, Moraes, Dror, Shaw, 2011) at counter (e / 4 low, e / 4 high, offset low, offset high), key
+ * (seed low, seed high) is >= p * 2^32 rounded to the nearest whole number.  The same call on dy without a residual is the
+ * backward pass.  The mask depends on rows, cols, seed and offset only, not on strides or alignment.  Dropped elements of x are
+ * not looked at: NaN or infinity there does not reach y.  0 <= p <= 1; residual may be NULL; y may be x. */
+BNN_API int bnn_dropout(bnn_ctx *ctx, int dtype, const void *x, int64_t ldx, const void *residual, int64_t ldr, void *y, int64_t ldy,
+                        int64_t rows, int64_t cols, double p, uint64_t seed, uint64_t offset);
 
 #ifdef __cplusplus
 }

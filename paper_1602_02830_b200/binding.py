@@ -9,14 +9,18 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, Structure, c_double, c_int, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import POINTER, Structure, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_uint64, c_void_p
 
 import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libbnn_b200.so")
 
-BNN_F32, BNN_F16, BNN_I8 = 0, 1, 2
+BNN_F32, BNN_F16, BNN_I8, BNN_BF16 = 0, 1, 2, 3
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4, "sigmoid": 5, "htanh": 6}
+NORMS = {"rms": 0, "layer": 1}
+_REAL_TYPES = {torch.float32: BNN_F32, torch.float16: BNN_F16, torch.bfloat16: BNN_BF16}
+_PRODUCT_TYPES = (torch.float16, torch.bfloat16)
 VARIANT_AUTO, VARIANT_PLAIN, VARIANT_CSA = 0, 1, 2
 ENGINE_AUTO, ENGINE_POPC, ENGINE_TENSOR = 0, 1, 2
 
@@ -31,6 +35,8 @@ EXPORTS = (
     "bnn_expanded_bytes_f4", "bnn_expand_signs_f4", "bnn_binary_dense_expanded", "bnn_set_wait_limit_ns",
     "bnn_debug_drop_loads", "bnn_debug_ring_position", "bnn_set_conv_form", "bnn_measure_pipe_rates", "bnn_last_tensor_kernel", "bnn_last_tensor_kernel_clock", "bnn_set_conv_filter_repetition",
     "bnn_filter_repetition_workspace_bytes", "bnn_filter_repetition_count",
+    "bnn_linear_workspace_bytes", "bnn_linear", "bnn_linear_backward", "bnn_gated_workspace_bytes", "bnn_gated",
+    "bnn_gated_backward", "bnn_block_norm", "bnn_block_norm_workspace_bytes", "bnn_block_norm_backward", "bnn_dropout",
 )
 
 
@@ -51,6 +57,37 @@ class ConvLayerDesc(Structure):
 
 class ConvNetDesc(Structure):
     _fields_ = [("n_layers", c_int32), ("layers", POINTER(ConvLayerDesc))]
+
+
+class LinearDesc(Structure):
+    _fields_ = [("dtype", c_int32), ("act", c_int32), ("K", c_int64), ("N", c_int64), ("W", c_void_p), ("ldw", c_int64),
+                ("bias", c_void_p)]
+
+
+class GatedDesc(Structure):
+    _fields_ = [("dtype", c_int32), ("act", c_int32), ("K", c_int64), ("N", c_int64), ("Wg", c_void_p), ("ldg", c_int64),
+                ("Wu", c_void_p), ("ldu", c_int64)]
+
+
+class BlockNormDesc(Structure):
+    _fields_ = [("dtype", c_int32), ("kind", c_int32), ("D", c_int64), ("eps", c_float), ("alpha", c_float), ("post", c_int32),
+                ("pre", c_int32), ("post_weight", c_void_p), ("post_shift", c_void_p), ("pre_weight", c_void_p),
+                ("pre_shift", c_void_p), ("gate", c_void_p), ("ld_gate", c_int64), ("rows_per_gate", c_int64)]
+
+
+class BlockNormGrads(Structure):
+    _fields_ = [("dx", c_void_p), ("lddx", c_int64), ("dblock", c_void_p), ("lddb", c_int64), ("dpost_weight", c_void_p),
+                ("dpost_shift", c_void_p), ("dpre_weight", c_void_p), ("dpre_shift", c_void_p), ("dgate", c_void_p),
+                ("ld_dgate", c_int64)]
+
+
+class Layer:
+    """A descriptor of the real-valued operators with the tensors it points to (made by Context.make_linear, make_gated and
+    make_block_norm).  The tensors' contents may change between calls, their storage may not."""
+
+    def __init__(self, desc, dtype, device, inner, outer, tensors):
+        self.desc, self.ref = desc, ctypes.byref(desc)
+        self.dtype, self.device, self.inner, self.outer, self.tensors = dtype, device, inner, outer, tensors
 
 
 class BnnError(RuntimeError):
@@ -129,6 +166,20 @@ def lib() -> ctypes.CDLL:
         L.bnn_mlp_forward.argtypes = [vp, POINTER(MlpDesc), vp, i64, i64, vp, i64, POINTER(vp)]
         L.bnn_mlp_forward_host.argtypes = [vp, POINTER(MlpDesc), vp, i64, i64, vp, i64]
         L.bnn_fold_batchnorm.argtypes = [vp, vp, vp, vp, c_double, i64, i64, vp, vp]
+        L.bnn_linear_workspace_bytes.argtypes = [POINTER(LinearDesc), i64, c_int, c_int]
+        L.bnn_linear_workspace_bytes.restype = c_size_t
+        L.bnn_linear.argtypes = [vp, POINTER(LinearDesc), vp, i64, i64, vp, i64, vp, i64, vp, i64]
+        L.bnn_linear_backward.argtypes = [vp, POINTER(LinearDesc), vp, i64, vp, i64, i64, vp, i64, vp, i64, vp, i64, vp]
+        L.bnn_gated_workspace_bytes.argtypes = [POINTER(GatedDesc), i64, c_int, c_int]
+        L.bnn_gated_workspace_bytes.restype = c_size_t
+        L.bnn_gated.argtypes = [vp, POINTER(GatedDesc), vp, i64, i64, vp, i64, vp, i64]
+        L.bnn_gated_backward.argtypes = [vp, POINTER(GatedDesc), vp, i64, vp, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64]
+        L.bnn_block_norm.argtypes = [vp, POINTER(BlockNormDesc), vp, i64, vp, i64, i64, vp, i64, vp, i64, vp]
+        L.bnn_block_norm_workspace_bytes.argtypes = [POINTER(BlockNormDesc), i64]
+        L.bnn_block_norm_workspace_bytes.restype = c_size_t
+        L.bnn_block_norm_backward.argtypes = [vp, POINTER(BlockNormDesc), vp, i64, vp, i64, vp, i64, vp, i64, vp, i64,
+                                              POINTER(BlockNormGrads)]
+        L.bnn_dropout.argtypes = [vp, c_int, vp, i64, vp, i64, vp, i64, i64, i64, c_double, c_uint64, c_uint64]
         L.bnn_mlp_noalloc_max_bytes.argtypes = []
         L.bnn_mlp_noalloc_max_bytes.restype = c_size_t
         L.bnn_mlp_forward_noalloc.argtypes = [vp, POINTER(MlpDesc), vp, i64, i64, vp, i64]
@@ -170,6 +221,7 @@ class Context:
             raise BnnError(st, "bnn_create")
         self._h = h
         self._ws = None
+        self._device = torch.device("cuda", device)
         self._destroy = lib().bnn_destroy      # kept here: module globals may be gone when __del__ runs at interpreter exit
 
     def close(self):
@@ -413,6 +465,242 @@ class Context:
         self._ck(lib().bnn_mlp_forward_host(self._h, ctypes.byref(desc), _ptr(X_host), X_host.stride(0), batch,
                                             _ptr(scores_host), n_out), "bnn_mlp_forward_host")
         return scores_host
+
+    # -- real-valued feed-forward sublayer ---------------------------------------------------------------
+    def _fit(self, t, rows, cols, dtype, what):
+        """Checks a row-major matrix; returns (address, leading dimension)."""
+        if t is None:
+            return None, 0
+        if t.dtype is not dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.get_device() != self.device:
+            raise ValueError(f"{what}: expected {dtype} [{rows}, {cols}] on cuda:{self.device}, got {t.dtype} {list(t.shape)} on {t.device}")
+        ld, step = t.stride()
+        if step != 1 and cols > 1 and rows:
+            raise ValueError(f"{what}: rows must be contiguous (row-major), strides are {t.stride()}")
+        if rows > 1 and ld < cols:
+            raise ValueError(f"{what}: rows overlap, strides are {t.stride()}")
+        return t.data_ptr(), ld if rows > 1 else cols
+
+    def _vector(self, t, n, dtype, what):
+        if t is None:
+            return None
+        if t.dtype is not dtype or t.dim() != 1 or t.shape[0] != n or t.get_device() != self.device or (n > 1 and t.stride(0) != 1):
+            raise ValueError(f"{what}: expected contiguous {dtype} [{n}] on cuda:{self.device}, got {t.dtype} {list(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    def _elsewhere(self):
+        """Whether torch's current stream is another one than the context's."""
+        return torch._C._cuda_getCurrentRawStream(self.device) != self.stream.cuda_stream
+
+    def _new(self, *shape, dtype):
+        """Memory for a result, from the pool of the stream that the library writes it on."""
+        if not self._elsewhere():
+            return torch.empty(shape, dtype=dtype, device=self._device)
+        with torch.cuda.stream(self.stream):
+            t = torch.empty(shape, dtype=dtype, device=self._device)
+        t.record_stream(torch.cuda.current_stream(self.device))
+        return t
+
+    def _used(self, *tensors):
+        """Keeps the memory of tensors of another stream until the work queued on the context's stream is done with it."""
+        if self._elsewhere():
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self.stream)
+
+    def make_linear(self, W, bias=None, act: str = "none") -> Layer:
+        """Dense layer y = residual + act(x W^T + bias): W [N, K] float16 or bfloat16, bias [N] or None."""
+        if W.dtype not in _PRODUCT_TYPES:
+            raise ValueError(f"W: expected float16 or bfloat16, got {W.dtype}")
+        if act not in ACTIVATIONS:
+            raise ValueError(f"act: one of {', '.join(ACTIVATIONS)}, got {act!r}")
+        N, K = W.shape
+        p, ld = self._fit(W, N, K, W.dtype, "W")
+        d = LinearDesc(_REAL_TYPES[W.dtype], ACTIVATIONS[act], K, N, p, ld, self._vector(bias, N, W.dtype, "bias"))
+        return Layer(d, W.dtype, self.device, K, N, (W, bias))
+
+    def make_gated(self, Wg, Wu, act: str = "silu") -> Layer:
+        """Gated projections h = act(x Wg^T) * (x Wu^T): Wg, Wu [N, K] float16 or bfloat16."""
+        if Wg.dtype not in _PRODUCT_TYPES:
+            raise ValueError(f"Wg: expected float16 or bfloat16, got {Wg.dtype}")
+        if act not in ACTIVATIONS:
+            raise ValueError(f"act: one of {', '.join(ACTIVATIONS)}, got {act!r}")
+        N, K = Wg.shape
+        pg, ldg = self._fit(Wg, N, K, Wg.dtype, "Wg")
+        pu, ldu = self._fit(Wu, N, K, Wg.dtype, "Wu")
+        return Layer(GatedDesc(_REAL_TYPES[Wg.dtype], ACTIVATIONS[act], K, N, pg, ldg, pu, ldu), Wg.dtype, self.device, K, N, (Wg, Wu))
+
+    def make_block_norm(self, D: int, dtype, kind: str = "rms", eps: float = 1e-6, alpha: float = 1.0, post: bool = False,
+                        post_weight=None, post_shift=None, pre: bool = True, pre_weight=None, pre_shift=None, gate=None,
+                        rows_per_gate: int | None = None) -> Layer:
+        """Norms around a block: stream = alpha x + gate * (post ? Norm(block) : block), normed = Norm(stream) if pre.
+        gate: [D] (one for all rows) or [G, D] with rows_per_gate."""
+        if kind not in NORMS:
+            raise ValueError(f"kind: one of {', '.join(NORMS)}, got {kind!r}")
+        if dtype not in _REAL_TYPES:
+            raise ValueError(f"dtype: expected float32, float16 or bfloat16, got {dtype}")
+        if gate is not None and gate.dim() == 1:
+            gate = gate.unsqueeze(0)
+        if gate is not None and rows_per_gate is None:
+            if gate.shape[0] != 1:
+                raise ValueError("rows_per_gate: needed for a gate of several rows")
+            rows_per_gate = 0x7fffffff
+        gp, gl = self._fit(gate, gate.shape[0], D, dtype, "gate") if gate is not None else (None, 0)
+        v = [self._vector(t, D, dtype, n) for t, n in ((post_weight, "post_weight"), (post_shift, "post_shift"), (pre_weight, "pre_weight"),
+                                                       (pre_shift, "pre_shift"))]
+        d = BlockNormDesc(_REAL_TYPES[dtype], NORMS[kind], D, eps, alpha, int(post), int(pre), *v, gp, gl, rows_per_gate or 1)
+        layer = Layer(d, dtype, self.device, D, D, (post_weight, post_shift, pre_weight, pre_shift, gate))
+        layer.gates = gate.shape[0] if gate is not None else 0
+        return layer
+
+    @staticmethod
+    def _rows16(*tensors):
+        return all(t is None or (t.data_ptr() % 16 == 0 and (t.shape[0] <= 1 or t.stride(0) * t.element_size() % 16 == 0)) for t in tensors)
+
+    def linear_workspace_bytes(self, layer: Layer, x, backward: bool = False, dy=None) -> int:
+        """Workspace of linear / linear_backward for inputs laid out like x (and dy)."""
+        return int(lib().bnn_linear_workspace_bytes(layer.ref, x.shape[0], int(backward), int(self._rows16(x, dy, layer.tensors[0]))))
+
+    def gated_workspace_bytes(self, layer: Layer, x, backward: bool = False) -> int:
+        """Workspace of gated / gated_backward for inputs laid out like x."""
+        return int(lib().bnn_gated_workspace_bytes(layer.ref, x.shape[0], int(backward), int(self._rows16(x, *layer.tensors))))
+
+    def block_norm_workspace_bytes(self, layer: Layer, rows: int) -> int:
+        return int(lib().bnn_block_norm_workspace_bytes(layer.ref, rows))
+
+    def linear(self, layer: Layer, x, residual=None, out=None, pre=None):
+        """bnn_linear.  pre: float32 [M, N] that receives x W^T + bias for linear_backward.  out may be residual."""
+        M, N = x.shape[0], layer.outer
+        xp, ldx = self._fit(x, M, layer.inner, layer.dtype, "x")
+        rp, ldr = self._fit(residual, M, N, layer.dtype, "residual")
+        pp, ldp = self._fit(pre, M, N, torch.float32, "pre")
+        if out is None:
+            out = self._new(M, N, dtype=layer.dtype)
+        op, ldo = self._fit(out, M, N, layer.dtype, "out")
+        self._ck(lib().bnn_linear(self._h, layer.ref, xp, ldx, M, rp, ldr, op, ldo, pp, ldp), "bnn_linear")
+        self._used(x, residual, out, pre, *layer.tensors)
+        return out
+
+    def linear_backward(self, layer: Layer, dy, x, pre=None, want_dx: bool = True, want_dW: bool = True, want_db: bool = True):
+        """bnn_linear_backward -> (dx, dW, dbias); dbias is None for a layer without bias, what is not wanted is None."""
+        M, N, K = x.shape[0], layer.outer, layer.inner
+        gp, ldg = self._fit(dy, M, N, layer.dtype, "dy")
+        xp, ldx = self._fit(x, M, K, layer.dtype, "x")
+        pp, ldp = self._fit(pre, M, N, torch.float32, "pre")
+        dx = self._new(M, K, dtype=layer.dtype) if want_dx else None
+        dW = self._new(N, K, dtype=layer.dtype) if want_dW else None
+        db = self._new(N, dtype=layer.dtype) if want_db and layer.tensors[1] is not None else None
+        self._ck(lib().bnn_linear_backward(self._h, layer.ref, gp, ldg, xp, ldx, M, pp, ldp, _ptr(dx), K, _ptr(dW), K, _ptr(db)),
+                 "bnn_linear_backward")
+        self._used(dy, x, pre, *layer.tensors)
+        return dx, dW, db
+
+    def gated(self, layer: Layer, x, out=None, pre=None):
+        """bnn_gated.  pre: contiguous float32 [2, M, N] that receives x Wg^T and x Wu^T for gated_backward."""
+        M, N = x.shape[0], layer.outer
+        xp, ldx = self._fit(x, M, layer.inner, layer.dtype, "x")
+        pp, ldp = self._planes(pre, M, N)
+        if out is None:
+            out = self._new(M, N, dtype=layer.dtype)
+        op, ldo = self._fit(out, M, N, layer.dtype, "out")
+        self._ck(lib().bnn_gated(self._h, layer.ref, xp, ldx, M, op, ldo, pp, ldp), "bnn_gated")
+        self._used(x, out, pre, *layer.tensors)
+        return out
+
+    def _planes(self, pre, M, N):
+        if pre is None:
+            return None, 0
+        if pre.shape != (2, M, N) or not pre.is_contiguous():
+            raise ValueError(f"pre: expected contiguous [2, {M}, {N}], got {list(pre.shape)} with strides {pre.stride()}")
+        return self._fit(pre.view(2 * M, N), 2 * M, N, torch.float32, "pre")
+
+    def gated_backward(self, layer: Layer, dh, x, pre=None, want_dx: bool = True, want_dW: bool = True):
+        """bnn_gated_backward -> (dx, dWg, dWu); what is not wanted is None.  Without pre both products are computed again."""
+        M, N, K = x.shape[0], layer.outer, layer.inner
+        gp, ldg = self._fit(dh, M, N, layer.dtype, "dh")
+        xp, ldx = self._fit(x, M, K, layer.dtype, "x")
+        pp, ldp = self._planes(pre, M, N)
+        dx = self._new(M, K, dtype=layer.dtype) if want_dx else None
+        dWg, dWu = (self._new(N, K, dtype=layer.dtype) if want_dW else None for _ in range(2))
+        self._ck(lib().bnn_gated_backward(self._h, layer.ref, gp, ldg, xp, ldx, M, pp, ldp, _ptr(dx), K, _ptr(dWg), K, _ptr(dWu), K),
+                 "bnn_gated_backward")
+        self._used(dh, x, pre, *layer.tensors)
+        return dx, dWg, dWu
+
+    def _gate_rows(self, layer: Layer, M: int):
+        if layer.gates and layer.gates * layer.desc.rows_per_gate < M:
+            raise ValueError(f"gate: {layer.gates} rows of {layer.desc.rows_per_gate} cover fewer than {M}")
+
+    def block_norm(self, layer: Layer, x, block=None, stream=None, normed=None, stats=None):
+        """bnn_block_norm -> (stream, normed); normed is None for a layer without pre.  stream may be x.
+        stats: contiguous float32 [M, 4] kept for block_norm_backward."""
+        M, D = x.shape[0], layer.inner
+        self._gate_rows(layer, M)
+        xp, ldx = self._fit(x, M, D, layer.dtype, "x")
+        bp, ldb = self._fit(block, M, D, layer.dtype, "block")
+        tp, ldt = self._fit(stats, M, 4, torch.float32, "stats")
+        if stats is not None and M > 1 and ldt != 4:
+            raise ValueError("stats: expected a contiguous tensor")
+        if stream is None:
+            stream = self._new(M, D, dtype=layer.dtype)
+        if normed is None and layer.desc.pre:
+            normed = self._new(M, D, dtype=layer.dtype)
+        sp, lds = self._fit(stream, M, D, layer.dtype, "stream")
+        np_, ldn = self._fit(normed, M, D, layer.dtype, "normed")
+        self._ck(lib().bnn_block_norm(self._h, layer.ref, xp, ldx, bp, ldb, M, sp, lds, np_, ldn, tp), "bnn_block_norm")
+        self._used(x, block, stream, normed, stats, *layer.tensors)
+        return stream, normed
+
+    def block_norm_backward(self, layer: Layer, dstream, dnormed, x, block=None, stats=None):
+        """bnn_block_norm_backward -> dict with dx, dblock and, as far as the layer has them, dgate, dpost_weight, dpost_shift,
+        dpre_weight, dpre_shift (None otherwise)."""
+        M, D, d = x.shape[0], layer.inner, layer.desc
+        self._gate_rows(layer, M)
+        sp, lds = self._fit(dstream, M, D, layer.dtype, "dstream")
+        np_, ldn = self._fit(dnormed, M, D, layer.dtype, "dnormed")
+        xp, ldx = self._fit(x, M, D, layer.dtype, "x")
+        bp, ldb = self._fit(block, M, D, layer.dtype, "block")
+        tp, ldt = self._fit(stats, M, 4, torch.float32, "stats")
+        if stats is not None and M > 1 and ldt != 4:
+            raise ValueError("stats: expected a contiguous tensor")
+        post_w, post_c, pre_w, pre_c, gate = layer.tensors
+
+        def like(t, wanted=True):
+            return self._new(D, dtype=layer.dtype) if t is not None and wanted else None
+
+        out = {"dx": self._new(M, D, dtype=layer.dtype), "dblock": self._new(M, D, dtype=layer.dtype) if block is not None else None,
+               "dgate": None, "dpost_weight": like(post_w, d.post), "dpost_shift": like(post_c, d.post),
+               "dpre_weight": like(pre_w, d.pre), "dpre_shift": like(pre_c, d.pre)}
+        if gate is not None and block is not None:
+            out["dgate"] = self._new(layer.gates, D, dtype=layer.dtype)
+            used = -(-M // d.rows_per_gate)
+            if used < layer.gates:                    # gate rows that no row of the stream uses
+                with torch.cuda.stream(self.stream):
+                    out["dgate"][used:].zero_()
+        g = BlockNormGrads(out["dx"].data_ptr(), D, *((out["dblock"].data_ptr(), D) if block is not None else (None, 0)),
+                           *(None if out[k] is None else out[k].data_ptr() for k in ("dpost_weight", "dpost_shift", "dpre_weight",
+                                                                                     "dpre_shift", "dgate")), D)
+        self._ck(lib().bnn_block_norm_backward(self._h, layer.ref, sp, lds, np_, ldn, xp, ldx, bp, ldb, tp, M, ctypes.byref(g)),
+                 "bnn_block_norm_backward")
+        self._used(dstream, dnormed, x, block, stats, *layer.tensors)
+        return out
+
+    def dropout(self, x, p: float, seed: int, offset: int = 0, residual=None, out=None):
+        """bnn_dropout: residual + (kept ? x / (1 - p) : 0); the backward pass is the same call on the gradient.  out may be x."""
+        if x.dtype not in _REAL_TYPES:
+            raise ValueError(f"x: expected float32, float16 or bfloat16, got {x.dtype}")
+        if not 0.0 <= p <= 1.0:
+            raise ValueError(f"p: expected 0 to 1, got {p}")
+        if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
+            raise ValueError("seed, offset: expected 64-bit unsigned numbers")
+        M, D = x.shape
+        xp, ldx = self._fit(x, M, D, x.dtype, "x")
+        rp, ldr = self._fit(residual, M, D, x.dtype, "residual")
+        if out is None:
+            out = self._new(M, D, dtype=x.dtype)
+        op, ldo = self._fit(out, M, D, x.dtype, "out")
+        self._ck(lib().bnn_dropout(self._h, _REAL_TYPES[x.dtype], xp, ldx, rp, ldr, op, ldo, M, D, p, seed, offset), "bnn_dropout")
+        self._used(x, residual, out)
+        return out
 
 
 def debug_ring_position(stage: int, slots: int, step: int = 1) -> dict:

@@ -14,7 +14,7 @@ LIB = os.path.join(HERE, "libbnn_b200.so")
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17", "-shared",
     "-Xcompiler", "-fPIC", "-Xcompiler", "-ffp-contract=off", "-Xcompiler", "-fvisibility=hidden",
-    "--expt-relaxed-constexpr",
+    "--expt-relaxed-constexpr", "--threads", "0",
 ]
 
 

@@ -56,3 +56,6 @@ int bnn_first_layer_planes_pre(bnn_ctx *ctx, const uint8_t *X, int64_t ldx, cons
 size_t bnn_fr_workspace_bytes(int64_t C_in, int64_t C_out);
 int bnn_fr_conv(bnn_ctx *ctx, const uint32_t *act, int64_t B, int64_t H, int64_t W, int64_t C_in, const uint32_t *Wp, int64_t C_out,
                 int pool, const int32_t *thr, const uint32_t *flip, uint32_t *out_bits, int32_t *out_sums);
+
+// ---- real-valued operators: out[c] = sum over i of part[i * pitch + c], in the order of i, rounded to dtype (bnn_norm.cu)
+int bnn_join_columns(bnn_ctx *ctx, int dtype, const float *part, int64_t pitch, int64_t count, void *out, int64_t columns);

@@ -109,3 +109,69 @@ def convnet_workspace_bytes(ctx, net, B: int, H: int, W: int) -> int:
         if L["pool"]:
             H, W = H // 2, W // 2
     return need
+
+
+def prepare_feed_forward(ctx, layers, first_weight=None, act: str = "silu", kind: str = "rms", eps: float = 1e-6, alpha: float = 1.0,
+                         drop: float = 0.0):
+    """Device weights of a stack of gated feed-forward layers (dicts with Wg, Wu [F, D], Wd [D, F] and optionally gate [D],
+    post_weight [D] and next_weight [D], the scale of the norm in front of the following layer) -> handles of the real-valued operators.
+    Layer i:  stream += gate * Norm(dropout((act(n Wg^T) * (n Wu^T)) Wd^T)),  n = Norm(stream)."""
+    D, dtype = layers[0]["Wd"].shape[0], layers[0]["Wd"].dtype
+    net = {"first": ctx.make_block_norm(D, dtype, kind=kind, eps=eps, pre_weight=first_weight), "layers": [], "drop": drop, "act": act}
+    for L in layers:
+        net["layers"].append({
+            "up": ctx.make_gated(L["Wg"], L["Wu"], act), "down": ctx.make_linear(L["Wd"]),
+            "norm": ctx.make_block_norm(D, dtype, kind=kind, eps=eps, alpha=alpha, gate=L.get("gate"), post=L.get("post_weight") is not None,
+                                        post_weight=L.get("post_weight"), pre_weight=L.get("next_weight"))})
+    return net
+
+
+def feed_forward_workspace_bytes(ctx, net, x, backward: bool = False) -> int:
+    """Workspace for feed_forward on rows like x, and for feed_forward_backward."""
+    need = 0
+    for L in net["layers"]:
+        h = torch.empty(x.shape[0], L["up"].outer, dtype=x.dtype, device=x.device)
+        need = max(need, ctx.gated_workspace_bytes(L["up"], x, backward), ctx.linear_workspace_bytes(L["down"], h, backward),
+                   ctx.block_norm_workspace_bytes(L["norm"], x.shape[0]) if backward else 0)
+    return max(need, ctx.block_norm_workspace_bytes(net["first"], x.shape[0]) if backward else 0)
+
+
+def feed_forward(ctx, net, x, seed: int | None = None, keep: list | None = None):
+    """x [M, D] through the stack: (stream, normed) after the last layer; one row is the form for a single token.
+    seed: trains with dropout (one offset per layer); keep: a list that receives what feed_forward_backward needs."""
+    def stats():
+        return ctx.empty(x.shape[0], 4, dtype=torch.float32) if keep is not None else None
+
+    st = stats()
+    stream, n = ctx.block_norm(net["first"], x, stats=st)
+    if keep is not None:
+        keep.append((x, st))
+    for i, L in enumerate(net["layers"]):
+        pre = ctx.empty(2, x.shape[0], L["up"].outer, dtype=torch.float32) if keep is not None else None
+        h = ctx.gated(L["up"], n, pre=pre)
+        block = ctx.linear(L["down"], h)
+        if seed is not None and net["drop"] > 0:
+            ctx.dropout(block, net["drop"], seed, i, out=block)
+        st = stats()
+        if keep is not None:
+            keep.append((n, pre, h, stream, block, st))
+        stream, n = ctx.block_norm(L["norm"], stream, block, stats=st)
+    return stream, n
+
+
+def feed_forward_backward(ctx, net, keep, dstream=None, dnormed=None, seed: int | None = None):
+    """Gradients of feed_forward (with the same seed) from those of its two results: (dx, first norm's gradients, a dict per
+    layer with dWg, dWu, dWd and the norm's dgate, dpost_weight, dpre_weight)."""
+    grads = []
+    for i in reversed(range(len(net["layers"]))):
+        L, (n, pre, h, stream, block, st) = net["layers"][i], keep[i + 1]
+        g = ctx.block_norm_backward(L["norm"], dstream, dnormed, stream, block, st)
+        dstream, dblock = g["dx"], g["dblock"]
+        if seed is not None and net["drop"] > 0:
+            ctx.dropout(dblock, net["drop"], seed, i, out=dblock)
+        dh, g["dWd"], _ = ctx.linear_backward(L["down"], dblock, h)
+        dnormed, g["dWg"], g["dWu"] = ctx.gated_backward(L["up"], dh, n, pre)
+        grads.insert(0, g)
+    x, st = keep[0]
+    first = ctx.block_norm_backward(net["first"], dstream, dnormed, x, stats=st)
+    return first["dx"], first, grads
