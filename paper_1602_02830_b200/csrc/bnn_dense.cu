@@ -3,90 +3,23 @@
 //   linear:  z = x W^T + bias, y = residual + act(z);   dz = dy act'(z), dx = dz W, dW = dz^T x, dbias = sum dz
 //   gated:   g = x Wg^T, u = x Wu^T, h = act(g) u;      dg = dh u act'(g), du = dh act(g), dx = dg Wg + du Wu, dWg = dg^T x, dWu = du^T x
 //
-// Every product is k_product with an epilogue; dz (dg, du) is rounded to 16 bits once, the operand type of the products that read it.
-#include "bnn_real.cuh"
+// Every product is bnn_product with an epilogue; dz (dg, du) is rounded to 16 bits once, the operand type of the products that read it.
 #include "bnn_internal.cuh"
+#include "bnn_product.cuh"
 
 namespace {
 
-enum Epilogue { EPI_LINEAR, EPI_LINEAR_BACK, EPI_GATED, EPI_GATED_BACK };
-
-struct Operand { const void *p; int64_t row, k; };        // element (i, k) at p[i * row + k * k]
-struct ProductArgs {
-    Operand a[2], b[2];      // EPI_GATED*: two products with one accumulator each; otherwise their sum (the second may be absent)
-    int pairs;
-    int64_t M, N, K;
-    const void *bias;
-    const void *add; int64_t ld_add;      // EPI_LINEAR: residual; *_BACK: the gradient dy / dh
-    void *out[2]; int64_t ldo;
-    float *pre; int64_t ldp;
-    int act;
-};
-
-template <typename T, int EPI>
-__global__ void __launch_bounds__(256) k_product(const ProductArgs p) {
-    constexpr int ACCS = (EPI == EPI_GATED || EPI == EPI_GATED_BACK) ? 2 : 1;
-    __shared__ float sa[16][65], sb[16][65];
-    float acc[ACCS][4][4] = {};
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const int64_t m0 = (int64_t)blockIdx.y * 64, n0 = (int64_t)blockIdx.x * 64;
+// Copies a matrix whose rows are not whole 16-byte groups to one whose rows are: what TMA can read.  Streaming, both sides coalesced.
+__global__ void __launch_bounds__(256) k_repitch(const uint16_t *__restrict__ src, int64_t ld, uint16_t *__restrict__ dst, int64_t pitch,
+                                                 int64_t rows, int64_t cols) {
+    for (int64_t m = blockIdx.y; m < rows; m += gridDim.y) {
+        const int64_t c0 = (int64_t)blockIdx.x * 2048 + threadIdx.x;
 #pragma unroll
-    for (int pair = 0; pair < 2; ++pair) {
-        if (pair >= p.pairs) break;
-        const T *A = static_cast<const T *>(p.a[pair].p), *B = static_cast<const T *>(p.b[pair].p);
-        for (int64_t k0 = 0; k0 < p.K; k0 += 16) {
-            for (int i = threadIdx.x; i < 1024; i += 256) {
-                const int r = i >> 4, k = i & 15;
-                sa[k][r] = (m0 + r < p.M && k0 + k < p.K) ? to_f32(A[(m0 + r) * p.a[pair].row + (k0 + k) * p.a[pair].k]) : 0.0f;
-                sb[k][r] = (n0 + r < p.N && k0 + k < p.K) ? to_f32(B[(n0 + r) * p.b[pair].row + (k0 + k) * p.b[pair].k]) : 0.0f;
-            }
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < 16; ++k)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[ACCS == 2 ? pair : 0][i][j] += sa[k][ty * 4 + i] * sb[k][tx * 4 + j];
-            __syncthreads();
+        for (int i = 0; i < 8; ++i) {
+            const int64_t c = c0 + i * 256;
+            if (c < cols) dst[m * pitch + c] = src[m * ld + c];
         }
     }
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const int64_t m = m0 + ty * 4 + i, n = n0 + tx * 4 + j;
-            if (m >= p.M || n >= p.N) continue;
-            float z = acc[0][i][j], value;
-            if constexpr (ACCS == 1) {
-                if (p.bias) z += to_f32(static_cast<const T *>(p.bias)[n]);
-                T *out = static_cast<T *>(p.out[0]) + m * p.ldo + n;
-                if constexpr (EPI == EPI_LINEAR) {
-                    if (p.pre) p.pre[m * p.ldp + n] = z;
-                    value = act_value(p.act, z);
-                    if (p.add) value += to_f32(static_cast<const T *>(p.add)[m * p.ld_add + n]);
-                } else {
-                    value = to_f32(static_cast<const T *>(p.add)[m * p.ld_add + n]) * act_slope(p.act, z, z);
-                }
-                *out = from_f32<T>(value);
-            } else {
-                const float u = acc[ACCS - 1][i][j];
-                if constexpr (EPI == EPI_GATED) {
-                    if (p.pre) { p.pre[m * p.ldp + n] = z; p.pre[(p.M + m) * p.ldp + n] = u; }
-                    static_cast<T *>(p.out[0])[m * p.ldo + n] = from_f32<T>(act_value(p.act, z) * u);
-                } else {
-                    const float d = to_f32(static_cast<const T *>(p.add)[m * p.ld_add + n]);
-                    const float slope = act_slope(p.act, z, value);
-                    static_cast<T *>(p.out[0])[m * p.ldo + n] = from_f32<T>(d * u * slope);
-                    static_cast<T *>(p.out[1])[m * p.ldo + n] = from_f32<T>(d * value);
-                }
-            }
-        }
-}
-
-template <int EPI> int product(bnn_ctx *ctx, int dtype, const ProductArgs &a) {
-    if (a.M == 0 || a.N == 0) return BNN_OK;
-    const dim3 grid((unsigned)((a.N + 63) / 64), (unsigned)((a.M + 63) / 64));
-    if (dtype == BNN_F16) k_product<__half, EPI><<<grid, 256, 0, ctx->stream>>>(a);
-    else k_product<__nv_bfloat16, EPI><<<grid, 256, 0, ctx->stream>>>(a);
-    return bnn_check_launch(ctx);
 }
 
 // dz = dy act'(pre) and/or the partial column sums of dz: a block takes 256 columns (8 per thread) of one chunk of rows, eight
@@ -212,16 +145,46 @@ int check_gated(const bnn_gated_desc *l, int64_t M) {
     if (int st = bnn_check_real(l->Wg, l->ldg, l->N, l->K, 2)) return st;
     return bnn_check_real(l->Wu, l->ldu, l->N, l->K, 2);
 }
-// Scratch of the backward passes: dz (or dg and du), then the partial column sums of the bias gradient.
 size_t dz_bytes(int64_t M, int64_t N) { return round256((size_t)M * pitch16(N) * 2); }
+size_t sums_bytes(int64_t M, int64_t N) { return round256((size_t)sum_chunks(M, N) * N * 4); }
+
+// Scratch of one call, handed out in order.  What does not fit is noticed at the end (`ok`), before anything is launched.
+struct Scratch {
+    bnn_ctx *ctx;
+    size_t used = 0;
+    explicit Scratch(bnn_ctx *c) : ctx(c) {}
+    uint8_t *take(size_t bytes) {
+        uint8_t *p = static_cast<uint8_t *>(ctx->ws) + used;
+        used += bytes;
+        return p;
+    }
+    bool ok() const { return used == 0 || (ctx->ws && ctx->ws_bytes >= used); }
+};
+// An operand as TMA can read it: itself, or room for its copy (made by `copy` once the scratch is known to suffice).
+struct Readable {
+    BnnOperand use;
+    const void *src = nullptr;
+    int64_t ld = 0, rows = 0, cols = 0;
+    Readable(Scratch &s, const void *p, int64_t ld_, int64_t rows_, int64_t cols_) : use{p, ld_} {
+        if (rows_ == 0 || cols_ == 0 || bnn_rows16(p, ld_, rows_, 2)) return;
+        src = p; ld = ld_; rows = rows_; cols = cols_;
+        use = {s.take(dz_bytes(rows, cols)), pitch16(cols)};
+    }
+    int copy(bnn_ctx *ctx) const {
+        if (!src) return BNN_OK;
+        const dim3 grid((unsigned)((cols + 2047) / 2048), (unsigned)(rows < 65535 ? rows : 65535));
+        k_repitch<<<grid, 256, 0, ctx->stream>>>(static_cast<const uint16_t *>(src), ld, static_cast<uint16_t *>(const_cast<void *>(use.p)), use.ld, rows, cols);
+        return bnn_check_launch(ctx);
+    }
+};
 
 }  // namespace
 
 extern "C" size_t bnn_linear_workspace_bytes(const bnn_linear_desc *l, int64_t M, int backward, int aligned) {
     if (check_linear(l, M) || M == 0 || l->N == 0) return 0;
-    (void)aligned;
-    if (!backward) return 0;
-    return (l->act == BNN_ACT_NONE ? 0 : dz_bytes(M, l->N)) + (l->bias ? round256((size_t)sum_chunks(M, l->N) * l->N * 4) : 0);
+    size_t n = aligned ? 0 : dz_bytes(M, l->K) + dz_bytes(l->N, l->K);
+    if (backward) n += (l->act == BNN_ACT_NONE ? (aligned ? 0 : dz_bytes(M, l->N)) : dz_bytes(M, l->N)) + (l->bias ? sums_bytes(M, l->N) : 0);
+    return n;
 }
 
 extern "C" int bnn_linear(bnn_ctx *ctx, const bnn_linear_desc *l, const void *x, int64_t ldx, int64_t M, const void *residual, int64_t ldr,
@@ -235,11 +198,16 @@ extern "C" int bnn_linear(bnn_ctx *ctx, const bnn_linear_desc *l, const void *x,
     if (M == 0 || l->N == 0) return BNN_OK;
     bnn_device_guard guard(ctx);
     if (!guard.ok) return BNN_ERR_CUDA;
-    ProductArgs a{};
-    a.a[0] = {x, ldx, 1}; a.b[0] = {l->W, l->ldw, 1}; a.pairs = 1;
-    a.M = M; a.N = l->N; a.K = l->K;
-    a.bias = l->bias; a.add = residual; a.ld_add = ldr; a.out[0] = y; a.ldo = ldy; a.pre = pre; a.ldp = ldp; a.act = l->act;
-    return product<EPI_LINEAR>(ctx, l->dtype, a);
+    Scratch scratch(ctx);
+    const Readable rx(scratch, x, ldx, M, l->K), rw(scratch, l->W, l->ldw, l->N, l->K);
+    if (!scratch.ok()) return BNN_ERR_WORKSPACE;
+    if (int st = rx.copy(ctx)) return st;
+    if (int st = rw.copy(ctx)) return st;
+    BnnProduct p{};
+    p.dtype = l->dtype; p.epilogue = BNN_EPI_LINEAR; p.pairs = p.groups = 1;
+    p.a[0] = rx.use; p.b[0] = rw.use; p.M = M; p.N = l->N; p.K = l->K;
+    p.bias = l->bias; p.add = residual; p.ld_add = ldr; p.out[0] = y; p.ldo[0] = ldy; p.pre = pre; p.ldp = ldp; p.act = l->act;
+    return bnn_product(ctx, p);
 }
 
 extern "C" int bnn_linear_backward(bnn_ctx *ctx, const bnn_linear_desc *l, const void *dy, int64_t lddy, const void *x, int64_t ldx,
@@ -256,30 +224,32 @@ extern "C" int bnn_linear_backward(bnn_ctx *ctx, const bnn_linear_desc *l, const
     bnn_device_guard guard(ctx);
     if (!guard.ok) return BNN_ERR_CUDA;
     if (dbias && M == 0 && l->N > 0) BNN_CUDA_TRY(ctx, cudaMemsetAsync(dbias, 0, (size_t)l->N * 2, ctx->stream));
-    const bool slopes = l->act != BNN_ACT_NONE && M > 0 && l->N > 0;
-    const bool sums = dbias && M > 0 && l->N > 0;
-    const size_t need = (slopes ? dz_bytes(M, l->N) : 0) + (sums ? round256((size_t)sum_chunks(M, l->N) * l->N * 4) : 0);
-    if (need && (!ctx->ws || ctx->ws_bytes < need)) return BNN_ERR_WORKSPACE;
-    uint8_t *ws = static_cast<uint8_t *>(ctx->ws);
-    const void *dz = dy;
-    int64_t lddz = lddy;
-    float *part = sums ? reinterpret_cast<float *>(ws + (slopes ? dz_bytes(M, l->N) : 0)) : nullptr;
-    if (slopes) {
-        dz = ws; lddz = pitch16(l->N);
-        if (!pre) {
-            ProductArgs a{};
-            a.a[0] = {x, ldx, 1}; a.b[0] = {l->W, l->ldw, 1}; a.pairs = 1;
-            a.M = M; a.N = l->N; a.K = l->K;
-            a.bias = l->bias; a.add = dy; a.ld_add = lddy; a.out[0] = ws; a.ldo = lddz; a.act = l->act;
-            if (int st = product<EPI_LINEAR_BACK>(ctx, l->dtype, a)) return st;
-        }
+    const bool some = M > 0 && l->N > 0, slopes = l->act != BNN_ACT_NONE && some, sums = dbias && some, again = slopes && !pre;
+    const bool products = (dx && M > 0 && l->K > 0) || (dW && l->N > 0 && l->K > 0);
+    if (!products && !sums) return BNN_OK;
+    Scratch scratch(ctx);
+    BnnOperand dz{dy, lddy};
+    if (slopes) dz = {scratch.take(dz_bytes(M, l->N)), pitch16(l->N)};
+    const Readable rz(scratch, dz.p, dz.ld, products && !slopes ? M : 0, l->N);
+    const Readable rx(scratch, x, ldx, dW || again ? M : 0, l->K), rw(scratch, l->W, l->ldw, dx || again ? l->N : 0, l->K);
+    float *part = sums ? reinterpret_cast<float *>(scratch.take(sums_bytes(M, l->N))) : nullptr;
+    if (!scratch.ok()) return BNN_ERR_WORKSPACE;
+    for (const Readable *r : {&rz, &rx, &rw})
+        if (int st = r->copy(ctx)) return st;
+    BnnProduct p{};
+    p.dtype = l->dtype; p.pairs = p.groups = 1;
+    if (again) {
+        p.epilogue = BNN_EPI_LINEAR_BACK;
+        p.a[0] = rx.use; p.b[0] = rw.use; p.M = M; p.N = l->N; p.K = l->K;
+        p.bias = l->bias; p.add = dy; p.ld_add = lddy; p.out[0] = const_cast<void *>(dz.p); p.ldo[0] = dz.ld; p.act = l->act;
+        if (int st = bnn_product(ctx, p)) return st;
     }
-    if ((slopes && pre) || sums) {
+    const bool kept = slopes && pre;
+    if (kept || sums) {
         SlopeArgs s{};
-        const bool kept = slopes && pre;
-        s.dy = kept ? dy : dz; s.lddy = kept ? lddy : lddz;
+        s.dy = kept ? dy : dz.p; s.lddy = kept ? lddy : dz.ld;
         s.pre = kept ? pre : nullptr; s.ldp = ldp;
-        s.dz = kept ? ws : nullptr; s.lddz = lddz;
+        s.dz = kept ? const_cast<void *>(dz.p) : nullptr; s.lddz = dz.ld;
         s.part = part; s.M = M; s.N = l->N; s.chunk_rows = sum_chunk_rows(M, l->N); s.act = l->act;
         s.vec = l->N % 8 == 0 && bnn_rows16(s.dy, s.lddy, M, 2) && (!kept || bnn_rows16(pre, ldp, M, 4));
         const dim3 grid((unsigned)((l->N + 255) / 256), (unsigned)sum_chunks(M, l->N));
@@ -289,25 +259,25 @@ extern "C" int bnn_linear_backward(bnn_ctx *ctx, const bnn_linear_desc *l, const
         if (sums)
             if (int st = bnn_join_columns(ctx, l->dtype, part, l->N, sum_chunks(M, l->N), dbias, l->N)) return st;
     }
-    if (dx) {
-        ProductArgs a{};
-        a.a[0] = {dz, lddz, 1}; a.b[0] = {l->W, 1, l->ldw}; a.pairs = 1;
-        a.M = M; a.N = l->K; a.K = l->N; a.out[0] = dx; a.ldo = lddx;
-        if (int st = product<EPI_LINEAR>(ctx, l->dtype, a)) return st;
+    const BnnOperand z = slopes ? dz : rz.use;
+    p = BnnProduct{};
+    p.dtype = l->dtype; p.epilogue = BNN_EPI_LINEAR; p.pairs = p.groups = 1;
+    if (dx && M > 0 && l->K > 0) {
+        p.a[0] = z; p.b[0] = rw.use; p.a_mn = 0; p.b_mn = 1;
+        p.M = M; p.N = l->K; p.K = l->N; p.out[0] = dx; p.ldo[0] = lddx;
+        if (int st = bnn_product(ctx, p)) return st;
     }
-    if (dW) {
-        ProductArgs a{};
-        a.a[0] = {dz, 1, lddz}; a.b[0] = {x, 1, ldx}; a.pairs = 1;
-        a.M = l->N; a.N = l->K; a.K = M; a.out[0] = dW; a.ldo = lddw;
-        if (int st = product<EPI_LINEAR>(ctx, l->dtype, a)) return st;
+    if (dW && l->N > 0 && l->K > 0) {
+        p.a[0] = z; p.b[0] = rx.use; p.a_mn = p.b_mn = 1;
+        p.M = l->N; p.N = l->K; p.K = M; p.out[0] = dW; p.ldo[0] = lddw;
+        if (int st = bnn_product(ctx, p)) return st;
     }
     return BNN_OK;
 }
 
 extern "C" size_t bnn_gated_workspace_bytes(const bnn_gated_desc *l, int64_t M, int backward, int aligned) {
     if (check_gated(l, M) || M == 0 || l->N == 0) return 0;
-    (void)aligned;
-    return backward ? 2 * dz_bytes(M, l->N) : 0;
+    return (aligned ? 0 : dz_bytes(M, l->K) + 2 * dz_bytes(l->N, l->K)) + (backward ? 2 * dz_bytes(M, l->N) : 0);
 }
 
 extern "C" int bnn_gated(bnn_ctx *ctx, const bnn_gated_desc *l, const void *x, int64_t ldx, int64_t M, void *h, int64_t ldh, float *pre,
@@ -320,11 +290,16 @@ extern "C" int bnn_gated(bnn_ctx *ctx, const bnn_gated_desc *l, const void *x, i
     if (M == 0 || l->N == 0) return BNN_OK;
     bnn_device_guard guard(ctx);
     if (!guard.ok) return BNN_ERR_CUDA;
-    ProductArgs a{};
-    a.a[0] = a.a[1] = {x, ldx, 1}; a.b[0] = {l->Wg, l->ldg, 1}; a.b[1] = {l->Wu, l->ldu, 1}; a.pairs = 2;
-    a.M = M; a.N = l->N; a.K = l->K;
-    a.out[0] = h; a.ldo = ldh; a.pre = pre; a.ldp = ldp; a.act = l->act;
-    return product<EPI_GATED>(ctx, l->dtype, a);
+    Scratch scratch(ctx);
+    const Readable rx(scratch, x, ldx, M, l->K), rg(scratch, l->Wg, l->ldg, l->N, l->K), ru(scratch, l->Wu, l->ldu, l->N, l->K);
+    if (!scratch.ok()) return BNN_ERR_WORKSPACE;
+    for (const Readable *r : {&rx, &rg, &ru})
+        if (int st = r->copy(ctx)) return st;
+    BnnProduct p{};
+    p.dtype = l->dtype; p.epilogue = BNN_EPI_GATED; p.pairs = p.groups = 1;
+    p.a[0] = rx.use; p.b[0] = rg.use; p.b[1] = ru.use; p.M = M; p.N = l->N; p.K = l->K;
+    p.out[0] = h; p.ldo[0] = ldh; p.pre = pre; p.ldp = ldp; p.act = l->act;
+    return bnn_product(ctx, p);
 }
 
 extern "C" int bnn_gated_backward(bnn_ctx *ctx, const bnn_gated_desc *l, const void *dh, int64_t lddh, const void *x, int64_t ldx, int64_t M,
@@ -339,11 +314,24 @@ extern "C" int bnn_gated_backward(bnn_ctx *ctx, const bnn_gated_desc *l, const v
     if (!ctx) return BNN_ERR_INVALID_ARG;
     bnn_device_guard guard(ctx);
     if (!guard.ok) return BNN_ERR_CUDA;
-    const size_t one = dz_bytes(M, l->N);
-    if (one && (!ctx->ws || ctx->ws_bytes < 2 * one)) return BNN_ERR_WORKSPACE;
-    uint8_t *dg = static_cast<uint8_t *>(ctx->ws), *du = dg + one;
+    const bool some = M > 0 && l->N > 0, again = some && !pre;
+    if (!(dx && M > 0 && l->K > 0) && !((dWg || dWu) && l->N > 0 && l->K > 0)) return BNN_OK;
+    Scratch scratch(ctx);
     const int64_t ldd = pitch16(l->N);
-    if (one && pre) {
+    void *dg = scratch.take(dz_bytes(M, l->N)), *du = scratch.take(dz_bytes(M, l->N));
+    const Readable rx(scratch, x, ldx, dWg || dWu || again ? M : 0, l->K);
+    const Readable rg(scratch, l->Wg, l->ldg, dx || again ? l->N : 0, l->K), ru(scratch, l->Wu, l->ldu, dx || again ? l->N : 0, l->K);
+    if (!scratch.ok()) return BNN_ERR_WORKSPACE;
+    for (const Readable *r : {&rx, &rg, &ru})
+        if (int st = r->copy(ctx)) return st;
+    BnnProduct p{};
+    p.dtype = l->dtype; p.pairs = p.groups = 1;
+    if (again) {
+        p.epilogue = BNN_EPI_GATED_BACK;
+        p.a[0] = rx.use; p.b[0] = rg.use; p.b[1] = ru.use; p.M = M; p.N = l->N; p.K = l->K;
+        p.add = dh; p.ld_add = lddh; p.out[0] = dg; p.out[1] = du; p.ldo[0] = p.ldo[1] = ldd; p.act = l->act;
+        if (int st = bnn_product(ctx, p)) return st;
+    } else if (some) {
         GatedSlopeArgs s{};
         s.dh = dh; s.lddh = lddh; s.pre = pre; s.ldp = ldp; s.dg = dg; s.du = du; s.ldd = ldd; s.M = M; s.N = l->N; s.act = l->act;
         s.vec = l->N % 8 == 0 && bnn_rows16(dh, lddh, M, 2) && bnn_rows16(pre, ldp, 2 * M, 4);
@@ -351,27 +339,23 @@ extern "C" int bnn_gated_backward(bnn_ctx *ctx, const bnn_gated_desc *l, const v
         if (l->dtype == BNN_F16) k_gated_slopes<__half><<<grid, 256, 0, ctx->stream>>>(s);
         else k_gated_slopes<__nv_bfloat16><<<grid, 256, 0, ctx->stream>>>(s);
         if (int st = bnn_check_launch(ctx)) return st;
-    } else if (one) {
-        ProductArgs a{};
-        a.a[0] = a.a[1] = {x, ldx, 1}; a.b[0] = {l->Wg, l->ldg, 1}; a.b[1] = {l->Wu, l->ldu, 1}; a.pairs = 2;
-        a.M = M; a.N = l->N; a.K = l->K;
-        a.add = dh; a.ld_add = lddh; a.out[0] = dg; a.out[1] = du; a.ldo = ldd; a.act = l->act;
-        if (int st = product<EPI_GATED_BACK>(ctx, l->dtype, a)) return st;
     }
-    if (dx) {
-        ProductArgs a{};
-        a.a[0] = {dg, ldd, 1}; a.b[0] = {l->Wg, 1, l->ldg}; a.a[1] = {du, ldd, 1}; a.b[1] = {l->Wu, 1, l->ldu}; a.pairs = 2;
-        a.M = M; a.N = l->K; a.K = l->N; a.out[0] = dx; a.ldo = lddx;
-        if (int st = product<EPI_LINEAR>(ctx, l->dtype, a)) return st;
+    p = BnnProduct{};
+    p.dtype = l->dtype; p.epilogue = BNN_EPI_LINEAR; p.pairs = p.groups = 1;
+    if (dx && M > 0 && l->K > 0) {
+        p.a[0] = {dg, ldd}; p.a[1] = {du, ldd}; p.b[0] = rg.use; p.b[1] = ru.use; p.b_mn = 1; p.pairs = 2;
+        p.M = M; p.N = l->K; p.K = l->N; p.out[0] = dx; p.ldo[0] = lddx;
+        if (int st = bnn_product(ctx, p)) return st;
     }
-    void *dw[2] = {dWg, dWu};
-    const int64_t ldw[2] = {lddg, lddu};
-    for (int k = 0; k < 2; ++k) {
-        if (!dw[k]) continue;
-        ProductArgs a{};
-        a.a[0] = {k ? du : dg, 1, ldd}; a.b[0] = {x, 1, ldx}; a.pairs = 1;
-        a.M = l->N; a.N = l->K; a.K = M; a.out[0] = dw[k]; a.ldo = ldw[k];
-        if (int st = product<EPI_LINEAR>(ctx, l->dtype, a)) return st;
+    if ((dWg || dWu) && l->N > 0 && l->K > 0) {
+        p = BnnProduct{};
+        p.dtype = l->dtype; p.epilogue = BNN_EPI_LINEAR; p.pairs = 1;
+        p.groups = dWg && dWu ? 2 : 1;              // both weight gradients in one launch
+        p.a[0] = {dWg ? dg : du, ldd}; p.b[0] = rx.use; p.a_mn = p.b_mn = 1;
+        p.out[0] = dWg ? dWg : dWu; p.ldo[0] = dWg ? lddg : lddu;
+        if (p.groups == 2) { p.a[1] = {du, ldd}; p.out[1] = dWu; p.ldo[1] = lddu; }
+        p.M = l->N; p.N = l->K; p.K = M;
+        if (int st = bnn_product(ctx, p)) return st;
     }
     return BNN_OK;
 }

@@ -2,6 +2,7 @@
 #pragma once
 #include "bnn_common.cuh"
 #include "bnn_tile.cuh"
+#include <cuda.h>
 
 enum { BNN_VARIANT_AUTO = 0, BNN_VARIANT_PLAIN = 1, BNN_VARIANT_CSA = 2 };
 static inline int ctx_variant(const bnn_ctx *ctx) { return ctx->variant; }
@@ -59,3 +60,7 @@ int bnn_fr_conv(bnn_ctx *ctx, const uint32_t *act, int64_t B, int64_t H, int64_t
 
 // ---- real-valued operators: out[c] = sum over i of part[i * pitch + c], in the order of i, rounded to dtype (bnn_norm.cu)
 int bnn_join_columns(bnn_ctx *ctx, int dtype, const float *part, int64_t pitch, int64_t count, void *out, int64_t columns);
+// Tensor map of 16-bit elements [rows][cols], row pitch ld elements, box box_cols x box_rows, 128-byte swizzle, zeros outside (bnn_umma.cu)
+int bnn_tensor_map16(bnn_ctx *ctx, CUtensorMap *map, const void *base, int64_t rows, int64_t cols, int64_t ld, int box_rows, int box_cols);
+// The error word of the product kernels; read and cleared (bnn_product.cu)
+int bnn_product_status(bnn_ctx *ctx, int *code);

@@ -6,8 +6,8 @@
 #include <cuda_fp16.h>
 
 static inline int bnn_real_size(int dtype) { return dtype == BNN_F32 ? 4 : (dtype == BNN_F16 || dtype == BNN_BF16) ? 2 : 0; }
-// Sizes and leading dimensions stay below 2^31 (tensor-map coordinates and 32-bit row / column indices); offsets are 64-bit.
-constexpr int64_t BNN_REAL_MAX = 0x7fffffff;
+// Sizes stay far enough below 2^31 that tile coordinates past an edge fit 32 bits; offsets are 64-bit.
+constexpr int64_t BNN_REAL_MAX = 0x7fff0000;
 static inline bool bnn_real_dim(int64_t n) { return n >= 0 && n <= BNN_REAL_MAX; }
 // A row-major matrix: needed unless one of its dimensions is 0; a single row may have any leading dimension.
 static inline int bnn_check_real(const void *p, int64_t ld, int64_t rows, int64_t cols, int size) {

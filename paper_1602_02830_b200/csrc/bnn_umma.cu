@@ -28,10 +28,11 @@
 // Every wait is bounded: after the limit the kernel records an error code and runs to its end without
 // touching the accumulators, so a failure surfaces as BNN_ERR_DEVICE_STATUS instead of a hang.
 #include "bnn_internal.cuh"
-#include <cuda.h>
+#include "bnn_ptx.cuh"
 #include <mutex>
 
 namespace {
+using namespace bnn_ptx;
 
 constexpr int BM = 128, BK = 128;               // BK in bytes = int8 elements
 constexpr int BN_MAX = 256;                     // tile width: 256, or 128 for narrow outputs; 192 = the 4-bit engine
@@ -110,37 +111,10 @@ struct UmmaArgs {
     int drop_loads;         // test hook (single-SM kernel): the producer issues no loads, every consumer's wait runs out
 };
 
-__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-// Bounded wait on a phase parity.  Returns false if the limit ran out.
-__device__ __forceinline__ unsigned long long global_ns() {
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
-}
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
-}
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, int c3, uint32_t bar) {
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
         ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
-}
-// Shared-memory matrix descriptor: K-major tile, rows of 128 bytes, 128-byte swizzle, 8-row groups 1024 bytes apart.
-__device__ __forceinline__ uint64_t smem_desc_sw128(uint32_t addr) {
-    uint64_t d = (uint64_t)((addr & 0x3ffffu) >> 4);
-    d |= (uint64_t)(1024u >> 4) << 32;   // stride byte offset
-    d |= 1ull << 46;                      // descriptor version of sm_100
-    d |= 2ull << 61;                      // SWIZZLE_128B
-    return d;
 }
 // The same for rows of 64 bytes with the 64-byte swizzle: groups of eight rows 512 bytes apart.
 __device__ __forceinline__ uint64_t smem_desc_sw64(uint32_t addr) {
@@ -169,27 +143,6 @@ __device__ __forceinline__ void umma_mxf4(uint32_t tmem_d, uint64_t adesc, uint6
 __device__ __forceinline__ void umma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr) : "memory");
-}
-// Completes every tcgen05.ld issued so far.  The registers are passed through so that no use of them can be
-// scheduled ahead of the wait.
-__device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[32]) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-        : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
-          "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
-          "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
-          "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
-        :: "memory");
-}
-
 // Zeroes 32 accumulator columns of the calling warp's 32 lanes.  Every epilogue warp does this to the columns it has
 // read (and every buffer is zeroed once at kernel start), so that every MMA of a tile ACCUMULATES: with an overwriting
 // first MMA the second issuing thread had to wait at the start of every tile until that MMA had completed, and the tensor
@@ -810,22 +763,6 @@ template <int BN> struct Cfg2 {
     static constexpr uint32_t STAGE_BYTES = A_BYTES + (BN / 2) * BK;    // own A rows + own half of the tile's B rows
     static constexpr int STAGES = (BN == 256) ? 6 : 7;                  // 192 / 196 KB
 };
-constexpr uint32_t PEER_MASK = 0xFEFFFFFFu;              // clears the CTA-rank bit of a shared::cluster address -> CTA 0 of the pair
-
-__device__ __forceinline__ uint32_t cluster_ctarank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync_all() {
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void tma_load_2d_2sm(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
-}
 __device__ __forceinline__ void tma_load_4d_2sm(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, int c3, uint32_t bar) {
     asm volatile(
         "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
@@ -838,22 +775,6 @@ __device__ __forceinline__ void umma_i8_2sm(uint32_t tmem_d, uint64_t adesc, uin
         "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
         ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
 }
-// Arrives on the barrier at this shared-memory offset in both CTAs of the pair once the MMAs issued so far are done.
-__device__ __forceinline__ void umma_commit_2sm(uint32_t bar) {
-    const uint16_t mask = 3;
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(bar), "h"(mask) : "memory");
-}
-// Arrive on the barrier at the same offset in CTA 0 of the cluster.  Relaxed: the barrier hands back tensor memory, whose
-// reads are ordered by tcgen05.wait::ld and the tcgen05 fence before the arrival; nothing written to memory is passed
-// on through it.  (With release semantics at cluster scope the arrival waited for the epilogue's global stores to
-// complete: ~3800 clocks per tile, during which the issuing warps could not reuse the accumulator buffer.)
-__device__ __forceinline__ void mbar_arrive_cta0(uint32_t bar) {
-    uint32_t remote;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(remote) : "r"(bar));
-    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(remote) : "memory");
-}
-
 // A failed wait in one CTA of a pair: recorded locally (fail) and in the partner's control block, so that the partner's
 // waiters stop at their next look instead of each running into the limit.  Both CTAs stay resident until the
 // cluster-wide barrier at the end of the kernel, so the partner's shared memory is there to be written.
@@ -1800,6 +1721,19 @@ extern "C" int bnn_expand_signs_f4(bnn_ctx *ctx, const uint32_t *src, int64_t ld
     return bnn_umma_expand_f4(ctx, src, ld_w, rows, K, dst);
 }
 
+int bnn_tensor_map16(bnn_ctx *ctx, CUtensorMap *map, const void *base, int64_t rows, int64_t cols, int64_t ld, int box_rows, int box_cols) {
+    encode_fn_t enc;
+    if (int st = get_encode(ctx, &enc)) return st;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
+    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, estr[2] = {1, 1};
+    const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void *>(base), dims, strides, box, estr,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) { ctx->last_cuda_error = (int)r; return BNN_ERR_CUDA; }
+    return BNN_OK;
+}
+
 // Reads (and clears) the error word the tensor-core kernel sets when one of its bounded waits gives up.
 // Synchronises the context's stream.
 #ifdef BNN_TRACE
@@ -1848,10 +1782,9 @@ extern "C" int bnn_device_status(bnn_ctx *ctx) {
     BNN_CUDA_TRY(ctx, cudaStreamSynchronize(ctx->stream));
     int code = 0;
     BNN_CUDA_TRY(ctx, cudaMemcpyFromSymbol(&code, g_umma_error, sizeof(int)));
-    if (code != 0) {
-        const int zero = 0;
-        BNN_CUDA_TRY(ctx, cudaMemcpyToSymbol(g_umma_error, &zero, sizeof(int)));
-        return BNN_ERR_DEVICE_STATUS;
-    }
-    return BNN_OK;
+    const int zero = 0;
+    if (code != 0) BNN_CUDA_TRY(ctx, cudaMemcpyToSymbol(g_umma_error, &zero, sizeof(int)));
+    int product = 0;
+    if (int st = bnn_product_status(ctx, &product)) return st;
+    return code != 0 || product != 0 ? BNN_ERR_DEVICE_STATUS : BNN_OK;
 }
