@@ -471,14 +471,16 @@ class Context:
         """Checks a row-major matrix; returns (address, leading dimension)."""
         if t is None:
             return None, 0
-        if t.dtype is not dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.get_device() != self.device:
+        if t.dtype is not dtype or t.shape != (rows, cols) or t.get_device() != self.device:
             raise ValueError(f"{what}: expected {dtype} [{rows}, {cols}] on cuda:{self.device}, got {t.dtype} {list(t.shape)} on {t.device}")
         ld, step = t.stride()
         if step != 1 and cols > 1 and rows:
             raise ValueError(f"{what}: rows must be contiguous (row-major), strides are {t.stride()}")
-        if rows > 1 and ld < cols:
+        if rows <= 1:
+            return t.data_ptr(), cols
+        if ld < cols:
             raise ValueError(f"{what}: rows overlap, strides are {t.stride()}")
-        return t.data_ptr(), ld if rows > 1 else cols
+        return t.data_ptr(), ld
 
     def _vector(self, t, n, dtype, what):
         if t is None:
@@ -499,6 +501,10 @@ class Context:
             t = torch.empty(shape, dtype=dtype, device=self._device)
         t.record_stream(torch.cuda.current_stream(self.device))
         return t
+
+    def _like(self, x):
+        """A contiguous matrix of x's shape and type."""
+        return torch.empty_like(x) if x.is_contiguous() and not self._elsewhere() else self._new(*x.shape, dtype=x.dtype)
 
     def _used(self, *tensors):
         """Keeps the memory of tensors of another stream until the work queued on the context's stream is done with it."""
@@ -549,7 +555,7 @@ class Context:
                                                        (pre_shift, "pre_shift"))]
         d = BlockNormDesc(_REAL_TYPES[dtype], NORMS[kind], D, eps, alpha, int(post), int(pre), *v, gp, gl, rows_per_gate or 1)
         layer = Layer(d, dtype, self.device, D, D, (post_weight, post_shift, pre_weight, pre_shift, gate))
-        layer.gates = gate.shape[0] if gate is not None else 0
+        layer.gates, layer.pre = gate.shape[0] if gate is not None else 0, bool(pre)
         return layer
 
     @staticmethod
@@ -575,7 +581,9 @@ class Context:
         pp, ldp = self._fit(pre, M, N, torch.float32, "pre")
         if out is None:
             out = self._new(M, N, dtype=layer.dtype)
-        op, ldo = self._fit(out, M, N, layer.dtype, "out")
+            op, ldo = out.data_ptr(), N
+        else:
+            op, ldo = self._fit(out, M, N, layer.dtype, "out")
         self._ck(lib().bnn_linear(self._h, layer.ref, xp, ldx, M, rp, ldr, op, ldo, pp, ldp), "bnn_linear")
         self._used(x, residual, out, pre, *layer.tensors)
         return out
@@ -601,7 +609,9 @@ class Context:
         pp, ldp = self._planes(pre, M, N)
         if out is None:
             out = self._new(M, N, dtype=layer.dtype)
-        op, ldo = self._fit(out, M, N, layer.dtype, "out")
+            op, ldo = out.data_ptr(), N
+        else:
+            op, ldo = self._fit(out, M, N, layer.dtype, "out")
         self._ck(lib().bnn_gated(self._h, layer.ref, xp, ldx, M, op, ldo, pp, ldp), "bnn_gated")
         self._used(x, out, pre, *layer.tensors)
         return out
@@ -641,11 +651,15 @@ class Context:
         if stats is not None and M > 1 and ldt != 4:
             raise ValueError("stats: expected a contiguous tensor")
         if stream is None:
-            stream = self._new(M, D, dtype=layer.dtype)
-        if normed is None and layer.desc.pre:
-            normed = self._new(M, D, dtype=layer.dtype)
-        sp, lds = self._fit(stream, M, D, layer.dtype, "stream")
-        np_, ldn = self._fit(normed, M, D, layer.dtype, "normed")
+            stream = self._like(x)
+            sp, lds = stream.data_ptr(), D
+        else:
+            sp, lds = self._fit(stream, M, D, layer.dtype, "stream")
+        if normed is None and layer.pre:
+            normed = self._like(x)
+            np_, ldn = normed.data_ptr(), D
+        else:
+            np_, ldn = self._fit(normed, M, D, layer.dtype, "normed")
         self._ck(lib().bnn_block_norm(self._h, layer.ref, xp, ldx, bp, ldb, M, sp, lds, np_, ldn, tp), "bnn_block_norm")
         self._used(x, block, stream, normed, stats, *layer.tensors)
         return stream, normed
@@ -667,7 +681,7 @@ class Context:
         def like(t, wanted=True):
             return self._new(D, dtype=layer.dtype) if t is not None and wanted else None
 
-        out = {"dx": self._new(M, D, dtype=layer.dtype), "dblock": self._new(M, D, dtype=layer.dtype) if block is not None else None,
+        out = {"dx": self._like(x), "dblock": self._like(x) if block is not None else None,
                "dgate": None, "dpost_weight": like(post_w, d.post), "dpost_shift": like(post_c, d.post),
                "dpre_weight": like(pre_w, d.pre), "dpre_shift": like(pre_c, d.pre)}
         if gate is not None and block is not None:
@@ -696,8 +710,10 @@ class Context:
         xp, ldx = self._fit(x, M, D, x.dtype, "x")
         rp, ldr = self._fit(residual, M, D, x.dtype, "residual")
         if out is None:
-            out = self._new(M, D, dtype=x.dtype)
-        op, ldo = self._fit(out, M, D, x.dtype, "out")
+            out = self._like(x)
+            op, ldo = out.data_ptr(), D
+        else:
+            op, ldo = self._fit(out, M, D, x.dtype, "out")
         self._ck(lib().bnn_dropout(self._h, _REAL_TYPES[x.dtype], xp, ldx, rp, ldr, op, ldo, M, D, p, seed, offset), "bnn_dropout")
         self._used(x, residual, out)
         return out

@@ -39,30 +39,49 @@ struct NormArgs {
 
 constexpr int PRE_W = 1, PRE_C = 2, POST_W = 4, POST_C = 8;
 
-// Eight columns of one row per thread and slot.  VEC: eight neighbouring columns in 16-byte accesses; otherwise (odd pitches
-// or widths) columns a team apart, so that neighbouring threads still read neighbouring elements.
+// Eight columns of one row per thread and slot, as they are in memory.  VEC: neighbouring columns in 16-byte accesses; otherwise
+// (odd pitches or widths) columns a team apart, so that neighbouring threads still touch neighbouring elements.
+template <typename T> struct Eight {
+    uint32_t w[2 * sizeof(T)];
+    __device__ __forceinline__ float operator[](int j) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[j]);
+        else { const float2 f = unpack2<T>(w[j >> 1]); return (j & 1) ? f.y : f.x; }
+    }
+    __device__ __forceinline__ void fill(float v) {
+#pragma unroll
+        for (int i = 0; i < (int)(2 * sizeof(T)); ++i) {
+            if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(v);
+            else w[i] = pack2<T>(v, v);
+        }
+    }
+};
 template <bool VEC> __device__ __forceinline__ int column(int slot, int j, int tid, int team) {
     return VEC ? (slot * team + tid) * 8 + j : (slot * 8 + j) * team + tid;
 }
-template <typename T, bool VEC>
-__device__ __forceinline__ void read_row(const T *row, int slot, int tid, int team, int D, float (&v)[8]) {
+template <typename T, bool VEC> __device__ __forceinline__ Eight<T> read8(const T *row, int slot, int tid, int team, int D) {
+    Eight<T> e;
     if constexpr (VEC) {
         const int c = column<true>(slot, 0, tid, team);
-        if (c < D) load8(row + c, v);
-        else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+            const uint4 q = c < D ? reinterpret_cast<const uint4 *>(row + c)[i] : make_uint4(0u, 0u, 0u, 0u);
+            e.w[4 * i] = q.x; e.w[4 * i + 1] = q.y; e.w[4 * i + 2] = q.z; e.w[4 * i + 3] = q.w;
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int c = column<false>(slot, j, tid, team);
-            v[j] = c < D ? to_f32(row[c]) : 0.0f;
+        for (int j = 0; j < 8; j += 8 / (2 * (int)sizeof(T))) {
+            const int c = column<false>(slot, j, tid, team), c1 = c + team;
+            if constexpr (sizeof(T) == 4) e.w[j] = c < D ? __float_as_uint(row[c]) : 0u;
+            else {
+                const uint16_t *bits = reinterpret_cast<const uint16_t *>(row);
+                e.w[j >> 1] = (c < D ? bits[c] : 0u) | ((c1 < D ? (uint32_t)bits[c1] : 0u) << 16);
+            }
         }
     }
+    return e;
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void write_row(T *row, int slot, int tid, int team, int D, const float (&v)[8]) {
+__device__ __forceinline__ void write8(T *row, int slot, int tid, int team, int D, const float (&v)[8]) {
     if constexpr (VEC) {
         const int c = column<true>(slot, 0, tid, team);
         if (c < D) store8(row + c, v);
@@ -82,264 +101,262 @@ __device__ __forceinline__ float warp_sum(float v) {
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
-// Sums of two values over the block, in a fixed order; `slots` alternates between two buffers so that one barrier per sum is enough.
-__device__ __forceinline__ float2 block_sum2(float a, float b, float2 *buf, int warps, int warp, int lane) {
-    a = warp_sum(a); b = warp_sum(b);
+// Sums over the block in a fixed order.  One barrier each: successive sums use different buffers.
+__device__ __forceinline__ float block_sum(float a, float *buf, int warps, int warp, int lane) {
+    a = warp_sum(a);
+    if (warps == 1) return a;
+    if (lane == 0) buf[warp] = a;
+    __syncthreads();
+    return warp_sum(lane < warps ? buf[lane] : 0.0f);
+}
+template <bool BOTH> __device__ __forceinline__ float2 block_sum2(float a, float b, float2 *buf, int warps, int warp, int lane) {
+    a = warp_sum(a);
+    if (BOTH) b = warp_sum(b);
     if (warps == 1) return make_float2(a, b);
     if (lane == 0) buf[warp] = make_float2(a, b);
     __syncthreads();
     const float2 t = lane < warps ? buf[lane] : make_float2(0.0f, 0.0f);
-    return make_float2(warp_sum(t.x), warp_sum(t.y));
+    return make_float2(warp_sum(t.x), BOTH ? warp_sum(t.y) : 0.0f);
 }
 
-template <typename T, int SLOTS, bool VEC>
-__global__ void __launch_bounds__(1024) k_block_norm(const NormArgs p) {
-    __shared__ float2 buf[4][32];
+// One row per CTA: both rows are requested before anything is computed from them.
+template <typename T, int SLOTS, int THREADS, bool VEC>
+__global__ void __launch_bounds__(THREADS, 1) k_block_norm(const NormArgs p) {
+    __shared__ float buf[4][32];
     const int tid = threadIdx.x, team = blockDim.x, warps = team >> 5, warp = tid >> 5, lane = tid & 31;
     const T *pw = static_cast<const T *>(p.post_w), *pc = static_cast<const T *>(p.post_c);
     const T *nw = static_cast<const T *>(p.pre_w), *nc = static_cast<const T *>(p.pre_c);
-    for (int64_t m = blockIdx.x; m < p.M; m += gridDim.x) {
-        float s[SLOTS][8];
-        {
-            const T *x = static_cast<const T *>(p.x) + m * p.ldx;
+    const int64_t m = blockIdx.x;
+    bnn_pdl_wait();
+    bnn_pdl_launch_next();
+    Eight<T> rx[SLOTS], rb[SLOTS];
 #pragma unroll
-            for (int i = 0; i < SLOTS; ++i) {
-                read_row<T, VEC>(x, i, tid, team, p.D, s[i]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) s[i][j] *= p.alpha;
-            }
-        }
-        if (p.block) {
-            const T *b = static_cast<const T *>(p.block) + m * p.ldb;
-            const T *gate = p.gate ? static_cast<const T *>(p.gate) + (m / p.rows_per_gate) * p.ld_gate : nullptr;
-            float v[SLOTS][8];
-#pragma unroll
-            for (int i = 0; i < SLOTS; ++i) read_row<T, VEC>(b, i, tid, team, p.D, v[i]);
-            if (p.post) {
-                float mean = 0.0f;
-                if (p.layer) {
-                    float t = 0.0f;
-#pragma unroll
-                    for (int i = 0; i < SLOTS; ++i)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) t += v[i][j];
-                    mean = block_sum2(t, 0.0f, buf[0], warps, warp, lane).x * p.inv_d;
-                }
-                float q = 0.0f;
-#pragma unroll
-                for (int i = 0; i < SLOTS; ++i)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        v[i][j] = inside<VEC>(i, j, tid, team, p.D) ? v[i][j] - mean : 0.0f;
-                        q += v[i][j] * v[i][j];
-                    }
-                const float r = 1.0f / sqrtf(block_sum2(q, 0.0f, buf[1], warps, warp, lane).x * p.inv_d + p.eps);
-                if (p.stats && tid == 0) { p.stats[4 * m] = mean; p.stats[4 * m + 1] = r; }
-#pragma unroll
-                for (int i = 0; i < SLOTS; ++i) {
-                    float w[8], c[8];
-                    if (pw) read_row<T, VEC>(pw, i, tid, team, p.D, w);
-                    if (pc) read_row<T, VEC>(pc, i, tid, team, p.D, c);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        v[i][j] *= r;
-                        if (pw) v[i][j] *= w[j];
-                        if (pc) v[i][j] += c[j];
-                    }
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < SLOTS; ++i) {
-                float g[8];
-                if (gate) read_row<T, VEC>(gate, i, tid, team, p.D, g);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) s[i][j] += gate ? g[j] * v[i][j] : v[i][j];
-            }
-        }
-        if (p.stream) {
-            T *out = static_cast<T *>(p.stream) + m * p.lds;
-#pragma unroll
-            for (int i = 0; i < SLOTS; ++i) write_row<T, VEC>(out, i, tid, team, p.D, s[i]);
-        }
-        if (p.pre) {
-            float mean = 0.0f;
+    for (int i = 0; i < SLOTS; ++i) {
+        rx[i] = read8<T, VEC>(static_cast<const T *>(p.x) + m * p.ldx, i, tid, team, p.D);
+        if (p.block) rb[i] = read8<T, VEC>(static_cast<const T *>(p.block) + m * p.ldb, i, tid, team, p.D);
+    }
+    float s[SLOTS][8];
+    if (p.block) {
+        const T *gate = p.gate ? static_cast<const T *>(p.gate) + (m / p.rows_per_gate) * p.ld_gate : nullptr;
+        float mean = 0.0f, r = 1.0f;
+        if (p.post) {
             if (p.layer) {
                 float t = 0.0f;
 #pragma unroll
                 for (int i = 0; i < SLOTS; ++i)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) t += inside<VEC>(i, j, tid, team, p.D) ? s[i][j] : 0.0f;
-                mean = block_sum2(t, 0.0f, buf[2], warps, warp, lane).x * p.inv_d;
+                    for (int j = 0; j < 8; ++j) t += rb[i][j];
+                mean = block_sum(t, buf[0], warps, warp, lane) * p.inv_d;
             }
             float q = 0.0f;
 #pragma unroll
             for (int i = 0; i < SLOTS; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    s[i][j] = inside<VEC>(i, j, tid, team, p.D) ? s[i][j] - mean : 0.0f;
-                    q += s[i][j] * s[i][j];
+                    const float v = inside<VEC>(i, j, tid, team, p.D) ? rb[i][j] - mean : 0.0f;
+                    q += v * v;
                 }
-            const float r = 1.0f / sqrtf(block_sum2(q, 0.0f, buf[3], warps, warp, lane).x * p.inv_d + p.eps);
-            if (p.stats && tid == 0) { p.stats[4 * m + 2] = mean; p.stats[4 * m + 3] = r; }
-            if (p.normed) {
-                T *out = static_cast<T *>(p.normed) + m * p.ldn;
+            r = 1.0f / sqrtf(block_sum(q, buf[1], warps, warp, lane) * p.inv_d + p.eps);
+            if (p.stats && tid == 0) { p.stats[4 * m] = mean; p.stats[4 * m + 1] = r; }
+        }
 #pragma unroll
-                for (int i = 0; i < SLOTS; ++i) {
-                    float w[8], c[8];
-                    if (nw) read_row<T, VEC>(nw, i, tid, team, p.D, w);
-                    if (nc) read_row<T, VEC>(nc, i, tid, team, p.D, c);
+        for (int i = 0; i < SLOTS; ++i) {
+            Eight<T> w, c, g;
+            if (pw) w = read8<T, VEC>(pw, i, tid, team, p.D);
+            if (pc) c = read8<T, VEC>(pc, i, tid, team, p.D);
+            if (gate) g = read8<T, VEC>(gate, i, tid, team, p.D);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        s[i][j] *= r;
-                        if (nw) s[i][j] *= w[j];
-                        if (nc) s[i][j] += c[j];
-                    }
-                    write_row<T, VEC>(out, i, tid, team, p.D, s[i]);
-                }
+            for (int j = 0; j < 8; ++j) {
+                float v = (rb[i][j] - mean) * r;
+                if (pw) v *= w[j];
+                if (pc) v += c[j];
+                if (gate) v *= g[j];
+                s[i][j] = p.alpha * rx[i][j] + v;
             }
         }
-        if (warps > 1) __syncthreads();      // the next row reuses the buffers
+    } else {
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[i][j] = p.alpha * rx[i][j];
+    }
+    if (p.stream) {
+        T *out = static_cast<T *>(p.stream) + m * p.lds;
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) write8<T, VEC>(out, i, tid, team, p.D, s[i]);
+    }
+    if (!p.pre) return;
+    float mean = 0.0f;
+    if (p.layer) {
+        float t = 0.0f;
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) t += inside<VEC>(i, j, tid, team, p.D) ? s[i][j] : 0.0f;
+        mean = block_sum(t, buf[2], warps, warp, lane) * p.inv_d;
+    }
+    float q = 0.0f;
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            s[i][j] = inside<VEC>(i, j, tid, team, p.D) ? s[i][j] - mean : 0.0f;
+            q += s[i][j] * s[i][j];
+        }
+    const float r = 1.0f / sqrtf(block_sum(q, buf[3], warps, warp, lane) * p.inv_d + p.eps);
+    if (p.stats && tid == 0) { p.stats[4 * m + 2] = mean; p.stats[4 * m + 3] = r; }
+    if (!p.normed) return;
+    T *out = static_cast<T *>(p.normed) + m * p.ldn;
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+        Eight<T> w, c;
+        if (nw) w = read8<T, VEC>(nw, i, tid, team, p.D);
+        if (nc) c = read8<T, VEC>(nc, i, tid, team, p.D);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            s[i][j] *= r;
+            if (nw) s[i][j] *= w[j];
+            if (nc) s[i][j] += c[j];
+        }
+        write8<T, VEC>(out, i, tid, team, p.D, s[i]);
     }
 }
 
 // A CTA takes whole units (a unit: chunk_rows rows that share one gate row), so every thread keeps the column sums of its own
-// columns in registers from row to row: the four parameter sums for all its units, the gate's for one unit.
-template <typename T, int SLOTS, bool VEC, int THREADS>
-__global__ void __launch_bounds__(THREADS) k_block_norm_backward(const NormArgs p) {
-    __shared__ float2 buf[2][32];
+// columns in registers from row to row: the four parameter sums for all its units, the gate's for one unit.  The next row is
+// requested before the current one is worked on (SLOTS = 1; wider rows leave no registers for it).
+// PLAIN: no means and no shifts (BNN_NORM_RMS without shift vectors or their gradients): two of the four parameter sums.
+template <typename T, int SLOTS, int THREADS, bool VEC, bool PLAIN>
+__global__ void __launch_bounds__(THREADS, 1) k_block_norm_backward(const NormArgs p) {
+    constexpr bool AHEAD = SLOTS == 1, LAYER = !PLAIN;
+    __shared__ float2 buf[4][32];
     const int tid = threadIdx.x, team = blockDim.x, warps = team >> 5, warp = tid >> 5, lane = tid & 31;
-    const T *pw = static_cast<const T *>(p.post_w), *pc = static_cast<const T *>(p.post_c), *nw = static_cast<const T *>(p.pre_w);
+    const T *pw = static_cast<const T *>(p.post_w), *pc = PLAIN ? nullptr : static_cast<const T *>(p.post_c), *nw = static_cast<const T *>(p.pre_w);
+    const T *X = static_cast<const T *>(p.x), *B = static_cast<const T *>(p.block), *S = static_cast<const T *>(p.ds), *N = static_cast<const T *>(p.dn);
+    const bool inner = p.pre && p.dn;
+    bnn_pdl_wait();
+    bnn_pdl_launch_next();
+    Eight<T> w_post[SLOTS], w_pre[SLOTS], gates[SLOTS];
     float sum_nw[SLOTS][8], sum_nc[SLOTS][8], sum_pw[SLOTS][8], sum_pc[SLOTS][8], sum_g[SLOTS][8];
 #pragma unroll
-    for (int i = 0; i < SLOTS; ++i)
+    for (int i = 0; i < SLOTS; ++i) {
+        if (pw) w_post[i] = read8<T, VEC>(pw, i, tid, team, p.D);
+        if (nw) w_pre[i] = read8<T, VEC>(nw, i, tid, team, p.D);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) { sum_nw[i][j] = 0.0f; sum_nc[i][j] = 0.0f; sum_pw[i][j] = 0.0f; sum_pc[i][j] = 0.0f; }
+        for (int j = 0; j < 8; ++j) {
+            sum_nw[i][j] = 0.0f; sum_nc[i][j] = 0.0f; sum_pw[i][j] = 0.0f; sum_pc[i][j] = 0.0f;
+        }
+        if (!pw) w_post[i].fill(1.0f);
+        if (!nw) w_pre[i].fill(1.0f);
+    }
+    uint32_t turn = 0;                     // rows done: alternates the buffers of the sums
     for (int64_t unit = blockIdx.x; unit < p.units; unit += gridDim.x) {
         const int64_t group = unit / p.chunks, chunk = unit - group * p.chunks;
         const int64_t first = group * p.rows_per_gate + chunk * p.chunk_rows;
         const int64_t group_end = (group + 1) * p.rows_per_gate < p.M ? (group + 1) * p.rows_per_gate : p.M;
         const int64_t end = first + p.chunk_rows < group_end ? first + p.chunk_rows : group_end;
-        const T *gate = p.gate ? static_cast<const T *>(p.gate) + group * p.ld_gate : nullptr;
 #pragma unroll
-        for (int i = 0; i < SLOTS; ++i)
+        for (int i = 0; i < SLOTS; ++i) {
+            if (p.gate) gates[i] = read8<T, VEC>(static_cast<const T *>(p.gate) + group * p.ld_gate, i, tid, team, p.D);
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum_g[i][j] = 0.0f;
-        for (int64_t m = first; m < end; ++m) {
-            float e[SLOTS][8], u[SLOTS][8], bh[SLOTS][8], dn[SLOTS][8];      // dn w_pre; unit rows of the stream and of the block; dn
-            float4 st = make_float4(0.0f, 1.0f, 0.0f, 1.0f);
+            if (!p.gate) gates[i].fill(1.0f);
+        }
+        Eight<T> rx[SLOTS], rb[SLOTS], rs[SLOTS], rn[SLOTS];
+        float4 st = make_float4(0.0f, 1.0f, 0.0f, 1.0f);
+        auto request = [&](int64_t m) {
+#pragma unroll
+            for (int i = 0; i < SLOTS; ++i) {
+                if (B) rb[i] = read8<T, VEC>(B + m * p.ldb, i, tid, team, p.D);
+                if (inner) {
+                    rx[i] = read8<T, VEC>(X + m * p.ldx, i, tid, team, p.D);
+                    rn[i] = read8<T, VEC>(N + m * p.lddn, i, tid, team, p.D);
+                }
+                if (S) rs[i] = read8<T, VEC>(S + m * p.ldds, i, tid, team, p.D);
+            }
             if (p.stats) st = make_float4(p.stats[4 * m], p.stats[4 * m + 1], p.stats[4 * m + 2], p.stats[4 * m + 3]);
-            const float mean_b = p.post ? st.x : 0.0f, r_b = p.post ? st.y : 1.0f;
+        };
+        if (AHEAD && first < end) request(first);
+        for (int64_t m = first; m < end; ++m, turn ^= 1u) {
+            if (!AHEAD) request(m);
+            const float mean_b = p.post ? st.x : 0.0f, r_b = p.post ? st.y : 1.0f, mean_s = st.z, r_s = st.w;
+            float u[SLOTS][8], e[SLOTS][8], bh[SLOTS][8], ds[SLOTS][8];      // unit row of the stream, dn w_pre, unit row of the block
             float a1 = 0.0f, a2 = 0.0f;
 #pragma unroll
             for (int i = 0; i < SLOTS; ++i) {
-                if (p.block) {
-                    read_row<T, VEC>(static_cast<const T *>(p.block) + m * p.ldb, i, tid, team, p.D, bh[i]);
+                Eight<T> c;
+                if (pc) c = read8<T, VEC>(pc, i, tid, team, p.D);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) bh[i][j] = (bh[i][j] - mean_b) * r_b;
-                }
-                if (p.pre && p.dn) {
-                    read_row<T, VEC>(static_cast<const T *>(p.x) + m * p.ldx, i, tid, team, p.D, u[i]);
-                    read_row<T, VEC>(static_cast<const T *>(p.dn) + m * p.lddn, i, tid, team, p.D, dn[i]);
-                    float w[8], c[8], g[8], v[8];
-                    if (pw) read_row<T, VEC>(pw, i, tid, team, p.D, w);
-                    if (pc) read_row<T, VEC>(pc, i, tid, team, p.D, c);
-                    if (gate) read_row<T, VEC>(gate, i, tid, team, p.D, g);
-                    if (nw) read_row<T, VEC>(nw, i, tid, team, p.D, v);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        float q = 0.0f;
-                        if (p.block) {
-                            q = bh[i][j];
-                            if (p.post && pw) q *= w[j];
-                            if (p.post && pc) q += c[j];
-                            if (gate) q *= g[j];
-                        }
-                        const bool in = inside<VEC>(i, j, tid, team, p.D);
-                        u[i][j] = in ? (p.alpha * u[i][j] + q - st.z) * st.w : 0.0f;
-                        e[i][j] = nw ? dn[i][j] * v[j] : dn[i][j];
+                for (int j = 0; j < 8; ++j) {
+                    const bool in = inside<VEC>(i, j, tid, team, p.D);
+                    bh[i][j] = B && in ? (LAYER ? (rb[i][j] - mean_b) * r_b : rb[i][j] * r_b) : 0.0f;
+                    ds[i][j] = S ? rs[i][j] : 0.0f;
+                    if (inner) {
+                        float q = bh[i][j] * w_post[i][j];
+                        if (pc) q += c[j];
+                        const float s = p.alpha * rx[i][j] + q * gates[i][j], d = rn[i][j];
+                        u[i][j] = LAYER ? (in ? (s - mean_s) * r_s : 0.0f) : s * r_s;
+                        e[i][j] = d * w_pre[i][j];
                         a1 += e[i][j] * u[i][j];
-                        a2 += e[i][j];
-                        sum_nw[i][j] += dn[i][j] * u[i][j];
-                        sum_nc[i][j] += dn[i][j];
+                        if (LAYER) a2 += e[i][j];
+                        sum_nw[i][j] += d * u[i][j];
+                        if (!PLAIN) sum_nc[i][j] += d;
                     }
                 }
             }
-            if (p.pre && p.dn) {
-                const float2 t = block_sum2(a1, p.layer ? a2 : 0.0f, buf[0], warps, warp, lane);
-                const float m1 = t.x * p.inv_d, m2 = t.y * p.inv_d;
-#pragma unroll
-                for (int i = 0; i < SLOTS; ++i)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) u[i][j] = st.w * (e[i][j] - u[i][j] * m1 - m2);
-            } else {
-#pragma unroll
-                for (int i = 0; i < SLOTS; ++i)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) u[i][j] = 0.0f;
+            if (AHEAD && m + 1 < end) request(m + 1);
+            float m1 = 0.0f, m2 = 0.0f;
+            if (inner) {
+                const float2 t = block_sum2<LAYER>(a1, a2, buf[turn], warps, warp, lane);
+                m1 = t.x * p.inv_d; m2 = p.layer ? t.y * p.inv_d : 0.0f;
             }
-            // u becomes T, e becomes dp, then its product with w_post
             float b1 = 0.0f, b2 = 0.0f;
 #pragma unroll
             for (int i = 0; i < SLOTS; ++i) {
-                if (p.ds) {
-                    float d[8];
-                    read_row<T, VEC>(static_cast<const T *>(p.ds) + m * p.ldds, i, tid, team, p.D, d);
+                float d[8];
+                Eight<T> c;
+                if (pc) c = read8<T, VEC>(pc, i, tid, team, p.D);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) u[i][j] += d[j];
-                }
-                if (p.dx) {
-                    float d[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) d[j] = p.alpha * u[i][j];
-                    write_row<T, VEC>(static_cast<T *>(p.dx) + m * p.lddx, i, tid, team, p.D, d);
-                }
-                if (p.block) {
-                    float w[8], c[8], g[8];
-                    if (pw) read_row<T, VEC>(pw, i, tid, team, p.D, w);
-                    if (pc) read_row<T, VEC>(pc, i, tid, team, p.D, c);
-                    if (gate) read_row<T, VEC>(gate, i, tid, team, p.D, g);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const bool in = inside<VEC>(i, j, tid, team, p.D);
-                        const float tj = in ? u[i][j] : 0.0f;
-                        const float unit_b = in ? bh[i][j] : 0.0f;
-                        float q = unit_b;
-                        if (p.post && pw) q *= w[j];
-                        if (p.post && pc) q += c[j];
-                        sum_g[i][j] += tj * q;
-                        const float dp = gate ? g[j] * tj : tj;
-                        e[i][j] = dp;
-                        bh[i][j] = unit_b;
-                        if (p.post) {
-                            sum_pw[i][j] += dp * unit_b;
-                            sum_pc[i][j] += dp;
-                            e[i][j] = pw ? dp * w[j] : dp;
-                            b1 += e[i][j] * unit_b;
-                            b2 += e[i][j];
-                        }
+                for (int j = 0; j < 8; ++j) {
+                    const bool in = VEC || inside<VEC>(i, j, tid, team, p.D);
+                    float t = ds[i][j];
+                    if (inner) t += r_s * (e[i][j] - u[i][j] * m1 - (LAYER ? m2 : 0.0f));
+                    d[j] = p.alpha * t;
+                    if (B) {
+                        const float w = w_post[i][j];
+                        float q = bh[i][j] * w;
+                        if (pc) q += c[j];
+                        sum_g[i][j] += t * q;
+                        const float dp = gates[i][j] * t;
+                        e[i][j] = in ? dp * w : 0.0f;
+                        if (LAYER && VEC && !inside<VEC>(i, j, tid, team, p.D)) e[i][j] = 0.0f;
+                        sum_pw[i][j] += dp * bh[i][j];
+                        if (!PLAIN) sum_pc[i][j] += dp;
+                        b1 += e[i][j] * bh[i][j];
+                        if (LAYER) b2 += e[i][j];
                     }
                 }
+                if (p.dx) write8<T, VEC>(static_cast<T *>(p.dx) + m * p.lddx, i, tid, team, p.D, d);
             }
-            if (p.block && p.db) {
-                float m1 = 0.0f, m2 = 0.0f;
+            if (B && p.db) {
+                m1 = m2 = 0.0f;
                 if (p.post) {
-                    const float2 t = block_sum2(b1, p.layer ? b2 : 0.0f, buf[1], warps, warp, lane);
-                    m1 = t.x * p.inv_d; m2 = t.y * p.inv_d;
+                    const float2 t = block_sum2<LAYER>(b1, b2, buf[2 + turn], warps, warp, lane);
+                    m1 = t.x * p.inv_d; m2 = p.layer ? t.y * p.inv_d : 0.0f;
                 }
 #pragma unroll
                 for (int i = 0; i < SLOTS; ++i) {
                     float d[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) d[j] = p.post ? r_b * (e[i][j] - bh[i][j] * m1 - m2) : e[i][j];
-                    write_row<T, VEC>(static_cast<T *>(p.db) + m * p.lddb, i, tid, team, p.D, d);
+                    for (int j = 0; j < 8; ++j) d[j] = p.post ? r_b * (e[i][j] - bh[i][j] * m1 - (LAYER ? m2 : 0.0f)) : e[i][j];
+                    write8<T, VEC>(static_cast<T *>(p.db) + m * p.lddb, i, tid, team, p.D, d);
                 }
             }
-            if (warps > 1) __syncthreads();
         }
         if (p.dgate) {
 #pragma unroll
             for (int i = 0; i < SLOTS; ++i) {
-                if (p.chunks == 1) write_row<T, VEC>(static_cast<T *>(p.dgate) + group * p.ld_dgate, i, tid, team, p.D, sum_g[i]);
+                if (p.chunks == 1) write8<T, VEC>(static_cast<T *>(p.dgate) + group * p.ld_dgate, i, tid, team, p.D, sum_g[i]);
                 else {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
@@ -358,9 +375,9 @@ __global__ void __launch_bounds__(THREADS) k_block_norm_backward(const NormArgs 
             const int c = column<VEC>(i, j, tid, team);
             if (c >= p.D) continue;
             if (p.want & PRE_W) part[c] = sum_nw[i][j];
-            if (p.want & PRE_C) part[p.D + c] = sum_nc[i][j];
+            if (!PLAIN && (p.want & PRE_C)) part[p.D + c] = sum_nc[i][j];
             if (p.want & POST_W) part[2 * p.D + c] = sum_pw[i][j];
-            if (p.want & POST_C) part[3 * p.D + c] = sum_pc[i][j];
+            if (!PLAIN && (p.want & POST_C)) part[3 * p.D + c] = sum_pc[i][j];
         }
 }
 
@@ -376,6 +393,8 @@ template <typename T>
 __global__ void __launch_bounds__(256) k_join_columns(const JoinArgs p) {
     __shared__ float sum[8][33];
     const int which = blockIdx.y, cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
+    bnn_pdl_wait();
+    bnn_pdl_launch_next();
     if (!p.out[which]) return;
     const int c = blockIdx.x * 32 + cx;
     for (int64_t o = blockIdx.z; o < p.outs[which]; o += gridDim.z) {
@@ -397,9 +416,8 @@ __global__ void __launch_bounds__(256) k_join_columns(const JoinArgs p) {
 int launch_join(bnn_ctx *ctx, int dtype, const JoinArgs &j, int sums) {
     const int outs = j.outs[sums - 1];
     const dim3 grid((unsigned)((j.D + 31) / 32), (unsigned)sums, (unsigned)(outs > 1 ? (outs < 1024 ? outs : 1024) : 1));
-    if (dtype == BNN_F32) k_join_columns<float><<<grid, 256, 0, ctx->stream>>>(j);
-    else if (dtype == BNN_F16) k_join_columns<__half><<<grid, 256, 0, ctx->stream>>>(j);
-    else k_join_columns<__nv_bfloat16><<<grid, 256, 0, ctx->stream>>>(j);
+    auto kernel = dtype == BNN_F32 ? k_join_columns<float> : dtype == BNN_F16 ? k_join_columns<__half> : k_join_columns<__nv_bfloat16>;
+    BNN_CUDA_TRY(ctx, bnn_launch_dependent(kernel, grid, dim3(256), 0, ctx->stream, j));
     return bnn_check_launch(ctx);
 }
 
@@ -441,24 +459,36 @@ bool norm_vec(const bnn_block_norm_desc *n, int64_t M, const NormArgs &a) {
     return true;
 }
 
-template <typename T, bool VEC> void launch_forward(bnn_ctx *ctx, const NormArgs &a) {
+// Teams.  Forward: many rows take four slots a thread (few warps per row, few barriers, many rows in flight), few rows one slot
+// (the shortest chain for a single token).  Backward: one slot up to 8192 columns, so that the column sums fit the registers.
+template <typename T, bool VEC> int launch_forward(bnn_ctx *ctx, const NormArgs &a) {
     const int groups = (a.D + 7) / 8;
-    const int slots = groups <= 1024 ? 1 : groups <= 2048 ? 2 : 4;
+    const bool few = a.M <= 2 * ctx->sm_count;
+    const int slots = groups > 1024 ? 4 : (few || groups <= 32) ? 1 : groups <= 64 ? 2 : 4;
     const int team = ((groups + slots - 1) / slots + 31) & ~31;
-    const int64_t most = (int64_t)ctx->sm_count * 16;
-    const dim3 grid((unsigned)(a.M < most ? a.M : most));
-    if (slots == 1) k_block_norm<T, 1, VEC><<<grid, team, 0, ctx->stream>>>(a);
-    else if (slots == 2) k_block_norm<T, 2, VEC><<<grid, team, 0, ctx->stream>>>(a);
-    else k_block_norm<T, 4, VEC><<<grid, team, 0, ctx->stream>>>(a);
+    const dim3 grid((unsigned)a.M), block(team);
+    if (slots == 1) BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_block_norm<T, 1, 1024, VEC>, grid, block, 0, ctx->stream, a));
+    else if (slots == 2) BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_block_norm<T, 2, 256, VEC>, grid, block, 0, ctx->stream, a));
+    else if (team <= 256) BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_block_norm<T, 4, 256, VEC>, grid, block, 0, ctx->stream, a));
+    else BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_block_norm<T, 4, 1024, VEC>, grid, block, 0, ctx->stream, a));
+    return bnn_check_launch(ctx);
 }
-template <typename T, bool VEC> void launch_backward(bnn_ctx *ctx, const NormArgs &a, unsigned ctas) {
-    const int groups = (a.D + 7) / 8;
-    const int slots = groups <= 1024 ? 1 : groups <= 2048 ? 2 : 4;
-    const int team = ((groups + slots - 1) / slots + 31) & ~31;
-    if (slots == 1 && team <= 512) k_block_norm_backward<T, 1, VEC, 512><<<ctas, team, 0, ctx->stream>>>(a);
-    else if (slots == 1) k_block_norm_backward<T, 1, VEC, 1024><<<ctas, team, 0, ctx->stream>>>(a);
-    else if (slots == 2) k_block_norm_backward<T, 2, VEC, 1024><<<ctas, team, 0, ctx->stream>>>(a);
-    else k_block_norm_backward<T, 4, VEC, 1024><<<ctas, team, 0, ctx->stream>>>(a);
+int backward_slots(int64_t D) { return D <= 8192 ? 1 : D <= 16384 ? 2 : 4; }
+int backward_team(int64_t D) {
+    const int groups = (int)((D + 7) / 8), slots = backward_slots(D);
+    return ((groups + slots - 1) / slots + 31) & ~31;
+}
+template <typename T, bool VEC> int launch_backward(bnn_ctx *ctx, const NormArgs &a, unsigned ctas) {
+    const int slots = backward_slots(a.D), team = backward_team(a.D);
+    const bool plain = VEC && !a.layer && !a.post_c && !(a.want & (PRE_C | POST_C));
+    const dim3 grid(ctas), block(team);
+    if (slots == 1 && team <= 512 && plain) BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_block_norm_backward<T, 1, 512, VEC, VEC>, grid, block, 0, ctx->stream, a));
+    else if (slots == 1 && team <= 512) BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_block_norm_backward<T, 1, 512, VEC, false>, grid, block, 0, ctx->stream, a));
+    else if (slots == 1 && plain) BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_block_norm_backward<T, 1, 1024, VEC, VEC>, grid, block, 0, ctx->stream, a));
+    else if (slots == 1) BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_block_norm_backward<T, 1, 1024, VEC, false>, grid, block, 0, ctx->stream, a));
+    else if (slots == 2) BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_block_norm_backward<T, 2, 1024, VEC, false>, grid, block, 0, ctx->stream, a));
+    else BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_block_norm_backward<T, 4, 1024, VEC, false>, grid, block, 0, ctx->stream, a));
+    return bnn_check_launch(ctx);
 }
 
 // How the rows of the backward pass are divided: units of rows that share a gate row, at least `ctas` of them if the rows allow.
@@ -475,7 +505,11 @@ Division divide_rows(int64_t M, int64_t rows_per_gate, int64_t ctas) {
     d.ctas = d.units < ctas ? d.units : ctas;
     return d;
 }
-constexpr int64_t NORM_CTAS = 296;          // two per SM
+// CTAs of the backward pass: 512 threads per SM (their registers hold the column sums), at most eight CTAs.
+int64_t norm_ctas(int64_t D) {
+    const int per = 512 / backward_team(D);
+    return 148 * (per < 1 ? 1 : per > 8 ? 8 : per);
+}
 size_t norm_part_floats(const Division &d, int64_t D) { return (size_t)d.ctas * 4 * D + (d.chunks > 1 ? (size_t)d.units * D : 0); }
 
 }  // namespace
@@ -504,15 +538,14 @@ extern "C" int bnn_block_norm(bnn_ctx *ctx, const bnn_block_norm_desc *norm, con
     NormArgs a = norm_args(norm, M);
     a.x = x; a.ldx = ldx; a.block = block; a.ldb = ldb; a.stream = stream; a.lds = lds; a.normed = normed; a.ldn = ldn; a.stats = stats;
     const bool vec = norm_vec(norm, M, a);
-    if (norm->dtype == BNN_F32) vec ? launch_forward<float, true>(ctx, a) : launch_forward<float, false>(ctx, a);
-    else if (norm->dtype == BNN_F16) vec ? launch_forward<__half, true>(ctx, a) : launch_forward<__half, false>(ctx, a);
-    else vec ? launch_forward<__nv_bfloat16, true>(ctx, a) : launch_forward<__nv_bfloat16, false>(ctx, a);
-    return bnn_check_launch(ctx);
+    if (norm->dtype == BNN_F32) return vec ? launch_forward<float, true>(ctx, a) : launch_forward<float, false>(ctx, a);
+    if (norm->dtype == BNN_F16) return vec ? launch_forward<__half, true>(ctx, a) : launch_forward<__half, false>(ctx, a);
+    return vec ? launch_forward<__nv_bfloat16, true>(ctx, a) : launch_forward<__nv_bfloat16, false>(ctx, a);
 }
 
 extern "C" size_t bnn_block_norm_workspace_bytes(const bnn_block_norm_desc *norm, int64_t M) {
     if (check_norm(norm, M) || M == 0) return 0;
-    return (norm_part_floats(divide_rows(M, norm->gate ? norm->rows_per_gate : M, NORM_CTAS), norm->D) * 4 + 255) & ~size_t(255);
+    return (norm_part_floats(divide_rows(M, norm->gate ? norm->rows_per_gate : M, norm_ctas(norm->D)), norm->D) * 4 + 255) & ~size_t(255);
 }
 
 extern "C" int bnn_block_norm_backward(bnn_ctx *ctx, const bnn_block_norm_desc *norm, const void *dstream, int64_t ldds, const void *dnormed,
@@ -549,17 +582,19 @@ extern "C" int bnn_block_norm_backward(bnn_ctx *ctx, const bnn_block_norm_desc *
     a.ds = dstream; a.ldds = ldds; a.dn = dnormed; a.lddn = lddn;
     a.dx = g->dx; a.lddx = g->lddx; a.db = g->dblock; a.lddb = g->lddb; a.dgate = g->dgate; a.ld_dgate = g->ld_dgate;
     for (int k = 0; k < 4; ++k) a.want |= sums[k] ? (1 << k) : 0;
-    const Division d = divide_rows(M, a.rows_per_gate, NORM_CTAS);
+    const Division d = divide_rows(M, a.rows_per_gate, norm_ctas(norm->D));
     a.groups = d.groups; a.chunks = d.chunks; a.chunk_rows = d.chunk_rows; a.units = d.units;
     const bool joins = a.want || (a.dgate && d.chunks > 1);
     if (joins && (!ctx->ws || ctx->ws_bytes < norm_part_floats(d, norm->D) * 4)) return BNN_ERR_WORKSPACE;
     a.part = static_cast<float *>(ctx->ws);
     a.part_gate = a.part + (size_t)d.ctas * 4 * norm->D;
     const bool vec = norm_vec(norm, M, a);
-    if (norm->dtype == BNN_F32) vec ? launch_backward<float, true>(ctx, a, (unsigned)d.ctas) : launch_backward<float, false>(ctx, a, (unsigned)d.ctas);
-    else if (norm->dtype == BNN_F16) vec ? launch_backward<__half, true>(ctx, a, (unsigned)d.ctas) : launch_backward<__half, false>(ctx, a, (unsigned)d.ctas);
-    else vec ? launch_backward<__nv_bfloat16, true>(ctx, a, (unsigned)d.ctas) : launch_backward<__nv_bfloat16, false>(ctx, a, (unsigned)d.ctas);
-    if (int st = bnn_check_launch(ctx)) return st;
+    const unsigned ctas = (unsigned)d.ctas;
+    int st;
+    if (norm->dtype == BNN_F32) st = vec ? launch_backward<float, true>(ctx, a, ctas) : launch_backward<float, false>(ctx, a, ctas);
+    else if (norm->dtype == BNN_F16) st = vec ? launch_backward<__half, true>(ctx, a, ctas) : launch_backward<__half, false>(ctx, a, ctas);
+    else st = vec ? launch_backward<__nv_bfloat16, true>(ctx, a, ctas) : launch_backward<__nv_bfloat16, false>(ctx, a, ctas);
+    if (st) return st;
     if (!joins) return BNN_OK;
     JoinArgs j{};
     j.D = (int)norm->D;
