@@ -70,7 +70,7 @@ __device__ __forceinline__ void fail(Control *ctl, int code) {
     atomicCAS(&g_product_error, 0, code);
 }
 // Bounded wait on a phase parity; false once the limit has passed or another wait of the pair has given up (`look`: whether to ask).
-__device__ __forceinline__ bool wait(const Control *ctl, unsigned long long limit, const uint64_t *barrier, uint32_t parity, bool look = true) {
+template <typename C> __device__ __forceinline__ bool wait(const C *ctl, unsigned long long limit, const uint64_t *barrier, uint32_t parity, bool look = true) {
     const uint32_t bar = smem_u32(barrier);
     unsigned long long t0 = 0;
     for (uint32_t i = 0;; ++i) {
@@ -374,6 +374,204 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_produc
 }
 
 // ---------------------------------------------------------------------------------------------------------
+// Few output rows (tokens): k_product_few.  The roles are swapped -- 128 weight rows are the M side of the tensor-core tile and the
+// tokens, 16 to 256 of them, its N side -- so a single token costs a tile of 16 columns and not of 256 rows, and every SM streams
+// weights.  Bound: the weights' bytes (HBM).  The sum is split over the CTAs of a cluster when there are too few tiles of
+// weight rows to keep every SM loading: each takes a share of the K steps, leaves its partial tile in its shared memory, and after a
+// cluster barrier every CTA adds up and finishes its part of the tile through distributed shared memory, in the order of the ranks:
+// one launch, no workspace, the same bits every time.
+// Gated projections: 64 gate rows and the up rows of the same 64 hidden units form the 128 rows of a tile.
+//   warp 0  TMA producer, warp 1  MMA issuer (cta_group::1), warps 2 .. 5  tensor memory -> shared memory, all warps  sum and epilogue
+constexpr int FEW_SMEM = 200 * 1024;
+constexpr int FEW_THREADS = 192;
+constexpr int FEW_STAGES = 12;
+constexpr int FEW_TOKENS = 256;
+constexpr int64_t FEW_ROWS = 256;        // rows from which on the pair kernel is the faster one
+
+struct FewArgs {
+    ProductArgs p;                      // a: weights (a[1]: up rows, or the second pair), b: tokens; M tokens, N outputs
+    int tokens;                         // N of the MMA: tokens per tile, a multiple of 16
+    int stages;
+    uint32_t stage_bytes, tmem_cols;
+};
+struct __align__(16) FewControl {
+    uint64_t full[FEW_STAGES], empty[FEW_STAGES], acc_full;
+    uint32_t tmem_base, failed;
+};
+__device__ __forceinline__ void few_fail(FewControl *ctl, int code) {
+    *reinterpret_cast<volatile uint32_t *>(&ctl->failed) = (uint32_t)code;
+    atomicCAS(&g_product_error, 0, code);
+}
+__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint64_t *bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ float cluster_load(uint32_t addr, uint32_t rank) {
+    uint32_t remote;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
+    return v;
+}
+
+template <int EPI, typename T> __device__ __forceinline__ void finish1(const ProductArgs &p, int64_t m, int64_t n, float a, float b) {
+    const T *add = static_cast<const T *>(p.add) + m * p.ld_add + n;
+    T *out = static_cast<T *>(p.out[0]) + m * p.ldo[0] + n;
+    float value;
+    if constexpr (EPI == BNN_EPI_LINEAR || EPI == BNN_EPI_LINEAR_BACK) {
+        if (p.bias) a += to_f32(static_cast<const T *>(p.bias)[n]);
+    }
+    if constexpr (EPI == BNN_EPI_LINEAR) {
+        if (p.pre) p.pre[m * p.ldp + n] = a;
+        a = act_value(p.act, a);
+        if (p.add) a += to_f32(*add);
+        *out = from_f32<T>(a);
+    } else if constexpr (EPI == BNN_EPI_LINEAR_BACK) {
+        *out = from_f32<T>(to_f32(*add) * act_slope(p.act, a, value));
+    } else if constexpr (EPI == BNN_EPI_GATED) {
+        if (p.pre) { p.pre[m * p.ldp + n] = a; p.pre[(p.M + m) * p.ldp + n] = b; }
+        *out = from_f32<T>(act_value(p.act, a) * b);
+    } else {
+        const float d = to_f32(*add), slope = act_slope(p.act, a, value);
+        *out = from_f32<T>(d * b * slope);
+        static_cast<T *>(p.out[1])[m * p.ldo[1] + n] = from_f32<T>(d * value);
+    }
+}
+
+template <bool W_MN, int EPI> __global__ void __launch_bounds__(FEW_THREADS) k_product_few(const __grid_constant__ FewArgs f) {
+    constexpr bool GATED = EPI == BNN_EPI_GATED || EPI == BNN_EPI_GATED_BACK;
+    constexpr int ROWS = GATED ? 64 : 128;                        // outputs of a tile
+    const ProductArgs &p = f.p;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *tiles = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    __shared__ FewControl control;
+    FewControl *ctl = &control;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    uint32_t split;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(split));
+    const uint32_t tile = blockIdx.x / split, tn = tile % p.tiles_n, tt = tile / p.tiles_n;
+    const int64_t n0 = (int64_t)tn * ROWS, t0 = (int64_t)tt * f.tokens;
+    const int first = (int)((int64_t)p.k_iters * rank / split), last = (int)((int64_t)p.k_iters * (rank + 1) / split);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < f.stages; ++s) { mbar_init(smem_u32(&ctl->full[s]), 1); mbar_init(smem_u32(&ctl->empty[s]), 1); }
+        mbar_init(smem_u32(&ctl->acc_full), 1);
+        ctl->failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(f.tmem_cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem_base = ctl->tmem_base;
+    bnn_pdl_wait();
+    bnn_pdl_launch_next();
+
+    if (warp == 0) {
+        if (lane == 0 && !p.drop_loads) {
+            int stage = 0, lap = 0;
+            for (int kit = first; kit < last; ++kit) {
+                if (lap > 0 && !wait(ctl, p.wait_ns, &ctl->empty[stage], (lap - 1) & 1)) { few_fail(ctl, 21); break; }
+                const int second = kit >= p.k_pair ? 1 : 0, k = (kit - (second ? p.k_pair : 0)) * BK;
+                const uint32_t dst = smem_u32(tiles) + stage * f.stage_bytes, bar = smem_u32(&ctl->full[stage]);
+                mbar_expect_tx(bar, f.stage_bytes);
+                if constexpr (GATED) {
+                    tma_load_2d(dst, &p.a[0], k, (int)n0, bar);
+                    tma_load_2d(dst + 8192, &p.a[1], k, (int)n0, bar);
+                } else if constexpr (W_MN) {
+                    tma_load_2d(dst, &p.a[second], (int)n0, k, bar);
+                    tma_load_2d(dst + 8192, &p.a[second], (int)n0 + 64, k, bar);
+                } else tma_load_2d(dst, &p.a[second], k, (int)n0, bar);
+                tma_load_2d(dst + A_STAGE, &p.b[second], k, (int)t0, bar);
+                if (++stage == f.stages) { stage = 0; ++lap; }
+            }
+            if (*reinterpret_cast<volatile uint32_t *>(&ctl->failed) != 0u) {      // copies in flight land before the shared memory is given up
+                const int issued = lap * f.stages + stage;
+                for (int i = issued > f.stages ? issued - f.stages : 0; i < issued; ++i)
+                    if (!wait(ctl, p.wait_ns, &ctl->full[i % f.stages], (i / f.stages) & 1, false)) break;
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            constexpr uint64_t A_STEP = W_MN ? 2048 >> 4 : 32 >> 4;
+            const uint64_t a0 = W_MN ? smem_desc_mn(smem_u32(tiles)) : smem_desc_sw128(smem_u32(tiles)), b0 = smem_desc_sw128(smem_u32(tiles + A_STAGE));
+            int stage = 0;
+            uint32_t phase = 0;
+            for (int kit = first; kit < last; ++kit) {
+                if (!wait(ctl, p.wait_ns, &ctl->full[stage], phase)) { few_fail(ctl, 22); break; }
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint64_t at = (uint64_t)(stage * (f.stage_bytes >> 4));
+#pragma unroll
+                for (int k = 0; k < BK / 16; ++k) mma_f16(tmem_base, a0 + at + k * A_STEP, b0 + at + k * (32 >> 4), p.idesc, (kit > first || k) ? 1u : 0u);
+                mma_commit(&ctl->empty[stage]);
+                if (++stage == f.stages) { stage = 0; phase ^= 1; }
+            }
+            mma_commit(&ctl->acc_full);
+        }
+    }
+    // The partial tile as part[token][row]: the ring is drained by now and its memory is free.  The MMAs issued before a failure end
+    // before tensor memory is given back, hence a wait that does not look at the failure word.
+    float *part = reinterpret_cast<float *>(tiles);
+    if (warp >= 2) {
+        const bool done = wait(ctl, 2 * p.wait_ns, &ctl->acc_full, 0, false);
+        if (!done) few_fail(ctl, 23);
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (done && *reinterpret_cast<volatile uint32_t *>(&ctl->failed) == 0u) {
+            const int q = warp & 3, row = 32 * q + lane;
+            for (int c = 0; c < f.tokens; c += 16) {
+                if (t0 + c >= p.M) break;
+                uint32_t r[16];
+                asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                             : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                               "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                             : "r"(tmem_base + ((uint32_t)(32 * q) << 16) + c) : "memory");
+                asm volatile("tcgen05.wait::ld.sync.aligned;"
+                             : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                               "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
+#pragma unroll
+                for (int j = 0; j < 16; ++j) part[(c + j) * 128 + row] = last > first ? __uint_as_float(r[j]) : 0.0f;
+            }
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(f.tmem_cols) : "memory");
+    }
+    if (split > 1) cluster_sync_all();
+    const bool failed = *reinterpret_cast<volatile uint32_t *>(&ctl->failed) != 0u;
+    if (!failed) {
+        const int valid = (int)(p.M - t0 < f.tokens ? p.M - t0 : f.tokens), rows = (int)(p.N - n0 < ROWS ? p.N - n0 : ROWS);
+        for (int i = threadIdx.x + FEW_THREADS * (int)rank; i < valid * ROWS; i += FEW_THREADS * (int)split) {
+            const int t = i / ROWS, row = i - t * ROWS;
+            if (row >= rows) continue;
+            float a = 0.0f, b = 0.0f;
+            if (split == 1) {
+                a = part[t * 128 + row];
+                if (GATED) b = part[t * 128 + 64 + row];
+            } else {
+                for (uint32_t r = 0; r < split; ++r) {
+                    a += cluster_load(smem_u32(part + t * 128 + row), r);
+                    if (GATED) b += cluster_load(smem_u32(part + t * 128 + 64 + row), r);
+                }
+            }
+            if (p.f16) finish1<EPI, __half>(p, t0 + t, n0 + row, a, b);
+            else finish1<EPI, __nv_bfloat16>(p, t0 + t, n0 + row, a, b);
+        }
+    }
+    __syncwarp();
+    if (split > 1) cluster_sync_all();                            // nobody leaves while others still read its partial tile
+}
+
+// ---------------------------------------------------------------------------------------------------------
 template <int BN> constexpr size_t pair_smem() { return (size_t)Ring<BN>::STAGES * Ring<BN>::STAGE + sizeof(Control) + 1024; }
 
 // Opts in to the shared memory and asks how many pairs fit the device, once per device and kernel; 0 = cannot run.
@@ -408,6 +606,29 @@ template <bool A_MN, bool B_MN, int EPI, int BN> int launch(bnn_ctx *ctx, const 
     return bnn_check_launch(ctx);
 }
 
+template <bool W_MN, int EPI> int launch_few(bnn_ctx *ctx, const FewArgs &f, unsigned tiles, unsigned split) {
+    auto kernel = k_product_few<W_MN, EPI>;
+    static std::mutex lock;
+    static bool ready[64];
+    if (ctx->device < 0 || ctx->device >= 64) return BNN_ERR_INVALID_ARG;
+    {
+        std::lock_guard<std::mutex> guard(lock);
+        if (!ready[ctx->device]) BNN_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FEW_SMEM + 1024));
+        ready[ctx->device] = true;
+    }
+    cudaLaunchConfig_t cfg{};
+    const size_t ring = (size_t)f.stages * f.stage_bytes, part = (size_t)f.tokens * 512;
+    cfg.gridDim = dim3(tiles * split); cfg.blockDim = dim3(FEW_THREADS); cfg.dynamicSmemBytes = (ring > part ? ring : part) + 1024; cfg.stream = ctx->stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = split; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    BNN_CUDA_TRY(ctx, cudaLaunchKernelEx(&cfg, kernel, f));
+    return bnn_check_launch(ctx);
+}
+
 int map16(bnn_ctx *ctx, CUtensorMap *map, const void *p, int64_t ld, int64_t rows, int64_t cols, int box_rows) {
     return bnn_tensor_map16(ctx, map, p, rows, cols, rows > 1 ? ld : (cols + 7) & ~int64_t(7), box_rows, BK);
 }
@@ -426,26 +647,75 @@ int bnn_product_status(bnn_ctx *ctx, int *code) {
     return BNN_OK;
 }
 
+namespace {
+ProductArgs common_args(bnn_ctx *ctx, const BnnProduct &q) {
+    ProductArgs a{};
+    a.M = q.M; a.N = q.N; a.groups = q.groups;
+    const bool gated = q.epilogue == BNN_EPI_GATED || q.epilogue == BNN_EPI_GATED_BACK;
+    const int64_t steps = (q.K + BK - 1) / BK;
+    a.k_pair = (int)steps; a.k_iters = (int)(steps * (gated ? 1 : q.pairs));
+    a.bias = q.bias; a.add = q.add; a.ld_add = q.ld_add; a.pre = q.pre; a.ldp = q.ldp; a.act = q.act; a.f16 = q.dtype == BNN_F16;
+    for (int i = 0; i < 2; ++i) { a.out[i] = q.out[i]; a.ldo[i] = q.ldo[i]; }
+    a.wait_ns = ctx->wait_limit_ns; a.drop_loads = ctx->drop_loads;
+    return a;
+}
+// float32 accumulators, both operands of the call's type, N columns, M rows; whether each operand lies against the sum.
+uint32_t instruction(int dtype, int a_mn, int b_mn, int n, int m) {
+    const uint32_t type = dtype == BNN_BF16 ? 1u : 0u;
+    return (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+int product_few(bnn_ctx *ctx, const BnnProduct &q) {
+    const bool gated = q.epilogue == BNN_EPI_GATED || q.epilogue == BNN_EPI_GATED_BACK;
+    FewArgs f{};
+    f.p = common_args(ctx, q);
+    const int rows = gated ? 64 : 128;
+    const int64_t token_tiles = (q.M + FEW_TOKENS - 1) / FEW_TOKENS;
+    f.tokens = (int)(((q.M + token_tiles - 1) / token_tiles + 15) & ~int64_t(15));
+    f.p.tiles_n = (uint32_t)((q.N + rows - 1) / rows);
+    const int64_t tiles = f.p.tiles_n * token_tiles;
+    f.p.idesc = instruction(q.dtype, q.b_mn, 0, f.tokens, 128);
+    f.stage_bytes = A_STAGE + (uint32_t)f.tokens * BK * 2;
+    f.tmem_cols = 32;
+    while ((int)f.tmem_cols < f.tokens) f.tmem_cols *= 2;
+    // Split the sum while that brings more SMs to load and leaves every CTA at least four K steps.
+    int split = 1;
+    while (split < 8 && tiles * split * 2 <= 2 * ctx->sm_count && f.p.k_iters >= split * 2 * 4) split *= 2;
+    const int budget = tiles * split > ctx->sm_count ? FEW_SMEM / 2 : FEW_SMEM, steps = (f.p.k_iters + split - 1) / split;
+    f.stages = budget / (int)f.stage_bytes;
+    f.stages = f.stages < 2 ? 2 : f.stages > FEW_STAGES ? FEW_STAGES : f.stages;
+    if (f.stages > steps) f.stages = steps > 0 ? steps : 1;
+    if (q.K > 0) {
+        for (int i = 0; i < 2; ++i) {
+            if (q.b[i].p)
+                if (int st = q.b_mn ? map16(ctx, &f.p.a[i], q.b[i].p, q.b[i].ld, q.K, q.N, BK) : map16(ctx, &f.p.a[i], q.b[i].p, q.b[i].ld, q.N, q.K, rows)) return st;
+            if (q.a[i].p)
+                if (int st = map16(ctx, &f.p.b[i], q.a[i].p, q.a[i].ld, q.M, q.K, f.tokens)) return st;
+        }
+    }
+    if (q.b_mn) return launch_few<true, BNN_EPI_LINEAR>(ctx, f, (unsigned)tiles, (unsigned)split);
+    switch (q.epilogue) {
+        case BNN_EPI_LINEAR: return launch_few<false, BNN_EPI_LINEAR>(ctx, f, (unsigned)tiles, (unsigned)split);
+        case BNN_EPI_LINEAR_BACK: return launch_few<false, BNN_EPI_LINEAR_BACK>(ctx, f, (unsigned)tiles, (unsigned)split);
+        case BNN_EPI_GATED: return launch_few<false, BNN_EPI_GATED>(ctx, f, (unsigned)tiles, (unsigned)split);
+        default: return launch_few<false, BNN_EPI_GATED_BACK>(ctx, f, (unsigned)tiles, (unsigned)split);
+    }
+}
+}  // namespace
+
 int bnn_product(bnn_ctx *ctx, const BnnProduct &q) {
     const bool gated = q.epilogue == BNN_EPI_GATED || q.epilogue == BNN_EPI_GATED_BACK;
     const int bn = 256;
-    ProductArgs a{};
-    a.M = q.M; a.N = q.N;
-    const int64_t steps = (q.K + BK - 1) / BK;
-    a.k_pair = (int)steps; a.k_iters = (int)(steps * (gated ? 1 : q.pairs)); a.groups = q.groups;
     const int64_t width = gated ? bn / 2 : bn;
     const int64_t tm = (q.M + TM - 1) / TM, tn = (q.N + width - 1) / width;
+    if (!q.a_mn && q.groups == 1 && q.M <= FEW_ROWS) return product_few(ctx, q);
     if (tm * tn * q.groups > 0x7fffffff) return BNN_ERR_INVALID_ARG;
+    ProductArgs a = common_args(ctx, q);
     a.tiles_m = (uint32_t)tm; a.tiles_n = (uint32_t)tn; a.tiles = (uint32_t)(tm * tn * q.groups);
-    const uint32_t type = q.dtype == BNN_BF16 ? 1u : 0u;
-    a.idesc = (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)q.a_mn << 15) | ((uint32_t)q.b_mn << 16) | ((uint32_t)(bn >> 3) << 17) |
-              ((uint32_t)(TM >> 4) << 24);
-    a.bias = q.bias; a.add = q.add; a.ld_add = q.ld_add; a.pre = q.pre; a.ldp = q.ldp; a.act = q.act; a.f16 = q.dtype == BNN_F16;
-    for (int i = 0; i < 2; ++i) { a.out[i] = q.out[i]; a.ldo[i] = q.ldo[i]; }
+    a.idesc = instruction(q.dtype, q.a_mn, q.b_mn, bn, TM);
     a.vec_bias = width_of(q.bias, 0, 1, 2); a.vec_add = width_of(q.add, q.ld_add, q.M, 2); a.vec_pre = width_of(q.pre, q.ldp, 2 * q.M, 4);
     a.vec_out = width_of(q.out[0], q.ldo[0], q.M, 2);
     if (q.out[1]) { const int v = width_of(q.out[1], q.ldo[1], q.M, 2); a.vec_out = v < a.vec_out ? v : a.vec_out; }
-    a.wait_ns = ctx->wait_limit_ns; a.drop_loads = ctx->drop_loads;
     if (q.K > 0) {
         for (int i = 0; i < 2; ++i) {
             if (q.a[i].p)
