@@ -105,13 +105,19 @@ template <int WIDTH> __device__ __forceinline__ Tile tile_at(const ProductArgs &
     return {(int64_t)(band * BAND + w - n * high) * TM, (int64_t)n * WIDTH, (int)g};
 }
 
-// 32 neighbouring elements of a row, n of them inside the matrix, as floats.
-template <typename T> __device__ __forceinline__ void read32(const T *p, int n, int vec, float (&v)[32]) {
-    if (vec && n >= 32) {
-        if constexpr (sizeof(T) == 2) {
+// A warp's 32 x 32 block in memory: the lane's row starts at `row` (element n0 of it), rows are `ld` apart, `rows` x n of it
+// exist.  Rows of whole 16-byte groups are accessed by their own lane, 64 (128) bytes each.  Others go through the warp's
+// piece of shared memory, one row at a time across the lanes, so that neighbouring lanes touch neighbouring elements:
+// lane-private rows of 2-byte accesses took 40 us for a 700 x 700 output, this takes one row's transaction per instruction.
+struct Block { int rows, n; float *stage; };          // stage: 32 x 33 floats
+constexpr int STAGE_PITCH = 33;
+template <typename T> __device__ __forceinline__ void read32(const T *row, int64_t ld, int vec, const Block &k, float (&v)[32]) {
+    const int lane = threadIdx.x & 31;
+    if (vec && k.n >= 32) {
+        if (lane < k.rows) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint4 w = reinterpret_cast<const uint4 *>(p)[i];
+                const uint4 w = reinterpret_cast<const uint4 *>(row)[i];
                 const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -121,44 +127,52 @@ template <typename T> __device__ __forceinline__ void read32(const T *p, int n, 
             }
         }
     } else {
+        const T *first = row - (int64_t)lane * ld;
+        if (lane < k.n) {
+#pragma unroll 8
+            for (int r = 0; r < 32; ++r)
+                if (r < k.rows) k.stage[r * STAGE_PITCH + lane] = to_f32(first[r * ld + lane]);
+        }
+        __syncwarp();
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = j < n ? to_f32(p[j]) : 0.0f;
+        for (int j = 0; j < 32; ++j) v[j] = k.stage[lane * STAGE_PITCH + j];
+        __syncwarp();
     }
 }
 __device__ __forceinline__ void st256(void *p, const uint32_t *w) {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
                  ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
 }
-template <typename T> __device__ __forceinline__ void write32(T *p, int n, int vec, const float (&v)[32]) {
-    if (vec && n >= 32) {
-        uint32_t w[16];
+template <typename T> __device__ __forceinline__ void write32(T *row, int64_t ld, int vec, const Block &k, const float (&v)[32]) {
+    const int lane = threadIdx.x & 31;
+    if (vec && k.n >= 32) {
+        if (lane < k.rows) {
+            constexpr int WORDS = 8 * (int)sizeof(T);
+            uint32_t w[WORDS];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) w[j] = pack2<T>(v[2 * j], v[2 * j + 1]);
-        if (vec == 2) { st256(p, w); st256(p + 16, w + 8); }
-        else {
+            for (int j = 0; j < WORDS; ++j) {
+                if constexpr (sizeof(T) == 4) w[j] = __float_as_uint(v[j]);
+                else w[j] = pack2<T>(v[2 * j], v[2 * j + 1]);
+            }
+            if (vec == 2) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) reinterpret_cast<uint4 *>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                for (int i = 0; i < WORDS / 8; ++i) st256(reinterpret_cast<uint32_t *>(row) + 8 * i, w + 8 * i);
+            } else {
+#pragma unroll
+                for (int i = 0; i < WORDS / 4; ++i) reinterpret_cast<uint4 *>(row)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+            }
         }
     } else {
+        T *first = row - (int64_t)lane * ld;
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (j < n) p[j] = from_f32<T>(v[j]);
-    }
-}
-__device__ __forceinline__ void write32f(float *p, int n, int vec, const float (&v)[32]) {
-    if (vec && n >= 32) {
-        const uint32_t *w = reinterpret_cast<const uint32_t *>(v);
-        if (vec == 2) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) st256(p + 8 * i, w + 8 * i);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) reinterpret_cast<uint4 *>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        for (int j = 0; j < 32; ++j) k.stage[lane * STAGE_PITCH + j] = v[j];
+        __syncwarp();
+        if (lane < k.n) {
+#pragma unroll 8
+            for (int r = 0; r < 32; ++r)
+                if (r < k.rows) first[r * ld + lane] = from_f32<T>(k.stage[r * STAGE_PITCH + lane]);
         }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (j < n) p[j] = v[j];
+        __syncwarp();
     }
 }
 
@@ -178,47 +192,62 @@ __device__ __forceinline__ void act_values(int act, float (&v)[32]) {
     }
 }
 
-// 32 columns of one row, from accumulators to memory.  b: the second accumulator of the gated epilogues.
+// 32 rows x 32 columns of a warp, from accumulators to memory; m: the lane's row.  b: the second accumulator of the gated epilogues.
 template <int EPI, typename T>
-__device__ __forceinline__ void finish32(const ProductArgs &p, int group, int64_t m, int64_t n0, float (&a)[32], float (&b)[32]) {
-    const int n = (int)(p.N - n0 < 32 ? p.N - n0 : 32);
+__device__ __forceinline__ void finish32(const ProductArgs &p, int group, int64_t m, int64_t n0, float *stage, float (&a)[32], float (&b)[32]) {
+    const int lane = threadIdx.x & 31;
+    const int64_t below = p.M - (m - lane);
+    const Block k{(int)(below < 32 ? below : 32), (int)(p.N - n0 < 32 ? p.N - n0 : 32), stage};
+    if (k.rows <= 0) return;
     float d[32];
     if constexpr (EPI == BNN_EPI_LINEAR || EPI == BNN_EPI_LINEAR_BACK) {
         if (p.bias) {
-            read32(static_cast<const T *>(p.bias) + n0, n, p.vec_bias, d);
+            const T *bias = static_cast<const T *>(p.bias) + n0;
+            if (p.vec_bias && k.n >= 32) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) a[j] += d[j];
+                for (int i = 0; i < 4; ++i) {
+                    float c[8];
+                    load8(bias + 8 * i, c);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) a[8 * i + j] += c[j];
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (j < k.n) a[j] += to_f32(bias[j]);
+            }
         }
     }
-    if (m >= p.M) return;
+    const T *add = static_cast<const T *>(p.add) + m * p.ld_add + n0;
+    T *out = static_cast<T *>(p.out[group]) + m * p.ldo[group] + n0;
     if constexpr (EPI == BNN_EPI_LINEAR) {
-        if (p.pre) write32f(p.pre + m * p.ldp + n0, n, p.vec_pre, a);
+        if (p.pre) write32(p.pre + m * p.ldp + n0, p.ldp, p.vec_pre, k, a);
         act_values(p.act, a);
         if (p.add) {
-            read32(static_cast<const T *>(p.add) + m * p.ld_add + n0, n, p.vec_add, d);
+            read32(add, p.ld_add, p.vec_add, k, d);
 #pragma unroll
             for (int j = 0; j < 32; ++j) a[j] += d[j];
         }
-        write32(static_cast<T *>(p.out[group]) + m * p.ldo[group] + n0, n, p.vec_out, a);
+        write32(out, p.ldo[group], p.vec_out, k, a);
     } else if constexpr (EPI == BNN_EPI_LINEAR_BACK) {
-        read32(static_cast<const T *>(p.add) + m * p.ld_add + n0, n, p.vec_add, d);
+        read32(add, p.ld_add, p.vec_add, k, d);
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
             float value;
             d[j] *= act_slope(p.act, a[j], value);
         }
-        write32(static_cast<T *>(p.out[0]) + m * p.ldo[0] + n0, n, p.vec_out, d);
+        write32(out, p.ldo[0], p.vec_out, k, d);
     } else if constexpr (EPI == BNN_EPI_GATED) {
         if (p.pre) {
-            write32f(p.pre + m * p.ldp + n0, n, p.vec_pre, a);
-            write32f(p.pre + (p.M + m) * p.ldp + n0, n, p.vec_pre, b);
+            write32(p.pre + m * p.ldp + n0, p.ldp, p.vec_pre, k, a);
+            write32(p.pre + (p.M + m) * p.ldp + n0, p.ldp, p.vec_pre, k, b);
         }
         act_values(p.act, a);
 #pragma unroll
         for (int j = 0; j < 32; ++j) a[j] *= b[j];
-        write32(static_cast<T *>(p.out[0]) + m * p.ldo[0] + n0, n, p.vec_out, a);
+        write32(out, p.ldo[0], p.vec_out, k, a);
     } else {
-        read32(static_cast<const T *>(p.add) + m * p.ld_add + n0, n, p.vec_add, d);
+        read32(add, p.ld_add, p.vec_add, k, d);
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
             float value;
@@ -226,8 +255,8 @@ __device__ __forceinline__ void finish32(const ProductArgs &p, int group, int64_
             a[j] = d[j] * b[j] * slope;
             b[j] = d[j] * value;
         }
-        write32(static_cast<T *>(p.out[0]) + m * p.ldo[0] + n0, n, p.vec_out, a);
-        write32(static_cast<T *>(p.out[1]) + m * p.ldo[1] + n0, n, p.vec_out, b);
+        write32(out, p.ldo[0], p.vec_out, k, a);
+        write32(static_cast<T *>(p.out[1]) + m * p.ldo[1] + n0, p.ldo[1], p.vec_out, k, b);
     }
 }
 
@@ -333,6 +362,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_produc
         bnn_pdl_launch_next();
         const int q = warp & 3, half = (warp - 2) >> 2;
         const uint32_t quadrant = (uint32_t)(32 * q) << 16;
+        float *stage = reinterpret_cast<float *>(ctl + 1) + (warp - 2) * 32 * STAGE_PITCH;
         uint32_t count = 0;
         for (uint32_t t = pair; t < p.tiles; t += pairs, ++count) {
             const uint32_t buf = count & 1;
@@ -355,8 +385,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_produc
                     a[j] = p.k_iters ? __uint_as_float(ra[j]) : 0.0f;
                     if (GATED) b[j] = p.k_iters ? __uint_as_float(rb[j]) : 0.0f;
                 }
-                if (p.f16) finish32<EPI, __half>(p, tile.group, m, tile.n0 + c, a, b);
-                else finish32<EPI, __nv_bfloat16>(p, tile.group, m, tile.n0 + c, a, b);
+                if (p.f16) finish32<EPI, __half>(p, tile.group, m, tile.n0 + c, stage, a, b);
+                else finish32<EPI, __nv_bfloat16>(p, tile.group, m, tile.n0 + c, stage, a, b);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
@@ -409,36 +439,84 @@ __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint
 __device__ __forceinline__ void mma_commit(uint64_t *bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
-__device__ __forceinline__ float cluster_load(uint32_t addr, uint32_t rank) {
+__device__ __forceinline__ float4 cluster_load4(uint32_t addr, uint32_t rank) {
     uint32_t remote;
-    float v;
+    float4 v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(remote) : "memory");
     return v;
 }
+// The sum of four neighbouring values of all partial tiles, in the order of the ranks; every load is on its way before the first is used.
+__device__ __forceinline__ void sum_parts(const float *at, uint32_t split, float (&v)[4]) {
+    float4 r[8];
+    if (split == 1) r[0] = *reinterpret_cast<const float4 *>(at);
+    else {
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i)
+            if (i < split) r[i] = cluster_load4(smem_u32(at), i);
+    }
+    v[0] = r[0].x; v[1] = r[0].y; v[2] = r[0].z; v[3] = r[0].w;
+#pragma unroll
+    for (uint32_t i = 1; i < 8; ++i)
+        if (i < split) { v[0] += r[i].x; v[1] += r[i].y; v[2] += r[i].z; v[3] += r[i].w; }
+}
 
-template <int EPI, typename T> __device__ __forceinline__ void finish1(const ProductArgs &p, int64_t m, int64_t n, float a, float b) {
-    const T *add = static_cast<const T *>(p.add) + m * p.ld_add + n;
-    T *out = static_cast<T *>(p.out[0]) + m * p.ldo[0] + n;
-    float value;
-    if constexpr (EPI == BNN_EPI_LINEAR || EPI == BNN_EPI_LINEAR_BACK) {
-        if (p.bias) a += to_f32(static_cast<const T *>(p.bias)[n]);
-    }
-    if constexpr (EPI == BNN_EPI_LINEAR) {
-        if (p.pre) p.pre[m * p.ldp + n] = a;
-        a = act_value(p.act, a);
-        if (p.add) a += to_f32(*add);
-        *out = from_f32<T>(a);
-    } else if constexpr (EPI == BNN_EPI_LINEAR_BACK) {
-        *out = from_f32<T>(to_f32(*add) * act_slope(p.act, a, value));
-    } else if constexpr (EPI == BNN_EPI_GATED) {
-        if (p.pre) { p.pre[m * p.ldp + n] = a; p.pre[(p.M + m) * p.ldp + n] = b; }
-        *out = from_f32<T>(act_value(p.act, a) * b);
+// Four neighbouring outputs of one token, n of them inside; vec: on 8-byte (pre: 16-byte) boundaries.
+template <typename T> __device__ __forceinline__ void read4(const T *p, int n, int vec, float (&v)[4]) {
+    if (vec && n >= 4) {
+        const uint2 w = *reinterpret_cast<const uint2 *>(p);
+        const float2 a = unpack2<T>(w.x), b = unpack2<T>(w.y);
+        v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
     } else {
-        const float d = to_f32(*add), slope = act_slope(p.act, a, value);
-        *out = from_f32<T>(d * b * slope);
-        static_cast<T *>(p.out[1])[m * p.ldo[1] + n] = from_f32<T>(d * value);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = j < n ? to_f32(p[j]) : 0.0f;
     }
+}
+template <typename T> __device__ __forceinline__ void write4(T *p, int n, int vec, const float (&v)[4]) {
+    if (vec && n >= 4) {
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
+        else *reinterpret_cast<uint2 *>(p) = make_uint2(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < n) p[j] = from_f32<T>(v[j]);
+    }
+}
+template <int EPI, typename T> __device__ __forceinline__ void finish4(const ProductArgs &p, int64_t m, int64_t n0, float (&a)[4], float (&b)[4]) {
+    const int n = (int)(p.N - n0 < 4 ? p.N - n0 : 4);
+    const T *add = static_cast<const T *>(p.add) + m * p.ld_add + n0;
+    T *out = static_cast<T *>(p.out[0]) + m * p.ldo[0] + n0;
+    float d[4];
+    if constexpr (EPI == BNN_EPI_LINEAR || EPI == BNN_EPI_LINEAR_BACK) {
+        if (p.bias) {
+            read4(static_cast<const T *>(p.bias) + n0, n, p.vec_bias, d);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) a[j] += d[j];
+        }
+    }
+    if (EPI != BNN_EPI_GATED && p.add) read4(add, n, p.vec_add, d);
+    if ((EPI == BNN_EPI_LINEAR || EPI == BNN_EPI_GATED) && p.pre) {
+        write4(p.pre + m * p.ldp + n0, n, p.vec_pre, a);
+        if (EPI == BNN_EPI_GATED) write4(p.pre + (p.M + m) * p.ldp + n0, n, p.vec_pre, b);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float value;
+        if constexpr (EPI == BNN_EPI_LINEAR) {
+            a[j] = act_value(p.act, a[j]);
+            if (p.add) a[j] += d[j];
+        } else if constexpr (EPI == BNN_EPI_LINEAR_BACK) {
+            a[j] = d[j] * act_slope(p.act, a[j], value);
+        } else if constexpr (EPI == BNN_EPI_GATED) {
+            a[j] = act_value(p.act, a[j]) * b[j];
+        } else {
+            const float slope = act_slope(p.act, a[j], value);
+            a[j] = d[j] * b[j] * slope;
+            b[j] = d[j] * value;
+        }
+    }
+    write4(out, n, p.vec_out, a);
+    if constexpr (EPI == BNN_EPI_GATED_BACK) write4(static_cast<T *>(p.out[1]) + m * p.ldo[1] + n0, n, p.vec_out, b);
 }
 
 template <bool W_MN, int EPI> __global__ void __launch_bounds__(FEW_THREADS) k_product_few(const __grid_constant__ FewArgs f) {
@@ -550,21 +628,14 @@ template <bool W_MN, int EPI> __global__ void __launch_bounds__(FEW_THREADS) k_p
     const bool failed = *reinterpret_cast<volatile uint32_t *>(&ctl->failed) != 0u;
     if (!failed) {
         const int valid = (int)(p.M - t0 < f.tokens ? p.M - t0 : f.tokens), rows = (int)(p.N - n0 < ROWS ? p.N - n0 : ROWS);
-        for (int i = threadIdx.x + FEW_THREADS * (int)rank; i < valid * ROWS; i += FEW_THREADS * (int)split) {
-            const int t = i / ROWS, row = i - t * ROWS;
+        for (int i = threadIdx.x + FEW_THREADS * (int)rank; i < valid * (ROWS / 4); i += FEW_THREADS * (int)split) {
+            const int t = i / (ROWS / 4), row = (i - t * (ROWS / 4)) * 4;
             if (row >= rows) continue;
-            float a = 0.0f, b = 0.0f;
-            if (split == 1) {
-                a = part[t * 128 + row];
-                if (GATED) b = part[t * 128 + 64 + row];
-            } else {
-                for (uint32_t r = 0; r < split; ++r) {
-                    a += cluster_load(smem_u32(part + t * 128 + row), r);
-                    if (GATED) b += cluster_load(smem_u32(part + t * 128 + 64 + row), r);
-                }
-            }
-            if (p.f16) finish1<EPI, __half>(p, t0 + t, n0 + row, a, b);
-            else finish1<EPI, __nv_bfloat16>(p, t0 + t, n0 + row, a, b);
+            float a[4], b[4];
+            sum_parts(part + t * 128 + row, split, a);
+            if (GATED) sum_parts(part + t * 128 + 64 + row, split, b);
+            if (p.f16) finish4<EPI, __half>(p, t0 + t, n0 + row, a, b);
+            else finish4<EPI, __nv_bfloat16>(p, t0 + t, n0 + row, a, b);
         }
     }
     __syncwarp();
@@ -572,7 +643,10 @@ template <bool W_MN, int EPI> __global__ void __launch_bounds__(FEW_THREADS) k_p
 }
 
 // ---------------------------------------------------------------------------------------------------------
-template <int BN> constexpr size_t pair_smem() { return (size_t)Ring<BN>::STAGES * Ring<BN>::STAGE + sizeof(Control) + 1024; }
+template <int BN> constexpr size_t pair_smem() {
+    return (size_t)Ring<BN>::STAGES * Ring<BN>::STAGE + sizeof(Control) + EPI_WARPS * 32 * STAGE_PITCH * 4 + 1024;
+}
+static_assert(pair_smem<256>() <= 227 * 1024 && pair_smem<128>() <= 227 * 1024, "fits the shared memory of an SM");
 
 // Opts in to the shared memory and asks how many pairs fit the device, once per device and kernel; 0 = cannot run.
 template <bool A_MN, bool B_MN, int EPI, int BN> int pairs_of(int device, int sm_count) {
@@ -669,6 +743,9 @@ int product_few(bnn_ctx *ctx, const BnnProduct &q) {
     const bool gated = q.epilogue == BNN_EPI_GATED || q.epilogue == BNN_EPI_GATED_BACK;
     FewArgs f{};
     f.p = common_args(ctx, q);
+    const auto fours = [](const void *at, int64_t ld, int64_t n, int size) { return reinterpret_cast<uintptr_t>(at) % (4 * size) == 0 && (n <= 1 || ld % 4 == 0); };
+    f.p.vec_bias = fours(q.bias, 0, 1, 2); f.p.vec_add = fours(q.add, q.ld_add, q.M, 2); f.p.vec_pre = fours(q.pre, q.ldp, 2 * q.M, 4);
+    f.p.vec_out = fours(q.out[0], q.ldo[0], q.M, 2) && fours(q.out[1], q.ldo[1], q.M, 2);
     const int rows = gated ? 64 : 128;
     const int64_t token_tiles = (q.M + FEW_TOKENS - 1) / FEW_TOKENS;
     f.tokens = (int)(((q.M + token_tiles - 1) / token_tiles + 15) & ~int64_t(15));
@@ -678,10 +755,12 @@ int product_few(bnn_ctx *ctx, const BnnProduct &q) {
     f.stage_bytes = A_STAGE + (uint32_t)f.tokens * BK * 2;
     f.tmem_cols = 32;
     while ((int)f.tmem_cols < f.tokens) f.tmem_cols *= 2;
-    // Split the sum while that brings more SMs to load and leaves every CTA at least four K steps.
+    // Split the sum while that brings more SMs to load and leaves every CTA at least four K steps.  Two CTAs share an SM where half of its
+    // memory still holds four stages (up to 64 tokens).
+    const int per_sm = f.tokens <= 64 ? 2 : 1;
     int split = 1;
-    while (split < 8 && tiles * split * 2 <= 2 * ctx->sm_count && f.p.k_iters >= split * 2 * 4) split *= 2;
-    const int budget = tiles * split > ctx->sm_count ? FEW_SMEM / 2 : FEW_SMEM, steps = (f.p.k_iters + split - 1) / split;
+    while (split < 8 && tiles * split * 2 <= per_sm * ctx->sm_count && f.p.k_iters >= split * 2 * 4) split *= 2;
+    const int budget = tiles * split > ctx->sm_count && per_sm == 2 ? FEW_SMEM / 2 : FEW_SMEM, steps = (f.p.k_iters + split - 1) / split;
     f.stages = budget / (int)f.stage_bytes;
     f.stages = f.stages < 2 ? 2 : f.stages > FEW_STAGES ? FEW_STAGES : f.stages;
     if (f.stages > steps) f.stages = steps > 0 ? steps : 1;
@@ -705,10 +784,11 @@ int product_few(bnn_ctx *ctx, const BnnProduct &q) {
 
 int bnn_product(bnn_ctx *ctx, const BnnProduct &q) {
     const bool gated = q.epilogue == BNN_EPI_GATED || q.epilogue == BNN_EPI_GATED_BACK;
-    const int bn = 256;
-    const int64_t width = gated ? bn / 2 : bn;
-    const int64_t tm = (q.M + TM - 1) / TM, tn = (q.N + width - 1) / width;
     if (!q.a_mn && q.groups == 1 && q.M <= FEW_ROWS) return product_few(ctx, q);
+    // Half-width tiles where whole ones would leave half of the pairs without work.
+    const int64_t tm = (q.M + TM - 1) / TM, whole = tm * ((q.N + (gated ? 127 : 255)) / (gated ? 128 : 256)) * q.groups;
+    const int bn = 2 * whole <= ctx->sm_count / 2 ? 128 : 256;
+    const int64_t width = gated ? bn / 2 : bn, tn = (q.N + width - 1) / width;
     if (tm * tn * q.groups > 0x7fffffff) return BNN_ERR_INVALID_ARG;
     ProductArgs a = common_args(ctx, q);
     a.tiles_m = (uint32_t)tm; a.tiles_n = (uint32_t)tn; a.tiles = (uint32_t)(tm * tn * q.groups);
@@ -724,12 +804,14 @@ int bnn_product(bnn_ctx *ctx, const BnnProduct &q) {
                 if (int st = q.b_mn ? map16(ctx, &a.b[i], q.b[i].p, q.b[i].ld, q.K, q.N, BK) : map16(ctx, &a.b[i], q.b[i].p, q.b[i].ld, q.N, q.K, bn / 2)) return st;
         }
     }
-    if (q.a_mn) return launch<true, true, BNN_EPI_LINEAR, 256>(ctx, a);
-    if (q.b_mn) return launch<false, true, BNN_EPI_LINEAR, 256>(ctx, a);
+#define BNN_LAUNCH(A_MN, B_MN, EPI) (bn == 256 ? launch<A_MN, B_MN, EPI, 256>(ctx, a) : launch<A_MN, B_MN, EPI, 128>(ctx, a))
+    if (q.a_mn) return BNN_LAUNCH(true, true, BNN_EPI_LINEAR);
+    if (q.b_mn) return BNN_LAUNCH(false, true, BNN_EPI_LINEAR);
     switch (q.epilogue) {
-        case BNN_EPI_LINEAR: return launch<false, false, BNN_EPI_LINEAR, 256>(ctx, a);
-        case BNN_EPI_LINEAR_BACK: return launch<false, false, BNN_EPI_LINEAR_BACK, 256>(ctx, a);
-        case BNN_EPI_GATED: return launch<false, false, BNN_EPI_GATED, 256>(ctx, a);
-        default: return launch<false, false, BNN_EPI_GATED_BACK, 256>(ctx, a);
+        case BNN_EPI_LINEAR: return BNN_LAUNCH(false, false, BNN_EPI_LINEAR);
+        case BNN_EPI_LINEAR_BACK: return BNN_LAUNCH(false, false, BNN_EPI_LINEAR_BACK);
+        case BNN_EPI_GATED: return BNN_LAUNCH(false, false, BNN_EPI_GATED);
+        default: return BNN_LAUNCH(false, false, BNN_EPI_GATED_BACK);
     }
+#undef BNN_LAUNCH
 }
