@@ -178,6 +178,17 @@ struct Readable {
     }
 };
 
+// The gradients of a layer in one launch, so that the tiles of all of them fill the GPU together; a first one (dx) of few rows
+// runs on the kernel for those.
+int gradients(bnn_ctx *ctx, int dtype, BnnProduct *g, int n) {
+    for (int i = 0; i < n; ++i) { g[i].dtype = dtype; g[i].epilogue = BNN_EPI_LINEAR; if (!g[i].pairs) g[i].pairs = 1; }
+    if (n > 1 && bnn_product_few(ctx, g[0])) {
+        if (int st = bnn_product(ctx, g, 1)) return st;
+        ++g; --n;
+    }
+    return n ? bnn_product(ctx, g, n) : BNN_OK;
+}
+
 }  // namespace
 
 extern "C" size_t bnn_linear_workspace_bytes(const bnn_linear_desc *l, int64_t M, int backward, int aligned) {
@@ -204,10 +215,10 @@ extern "C" int bnn_linear(bnn_ctx *ctx, const bnn_linear_desc *l, const void *x,
     if (int st = rx.copy(ctx)) return st;
     if (int st = rw.copy(ctx)) return st;
     BnnProduct p{};
-    p.dtype = l->dtype; p.epilogue = BNN_EPI_LINEAR; p.pairs = p.groups = 1;
+    p.dtype = l->dtype; p.epilogue = BNN_EPI_LINEAR; p.pairs = 1;
     p.a[0] = rx.use; p.b[0] = rw.use; p.M = M; p.N = l->N; p.K = l->K;
     p.bias = l->bias; p.add = residual; p.ld_add = ldr; p.out[0] = y; p.ldo[0] = ldy; p.pre = pre; p.ldp = ldp; p.act = l->act;
-    return bnn_product(ctx, p);
+    return bnn_product(ctx, &p, 1);
 }
 
 extern "C" int bnn_linear_backward(bnn_ctx *ctx, const bnn_linear_desc *l, const void *dy, int64_t lddy, const void *x, int64_t ldx,
@@ -237,12 +248,12 @@ extern "C" int bnn_linear_backward(bnn_ctx *ctx, const bnn_linear_desc *l, const
     for (const Readable *r : {&rz, &rx, &rw})
         if (int st = r->copy(ctx)) return st;
     BnnProduct p{};
-    p.dtype = l->dtype; p.pairs = p.groups = 1;
+    p.dtype = l->dtype; p.pairs = 1;
     if (again) {
         p.epilogue = BNN_EPI_LINEAR_BACK;
         p.a[0] = rx.use; p.b[0] = rw.use; p.M = M; p.N = l->N; p.K = l->K;
         p.bias = l->bias; p.add = dy; p.ld_add = lddy; p.out[0] = const_cast<void *>(dz.p); p.ldo[0] = dz.ld; p.act = l->act;
-        if (int st = bnn_product(ctx, p)) return st;
+        if (int st = bnn_product(ctx, &p, 1)) return st;
     }
     const bool kept = slopes && pre;
     if (kept || sums) {
@@ -260,19 +271,19 @@ extern "C" int bnn_linear_backward(bnn_ctx *ctx, const bnn_linear_desc *l, const
             if (int st = bnn_join_columns(ctx, l->dtype, part, l->N, sum_chunks(M, l->N), dbias, l->N)) return st;
     }
     const BnnOperand z = slopes ? dz : rz.use;
-    p = BnnProduct{};
-    p.dtype = l->dtype; p.epilogue = BNN_EPI_LINEAR; p.pairs = p.groups = 1;
+    BnnProduct g[2] = {};
+    int n = 0;
     if (dx && M > 0 && l->K > 0) {
-        p.a[0] = z; p.b[0] = rw.use; p.a_mn = 0; p.b_mn = 1;
-        p.M = M; p.N = l->K; p.K = l->N; p.out[0] = dx; p.ldo[0] = lddx;
-        if (int st = bnn_product(ctx, p)) return st;
+        BnnProduct &d = g[n++];
+        d.a[0] = z; d.b[0] = rw.use; d.b_mn = 1;
+        d.M = M; d.N = l->K; d.K = l->N; d.out[0] = dx; d.ldo[0] = lddx;
     }
     if (dW && l->N > 0 && l->K > 0) {
-        p.a[0] = z; p.b[0] = rx.use; p.a_mn = p.b_mn = 1;
-        p.M = l->N; p.N = l->K; p.K = M; p.out[0] = dW; p.ldo[0] = lddw;
-        if (int st = bnn_product(ctx, p)) return st;
+        BnnProduct &d = g[n++];
+        d.a[0] = z; d.b[0] = rx.use; d.a_mn = d.b_mn = 1;
+        d.M = l->N; d.N = l->K; d.K = M; d.out[0] = dW; d.ldo[0] = lddw;
     }
-    return BNN_OK;
+    return gradients(ctx, l->dtype, g, n);
 }
 
 extern "C" size_t bnn_gated_workspace_bytes(const bnn_gated_desc *l, int64_t M, int backward, int aligned) {
@@ -296,10 +307,10 @@ extern "C" int bnn_gated(bnn_ctx *ctx, const bnn_gated_desc *l, const void *x, i
     for (const Readable *r : {&rx, &rg, &ru})
         if (int st = r->copy(ctx)) return st;
     BnnProduct p{};
-    p.dtype = l->dtype; p.epilogue = BNN_EPI_GATED; p.pairs = p.groups = 1;
+    p.dtype = l->dtype; p.epilogue = BNN_EPI_GATED; p.pairs = 1;
     p.a[0] = rx.use; p.b[0] = rg.use; p.b[1] = ru.use; p.M = M; p.N = l->N; p.K = l->K;
     p.out[0] = h; p.ldo[0] = ldh; p.pre = pre; p.ldp = ldp; p.act = l->act;
-    return bnn_product(ctx, p);
+    return bnn_product(ctx, &p, 1);
 }
 
 extern "C" int bnn_gated_backward(bnn_ctx *ctx, const bnn_gated_desc *l, const void *dh, int64_t lddh, const void *x, int64_t ldx, int64_t M,
@@ -325,12 +336,12 @@ extern "C" int bnn_gated_backward(bnn_ctx *ctx, const bnn_gated_desc *l, const v
     for (const Readable *r : {&rx, &rg, &ru})
         if (int st = r->copy(ctx)) return st;
     BnnProduct p{};
-    p.dtype = l->dtype; p.pairs = p.groups = 1;
+    p.dtype = l->dtype; p.pairs = 1;
     if (again) {
         p.epilogue = BNN_EPI_GATED_BACK;
         p.a[0] = rx.use; p.b[0] = rg.use; p.b[1] = ru.use; p.M = M; p.N = l->N; p.K = l->K;
         p.add = dh; p.ld_add = lddh; p.out[0] = dg; p.out[1] = du; p.ldo[0] = p.ldo[1] = ldd; p.act = l->act;
-        if (int st = bnn_product(ctx, p)) return st;
+        if (int st = bnn_product(ctx, &p, 1)) return st;
     } else if (some) {
         GatedSlopeArgs s{};
         s.dh = dh; s.lddh = lddh; s.pre = pre; s.ldp = ldp; s.dg = dg; s.du = du; s.ldd = ldd; s.M = M; s.N = l->N; s.act = l->act;
@@ -340,22 +351,20 @@ extern "C" int bnn_gated_backward(bnn_ctx *ctx, const bnn_gated_desc *l, const v
         else k_gated_slopes<__nv_bfloat16><<<grid, 256, 0, ctx->stream>>>(s);
         if (int st = bnn_check_launch(ctx)) return st;
     }
-    p = BnnProduct{};
-    p.dtype = l->dtype; p.epilogue = BNN_EPI_LINEAR; p.pairs = p.groups = 1;
+    BnnProduct g[3] = {};
+    int n = 0;
     if (dx && M > 0 && l->K > 0) {
-        p.a[0] = {dg, ldd}; p.a[1] = {du, ldd}; p.b[0] = rg.use; p.b[1] = ru.use; p.b_mn = 1; p.pairs = 2;
-        p.M = M; p.N = l->K; p.K = l->N; p.out[0] = dx; p.ldo[0] = lddx;
-        if (int st = bnn_product(ctx, p)) return st;
+        BnnProduct &d = g[n++];
+        d.a[0] = {dg, ldd}; d.a[1] = {du, ldd}; d.b[0] = rg.use; d.b[1] = ru.use; d.b_mn = 1; d.pairs = 2;
+        d.M = M; d.N = l->K; d.K = l->N; d.out[0] = dx; d.ldo[0] = lddx;
     }
-    if ((dWg || dWu) && l->N > 0 && l->K > 0) {
-        p = BnnProduct{};
-        p.dtype = l->dtype; p.epilogue = BNN_EPI_LINEAR; p.pairs = 1;
-        p.groups = dWg && dWu ? 2 : 1;              // both weight gradients in one launch
-        p.a[0] = {dWg ? dg : du, ldd}; p.b[0] = rx.use; p.a_mn = p.b_mn = 1;
-        p.out[0] = dWg ? dWg : dWu; p.ldo[0] = dWg ? lddg : lddu;
-        if (p.groups == 2) { p.a[1] = {du, ldd}; p.out[1] = dWu; p.ldo[1] = lddu; }
-        p.M = l->N; p.N = l->K; p.K = M;
-        if (int st = bnn_product(ctx, p)) return st;
+    void *const dw[2] = {dWg, dWu};
+    const int64_t ldw[2] = {lddg, lddu};
+    for (int k = 0; k < 2; ++k) {
+        if (!dw[k] || l->N == 0 || l->K == 0) continue;
+        BnnProduct &d = g[n++];
+        d.a[0] = {k ? du : dg, ldd}; d.b[0] = rx.use; d.a_mn = d.b_mn = 1;
+        d.M = l->N; d.N = l->K; d.K = M; d.out[0] = dw[k]; d.ldo[0] = ldw[k];
     }
-    return BNN_OK;
+    return gradients(ctx, l->dtype, g, n);
 }

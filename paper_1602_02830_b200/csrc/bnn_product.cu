@@ -8,7 +8,7 @@
 // k_product_pair: a cluster of two CTAs works on one 256 x BN tile (tcgen05.mma cta_group::2): each CTA holds its 128 rows of A
 // and half of the tile's columns of B, so a pair reads 256 + BN rows of operands for 256 x BN products.  Persistent, one CTA per
 // SM, tiles in bands of eight tile rows so that the operands of the tiles in flight stay in L2.
-//   warp 0, last warp  TMA producers (A and B): 64-element K slices, 128-byte swizzle, a ring of shared-memory stages
+//   warp 0, last warp  TMA producers, K steps in turn: 64-element K slices of both operands, 128-byte swizzle, a ring of stages
 //   warp 1             MMA issuer (CTA 0 of the pair): four K = 16 MMAs per stage; tcgen05.commit frees the stage
 //   warps 2 .. 9       epilogue: two per TMEM lane quadrant, each half of the columns, one output row per thread
 // Two accumulator buffers: the epilogue of a tile runs under the MMAs of the next one.
@@ -37,22 +37,31 @@ template <int BN> struct Ring {
     static constexpr int STAGES = BN == 256 ? 6 : 8;                // 192 KB
     static constexpr uint32_t TMEM = 2 * BN;
 };
-constexpr int STAGES_MAX = 8;
+constexpr int STAGES_MAX = 8;             // even numbers of stages: each belongs to one of the two producers
 constexpr int BAND = 8;                  // tile rows per band
 
-struct ProductArgs {
+// One product of a launch.  a_mn / b_mn: the operand is stored against the sum.
+struct Problem {
     CUtensorMap a[2], b[2];
     int64_t M, N;
-    int k_pair, k_iters;                 // K steps of the first pair; of all
-    int groups;
-    uint32_t tiles_m, tiles_n, tiles;
+    int k_pair, k_iters;                 // K steps of the first pair of operands; of all
+    uint32_t first, tiles_m, tiles_n;    // first tile of the launch's numbering; tile rows and columns
     uint32_t idesc;
-    const void *bias, *add;
+    int a_mn, b_mn;
     void *out[2];
+    int64_t ldo[2];
+    int vec_out;                         // widest access that every row allows: 2 = 32 bytes, 1 = 16 bytes, 0 = one element
+};
+constexpr int PROBLEMS = 3;              // a gated layer's gradients: dx, dWg, dWu
+struct ProductArgs {
+    Problem q[PROBLEMS];
+    int problems;
+    uint32_t tiles;
+    const void *bias, *add;              // of a single problem
     float *pre;
-    int64_t ld_add, ldo[2], ldp;
+    int64_t ld_add, ldp;
     int act, f16;
-    int vec_bias, vec_add, vec_out, vec_pre;   // widest access that every row allows: 2 = 32 bytes, 1 = 16 bytes, 0 = one element
+    int vec_bias, vec_add, vec_pre;
     unsigned long long wait_ns;
     int drop_loads;                      // test hook: the producers request nothing, every consumer's wait runs out
 };
@@ -95,14 +104,16 @@ __device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr) {
     return smem_desc_sw128(addr) | ((uint64_t)(8192u >> 4) << 16);
 }
 
-struct Tile { int64_t m0, n0; int group; };
+struct Tile { int problem, m0, n0; };
 template <int WIDTH> __device__ __forceinline__ Tile tile_at(const ProductArgs &p, uint32_t t) {
-    const uint32_t per = p.tiles_m * p.tiles_n, g = t / per;
-    t -= g * per;
-    const uint32_t band = t / (BAND * p.tiles_n), w = t - band * BAND * p.tiles_n;
-    const uint32_t high = p.tiles_m - band * BAND < BAND ? p.tiles_m - band * BAND : BAND;
+    int i = 0;
+    while (i + 1 < p.problems && t >= p.q[i + 1].first) ++i;
+    const Problem &q = p.q[i];
+    t -= q.first;
+    const uint32_t band = t / (BAND * q.tiles_n), w = t - band * BAND * q.tiles_n;
+    const uint32_t high = q.tiles_m - band * BAND < BAND ? q.tiles_m - band * BAND : BAND;
     const uint32_t n = w / high;
-    return {(int64_t)(band * BAND + w - n * high) * TM, (int64_t)n * WIDTH, (int)g};
+    return {i, (int)((band * BAND + w - n * high) * TM), (int)(n * WIDTH)};
 }
 
 // A warp's 32 x 32 block in memory: the lane's row starts at `row` (element n0 of it), rows are `ld` apart, `rows` x n of it
@@ -194,10 +205,10 @@ __device__ __forceinline__ void act_values(int act, float (&v)[32]) {
 
 // 32 rows x 32 columns of a warp, from accumulators to memory; m: the lane's row.  b: the second accumulator of the gated epilogues.
 template <int EPI, typename T>
-__device__ __forceinline__ void finish32(const ProductArgs &p, int group, int64_t m, int64_t n0, float *stage, float (&a)[32], float (&b)[32]) {
+__device__ __forceinline__ void finish32(const ProductArgs &p, const Problem &q, int64_t m, int64_t n0, float *stage, float (&a)[32], float (&b)[32]) {
     const int lane = threadIdx.x & 31;
-    const int64_t below = p.M - (m - lane);
-    const Block k{(int)(below < 32 ? below : 32), (int)(p.N - n0 < 32 ? p.N - n0 : 32), stage};
+    const int64_t below = q.M - (m - lane);
+    const Block k{(int)(below < 32 ? below : 32), (int)(q.N - n0 < 32 ? q.N - n0 : 32), stage};
     if (k.rows <= 0) return;
     float d[32];
     if constexpr (EPI == BNN_EPI_LINEAR || EPI == BNN_EPI_LINEAR_BACK) {
@@ -219,7 +230,7 @@ __device__ __forceinline__ void finish32(const ProductArgs &p, int group, int64_
         }
     }
     const T *add = static_cast<const T *>(p.add) + m * p.ld_add + n0;
-    T *out = static_cast<T *>(p.out[group]) + m * p.ldo[group] + n0;
+    T *out = static_cast<T *>(q.out[0]) + m * q.ldo[0] + n0;
     if constexpr (EPI == BNN_EPI_LINEAR) {
         if (p.pre) write32(p.pre + m * p.ldp + n0, p.ldp, p.vec_pre, k, a);
         act_values(p.act, a);
@@ -228,7 +239,7 @@ __device__ __forceinline__ void finish32(const ProductArgs &p, int group, int64_
 #pragma unroll
             for (int j = 0; j < 32; ++j) a[j] += d[j];
         }
-        write32(out, p.ldo[group], p.vec_out, k, a);
+        write32(out, q.ldo[0], q.vec_out, k, a);
     } else if constexpr (EPI == BNN_EPI_LINEAR_BACK) {
         read32(add, p.ld_add, p.vec_add, k, d);
 #pragma unroll
@@ -236,16 +247,16 @@ __device__ __forceinline__ void finish32(const ProductArgs &p, int group, int64_
             float value;
             d[j] *= act_slope(p.act, a[j], value);
         }
-        write32(out, p.ldo[0], p.vec_out, k, d);
+        write32(out, q.ldo[0], q.vec_out, k, d);
     } else if constexpr (EPI == BNN_EPI_GATED) {
         if (p.pre) {
             write32(p.pre + m * p.ldp + n0, p.ldp, p.vec_pre, k, a);
-            write32(p.pre + (p.M + m) * p.ldp + n0, p.ldp, p.vec_pre, k, b);
+            write32(p.pre + (q.M + m) * p.ldp + n0, p.ldp, p.vec_pre, k, b);
         }
         act_values(p.act, a);
 #pragma unroll
         for (int j = 0; j < 32; ++j) a[j] *= b[j];
-        write32(out, p.ldo[0], p.vec_out, k, a);
+        write32(out, q.ldo[0], q.vec_out, k, a);
     } else {
         read32(add, p.ld_add, p.vec_add, k, d);
 #pragma unroll
@@ -255,17 +266,17 @@ __device__ __forceinline__ void finish32(const ProductArgs &p, int group, int64_
             a[j] = d[j] * b[j] * slope;
             b[j] = d[j] * value;
         }
-        write32(out, p.ldo[0], p.vec_out, k, a);
-        write32(static_cast<T *>(p.out[1]) + m * p.ldo[1] + n0, p.ldo[1], p.vec_out, k, b);
+        write32(out, q.ldo[0], q.vec_out, k, a);
+        write32(static_cast<T *>(q.out[1]) + m * q.ldo[1] + n0, q.ldo[1], q.vec_out, k, b);
     }
 }
 
-template <bool A_MN, bool B_MN, int EPI, int BN>
+template <int EPI, int BN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_product_pair(const __grid_constant__ ProductArgs p) {
     constexpr bool GATED = EPI == BNN_EPI_GATED || EPI == BNN_EPI_GATED_BACK;
     constexpr int WIDTH = GATED ? BN / 2 : BN;                   // output columns of a tile
     constexpr int STAGES = Ring<BN>::STAGES;
-    constexpr uint32_t STAGE = Ring<BN>::STAGE, B_STAGE = Ring<BN>::B_STAGE, TMEM = Ring<BN>::TMEM;
+    constexpr uint32_t STAGE = Ring<BN>::STAGE, TMEM = Ring<BN>::TMEM;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *tiles = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     Control *ctl = reinterpret_cast<Control *>(tiles + STAGES * STAGE);
@@ -273,7 +284,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_produc
     const uint32_t rank = cluster_ctarank(), pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(smem_u32(&ctl->full[s]), 2); mbar_init(smem_u32(&ctl->empty[s]), 1); }
+        for (int s = 0; s < STAGES; ++s) { mbar_init(smem_u32(&ctl->full[s]), 1); mbar_init(smem_u32(&ctl->empty[s]), 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&ctl->acc_full[b]), 1); mbar_init(smem_u32(&ctl->acc_empty[b]), 2 * EPI_WARPS); }
         mbar_init(smem_u32(&ctl->drain), 1);
         ctl->failed = 0;
@@ -290,50 +301,49 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_produc
     const uint32_t tmem_base = ctl->tmem_base;
 
     if (warp == 0 || warp == 2 + EPI_WARPS) {
-        // ---------------- producers: the thread of warp 0 loads A, the other one B.  The "full" barrier of a stage (in CTA 0)
-        // completes with the arrivals of CTA 0's two producers and the bytes of both CTAs.
+        // ---------------- producers: two threads take the K steps in turn.  One pass of this loop costs a thread about 480 clocks
+        // (0.256 us a step alone, 0.144 two in turn; a further box 0.035), as much as the step's MMAs take.
+        // The "full" barrier of a stage (in CTA 0) completes with the arrival of CTA 0's producer and the bytes of both CTAs.
+        // The two need no order between them: the use before last of a stage is consumed whenever one of them gets to its next use.
         if (lane == 0 && !p.drop_loads) {
-            const bool is_a = warp == 0;
+            const uint32_t mine = warp == 0 ? 0 : 1;
             bool ok = true;
-            uint32_t stage = 0, lap = 0;
+            uint32_t step = 0, stage = mine, lap = 0;                // step: of the launch, before the current tile
             bnn_pdl_wait();
             for (uint32_t t = pair; t < p.tiles && ok; t += pairs) {
                 const Tile tile = tile_at<WIDTH>(p, t);
-                const int m0 = (int)tile.m0 + (int)rank * 128;
-                const int n0 = (int)tile.n0 + (GATED ? 0 : (int)rank * (BN / 2));
-                for (int kit = 0; kit < p.k_iters; ++kit) {
+                const Problem &q = p.q[tile.problem];
+                const int m0 = tile.m0 + (int)rank * 128, n0 = tile.n0 + (GATED ? 0 : (int)rank * (BN / 2));
+                const int k_pair = q.k_pair, k_iters = q.k_iters, a_mn = q.a_mn, b_mn = q.b_mn;
+                for (int kit = (int)((mine + step) & 1u); kit < k_iters; kit += 2) {
                     if (lap > 0 && !wait(ctl, p.wait_ns, &ctl->empty[stage], (lap - 1) & 1)) { fail(ctl, 1); ok = false; break; }
-                    const int second = kit >= p.k_pair ? 1 : 0, k = (kit - (second ? p.k_pair : 0)) * BK;
-                    const uint32_t dst = smem_u32(tiles + stage * STAGE) + (is_a ? 0 : A_STAGE), bar = smem_u32(&ctl->full[stage]);
-                    if (rank == 0) mbar_expect_tx(bar, 2 * (is_a ? A_STAGE : B_STAGE));
-                    if (is_a) {
-                        const CUtensorMap *map = &p.a[p.groups == 2 ? tile.group : second];
-                        if constexpr (A_MN) {
-                            tma_load_2d_2sm(dst, map, m0, k, bar & PEER_MASK);
-                            tma_load_2d_2sm(dst + 8192, map, m0 + 64, k, bar & PEER_MASK);
-                        } else tma_load_2d_2sm(dst, map, k, m0, bar & PEER_MASK);
-                    } else {
-                        const CUtensorMap *map = &p.b[GATED ? (int)rank : second];
-                        if constexpr (B_MN) {
-#pragma unroll
-                            for (int i = 0; i < BN / 128; ++i) tma_load_2d_2sm(dst + i * 8192, map, n0 + i * 64, k, bar & PEER_MASK);
-                        } else tma_load_2d_2sm(dst, map, k, n0, bar & PEER_MASK);
-                    }
-                    if (++stage == STAGES) { stage = 0; ++lap; }
+                    const int second = kit >= k_pair ? 1 : 0, k = (kit - (second ? k_pair : 0)) * BK;
+                    const uint32_t dst = smem_u32(tiles + stage * STAGE), bar = smem_u32(&ctl->full[stage]) & PEER_MASK;
+                    if (rank == 0) mbar_expect_tx(smem_u32(&ctl->full[stage]), 2 * STAGE);
+                    const CUtensorMap *am = &q.a[second], *bm = &q.b[GATED ? (int)rank : second];
+                    if (a_mn) {
+                        tma_load_2d_2sm(dst, am, m0, k, bar);
+                        tma_load_2d_2sm(dst + 8192, am, m0 + 64, k, bar);
+                    } else tma_load_2d_2sm(dst, am, k, m0, bar);
+                    if (b_mn) {
+                        tma_load_2d_2sm(dst + A_STAGE, bm, n0, k, bar);
+                        if (BN == 256) tma_load_2d_2sm(dst + A_STAGE + 8192, bm, n0 + 64, k, bar);
+                    } else tma_load_2d_2sm(dst + A_STAGE, bm, k, n0, bar);
+                    stage += 2;
+                    if (stage >= (uint32_t)STAGES) { stage -= STAGES; ++lap; }
                 }
+                step += (uint32_t)k_iters;
             }
             // after a failure: the copies still in flight land before the CTA gives its shared memory up
-            if (is_a && rank == 0 && *reinterpret_cast<volatile uint32_t *>(&ctl->failed) != 0u) {
-                const uint32_t issued = lap * STAGES + stage, first = issued > STAGES ? issued - STAGES : 0;
-                for (uint32_t i = first; i < issued; ++i)
-                    if (!wait(ctl, p.wait_ns, &ctl->full[i % STAGES], (i / STAGES) & 1, false)) break;
-            }
+            if (rank == 0 && *reinterpret_cast<volatile uint32_t *>(&ctl->failed) != 0u)
+                for (uint32_t i = 0, s = stage, l = lap; i < (uint32_t)STAGES; i += 2) {      // this thread's last uses, newest first
+                    if (s < 2) { if (l == 0) break; s += STAGES; --l; }
+                    s -= 2;
+                    if (!wait(ctl, p.wait_ns, &ctl->full[s], l & 1, false)) break;
+                }
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            const uint64_t a0 = A_MN ? smem_desc_mn(smem_u32(tiles)) : smem_desc_sw128(smem_u32(tiles));
-            const uint64_t b0 = B_MN ? smem_desc_mn(smem_u32(tiles + A_STAGE)) : smem_desc_sw128(smem_u32(tiles + A_STAGE));
-            constexpr uint64_t A_STEP = A_MN ? 2048 >> 4 : 32 >> 4, B_STEP = B_MN ? 2048 >> 4 : 32 >> 4;   // 16 elements of K
             uint32_t stage = 0, phase = 0, count = 0;
             bool ok = true;
             for (uint32_t t = pair; t < p.tiles && ok; t += pairs, ++count) {
@@ -341,12 +351,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_produc
                 if (use > 0 && !wait(ctl, p.wait_ns, &ctl->acc_empty[buf], (use - 1) & 1)) { fail(ctl, 4); ok = false; break; }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t d = tmem_base + buf * BN;
-                for (int kit = 0; kit < p.k_iters; ++kit) {
+                const Problem &q = p.q[tile_at<WIDTH>(p, t).problem];
+                const uint64_t a0 = q.a_mn ? smem_desc_mn(smem_u32(tiles)) : smem_desc_sw128(smem_u32(tiles));
+                const uint64_t b0 = q.b_mn ? smem_desc_mn(smem_u32(tiles + A_STAGE)) : smem_desc_sw128(smem_u32(tiles + A_STAGE));
+                const uint64_t a_step = q.a_mn ? 2048 >> 4 : 32 >> 4, b_step = q.b_mn ? 2048 >> 4 : 32 >> 4;      // 16 elements of K
+                const uint32_t idesc = q.idesc;
+                const int k_iters = q.k_iters;
+                for (int kit = 0; kit < k_iters; ++kit) {
                     if (!wait(ctl, p.wait_ns, &ctl->full[stage], phase)) { fail(ctl, 2); ok = false; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint64_t a = a0 + (uint64_t)(stage * (STAGE >> 4)), b = b0 + (uint64_t)(stage * (STAGE >> 4));
 #pragma unroll
-                    for (int k = 0; k < BK / 16; ++k) mma_f16_2sm(d, a + k * A_STEP, b + k * B_STEP, p.idesc, (kit | k) != 0 ? 1u : 0u);
+                    for (int k = 0; k < BK / 16; ++k) mma_f16_2sm(d, a + k * a_step, b + k * b_step, idesc, (kit | k) != 0 ? 1u : 0u);
                     umma_commit_2sm(smem_u32(&ctl->empty[stage]));
                     if (++stage == STAGES) { stage = 0; phase ^= 1; }
                 }
@@ -360,20 +376,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_produc
     } else if (warp < 2 + EPI_WARPS) {
         bnn_pdl_wait();
         bnn_pdl_launch_next();
-        const int q = warp & 3, half = (warp - 2) >> 2;
-        const uint32_t quadrant = (uint32_t)(32 * q) << 16;
+        const int quad = warp & 3, half = (warp - 2) >> 2;
+        const uint32_t quadrant = (uint32_t)(32 * quad) << 16;
         float *stage = reinterpret_cast<float *>(ctl + 1) + (warp - 2) * 32 * STAGE_PITCH;
         uint32_t count = 0;
         for (uint32_t t = pair; t < p.tiles; t += pairs, ++count) {
             const uint32_t buf = count & 1;
             const Tile tile = tile_at<WIDTH>(p, t);
+            const Problem &q = p.q[tile.problem];
             if (!wait(ctl, p.wait_ns, &ctl->acc_full[buf], (count >> 1) & 1)) { fail(ctl, 3); break; }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const int64_t m = tile.m0 + rank * 128 + 32 * q + lane;
+            const int64_t m = tile.m0 + (int)rank * 128 + 32 * quad + lane;
             const uint32_t acc = tmem_base + buf * BN + quadrant;
 #pragma unroll 1
             for (int c = half * (WIDTH / 2); c < (half + 1) * (WIDTH / 2); c += 32) {
-                if (tile.n0 + c >= p.N) break;
+                if (tile.n0 + c >= q.N) break;
                 uint32_t ra[32], rb[32];
                 float a[32], b[32];
                 tmem_ld32(acc + c, ra);
@@ -382,11 +399,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_produc
                 if (GATED) tmem_ld_wait(rb);
 #pragma unroll
                 for (int j = 0; j < 32; ++j) {
-                    a[j] = p.k_iters ? __uint_as_float(ra[j]) : 0.0f;
-                    if (GATED) b[j] = p.k_iters ? __uint_as_float(rb[j]) : 0.0f;
+                    a[j] = q.k_iters ? __uint_as_float(ra[j]) : 0.0f;
+                    if (GATED) b[j] = q.k_iters ? __uint_as_float(rb[j]) : 0.0f;
                 }
-                if (p.f16) finish32<EPI, __half>(p, tile.group, m, tile.n0 + c, stage, a, b);
-                else finish32<EPI, __nv_bfloat16>(p, tile.group, m, tile.n0 + c, stage, a, b);
+                if (p.f16) finish32<EPI, __half>(p, q, m, tile.n0 + c, stage, a, b);
+                else finish32<EPI, __nv_bfloat16>(p, q, m, tile.n0 + c, stage, a, b);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
@@ -411,15 +428,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_produc
 // cluster barrier every CTA adds up and finishes its part of the tile through distributed shared memory, in the order of the ranks:
 // one launch, no workspace, the same bits every time.
 // Gated projections: 64 gate rows and the up rows of the same 64 hidden units form the 128 rows of a tile.
-//   warp 0  TMA producer, warp 1  MMA issuer (cta_group::1), warps 2 .. 5  tensor memory -> shared memory, all warps  sum and epilogue
+//   warps 0 and 11  TMA producers, warp 1  MMA issuer (cta_group::1), warps 2 .. 9  tensor memory -> shared memory, all warps  sum and epilogue
 constexpr int FEW_SMEM = 200 * 1024;
-constexpr int FEW_THREADS = 192;
+constexpr int FEW_THREADS = 384;
 constexpr int FEW_STAGES = 12;
 constexpr int FEW_TOKENS = 256;
-constexpr int64_t FEW_ROWS = 256;        // rows from which on the pair kernel is the faster one
+constexpr int64_t FEW_ROWS = 1024;         // beyond, the pair kernel's tiles fill the GPU
 
 struct FewArgs {
     ProductArgs p;                      // a: weights (a[1]: up rows, or the second pair), b: tokens; M tokens, N outputs
+    uint32_t token_tiles;
     int tokens;                         // N of the MMA: tokens per tile, a multiple of 16
     int stages;
     uint32_t stage_bytes, tmem_cols;
@@ -483,9 +501,10 @@ template <typename T> __device__ __forceinline__ void write4(T *p, int n, int ve
     }
 }
 template <int EPI, typename T> __device__ __forceinline__ void finish4(const ProductArgs &p, int64_t m, int64_t n0, float (&a)[4], float (&b)[4]) {
-    const int n = (int)(p.N - n0 < 4 ? p.N - n0 : 4);
+    const Problem &q = p.q[0];
+    const int n = (int)(q.N - n0 < 4 ? q.N - n0 : 4);
     const T *add = static_cast<const T *>(p.add) + m * p.ld_add + n0;
-    T *out = static_cast<T *>(p.out[0]) + m * p.ldo[0] + n0;
+    T *out = static_cast<T *>(q.out[0]) + m * q.ldo[0] + n0;
     float d[4];
     if constexpr (EPI == BNN_EPI_LINEAR || EPI == BNN_EPI_LINEAR_BACK) {
         if (p.bias) {
@@ -497,7 +516,7 @@ template <int EPI, typename T> __device__ __forceinline__ void finish4(const Pro
     if (EPI != BNN_EPI_GATED && p.add) read4(add, n, p.vec_add, d);
     if ((EPI == BNN_EPI_LINEAR || EPI == BNN_EPI_GATED) && p.pre) {
         write4(p.pre + m * p.ldp + n0, n, p.vec_pre, a);
-        if (EPI == BNN_EPI_GATED) write4(p.pre + (p.M + m) * p.ldp + n0, n, p.vec_pre, b);
+        if (EPI == BNN_EPI_GATED) write4(p.pre + (q.M + m) * p.ldp + n0, n, p.vec_pre, b);
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -515,14 +534,15 @@ template <int EPI, typename T> __device__ __forceinline__ void finish4(const Pro
             b[j] = d[j] * value;
         }
     }
-    write4(out, n, p.vec_out, a);
-    if constexpr (EPI == BNN_EPI_GATED_BACK) write4(static_cast<T *>(p.out[1]) + m * p.ldo[1] + n0, n, p.vec_out, b);
+    write4(out, n, q.vec_out, a);
+    if constexpr (EPI == BNN_EPI_GATED_BACK) write4(static_cast<T *>(q.out[1]) + m * q.ldo[1] + n0, n, q.vec_out, b);
 }
 
-template <bool W_MN, int EPI> __global__ void __launch_bounds__(FEW_THREADS) k_product_few(const __grid_constant__ FewArgs f) {
+template <bool W_MN, int EPI> __global__ void __launch_bounds__(FEW_THREADS, 2) k_product_few(const __grid_constant__ FewArgs f) {
     constexpr bool GATED = EPI == BNN_EPI_GATED || EPI == BNN_EPI_GATED_BACK;
     constexpr int ROWS = GATED ? 64 : 128;                        // outputs of a tile
     const ProductArgs &p = f.p;
+    const Problem &q = p.q[0];
     extern __shared__ uint8_t smem_raw[];
     uint8_t *tiles = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ FewControl control;
@@ -531,9 +551,9 @@ template <bool W_MN, int EPI> __global__ void __launch_bounds__(FEW_THREADS) k_p
     const uint32_t rank = cluster_ctarank();
     uint32_t split;
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(split));
-    const uint32_t tile = blockIdx.x / split, tn = tile % p.tiles_n, tt = tile / p.tiles_n;
+    const uint32_t tile = blockIdx.x / split, tn = tile / f.token_tiles, tt = tile - tn * f.token_tiles;     // tiles of the same weights next to each other
     const int64_t n0 = (int64_t)tn * ROWS, t0 = (int64_t)tt * f.tokens;
-    const int first = (int)((int64_t)p.k_iters * rank / split), last = (int)((int64_t)p.k_iters * (rank + 1) / split);
+    const int first = (int)((int64_t)q.k_iters * rank / split), last = (int)((int64_t)q.k_iters * (rank + 1) / split);
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < f.stages; ++s) { mbar_init(smem_u32(&ctl->full[s]), 1); mbar_init(smem_u32(&ctl->empty[s]), 1); }
@@ -552,29 +572,32 @@ template <bool W_MN, int EPI> __global__ void __launch_bounds__(FEW_THREADS) k_p
     bnn_pdl_wait();
     bnn_pdl_launch_next();
 
-    if (warp == 0) {
+    if (warp == 0 || warp == FEW_THREADS / 32 - 1) {              // two producers take the K steps in turn, as in the pair kernel
         if (lane == 0 && !p.drop_loads) {
-            int stage = 0, lap = 0;
-            for (int kit = first; kit < last; ++kit) {
+            const int mine = warp == 0 ? 0 : 1;
+            int stage = mine % f.stages, lap = mine / f.stages;
+            for (int kit = first + mine; kit < last; kit += 2) {
                 if (lap > 0 && !wait(ctl, p.wait_ns, &ctl->empty[stage], (lap - 1) & 1)) { few_fail(ctl, 21); break; }
-                const int second = kit >= p.k_pair ? 1 : 0, k = (kit - (second ? p.k_pair : 0)) * BK;
+                const int second = kit >= q.k_pair ? 1 : 0, k = (kit - (second ? q.k_pair : 0)) * BK;
                 const uint32_t dst = smem_u32(tiles) + stage * f.stage_bytes, bar = smem_u32(&ctl->full[stage]);
                 mbar_expect_tx(bar, f.stage_bytes);
                 if constexpr (GATED) {
-                    tma_load_2d(dst, &p.a[0], k, (int)n0, bar);
-                    tma_load_2d(dst + 8192, &p.a[1], k, (int)n0, bar);
+                    tma_load_2d(dst, &q.a[0], k, (int)n0, bar);
+                    tma_load_2d(dst + 8192, &q.a[1], k, (int)n0, bar);
                 } else if constexpr (W_MN) {
-                    tma_load_2d(dst, &p.a[second], (int)n0, k, bar);
-                    tma_load_2d(dst + 8192, &p.a[second], (int)n0 + 64, k, bar);
-                } else tma_load_2d(dst, &p.a[second], k, (int)n0, bar);
-                tma_load_2d(dst + A_STAGE, &p.b[second], k, (int)t0, bar);
-                if (++stage == f.stages) { stage = 0; ++lap; }
+                    tma_load_2d(dst, &q.a[second], (int)n0, k, bar);
+                    tma_load_2d(dst + 8192, &q.a[second], (int)n0 + 64, k, bar);
+                } else tma_load_2d(dst, &q.a[second], k, (int)n0, bar);
+                tma_load_2d(dst + A_STAGE, &q.b[second], k, (int)t0, bar);
+                stage += 2;
+                while (stage >= f.stages) { stage -= f.stages; ++lap; }
             }
-            if (*reinterpret_cast<volatile uint32_t *>(&ctl->failed) != 0u) {      // copies in flight land before the shared memory is given up
-                const int issued = lap * f.stages + stage;
-                for (int i = issued > f.stages ? issued - f.stages : 0; i < issued; ++i)
-                    if (!wait(ctl, p.wait_ns, &ctl->full[i % f.stages], (i / f.stages) & 1, false)) break;
-            }
+            if (*reinterpret_cast<volatile uint32_t *>(&ctl->failed) != 0u)        // copies in flight land before the shared memory is given up
+                for (int i = 0, s = stage, l = lap; i < f.stages; i += 2) {
+                    s -= 2;
+                    while (s < 0) { s += f.stages; --l; }
+                    if (l < 0 || !wait(ctl, p.wait_ns, &ctl->full[s], l & 1, false)) break;
+                }
         }
     } else if (warp == 1) {
         if (lane == 0) {
@@ -587,7 +610,7 @@ template <bool W_MN, int EPI> __global__ void __launch_bounds__(FEW_THREADS) k_p
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint64_t at = (uint64_t)(stage * (f.stage_bytes >> 4));
 #pragma unroll
-                for (int k = 0; k < BK / 16; ++k) mma_f16(tmem_base, a0 + at + k * A_STEP, b0 + at + k * (32 >> 4), p.idesc, (kit > first || k) ? 1u : 0u);
+                for (int k = 0; k < BK / 16; ++k) mma_f16(tmem_base, a0 + at + k * A_STEP, b0 + at + k * (32 >> 4), q.idesc, (kit > first || k) ? 1u : 0u);
                 mma_commit(&ctl->empty[stage]);
                 if (++stage == f.stages) { stage = 0; phase ^= 1; }
             }
@@ -597,19 +620,19 @@ template <bool W_MN, int EPI> __global__ void __launch_bounds__(FEW_THREADS) k_p
     // The partial tile as part[token][row]: the ring is drained by now and its memory is free.  The MMAs issued before a failure end
     // before tensor memory is given back, hence a wait that does not look at the failure word.
     float *part = reinterpret_cast<float *>(tiles);
-    if (warp >= 2) {
+    if (warp >= 2 && warp < 10) {
         const bool done = wait(ctl, 2 * p.wait_ns, &ctl->acc_full, 0, false);
         if (!done) few_fail(ctl, 23);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         if (done && *reinterpret_cast<volatile uint32_t *>(&ctl->failed) == 0u) {
-            const int q = warp & 3, row = 32 * q + lane;
-            for (int c = 0; c < f.tokens; c += 16) {
-                if (t0 + c >= p.M) break;
+            const int quad = warp & 3, row = 32 * quad + lane;
+            for (int c = warp < 6 ? 0 : 16; c < f.tokens; c += 32) {
+                if (t0 + c >= q.M) break;
                 uint32_t r[16];
                 asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
                              : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
                                "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-                             : "r"(tmem_base + ((uint32_t)(32 * q) << 16) + c) : "memory");
+                             : "r"(tmem_base + ((uint32_t)(32 * quad) << 16) + c) : "memory");
                 asm volatile("tcgen05.wait::ld.sync.aligned;"
                              : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
                                "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
@@ -627,7 +650,7 @@ template <bool W_MN, int EPI> __global__ void __launch_bounds__(FEW_THREADS) k_p
     if (split > 1) cluster_sync_all();
     const bool failed = *reinterpret_cast<volatile uint32_t *>(&ctl->failed) != 0u;
     if (!failed) {
-        const int valid = (int)(p.M - t0 < f.tokens ? p.M - t0 : f.tokens), rows = (int)(p.N - n0 < ROWS ? p.N - n0 : ROWS);
+        const int valid = (int)(q.M - t0 < f.tokens ? q.M - t0 : f.tokens), rows = (int)(q.N - n0 < ROWS ? q.N - n0 : ROWS);
         for (int i = threadIdx.x + FEW_THREADS * (int)rank; i < valid * (ROWS / 4); i += FEW_THREADS * (int)split) {
             const int t = i / (ROWS / 4), row = (i - t * (ROWS / 4)) * 4;
             if (row >= rows) continue;
@@ -649,13 +672,13 @@ template <int BN> constexpr size_t pair_smem() {
 static_assert(pair_smem<256>() <= 227 * 1024 && pair_smem<128>() <= 227 * 1024, "fits the shared memory of an SM");
 
 // Opts in to the shared memory and asks how many pairs fit the device, once per device and kernel; 0 = cannot run.
-template <bool A_MN, bool B_MN, int EPI, int BN> int pairs_of(int device, int sm_count) {
+template <int EPI, int BN> int pairs_of(int device, int sm_count) {
     static std::mutex lock;
     static int cached[64];
     if (device < 0 || device >= 64) return 0;
     std::lock_guard<std::mutex> guard(lock);
     if (cached[device] == 0) {
-        auto kernel = k_product_pair<A_MN, B_MN, EPI, BN>;
+        auto kernel = k_product_pair<EPI, BN>;
         int pairs = 0;
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pair_smem<BN>()) == cudaSuccess) {
             cudaLaunchConfig_t cfg = {};
@@ -672,11 +695,11 @@ template <bool A_MN, bool B_MN, int EPI, int BN> int pairs_of(int device, int sm
     return cached[device] > 0 ? cached[device] : 0;
 }
 
-template <bool A_MN, bool B_MN, int EPI, int BN> int launch(bnn_ctx *ctx, const ProductArgs &a) {
-    const int pairs = pairs_of<A_MN, B_MN, EPI, BN>(ctx->device, ctx->sm_count);
+template <int EPI, int BN> int launch(bnn_ctx *ctx, const ProductArgs &a) {
+    const int pairs = pairs_of<EPI, BN>(ctx->device, ctx->sm_count);
     if (pairs == 0) return BNN_ERR_CUDA;
     const unsigned n = a.tiles < (uint32_t)pairs ? a.tiles : (unsigned)pairs;
-    BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_product_pair<A_MN, B_MN, EPI, BN>, dim3(2 * n), dim3(THREADS), pair_smem<BN>(), ctx->stream, a));
+    BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_product_pair<EPI, BN>, dim3(2 * n), dim3(THREADS), pair_smem<BN>(), ctx->stream, a));
     return bnn_check_launch(ctx);
 }
 
@@ -722,16 +745,20 @@ int bnn_product_status(bnn_ctx *ctx, int *code) {
 }
 
 namespace {
+bool is_gated(const BnnProduct &q) { return q.epilogue == BNN_EPI_GATED || q.epilogue == BNN_EPI_GATED_BACK; }
+int64_t steps_of(const BnnProduct &q) { return (q.K + BK - 1) / BK * (is_gated(q) ? 1 : q.pairs); }
 ProductArgs common_args(bnn_ctx *ctx, const BnnProduct &q) {
     ProductArgs a{};
-    a.M = q.M; a.N = q.N; a.groups = q.groups;
-    const bool gated = q.epilogue == BNN_EPI_GATED || q.epilogue == BNN_EPI_GATED_BACK;
-    const int64_t steps = (q.K + BK - 1) / BK;
-    a.k_pair = (int)steps; a.k_iters = (int)(steps * (gated ? 1 : q.pairs));
     a.bias = q.bias; a.add = q.add; a.ld_add = q.ld_add; a.pre = q.pre; a.ldp = q.ldp; a.act = q.act; a.f16 = q.dtype == BNN_F16;
-    for (int i = 0; i < 2; ++i) { a.out[i] = q.out[i]; a.ldo[i] = q.ldo[i]; }
     a.wait_ns = ctx->wait_limit_ns; a.drop_loads = ctx->drop_loads;
+    a.problems = 1;
     return a;
+}
+void common_problem(Problem &w, const BnnProduct &q) {
+    w.M = q.M; w.N = q.N;
+    w.k_pair = (int)((q.K + BK - 1) / BK); w.k_iters = (int)steps_of(q);
+    w.a_mn = q.a_mn; w.b_mn = q.b_mn;
+    for (int i = 0; i < 2; ++i) { w.out[i] = q.out[i]; w.ldo[i] = q.ldo[i]; }
 }
 // float32 accumulators, both operands of the call's type, N columns, M rows; whether each operand lies against the sum.
 uint32_t instruction(int dtype, int a_mn, int b_mn, int n, int m) {
@@ -739,79 +766,141 @@ uint32_t instruction(int dtype, int a_mn, int b_mn, int n, int m) {
     return (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
+int64_t pair_tiles(const BnnProduct &q, int bn) {
+    const int64_t width = is_gated(q) ? bn / 2 : bn;
+    return (q.M + TM - 1) / TM * ((q.N + width - 1) / width);
+}
+// Which kernel, and how k_product_few divides the work, by estimates of both in microseconds.  Fitted to measured times (N x K, rows,
+// few / pair): 4096 x 4096, 1: 10.7 / 27.8, 128: 14.2 / 25.8, 384: 22.5 / 26.8, 768: 37.5 / 30.4; 512 x 8192, 512: 16.0 / 44.1; 8192 x 1024,
+// 64: 9.5 / 10.6, 192: 14.1 / 11.3; 256 x 256, 1: 3.9 / 5.3, 128: 9.0 / 5.9.
+//   pair: 4.5 + 0.30 per K step and round of tiles, or the weights at 3.3 TB/s (gated, 5500 x 2048 twice: 20.9) if that takes longer.
+//   few:  3 for every round of CTAs, + per K step of an SM's CTAs 0.12 + 0.0012 per token of a tile, at least 0.28 (0.26 with
+//         two CTAs per SM): what one SM draws from HBM (8192 x 8192, one row: 40 us on 64 SMs, 26 on all); + 1 (2 with a split sum) + 0.041 per token of a CTA's share of the epilogue.
+// More, smaller token tiles keep more SMs busy, fewer read the weights less often; the sum is split while there are SMs left and
+// every CTA keeps four K steps.
+double pair_cost(const bnn_ctx *ctx, const BnnProduct &q) {
+    const int64_t pairs = ctx->sm_count / 2;
+    const double steps = 4.5 + 0.30 * (double)steps_of(q) * (double)((pair_tiles(q, 256) + pairs - 1) / pairs);
+    const double weights = 4.5 + 2.0 * (double)q.N * (double)q.K * (is_gated(q) ? 2 : q.pairs) / 3.3e6;
+    return steps > weights ? steps : weights;
+}
+// CTAs that are resident at once in clusters of 1, 2, 4 and 8, one or two per SM (cudaOccupancyMaxActiveClusters with the whole or half
+// of the shared memory: the SMs of a GPC are not a multiple of the larger clusters).
+constexpr int FEW_RESIDENT[2][4] = {{148, 148, 132, 120}, {296, 296, 284, 264}};
+struct FewPlan { int64_t tiles; int token_tiles, tokens, split, per_sm; double cost; };
+FewPlan few_plan(const BnnProduct &q) {
+    const int64_t rows = is_gated(q) ? 64 : 128, steps = steps_of(q), weight_tiles = (q.N + rows - 1) / rows;
+    FewPlan best{};
+    best.cost = 1e30;
+    int last = 0;
+    for (int most = FEW_TOKENS; most >= 16; most /= 2) {
+        FewPlan f{};
+        f.token_tiles = (int)((q.M + most - 1) / most);
+        if (f.token_tiles == last) continue;
+        last = f.token_tiles;
+        f.tokens = (int)(((q.M + f.token_tiles - 1) / f.token_tiles + 15) & ~int64_t(15));
+        f.tiles = weight_tiles * f.token_tiles;
+        for (int log = 0; log < 4; ++log) {
+            f.split = 1 << log;
+            if (log && steps < f.split * 4) break;
+            const int64_t ctas = f.tiles * f.split;
+            f.per_sm = ctas > FEW_RESIDENT[0][log] && f.tokens <= 64 ? 2 : 1;      // half of an SM's memory still holds four stages of 64 tokens
+            const int64_t resident = FEW_RESIDENT[f.per_sm - 1][log], rounds = (ctas + resident - 1) / resident;
+            const double load = (double)(rounds > 1 ? rounds * f.per_sm : (ctas + 147) / 148), cta_steps = (double)((steps + f.split - 1) / f.split);
+            double step = 0.12 + 0.0012 * f.tokens;
+            if (step < (f.per_sm == 2 ? 0.26 : 0.28)) step = f.per_sm == 2 ? 0.26 : 0.28;
+            f.cost = 3.0 * (double)rounds + load * cta_steps * step + (f.split > 1 ? 2.0 : 1.0) + 0.041 * f.tokens / f.split * load;
+            if (f.cost < best.cost) best = f;
+        }
+    }
+    return best;
+}
 int product_few(bnn_ctx *ctx, const BnnProduct &q) {
-    const bool gated = q.epilogue == BNN_EPI_GATED || q.epilogue == BNN_EPI_GATED_BACK;
+    const FewPlan plan = few_plan(q);
+    if (plan.tiles * plan.split > 0x7fffffff) return BNN_ERR_INVALID_ARG;
     FewArgs f{};
     f.p = common_args(ctx, q);
+    Problem &w = f.p.q[0];
+    common_problem(w, q);
     const auto fours = [](const void *at, int64_t ld, int64_t n, int size) { return reinterpret_cast<uintptr_t>(at) % (4 * size) == 0 && (n <= 1 || ld % 4 == 0); };
     f.p.vec_bias = fours(q.bias, 0, 1, 2); f.p.vec_add = fours(q.add, q.ld_add, q.M, 2); f.p.vec_pre = fours(q.pre, q.ldp, 2 * q.M, 4);
-    f.p.vec_out = fours(q.out[0], q.ldo[0], q.M, 2) && fours(q.out[1], q.ldo[1], q.M, 2);
-    const int rows = gated ? 64 : 128;
-    const int64_t token_tiles = (q.M + FEW_TOKENS - 1) / FEW_TOKENS;
-    f.tokens = (int)(((q.M + token_tiles - 1) / token_tiles + 15) & ~int64_t(15));
-    f.p.tiles_n = (uint32_t)((q.N + rows - 1) / rows);
-    const int64_t tiles = f.p.tiles_n * token_tiles;
-    f.p.idesc = instruction(q.dtype, q.b_mn, 0, f.tokens, 128);
+    w.vec_out = fours(q.out[0], q.ldo[0], q.M, 2) && fours(q.out[1], q.ldo[1], q.M, 2);
+    const int rows = is_gated(q) ? 64 : 128;
+    f.tokens = plan.tokens; f.token_tiles = (uint32_t)plan.token_tiles;
+    w.tiles_n = (uint32_t)((q.N + rows - 1) / rows);
+    w.idesc = instruction(q.dtype, q.b_mn, 0, f.tokens, 128);
     f.stage_bytes = A_STAGE + (uint32_t)f.tokens * BK * 2;
     f.tmem_cols = 32;
     while ((int)f.tmem_cols < f.tokens) f.tmem_cols *= 2;
-    // Split the sum while that brings more SMs to load and leaves every CTA at least four K steps.  Two CTAs share an SM where half of its
-    // memory still holds four stages (up to 64 tokens).
-    const int per_sm = f.tokens <= 64 ? 2 : 1;
-    int split = 1;
-    while (split < 8 && tiles * split * 2 <= per_sm * ctx->sm_count && f.p.k_iters >= split * 2 * 4) split *= 2;
-    const int budget = tiles * split > ctx->sm_count && per_sm == 2 ? FEW_SMEM / 2 : FEW_SMEM, steps = (f.p.k_iters + split - 1) / split;
+    const int budget = plan.per_sm == 2 ? FEW_SMEM / 2 : FEW_SMEM, steps = (w.k_iters + plan.split - 1) / plan.split;
     f.stages = budget / (int)f.stage_bytes;
-    f.stages = f.stages < 2 ? 2 : f.stages > FEW_STAGES ? FEW_STAGES : f.stages;
-    if (f.stages > steps) f.stages = steps > 0 ? steps : 1;
+    f.stages = f.stages > FEW_STAGES ? FEW_STAGES : f.stages;
+    if (f.stages > steps) f.stages = steps;
+    f.stages = f.stages < 2 ? 2 : f.stages & ~1;
     if (q.K > 0) {
         for (int i = 0; i < 2; ++i) {
             if (q.b[i].p)
-                if (int st = q.b_mn ? map16(ctx, &f.p.a[i], q.b[i].p, q.b[i].ld, q.K, q.N, BK) : map16(ctx, &f.p.a[i], q.b[i].p, q.b[i].ld, q.N, q.K, rows)) return st;
+                if (int st = q.b_mn ? map16(ctx, &w.a[i], q.b[i].p, q.b[i].ld, q.K, q.N, BK) : map16(ctx, &w.a[i], q.b[i].p, q.b[i].ld, q.N, q.K, rows)) return st;
             if (q.a[i].p)
-                if (int st = map16(ctx, &f.p.b[i], q.a[i].p, q.a[i].ld, q.M, q.K, f.tokens)) return st;
+                if (int st = map16(ctx, &w.b[i], q.a[i].p, q.a[i].ld, q.M, q.K, f.tokens)) return st;
         }
     }
-    if (q.b_mn) return launch_few<true, BNN_EPI_LINEAR>(ctx, f, (unsigned)tiles, (unsigned)split);
+    const unsigned tiles = (unsigned)plan.tiles, split = (unsigned)plan.split;
+    if (q.b_mn) return launch_few<true, BNN_EPI_LINEAR>(ctx, f, tiles, split);
     switch (q.epilogue) {
-        case BNN_EPI_LINEAR: return launch_few<false, BNN_EPI_LINEAR>(ctx, f, (unsigned)tiles, (unsigned)split);
-        case BNN_EPI_LINEAR_BACK: return launch_few<false, BNN_EPI_LINEAR_BACK>(ctx, f, (unsigned)tiles, (unsigned)split);
-        case BNN_EPI_GATED: return launch_few<false, BNN_EPI_GATED>(ctx, f, (unsigned)tiles, (unsigned)split);
-        default: return launch_few<false, BNN_EPI_GATED_BACK>(ctx, f, (unsigned)tiles, (unsigned)split);
+        case BNN_EPI_LINEAR: return launch_few<false, BNN_EPI_LINEAR>(ctx, f, tiles, split);
+        case BNN_EPI_LINEAR_BACK: return launch_few<false, BNN_EPI_LINEAR_BACK>(ctx, f, tiles, split);
+        case BNN_EPI_GATED: return launch_few<false, BNN_EPI_GATED>(ctx, f, tiles, split);
+        default: return launch_few<false, BNN_EPI_GATED_BACK>(ctx, f, tiles, split);
     }
 }
 }  // namespace
 
-int bnn_product(bnn_ctx *ctx, const BnnProduct &q) {
-    const bool gated = q.epilogue == BNN_EPI_GATED || q.epilogue == BNN_EPI_GATED_BACK;
-    if (!q.a_mn && q.groups == 1 && q.M <= FEW_ROWS) return product_few(ctx, q);
+bool bnn_product_few(const bnn_ctx *ctx, const BnnProduct &q) {
+    return !q.a_mn && q.M <= FEW_ROWS && few_plan(q).cost < pair_cost(ctx, q);
+}
+
+int bnn_product(bnn_ctx *ctx, const BnnProduct *list, int count) {
+    if (count < 1 || count > PROBLEMS) return BNN_ERR_INVALID_ARG;
+    if (count == 1 && bnn_product_few(ctx, list[0])) return product_few(ctx, list[0]);
     // Half-width tiles where whole ones would leave half of the pairs without work.
-    const int64_t tm = (q.M + TM - 1) / TM, whole = tm * ((q.N + (gated ? 127 : 255)) / (gated ? 128 : 256)) * q.groups;
+    int64_t whole = 0, tiles = 0;
+    for (int i = 0; i < count; ++i) whole += pair_tiles(list[i], 256);
     const int bn = 2 * whole <= ctx->sm_count / 2 ? 128 : 256;
-    const int64_t width = gated ? bn / 2 : bn, tn = (q.N + width - 1) / width;
-    if (tm * tn * q.groups > 0x7fffffff) return BNN_ERR_INVALID_ARG;
-    ProductArgs a = common_args(ctx, q);
-    a.tiles_m = (uint32_t)tm; a.tiles_n = (uint32_t)tn; a.tiles = (uint32_t)(tm * tn * q.groups);
-    a.idesc = instruction(q.dtype, q.a_mn, q.b_mn, bn, TM);
-    a.vec_bias = width_of(q.bias, 0, 1, 2); a.vec_add = width_of(q.add, q.ld_add, q.M, 2); a.vec_pre = width_of(q.pre, q.ldp, 2 * q.M, 4);
-    a.vec_out = width_of(q.out[0], q.ldo[0], q.M, 2);
-    if (q.out[1]) { const int v = width_of(q.out[1], q.ldo[1], q.M, 2); a.vec_out = v < a.vec_out ? v : a.vec_out; }
-    if (q.K > 0) {
-        for (int i = 0; i < 2; ++i) {
-            if (q.a[i].p)
-                if (int st = q.a_mn ? map16(ctx, &a.a[i], q.a[i].p, q.a[i].ld, q.K, q.M, BK) : map16(ctx, &a.a[i], q.a[i].p, q.a[i].ld, q.M, q.K, 128)) return st;
-            if (q.b[i].p)
-                if (int st = q.b_mn ? map16(ctx, &a.b[i], q.b[i].p, q.b[i].ld, q.K, q.N, BK) : map16(ctx, &a.b[i], q.b[i].p, q.b[i].ld, q.N, q.K, bn / 2)) return st;
+    ProductArgs a = common_args(ctx, list[0]);
+    a.problems = count;
+    const BnnProduct *order[PROBLEMS];
+    for (int i = 0; i < count; ++i) order[i] = &list[i];
+    for (int i = 1; i < count; ++i)                      // the longest sums first: short tiles fill the end of the launch
+        for (int j = i; j > 0 && steps_of(*order[j]) > steps_of(*order[j - 1]); --j) { const BnnProduct *t = order[j]; order[j] = order[j - 1]; order[j - 1] = t; }
+    for (int i = 0; i < count; ++i) {
+        const BnnProduct &q = *order[i];
+        Problem &w = a.q[i];
+        common_problem(w, q);
+        const int64_t width = is_gated(q) ? bn / 2 : bn;
+        w.first = (uint32_t)tiles; w.tiles_m = (uint32_t)((q.M + TM - 1) / TM); w.tiles_n = (uint32_t)((q.N + width - 1) / width);
+        tiles += pair_tiles(q, bn);
+        if (tiles > 0x7fffffff) return BNN_ERR_INVALID_ARG;
+        w.idesc = instruction(q.dtype, q.a_mn, q.b_mn, bn, TM);
+        w.vec_out = width_of(q.out[0], q.ldo[0], q.M, 2);
+        if (q.out[1]) { const int v = width_of(q.out[1], q.ldo[1], q.M, 2); w.vec_out = v < w.vec_out ? v : w.vec_out; }
+        if (q.K == 0) continue;
+        for (int k = 0; k < 2; ++k) {
+            if (q.a[k].p)
+                if (int st = q.a_mn ? map16(ctx, &w.a[k], q.a[k].p, q.a[k].ld, q.K, q.M, BK) : map16(ctx, &w.a[k], q.a[k].p, q.a[k].ld, q.M, q.K, 128)) return st;
+            if (q.b[k].p)
+                if (int st = q.b_mn ? map16(ctx, &w.b[k], q.b[k].p, q.b[k].ld, q.K, q.N, BK) : map16(ctx, &w.b[k], q.b[k].p, q.b[k].ld, q.N, q.K, bn / 2)) return st;
         }
     }
-#define BNN_LAUNCH(A_MN, B_MN, EPI) (bn == 256 ? launch<A_MN, B_MN, EPI, 256>(ctx, a) : launch<A_MN, B_MN, EPI, 128>(ctx, a))
-    if (q.a_mn) return BNN_LAUNCH(true, true, BNN_EPI_LINEAR);
-    if (q.b_mn) return BNN_LAUNCH(false, true, BNN_EPI_LINEAR);
+    a.tiles = (uint32_t)tiles;
+    const BnnProduct &q = list[0];
+    a.vec_bias = width_of(q.bias, 0, 1, 2); a.vec_add = width_of(q.add, q.ld_add, q.M, 2); a.vec_pre = width_of(q.pre, q.ldp, 2 * q.M, 4);
+#define BNN_LAUNCH(EPI) (bn == 256 ? launch<EPI, 256>(ctx, a) : launch<EPI, 128>(ctx, a))
     switch (q.epilogue) {
-        case BNN_EPI_LINEAR: return BNN_LAUNCH(false, false, BNN_EPI_LINEAR);
-        case BNN_EPI_LINEAR_BACK: return BNN_LAUNCH(false, false, BNN_EPI_LINEAR_BACK);
-        case BNN_EPI_GATED: return BNN_LAUNCH(false, false, BNN_EPI_GATED);
-        default: return BNN_LAUNCH(false, false, BNN_EPI_GATED_BACK);
+        case BNN_EPI_LINEAR: return BNN_LAUNCH(BNN_EPI_LINEAR);
+        case BNN_EPI_LINEAR_BACK: return BNN_LAUNCH(BNN_EPI_LINEAR_BACK);
+        case BNN_EPI_GATED: return BNN_LAUNCH(BNN_EPI_GATED);
+        default: return BNN_LAUNCH(BNN_EPI_GATED_BACK);
     }
 #undef BNN_LAUNCH
 }

@@ -17,7 +17,6 @@ struct BnnProduct {
     BnnOperand a[2], b[2];
     int a_mn, b_mn;
     int pairs;                    // 2: out = a0 b0 + a1 b1 (linear epilogues)
-    int groups;                   // 2: out0 = a0 b0, out1 = a1 b0 (linear epilogue)
     int64_t M, N, K;              // K: of each pair
     const void *bias;             // N or NULL
     const void *add; int64_t ld_add;
@@ -25,5 +24,8 @@ struct BnnProduct {
     float *pre; int64_t ldp;      // EPI_GATED: [2][M][ldp]
     int act;
 };
-// Every operand must satisfy bnn_rows16.  M, N > 0; K = 0 is the empty sum.
-int bnn_product(bnn_ctx *ctx, const BnnProduct &p);
+// Up to three products in one launch (several: linear epilogue without bias, add or pre).  Every operand must satisfy bnn_rows16.
+// M, N > 0; K = 0 is the empty sum.
+int bnn_product(bnn_ctx *ctx, const BnnProduct *list, int count);
+// Whether a product of few rows runs on the kernel for those (alone in its launch).
+bool bnn_product_few(const bnn_ctx *ctx, const BnnProduct &p);
