@@ -503,7 +503,7 @@ class Context:
         return t
 
     def _like(self, x):
-        """A contiguous matrix of x's shape and type."""
+        """A contiguous tensor of x's shape and type."""
         return torch.empty_like(x) if x.is_contiguous() and not self._elsewhere() else self._new(*x.shape, dtype=x.dtype)
 
     def _used(self, *tensors):
@@ -594,9 +594,10 @@ class Context:
         gp, ldg = self._fit(dy, M, N, layer.dtype, "dy")
         xp, ldx = self._fit(x, M, K, layer.dtype, "x")
         pp, ldp = self._fit(pre, M, N, torch.float32, "pre")
-        dx = self._new(M, K, dtype=layer.dtype) if want_dx else None
-        dW = self._new(N, K, dtype=layer.dtype) if want_dW else None
-        db = self._new(N, dtype=layer.dtype) if want_db and layer.tensors[1] is not None else None
+        W, bias = layer.tensors
+        dx = self._like(x) if want_dx else None
+        dW = self._like(W) if want_dW else None
+        db = self._like(bias) if want_db and bias is not None else None
         self._ck(lib().bnn_linear_backward(self._h, layer.ref, gp, ldg, xp, ldx, M, pp, ldp, _ptr(dx), K, _ptr(dW), K, _ptr(db)),
                  "bnn_linear_backward")
         self._used(dy, x, pre, *layer.tensors)
@@ -629,8 +630,8 @@ class Context:
         gp, ldg = self._fit(dh, M, N, layer.dtype, "dh")
         xp, ldx = self._fit(x, M, K, layer.dtype, "x")
         pp, ldp = self._planes(pre, M, N)
-        dx = self._new(M, K, dtype=layer.dtype) if want_dx else None
-        dWg, dWu = (self._new(N, K, dtype=layer.dtype) if want_dW else None for _ in range(2))
+        dx = self._like(x) if want_dx else None
+        dWg, dWu = (self._like(layer.tensors[0]) if want_dW else None for _ in range(2))
         self._ck(lib().bnn_gated_backward(self._h, layer.ref, gp, ldg, xp, ldx, M, pp, ldp, _ptr(dx), K, _ptr(dWg), K, _ptr(dWu), K),
                  "bnn_gated_backward")
         self._used(dh, x, pre, *layer.tensors)
@@ -679,13 +680,13 @@ class Context:
         post_w, post_c, pre_w, pre_c, gate = layer.tensors
 
         def like(t, wanted=True):
-            return self._new(D, dtype=layer.dtype) if t is not None and wanted else None
+            return self._like(t) if t is not None and wanted else None
 
         out = {"dx": self._like(x), "dblock": self._like(x) if block is not None else None,
                "dgate": None, "dpost_weight": like(post_w, d.post), "dpost_shift": like(post_c, d.post),
                "dpre_weight": like(pre_w, d.pre), "dpre_shift": like(pre_c, d.pre)}
         if gate is not None and block is not None:
-            out["dgate"] = self._new(layer.gates, D, dtype=layer.dtype)
+            out["dgate"] = self._like(gate)
             used = -(-M // d.rows_per_gate)
             if used < layer.gates:                    # gate rows that no row of the stream uses
                 with torch.cuda.stream(self.stream):

@@ -9,9 +9,52 @@
 
 namespace {
 
+// d *= act'(z), eight at a time; the choice of the activation is made once.
+template <int ACT> __device__ __forceinline__ void slopes8_of(const float (&z)[8], float (&d)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        float value;
+        d[j] *= act_slope(ACT, z[j], value);
+    }
+}
+__device__ __forceinline__ void slopes8(int act, const float (&z)[8], float (&d)[8]) {
+    switch (act) {
+        case BNN_ACT_RELU: slopes8_of<BNN_ACT_RELU>(z, d); break;
+        case BNN_ACT_GELU: slopes8_of<BNN_ACT_GELU>(z, d); break;
+        case BNN_ACT_GELU_TANH: slopes8_of<BNN_ACT_GELU_TANH>(z, d); break;
+        case BNN_ACT_SILU: slopes8_of<BNN_ACT_SILU>(z, d); break;
+        case BNN_ACT_SIGMOID: slopes8_of<BNN_ACT_SIGMOID>(z, d); break;
+        case BNN_ACT_HTANH: slopes8_of<BNN_ACT_HTANH>(z, d); break;
+        default: break;
+    }
+}
+// a = g, b = u, d = dh -> a = dg, b = du.
+template <int ACT> __device__ __forceinline__ void gated8_of(const float (&d)[8], float (&a)[8], float (&b)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        float value;
+        const float slope = act_slope(ACT, a[j], value);
+        a[j] = d[j] * b[j] * slope;
+        b[j] = d[j] * value;
+    }
+}
+__device__ __forceinline__ void gated8(int act, const float (&d)[8], float (&a)[8], float (&b)[8]) {
+    switch (act) {
+        case BNN_ACT_RELU: gated8_of<BNN_ACT_RELU>(d, a, b); break;
+        case BNN_ACT_GELU: gated8_of<BNN_ACT_GELU>(d, a, b); break;
+        case BNN_ACT_GELU_TANH: gated8_of<BNN_ACT_GELU_TANH>(d, a, b); break;
+        case BNN_ACT_SILU: gated8_of<BNN_ACT_SILU>(d, a, b); break;
+        case BNN_ACT_SIGMOID: gated8_of<BNN_ACT_SIGMOID>(d, a, b); break;
+        case BNN_ACT_HTANH: gated8_of<BNN_ACT_HTANH>(d, a, b); break;
+        default: gated8_of<BNN_ACT_NONE>(d, a, b); break;
+    }
+}
+
 // Copies a matrix whose rows are not whole 16-byte groups to one whose rows are: what TMA can read.  Streaming, both sides coalesced.
 __global__ void __launch_bounds__(256) k_repitch(const uint16_t *__restrict__ src, int64_t ld, uint16_t *__restrict__ dst, int64_t pitch,
                                                  int64_t rows, int64_t cols) {
+    bnn_pdl_wait();
+    bnn_pdl_launch_next();
     for (int64_t m = blockIdx.y; m < rows; m += gridDim.y) {
         const int64_t c0 = (int64_t)blockIdx.x * 2048 + threadIdx.x;
 #pragma unroll
@@ -22,63 +65,68 @@ __global__ void __launch_bounds__(256) k_repitch(const uint16_t *__restrict__ sr
     }
 }
 
-// dz = dy act'(pre) and/or the partial column sums of dz: a block takes 256 columns (8 per thread) of one chunk of rows, eight
-// rows at a time.  Without `pre` dz is dy itself and only the sums are taken.
+// dz = dy act'(pre) and/or the column sums of dz: a block takes 64 columns (8 per thread) of one chunk of rows, 32 rows at a time.  With
+// a single chunk (few rows) the sums are the bias gradient itself, otherwise partial sums.  Without `pre` dz is dy itself and only the
+// sums are taken.
 struct SlopeArgs {
     const void *dy; int64_t lddy;
     const float *pre; int64_t ldp;
     void *dz; int64_t lddz;
     float *part;                       // [chunk][N] or NULL
+    void *sum;                         // N or NULL
     int64_t M, N, chunk_rows;
     int act, vec;                      // vec: rows of dy, pre and dz in 16-byte groups, N % 8 == 0
 };
+constexpr int SUM_COLS = 64, SUM_ROWS = 32;
 template <typename T>
 __global__ void __launch_bounds__(256) k_act_backward(const SlopeArgs p) {
-    __shared__ float sums[8][256 + 8];
-    const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
-    const int64_t c0 = (int64_t)blockIdx.x * 256 + cx * 8;
+    __shared__ float sums[SUM_ROWS][SUM_COLS + 1];
+    const int cx = threadIdx.x & 7, ry = threadIdx.x >> 3;
+    const int64_t c0 = (int64_t)blockIdx.x * SUM_COLS + cx * 8;
     const int64_t first = (int64_t)blockIdx.y * p.chunk_rows, end = first + p.chunk_rows < p.M ? first + p.chunk_rows : p.M;
     const T *dy = static_cast<const T *>(p.dy);
     T *dz = static_cast<T *>(p.dz);
+    bnn_pdl_wait();
+    bnn_pdl_launch_next();
     float s[8] = {};
-    for (int64_t m = first + ry; m < end; m += 8) {
-        if (c0 >= p.N) break;
-        float d[8], z[8];
-        if (p.vec) {
-            load8(dy + m * p.lddy + c0, d);
-            if (p.pre) load8(p.pre + m * p.ldp + c0, z);
-        } else {
+    if (c0 < p.N) {
+#pragma unroll 2
+        for (int64_t m = first + ry; m < end; m += SUM_ROWS) {
+            float d[8], z[8];
+            if (p.vec) {
+                load8(dy + m * p.lddy + c0, d);
+                if (p.pre) load8(p.pre + m * p.ldp + c0, z);
+            } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                d[j] = c0 + j < p.N ? to_f32(dy[m * p.lddy + c0 + j]) : 0.0f;
-                z[j] = p.pre && c0 + j < p.N ? p.pre[m * p.ldp + c0 + j] : 0.0f;
+                for (int j = 0; j < 8; ++j) {
+                    d[j] = c0 + j < p.N ? to_f32(dy[m * p.lddy + c0 + j]) : 0.0f;
+                    z[j] = p.pre && c0 + j < p.N ? p.pre[m * p.ldp + c0 + j] : 0.0f;
+                }
             }
-        }
+            if (p.pre) slopes8(p.act, z, d);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float value;
-            if (p.pre && (p.vec || c0 + j < p.N)) d[j] *= act_slope(p.act, z[j], value);
-            s[j] += d[j];
-        }
-        if (dz) {
-            if (p.vec) store8(dz + m * p.lddz + c0, d);
-            else {
+            for (int j = 0; j < 8; ++j) s[j] += d[j];
+            if (dz) {
+                if (p.vec) store8(dz + m * p.lddz + c0, d);
+                else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (c0 + j < p.N) dz[m * p.lddz + c0 + j] = from_f32<T>(d[j]);
+                    for (int j = 0; j < 8; ++j)
+                        if (c0 + j < p.N) dz[m * p.lddz + c0 + j] = from_f32<T>(d[j]);
+                }
             }
         }
     }
-    if (!p.part) return;
+    if (!p.part && !p.sum) return;
 #pragma unroll
     for (int j = 0; j < 8; ++j) sums[ry][cx * 8 + j] = s[j];
     __syncthreads();
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (c < p.N) {
+    const int64_t c = (int64_t)blockIdx.x * SUM_COLS + threadIdx.x;
+    if (threadIdx.x < SUM_COLS && c < p.N) {
         float t = 0.0f;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) t += sums[k][threadIdx.x];
-        p.part[(int64_t)blockIdx.y * p.N + c] = t;
+        for (int k = 0; k < SUM_ROWS; ++k) t += sums[k][threadIdx.x];
+        if (p.sum) static_cast<T *>(p.sum)[c] = from_f32<T>(t);
+        else p.part[(int64_t)blockIdx.y * p.N + c] = t;
     }
 }
 
@@ -88,36 +136,34 @@ struct GatedSlopeArgs {
     const float *pre; int64_t ldp;
     void *dg, *du; int64_t ldd;
     int64_t M, N;
+    uint32_t groups;                   // of 8 columns in a row
     int act, vec;
 };
 template <typename T>
 __global__ void __launch_bounds__(256) k_gated_slopes(const GatedSlopeArgs p) {
-    const int64_t c0 = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
-    if (c0 >= p.N) return;
-    for (int64_t m = blockIdx.y; m < p.M; m += gridDim.y) {
+    bnn_pdl_wait();
+    bnn_pdl_launch_next();
+    const int64_t total = p.M * p.groups, stride = (int64_t)gridDim.x * 256;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += stride) {
+        const int64_t m = total <= 0xffffffffll ? (int64_t)((uint32_t)i / p.groups) : i / p.groups, c0 = (i - m * p.groups) * 8;
         const T *dh = static_cast<const T *>(p.dh) + m * p.lddh + c0;
         const float *g = p.pre + m * p.ldp + c0, *u = p.pre + (p.M + m) * p.ldp + c0;
         T *dg = static_cast<T *>(p.dg) + m * p.ldd + c0, *du = static_cast<T *>(p.du) + m * p.ldd + c0;
-        if (p.vec) {
-            float d[8], a[8], b[8];
-            load8(dh, d); load8(g, a); load8(u, b);
+        float d[8], a[8], b[8];
+        if (p.vec) { load8(dh, d); load8(g, a); load8(u, b); }
+        else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                float value;
-                const float slope = act_slope(p.act, a[j], value);
-                a[j] = d[j] * b[j] * slope;
-                b[j] = d[j] * value;
+                const bool in = c0 + j < p.N;
+                d[j] = in ? to_f32(dh[j]) : 0.0f; a[j] = in ? g[j] : 0.0f; b[j] = in ? u[j] : 0.0f;
             }
-            store8(dg, a); store8(du, b);
-        } else {
+        }
+        gated8(p.act, d, a, b);
+        if (p.vec) { store8(dg, a); store8(du, b); }
+        else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (c0 + j >= p.N) break;
-                float value;
-                const float d = to_f32(dh[j]), slope = act_slope(p.act, g[j], value);
-                dg[j] = from_f32<T>(d * u[j] * slope);
-                du[j] = from_f32<T>(d * value);
-            }
+            for (int j = 0; j < 8; ++j)
+                if (c0 + j < p.N) { dg[j] = from_f32<T>(a[j]); du[j] = from_f32<T>(b[j]); }
         }
     }
 }
@@ -125,11 +171,13 @@ __global__ void __launch_bounds__(256) k_gated_slopes(const GatedSlopeArgs p) {
 int64_t pitch16(int64_t n) { return (n + 7) & ~int64_t(7); }            // 16-bit rows of whole 16-byte groups
 size_t round256(size_t b) { return (b + 255) & ~size_t(255); }
 
-// Rows per chunk of the column sums: about four blocks per SM, at least eight rows each.
+// Rows per chunk of the column sums: about four blocks per SM; up to 256 rows one chunk, which needs no second kernel to join
+// the partial sums.
 int64_t sum_chunk_rows(int64_t M, int64_t N) {
-    const int64_t blocks_n = (N + 255) / 256, want = 592 / blocks_n + 1;
+    if (M <= 256) return M;
+    const int64_t blocks_n = (N + SUM_COLS - 1) / SUM_COLS, want = 592 / blocks_n + 1;
     const int64_t rows = (M + want - 1) / want;
-    return (rows + 7) & ~int64_t(7);
+    return (rows + SUM_ROWS - 1) / SUM_ROWS * SUM_ROWS;
 }
 int64_t sum_chunks(int64_t M, int64_t N) { const int64_t r = sum_chunk_rows(M, N); return (M + r - 1) / r; }
 
@@ -146,7 +194,7 @@ int check_gated(const bnn_gated_desc *l, int64_t M) {
     return bnn_check_real(l->Wu, l->ldu, l->N, l->K, 2);
 }
 size_t dz_bytes(int64_t M, int64_t N) { return round256((size_t)M * pitch16(N) * 2); }
-size_t sums_bytes(int64_t M, int64_t N) { return round256((size_t)sum_chunks(M, N) * N * 4); }
+size_t sums_bytes(int64_t M, int64_t N) { return M <= 256 ? 0 : round256((size_t)sum_chunks(M, N) * N * 4); }
 
 // Scratch of one call, handed out in order.  What does not fit is noticed at the end (`ok`), before anything is launched.
 struct Scratch {
@@ -173,20 +221,27 @@ struct Readable {
     int copy(bnn_ctx *ctx) const {
         if (!src) return BNN_OK;
         const dim3 grid((unsigned)((cols + 2047) / 2048), (unsigned)(rows < 65535 ? rows : 65535));
-        k_repitch<<<grid, 256, 0, ctx->stream>>>(static_cast<const uint16_t *>(src), ld, static_cast<uint16_t *>(const_cast<void *>(use.p)), use.ld, rows, cols);
+        BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_repitch, grid, dim3(256), 0, ctx->stream, static_cast<const uint16_t *>(src), ld,
+                                               static_cast<uint16_t *>(const_cast<void *>(use.p)), use.ld, rows, cols));
         return bnn_check_launch(ctx);
     }
 };
 
-// The gradients of a layer in one launch, so that the tiles of all of them fill the GPU together; a first one (dx) of few rows
-// runs on the kernel for those.
+// The gradients of a layer (dx first, if there is one) in one launch, so that the tiles of all of them fill the GPU together, or dx of
+// few rows on the kernel for those.  The choice is made for all of them and then what is not wanted (out[0] NULL) is left out, so that
+// a gradient has the same bits whatever is asked for beside it.
 int gradients(bnn_ctx *ctx, int dtype, BnnProduct *g, int n) {
-    for (int i = 0; i < n; ++i) { g[i].dtype = dtype; g[i].epilogue = BNN_EPI_LINEAR; if (!g[i].pairs) g[i].pairs = 1; }
-    if (n > 1 && bnn_product_few(ctx, g[0])) {
-        if (int st = bnn_product(ctx, g, 1)) return st;
+    for (int i = 0; i < n; ++i) { g[i].dtype = dtype; g[i].epilogue = BNN_EPI_LINEAR; g[i].whole = 1; if (!g[i].pairs) g[i].pairs = 1; }
+    if (n > 1 && !g[0].a_mn && bnn_product_few(ctx, g[0], g + 1, n - 1)) {
+        g[0].whole = 0;
+        if (g[0].out[0])
+            if (int st = bnn_product(ctx, g, 1)) return st;
         ++g; --n;
     }
-    return n ? bnn_product(ctx, g, n) : BNN_OK;
+    int kept = 0;
+    for (int i = 0; i < n; ++i)
+        if (g[i].out[0]) g[kept++] = g[i];
+    return kept ? bnn_product(ctx, g, kept) : BNN_OK;
 }
 
 }  // namespace
@@ -243,7 +298,8 @@ extern "C" int bnn_linear_backward(bnn_ctx *ctx, const bnn_linear_desc *l, const
     if (slopes) dz = {scratch.take(dz_bytes(M, l->N)), pitch16(l->N)};
     const Readable rz(scratch, dz.p, dz.ld, products && !slopes ? M : 0, l->N);
     const Readable rx(scratch, x, ldx, dW || again ? M : 0, l->K), rw(scratch, l->W, l->ldw, dx || again ? l->N : 0, l->K);
-    float *part = sums ? reinterpret_cast<float *>(scratch.take(sums_bytes(M, l->N))) : nullptr;
+    const int64_t chunks = sums ? sum_chunks(M, l->N) : 0;
+    float *part = chunks > 1 ? reinterpret_cast<float *>(scratch.take(sums_bytes(M, l->N))) : nullptr;
     if (!scratch.ok()) return BNN_ERR_WORKSPACE;
     for (const Readable *r : {&rz, &rx, &rw})
         if (int st = r->copy(ctx)) return st;
@@ -261,24 +317,25 @@ extern "C" int bnn_linear_backward(bnn_ctx *ctx, const bnn_linear_desc *l, const
         s.dy = kept ? dy : dz.p; s.lddy = kept ? lddy : dz.ld;
         s.pre = kept ? pre : nullptr; s.ldp = ldp;
         s.dz = kept ? const_cast<void *>(dz.p) : nullptr; s.lddz = dz.ld;
-        s.part = part; s.M = M; s.N = l->N; s.chunk_rows = sum_chunk_rows(M, l->N); s.act = l->act;
+        s.part = part; s.sum = chunks == 1 ? dbias : nullptr;
+        s.M = M; s.N = l->N; s.chunk_rows = sum_chunk_rows(M, l->N); s.act = l->act;
         s.vec = l->N % 8 == 0 && bnn_rows16(s.dy, s.lddy, M, 2) && (!kept || bnn_rows16(pre, ldp, M, 4));
-        const dim3 grid((unsigned)((l->N + 255) / 256), (unsigned)sum_chunks(M, l->N));
-        if (l->dtype == BNN_F16) k_act_backward<__half><<<grid, 256, 0, ctx->stream>>>(s);
-        else k_act_backward<__nv_bfloat16><<<grid, 256, 0, ctx->stream>>>(s);
+        const dim3 grid((unsigned)((l->N + SUM_COLS - 1) / SUM_COLS), (unsigned)sum_chunks(M, l->N));
+        auto kernel = l->dtype == BNN_F16 ? k_act_backward<__half> : k_act_backward<__nv_bfloat16>;
+        BNN_CUDA_TRY(ctx, bnn_launch_dependent(kernel, grid, dim3(256), 0, ctx->stream, s));
         if (int st = bnn_check_launch(ctx)) return st;
-        if (sums)
-            if (int st = bnn_join_columns(ctx, l->dtype, part, l->N, sum_chunks(M, l->N), dbias, l->N)) return st;
+        if (part)
+            if (int st = bnn_join_columns(ctx, l->dtype, part, l->N, chunks, dbias, l->N)) return st;
     }
     const BnnOperand z = slopes ? dz : rz.use;
     BnnProduct g[2] = {};
     int n = 0;
-    if (dx && M > 0 && l->K > 0) {
+    if (M > 0 && l->K > 0) {
         BnnProduct &d = g[n++];
         d.a[0] = z; d.b[0] = rw.use; d.b_mn = 1;
         d.M = M; d.N = l->K; d.K = l->N; d.out[0] = dx; d.ldo[0] = lddx;
     }
-    if (dW && l->N > 0 && l->K > 0) {
+    if (l->N > 0 && l->K > 0) {
         BnnProduct &d = g[n++];
         d.a[0] = z; d.b[0] = rx.use; d.a_mn = d.b_mn = 1;
         d.M = l->N; d.N = l->K; d.K = M; d.out[0] = dW; d.ldo[0] = lddw;
@@ -346,14 +403,15 @@ extern "C" int bnn_gated_backward(bnn_ctx *ctx, const bnn_gated_desc *l, const v
         GatedSlopeArgs s{};
         s.dh = dh; s.lddh = lddh; s.pre = pre; s.ldp = ldp; s.dg = dg; s.du = du; s.ldd = ldd; s.M = M; s.N = l->N; s.act = l->act;
         s.vec = l->N % 8 == 0 && bnn_rows16(dh, lddh, M, 2) && bnn_rows16(pre, ldp, 2 * M, 4);
-        const dim3 grid((unsigned)((l->N + 2047) / 2048), (unsigned)(M < 65535 ? M : 65535));
-        if (l->dtype == BNN_F16) k_gated_slopes<__half><<<grid, 256, 0, ctx->stream>>>(s);
-        else k_gated_slopes<__nv_bfloat16><<<grid, 256, 0, ctx->stream>>>(s);
+        s.groups = (uint32_t)((l->N + 7) / 8);
+        const int64_t blocks = (M * s.groups + 255) / 256, most = 8 * 148;
+        auto kernel = l->dtype == BNN_F16 ? k_gated_slopes<__half> : k_gated_slopes<__nv_bfloat16>;
+        BNN_CUDA_TRY(ctx, bnn_launch_dependent(kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, ctx->stream, s));
         if (int st = bnn_check_launch(ctx)) return st;
     }
     BnnProduct g[3] = {};
     int n = 0;
-    if (dx && M > 0 && l->K > 0) {
+    if (M > 0 && l->K > 0) {
         BnnProduct &d = g[n++];
         d.a[0] = {dg, ldd}; d.a[1] = {du, ldd}; d.b[0] = rg.use; d.b[1] = ru.use; d.b_mn = 1; d.pairs = 2;
         d.M = M; d.N = l->K; d.K = l->N; d.out[0] = dx; d.ldo[0] = lddx;
@@ -361,7 +419,7 @@ extern "C" int bnn_gated_backward(bnn_ctx *ctx, const bnn_gated_desc *l, const v
     void *const dw[2] = {dWg, dWu};
     const int64_t ldw[2] = {lddg, lddu};
     for (int k = 0; k < 2; ++k) {
-        if (!dw[k] || l->N == 0 || l->K == 0) continue;
+        if (l->N == 0 || l->K == 0) continue;
         BnnProduct &d = g[n++];
         d.a[0] = {k ? du : dg, ldd}; d.b[0] = rx.use; d.a_mn = d.b_mn = 1;
         d.M = l->N; d.N = l->K; d.K = M; d.out[0] = dw[k]; d.ldo[0] = ldw[k];

@@ -33,11 +33,13 @@ __device__ __forceinline__ uint4 philox4x32(uint32_t c0, uint32_t c1, uint32_t c
     return make_uint4(c0, c1, c2, c3);
 }
 
-// One thread per 8 consecutive elements (two counters).
+// One thread per 8 consecutive elements (two counters).  The row is requested before the generator runs, which covers the wait.
 template <typename T>
 __global__ void __launch_bounds__(256) k_dropout(const DropArgs p) {
     const int64_t total = p.rows * p.cols;
     const int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x, e0 = g * 8;
+    bnn_pdl_wait();
+    bnn_pdl_launch_next();
     if (e0 >= total) return;
     const T *x = static_cast<const T *>(p.x), *res = static_cast<const T *>(p.residual);
     T *y = static_cast<T *>(p.y);
@@ -46,14 +48,23 @@ __global__ void __launch_bounds__(256) k_dropout(const DropArgs p) {
         row = total <= 0xffffffffll ? (int64_t)((uint32_t)e0 / (uint32_t)p.cols) : e0 / p.cols;
         col = e0 - row * p.cols;
     }
+    const bool whole = p.vec && e0 + 8 <= total;
+    uint4 xw[sizeof(T) / 2], rw[sizeof(T) / 2];
+    if (whole) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+            xw[i] = __ldcs(reinterpret_cast<const uint4 *>(x + row * p.ldx + col) + i);
+            if (res) rw[i] = __ldcs(reinterpret_cast<const uint4 *>(res + row * p.ldr + col) + i);
+        }
+    }
     const uint64_t c = (uint64_t)g * 2;
     const uint4 a = philox4x32((uint32_t)c, (uint32_t)(c >> 32), p.o0, p.o1, p.k0, p.k1);
     const uint4 b = philox4x32((uint32_t)(c + 1), (uint32_t)((c + 1) >> 32), p.o0, p.o1, p.k0, p.k1);
     const uint32_t word[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    if (p.vec && e0 + 8 <= total) {
+    if (whole) {
         float v[8], r[8];
-        load8(x + row * p.ldx + col, v);
-        if (res) load8(res + row * p.ldr + col, r);
+        unpack8<T>(xw, v);
+        if (res) unpack8<T>(rw, r);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             v[j] = (word[j] >= p.thr && !p.drop_all) ? v[j] * p.scale : 0.0f;
@@ -100,8 +111,7 @@ extern "C" int bnn_dropout(bnn_ctx *ctx, int dtype, const void *x, int64_t ldx, 
     const int64_t blocks = (rows * cols + 2047) / 2048;
     if (blocks > BNN_REAL_MAX) return BNN_ERR_INVALID_ARG;
     const dim3 grid((unsigned)blocks);
-    if (dtype == BNN_F32) k_dropout<float><<<grid, 256, 0, ctx->stream>>>(a);
-    else if (dtype == BNN_F16) k_dropout<__half><<<grid, 256, 0, ctx->stream>>>(a);
-    else k_dropout<__nv_bfloat16><<<grid, 256, 0, ctx->stream>>>(a);
+    auto kernel = dtype == BNN_F32 ? k_dropout<float> : dtype == BNN_F16 ? k_dropout<__half> : k_dropout<__nv_bfloat16>;
+    BNN_CUDA_TRY(ctx, bnn_launch_dependent(kernel, grid, dim3(256), 0, ctx->stream, a));
     return bnn_check_launch(ctx);
 }

@@ -389,24 +389,29 @@ struct JoinArgs {
     int outs[5];             // rows of out (gate rows; 1 for the parameters)
     int D;
 };
+constexpr int JOIN_LANES = 32;      // partial sums read at a time per column
 template <typename T>
-__global__ void __launch_bounds__(256) k_join_columns(const JoinArgs p) {
-    __shared__ float sum[8][33];
+__global__ void __launch_bounds__(32 * JOIN_LANES) k_join_columns(const JoinArgs p) {
+    __shared__ float sum[JOIN_LANES][33];
     const int which = blockIdx.y, cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
     bnn_pdl_wait();
     bnn_pdl_launch_next();
     if (!p.out[which]) return;
     const int c = blockIdx.x * 32 + cx;
+    const int64_t count = p.count[which], pitch = p.pitch[which];
     for (int64_t o = blockIdx.z; o < p.outs[which]; o += gridDim.z) {
         float t = 0.0f;
-        if (c < p.D)
-            for (int64_t i = ry; i < p.count[which]; i += 8) t += p.part[which][(o * p.count[which] + i) * p.pitch[which] + c];
+        if (c < p.D) {
+            const float *part = p.part[which] + o * count * pitch + c;
+#pragma unroll 4
+            for (int64_t i = ry; i < count; i += JOIN_LANES) t += part[i * pitch];
+        }
         sum[ry][cx] = t;
         __syncthreads();
         if (ry == 0 && c < p.D) {
             t = 0.0f;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) t += sum[k][cx];
+            for (int k = 0; k < JOIN_LANES; ++k) t += sum[k][cx];
             static_cast<T *>(p.out[which])[o * p.ldo[which] + c] = from_f32<T>(t);
         }
         __syncthreads();
@@ -417,7 +422,7 @@ int launch_join(bnn_ctx *ctx, int dtype, const JoinArgs &j, int sums) {
     const int outs = j.outs[sums - 1];
     const dim3 grid((unsigned)((j.D + 31) / 32), (unsigned)sums, (unsigned)(outs > 1 ? (outs < 1024 ? outs : 1024) : 1));
     auto kernel = dtype == BNN_F32 ? k_join_columns<float> : dtype == BNN_F16 ? k_join_columns<__half> : k_join_columns<__nv_bfloat16>;
-    BNN_CUDA_TRY(ctx, bnn_launch_dependent(kernel, grid, dim3(256), 0, ctx->stream, j));
+    BNN_CUDA_TRY(ctx, bnn_launch_dependent(kernel, grid, dim3(32 * JOIN_LANES), 0, ctx->stream, j));
     return bnn_check_launch(ctx);
 }
 

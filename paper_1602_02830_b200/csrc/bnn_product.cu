@@ -773,15 +773,15 @@ int64_t pair_tiles(const BnnProduct &q, int bn) {
 // Which kernel, and how k_product_few divides the work, by estimates of both in microseconds.  Fitted to measured times (N x K, rows,
 // few / pair): 4096 x 4096, 1: 10.7 / 27.8, 128: 14.2 / 25.8, 384: 22.5 / 26.8, 768: 37.5 / 30.4; 512 x 8192, 512: 16.0 / 44.1; 8192 x 1024,
 // 64: 9.5 / 10.6, 192: 14.1 / 11.3; 256 x 256, 1: 3.9 / 5.3, 128: 9.0 / 5.9.
-//   pair: 4.5 + 0.30 per K step and round of tiles, or the weights at 3.3 TB/s (gated, 5500 x 2048 twice: 20.9) if that takes longer.
+//   pair: 5 + 0.30 per K step and round of tiles, or the weights at 3.3 TB/s (gated, 5500 x 2048 twice: 20.9) if that takes longer.
 //   few:  3 for every round of CTAs, + per K step of an SM's CTAs 0.12 + 0.0012 per token of a tile, at least 0.28 (0.26 with
 //         two CTAs per SM): what one SM draws from HBM (8192 x 8192, one row: 40 us on 64 SMs, 26 on all); + 1 (2 with a split sum) + 0.041 per token of a CTA's share of the epilogue.
 // More, smaller token tiles keep more SMs busy, fewer read the weights less often; the sum is split while there are SMs left and
 // every CTA keeps four K steps.
 double pair_cost(const bnn_ctx *ctx, const BnnProduct &q) {
     const int64_t pairs = ctx->sm_count / 2;
-    const double steps = 4.5 + 0.30 * (double)steps_of(q) * (double)((pair_tiles(q, 256) + pairs - 1) / pairs);
-    const double weights = 4.5 + 2.0 * (double)q.N * (double)q.K * (is_gated(q) ? 2 : q.pairs) / 3.3e6;
+    const double steps = 5.0 + 0.30 * (double)steps_of(q) * (double)((pair_tiles(q, 256) + pairs - 1) / pairs);
+    const double weights = 5.0 + 2.0 * (double)q.N * (double)q.K * (is_gated(q) ? 2 : q.pairs) / 3.3e6;
     return steps > weights ? steps : weights;
 }
 // CTAs that are resident at once in clusters of 1, 2, 4 and 8, one or two per SM (cudaOccupancyMaxActiveClusters with the whole or half
@@ -856,13 +856,22 @@ int product_few(bnn_ctx *ctx, const BnnProduct &q) {
 }
 }  // namespace
 
-bool bnn_product_few(const bnn_ctx *ctx, const BnnProduct &q) {
-    return !q.a_mn && q.M <= FEW_ROWS && few_plan(q).cost < pair_cost(ctx, q);
+bool bnn_product_few(const bnn_ctx *ctx, const BnnProduct &q, const BnnProduct *more, int n) {
+    if (q.a_mn || q.M > FEW_ROWS) return false;
+    if (n == 0) return few_plan(q).cost < pair_cost(ctx, q);
+    // beside others: alone and then the others, against all of them in one launch
+    int64_t tiles = pair_tiles(q, 256), others = 0, steps = 0;
+    for (int i = 0; i < n; ++i) {
+        others += pair_tiles(more[i], 256);
+        if (steps_of(more[i]) > steps) steps = steps_of(more[i]);
+    }
+    const int64_t pairs = ctx->sm_count / 2, longest = steps_of(q) > steps ? steps_of(q) : steps;
+    const double apart = few_plan(q).cost + 5.0 + 0.30 * (double)steps * (double)((others + pairs - 1) / pairs);
+    return apart < 5.0 + 0.30 * (double)longest * (double)((tiles + others + pairs - 1) / pairs);
 }
-
 int bnn_product(bnn_ctx *ctx, const BnnProduct *list, int count) {
     if (count < 1 || count > PROBLEMS) return BNN_ERR_INVALID_ARG;
-    if (count == 1 && bnn_product_few(ctx, list[0])) return product_few(ctx, list[0]);
+    if (count == 1 && !list[0].whole && bnn_product_few(ctx, list[0], nullptr, 0)) return product_few(ctx, list[0]);
     // Half-width tiles where whole ones would leave half of the pairs without work.
     int64_t whole = 0, tiles = 0;
     for (int i = 0; i < count; ++i) whole += pair_tiles(list[i], 256);

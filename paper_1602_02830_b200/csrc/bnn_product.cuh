@@ -23,9 +23,10 @@ struct BnnProduct {
     void *out[2]; int64_t ldo[2];
     float *pre; int64_t ldp;      // EPI_GATED: [2][M][ldp]
     int act;
+    int whole;                    // 1: on the pair kernel, however few rows
 };
 // Up to three products in one launch (several: linear epilogue without bias, add or pre).  Every operand must satisfy bnn_rows16.
 // M, N > 0; K = 0 is the empty sum.
 int bnn_product(bnn_ctx *ctx, const BnnProduct *list, int count);
-// Whether a product of few rows runs on the kernel for those (alone in its launch).
-bool bnn_product_few(const bnn_ctx *ctx, const BnnProduct &p);
+// Whether a product of few rows is better off on the kernel for those, alone in its launch, than with `more` in one launch of the other.
+bool bnn_product_few(const bnn_ctx *ctx, const BnnProduct &p, const BnnProduct *more, int n);

@@ -53,15 +53,20 @@ template <> __device__ __forceinline__ float2 unpack2<__nv_bfloat16>(uint32_t w)
 }
 
 // Eight consecutive values in 16-byte accesses.
-template <typename T> __device__ __forceinline__ void load8(const T *p, float (&v)[8]) {
+template <typename T> __device__ __forceinline__ void unpack8(const uint4 *w, float (&v)[8]) {
     if constexpr (sizeof(T) == 4) {
-        const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        v[0] = __uint_as_float(w[0].x); v[1] = __uint_as_float(w[0].y); v[2] = __uint_as_float(w[0].z); v[3] = __uint_as_float(w[0].w);
+        v[4] = __uint_as_float(w[1].x); v[5] = __uint_as_float(w[1].y); v[6] = __uint_as_float(w[1].z); v[7] = __uint_as_float(w[1].w);
     } else {
-        const uint4 a = *reinterpret_cast<const uint4 *>(p);
-        const float2 f0 = unpack2<T>(a.x), f1 = unpack2<T>(a.y), f2 = unpack2<T>(a.z), f3 = unpack2<T>(a.w);
+        const float2 f0 = unpack2<T>(w[0].x), f1 = unpack2<T>(w[0].y), f2 = unpack2<T>(w[0].z), f3 = unpack2<T>(w[0].w);
         v[0] = f0.x; v[1] = f0.y; v[2] = f1.x; v[3] = f1.y; v[4] = f2.x; v[5] = f2.y; v[6] = f3.x; v[7] = f3.y;
     }
+}
+template <typename T> __device__ __forceinline__ void load8(const T *p, float (&v)[8]) {
+    uint4 w[sizeof(T) / 2];
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = reinterpret_cast<const uint4 *>(p)[i];
+    unpack8<T>(w, v);
 }
 template <typename T> __device__ __forceinline__ void store8(T *p, const float (&v)[8]) {
     if constexpr (sizeof(T) == 4) {
