@@ -93,15 +93,12 @@ __device__ __forceinline__ void write8(T *row, int slot, int tid, int team, int 
         }
     }
 }
-// VEC rows have D % 8 == 0: a slot is inside the row or outside as a whole.
-template <bool VEC> __device__ __forceinline__ bool inside(int slot, int j, int tid, int team, int D) { return column<VEC>(slot, j, tid, team) < D; }
-
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
-// Sums over the block in a fixed order.  One barrier each: successive sums use different buffers.
+// Sum over the block in a fixed order.  One barrier each: successive sums use different buffers.
 __device__ __forceinline__ float block_sum(float a, float *buf, int warps, int warp, int lane) {
     a = warp_sum(a);
     if (warps == 1) return a;
@@ -109,23 +106,45 @@ __device__ __forceinline__ float block_sum(float a, float *buf, int warps, int w
     __syncthreads();
     return warp_sum(lane < warps ? buf[lane] : 0.0f);
 }
-template <bool BOTH> __device__ __forceinline__ float2 block_sum2(float a, float b, float2 *buf, int warps, int warp, int lane) {
-    a = warp_sum(a);
-    if (BOTH) b = warp_sum(b);
-    if (warps == 1) return make_float2(a, b);
-    if (lane == 0) buf[warp] = make_float2(a, b);
-    __syncthreads();
-    const float2 t = lane < warps ? buf[lane] : make_float2(0.0f, 0.0f);
-    return make_float2(warp_sum(t.x), BOTH ? warp_sum(t.y) : 0.0f);
+// N = 4 or 8 sums over the block at once, in a fixed order, with one barrier.  While several sums are left, half of them go to the
+// partner lane at every exchange, so N sums cost N + log2(32 / N) - 1 shuffles a warp instead of 5 N.
+template <int N> __device__ __forceinline__ void block_sums(float (&v)[N], float *buf, int warps, int warp, int lane) {
+    constexpr int G = 32 / N;                       // lanes that end up with the same sum: lane / G
+#pragma unroll
+    for (int o = 16, n = N; n > 1; o >>= 1, n >>= 1) {
+#pragma unroll
+        for (int k = 0; k < n / 2; ++k) {
+            const bool up = lane & o;
+            const float give = up ? v[k] : v[k + n / 2], keep = up ? v[k + n / 2] : v[k];
+            v[k] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        }
+    }
+    float t = v[0];
+#pragma unroll
+    for (int o = G / 2; o; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+    if (warps > 1) {
+        const int sum = lane / G, sub = lane - sum * G;
+        if (sub == 0) buf[warp * N + sum] = t;
+        __syncthreads();
+        t = 0.0f;
+        for (int w = sub; w < warps; w += G) t += buf[w * N + sum];
+#pragma unroll
+        for (int o = G / 2; o; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xffffffffu, t, k * G);
 }
 
 // One row per CTA: both rows are requested before anything is computed from them.
-template <typename T, int SLOTS, int THREADS, bool VEC>
+// PLAIN: BNN_NORM_RMS without shifts.  Columns beyond D read as zero, which adds nothing to the sums of squares; around a mean
+// (layer norm) they have to be left out.
+template <typename T, int SLOTS, int THREADS, bool VEC, bool PLAIN>
 __global__ void __launch_bounds__(THREADS, 1) k_block_norm(const NormArgs p) {
     __shared__ float buf[4][32];
     const int tid = threadIdx.x, team = blockDim.x, warps = team >> 5, warp = tid >> 5, lane = tid & 31;
-    const T *pw = static_cast<const T *>(p.post_w), *pc = static_cast<const T *>(p.post_c);
-    const T *nw = static_cast<const T *>(p.pre_w), *nc = static_cast<const T *>(p.pre_c);
+    const T *pw = static_cast<const T *>(p.post_w), *pc = PLAIN ? nullptr : static_cast<const T *>(p.post_c);
+    const T *nw = static_cast<const T *>(p.pre_w), *nc = PLAIN ? nullptr : static_cast<const T *>(p.pre_c);
+    const bool layer = !PLAIN && p.layer;
     const int64_t m = blockIdx.x;
     bnn_pdl_wait();
     bnn_pdl_launch_next();
@@ -135,119 +154,128 @@ __global__ void __launch_bounds__(THREADS, 1) k_block_norm(const NormArgs p) {
         rx[i] = read8<T, VEC>(static_cast<const T *>(p.x) + m * p.ldx, i, tid, team, p.D);
         if (p.block) rb[i] = read8<T, VEC>(static_cast<const T *>(p.block) + m * p.ldb, i, tid, team, p.D);
     }
-    float s[SLOTS][8];
-    if (p.block) {
-        const T *gate = p.gate ? static_cast<const T *>(p.gate) + (m / p.rows_per_gate) * p.ld_gate : nullptr;
-        float mean = 0.0f, r = 1.0f;
-        if (p.post) {
-            if (p.layer) {
-                float t = 0.0f;
-#pragma unroll
-                for (int i = 0; i < SLOTS; ++i)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) t += rb[i][j];
-                mean = block_sum(t, buf[0], warps, warp, lane) * p.inv_d;
-            }
-            float q = 0.0f;
+    const T *gate = p.gate ? static_cast<const T *>(p.gate) + (m / p.rows_per_gate) * p.ld_gate : nullptr;
+    float mean = 0.0f, r = 1.0f;
+    if (p.block && p.post) {
+        if (layer) {
+            float t = 0.0f;
 #pragma unroll
             for (int i = 0; i < SLOTS; ++i)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float v = inside<VEC>(i, j, tid, team, p.D) ? rb[i][j] - mean : 0.0f;
-                    q += v * v;
-                }
-            r = 1.0f / sqrtf(block_sum(q, buf[1], warps, warp, lane) * p.inv_d + p.eps);
-            if (p.stats && tid == 0) { p.stats[4 * m] = mean; p.stats[4 * m + 1] = r; }
+                for (int j = 0; j < 8; ++j) t += rb[i][j];
+            mean = block_sum(t, buf[0], warps, warp, lane) * p.inv_d;
         }
+        float q = 0.0f;
 #pragma unroll
         for (int i = 0; i < SLOTS; ++i) {
+            if (VEC && !PLAIN && column<VEC>(i, 0, tid, team) >= p.D) continue;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float v = rb[i][j];
+                if (!PLAIN) v = VEC || column<VEC>(i, j, tid, team) < p.D ? v - mean : 0.0f;
+                q += v * v;
+            }
+        }
+        r = 1.0f / sqrtf(block_sum(q, buf[1], warps, warp, lane) * p.inv_d + p.eps);
+        if (p.stats && tid == 0) { p.stats[4 * m] = mean; p.stats[4 * m + 1] = r; }
+    }
+    float s[SLOTS][8];
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+        float v[8];
+        if (p.block) {
             Eight<T> w, c, g;
             if (pw) w = read8<T, VEC>(pw, i, tid, team, p.D);
             if (pc) c = read8<T, VEC>(pc, i, tid, team, p.D);
             if (gate) g = read8<T, VEC>(gate, i, tid, team, p.D);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                float v = (rb[i][j] - mean) * r;
-                if (pw) v *= w[j];
-                if (pc) v += c[j];
-                if (gate) v *= g[j];
-                s[i][j] = p.alpha * rx[i][j] + v;
-            }
+            for (int j = 0; j < 8; ++j) v[j] = PLAIN ? rb[i][j] * r : (rb[i][j] - mean) * r;
+            if (pw)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] *= w[j];
+            if (pc)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += c[j];
+            if (gate)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] *= g[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = 0.0f;
         }
-    } else {
 #pragma unroll
-        for (int i = 0; i < SLOTS; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) s[i][j] = p.alpha * rx[i][j];
-    }
-    if (p.stream) {
-        T *out = static_cast<T *>(p.stream) + m * p.lds;
-#pragma unroll
-        for (int i = 0; i < SLOTS; ++i) write8<T, VEC>(out, i, tid, team, p.D, s[i]);
+        for (int j = 0; j < 8; ++j) s[i][j] = p.block ? p.alpha * rx[i][j] + v[j] : p.alpha * rx[i][j];
+        if (p.stream) write8<T, VEC>(static_cast<T *>(p.stream) + m * p.lds, i, tid, team, p.D, s[i]);
     }
     if (!p.pre) return;
-    float mean = 0.0f;
-    if (p.layer) {
+    mean = 0.0f;
+    if (layer) {
         float t = 0.0f;
 #pragma unroll
         for (int i = 0; i < SLOTS; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) t += inside<VEC>(i, j, tid, team, p.D) ? s[i][j] : 0.0f;
+            for (int j = 0; j < 8; ++j)
+                if (column<VEC>(i, VEC ? 0 : j, tid, team) < p.D) t += s[i][j];
         mean = block_sum(t, buf[2], warps, warp, lane) * p.inv_d;
     }
     float q = 0.0f;
 #pragma unroll
-    for (int i = 0; i < SLOTS; ++i)
+    for (int i = 0; i < SLOTS; ++i) {
+        if (VEC && !PLAIN && column<VEC>(i, 0, tid, team) >= p.D) continue;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            s[i][j] = inside<VEC>(i, j, tid, team, p.D) ? s[i][j] - mean : 0.0f;
-            q += s[i][j] * s[i][j];
+            float v = s[i][j];
+            if (!PLAIN) v = VEC || column<VEC>(i, j, tid, team) < p.D ? v - mean : 0.0f;
+            q += v * v;
         }
-    const float r = 1.0f / sqrtf(block_sum(q, buf[3], warps, warp, lane) * p.inv_d + p.eps);
+    }
+    r = 1.0f / sqrtf(block_sum(q, buf[3], warps, warp, lane) * p.inv_d + p.eps);
     if (p.stats && tid == 0) { p.stats[4 * m + 2] = mean; p.stats[4 * m + 3] = r; }
     if (!p.normed) return;
-    T *out = static_cast<T *>(p.normed) + m * p.ldn;
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
         Eight<T> w, c;
         if (nw) w = read8<T, VEC>(nw, i, tid, team, p.D);
         if (nc) c = read8<T, VEC>(nc, i, tid, team, p.D);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            s[i][j] *= r;
-            if (nw) s[i][j] *= w[j];
-            if (nc) s[i][j] += c[j];
-        }
-        write8<T, VEC>(out, i, tid, team, p.D, s[i]);
+        for (int j = 0; j < 8; ++j) s[i][j] = PLAIN ? s[i][j] * r : (s[i][j] - mean) * r;
+        if (nw)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[i][j] *= w[j];
+        if (nc)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[i][j] += c[j];
+        write8<T, VEC>(static_cast<T *>(p.normed) + m * p.ldn, i, tid, team, p.D, s[i]);
     }
 }
 
 // A CTA takes whole units (a unit: chunk_rows rows that share one gate row), so every thread keeps the column sums of its own
-// columns in registers from row to row: the four parameter sums for all its units, the gate's for one unit.  The next row is
-// requested before the current one is worked on (SLOTS = 1; wider rows leave no registers for it).
-// PLAIN: no means and no shifts (BNN_NORM_RMS without shift vectors or their gradients): two of the four parameter sums.
+// columns in registers from row to row.  The next row is requested before the current one is worked on (SLOTS = 1; wider rows
+// leave no registers for it).
+// One reduction per row: with y = gate w_post bh and z = ds + r_s e, the row's T is z - r_s (m1 u + m2), linear in the means m1 = mean(e u) and
+// m2 = mean(e) of the stream's norm, so the two sums that the block's norm needs, of T y and of T gate w_post, follow from sums that
+// are taken together with those of e u and e.  Of the parameter sums only sum T bh (and sum T) is kept per unit: the gate's gradient is
+// w_post times it, the post weight's the gate times it.
+// PLAIN: no means and no shifts (BNN_NORM_RMS without shift vectors or their gradients).
 template <typename T, int SLOTS, int THREADS, bool VEC, bool PLAIN>
 __global__ void __launch_bounds__(THREADS, 1) k_block_norm_backward(const NormArgs p) {
-    constexpr bool AHEAD = SLOTS == 1, LAYER = !PLAIN;
-    __shared__ float2 buf[4][32];
+    constexpr bool AHEAD = SLOTS == 1;
+    constexpr int SUMS = PLAIN ? 4 : 8;
+    __shared__ float buf[2][32 * SUMS];
     const int tid = threadIdx.x, team = blockDim.x, warps = team >> 5, warp = tid >> 5, lane = tid & 31;
     const T *pw = static_cast<const T *>(p.post_w), *pc = PLAIN ? nullptr : static_cast<const T *>(p.post_c), *nw = static_cast<const T *>(p.pre_w);
     const T *X = static_cast<const T *>(p.x), *B = static_cast<const T *>(p.block), *S = static_cast<const T *>(p.ds), *N = static_cast<const T *>(p.dn);
     const bool inner = p.pre && p.dn;
     bnn_pdl_wait();
     bnn_pdl_launch_next();
-    Eight<T> w_post[SLOTS], w_pre[SLOTS], gates[SLOTS];
-    float sum_nw[SLOTS][8], sum_nc[SLOTS][8], sum_pw[SLOTS][8], sum_pc[SLOTS][8], sum_g[SLOTS][8];
+    float w_pre[SLOTS][8], sum_nw[SLOTS][8], sum_nc[SLOTS][8], sum_pw[SLOTS][8], sum_pc[SLOTS][8];
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
-        if (pw) w_post[i] = read8<T, VEC>(pw, i, tid, team, p.D);
-        if (nw) w_pre[i] = read8<T, VEC>(nw, i, tid, team, p.D);
+        Eight<T> w;
+        w.fill(1.0f);
+        if (nw) w = read8<T, VEC>(nw, i, tid, team, p.D);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            sum_nw[i][j] = 0.0f; sum_nc[i][j] = 0.0f; sum_pw[i][j] = 0.0f; sum_pc[i][j] = 0.0f;
-        }
-        if (!pw) w_post[i].fill(1.0f);
-        if (!nw) w_pre[i].fill(1.0f);
+        for (int j = 0; j < 8; ++j) { w_pre[i][j] = w[j]; sum_nw[i][j] = 0.0f; sum_nc[i][j] = 0.0f; sum_pw[i][j] = 0.0f; sum_pc[i][j] = 0.0f; }
     }
     uint32_t turn = 0;                     // rows done: alternates the buffers of the sums
     for (int64_t unit = blockIdx.x; unit < p.units; unit += gridDim.x) {
@@ -255,15 +283,29 @@ __global__ void __launch_bounds__(THREADS, 1) k_block_norm_backward(const NormAr
         const int64_t first = group * p.rows_per_gate + chunk * p.chunk_rows;
         const int64_t group_end = (group + 1) * p.rows_per_gate < p.M ? (group + 1) * p.rows_per_gate : p.M;
         const int64_t end = first + p.chunk_rows < group_end ? first + p.chunk_rows : group_end;
+        // gate w_post (0 beyond D, which keeps those columns out of every sum), gate c_post, and what is summed over the unit
+        float gw[SLOTS][8], gc[SLOTS][8], sum_tb[SLOTS][8], sum_t[SLOTS][8];
+        auto parameters = [&](int i, Eight<T> &w, Eight<T> &c, Eight<T> &g) {
+            w.fill(1.0f); c.fill(0.0f); g.fill(1.0f);
+            if (pw) w = read8<T, VEC>(pw, i, tid, team, p.D);
+            if (pc) c = read8<T, VEC>(pc, i, tid, team, p.D);
+            if (p.gate) g = read8<T, VEC>(static_cast<const T *>(p.gate) + group * p.ld_gate, i, tid, team, p.D);
+        };
 #pragma unroll
         for (int i = 0; i < SLOTS; ++i) {
-            if (p.gate) gates[i] = read8<T, VEC>(static_cast<const T *>(p.gate) + group * p.ld_gate, i, tid, team, p.D);
+            Eight<T> w, c, g;
+            parameters(i, w, c, g);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum_g[i][j] = 0.0f;
-            if (!p.gate) gates[i].fill(1.0f);
+            for (int j = 0; j < 8; ++j) {
+                gw[i][j] = column<VEC>(i, VEC ? 0 : j, tid, team) < p.D ? w[j] * g[j] : 0.0f;
+                gc[i][j] = c[j] * g[j];
+                sum_tb[i][j] = 0.0f; sum_t[i][j] = 0.0f;
+            }
         }
         Eight<T> rx[SLOTS], rb[SLOTS], rs[SLOTS], rn[SLOTS];
         float4 st = make_float4(0.0f, 1.0f, 0.0f, 1.0f);
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) { rx[i].fill(0.0f); rb[i].fill(0.0f); rs[i].fill(0.0f); rn[i].fill(0.0f); }
         auto request = [&](int64_t m) {
 #pragma unroll
             for (int i = 0; i < SLOTS; ++i) {
@@ -279,90 +321,81 @@ __global__ void __launch_bounds__(THREADS, 1) k_block_norm_backward(const NormAr
         if (AHEAD && first < end) request(first);
         for (int64_t m = first; m < end; ++m, turn ^= 1u) {
             if (!AHEAD) request(m);
-            const float mean_b = p.post ? st.x : 0.0f, r_b = p.post ? st.y : 1.0f, mean_s = st.z, r_s = st.w;
-            float u[SLOTS][8], e[SLOTS][8], bh[SLOTS][8], ds[SLOTS][8];      // unit row of the stream, dn w_pre, unit row of the block
-            float a1 = 0.0f, a2 = 0.0f;
+            const float mean_b = p.post ? st.x : 0.0f, r_b = p.post ? st.y : 1.0f, mean_s = p.pre ? st.z : 0.0f, r_s = p.pre ? st.w : 1.0f;
+            float u[SLOTS][8], z[SLOTS][8], bh[SLOTS][8], v[SUMS];
 #pragma unroll
-            for (int i = 0; i < SLOTS; ++i) {
-                Eight<T> c;
-                if (pc) c = read8<T, VEC>(pc, i, tid, team, p.D);
+            for (int k = 0; k < SUMS; ++k) v[k] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < SLOTS; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const bool in = inside<VEC>(i, j, tid, team, p.D);
-                    bh[i][j] = B && in ? (LAYER ? (rb[i][j] - mean_b) * r_b : rb[i][j] * r_b) : 0.0f;
-                    ds[i][j] = S ? rs[i][j] : 0.0f;
-                    if (inner) {
-                        float q = bh[i][j] * w_post[i][j];
-                        if (pc) q += c[j];
-                        const float s = p.alpha * rx[i][j] + q * gates[i][j], d = rn[i][j];
-                        u[i][j] = LAYER ? (in ? (s - mean_s) * r_s : 0.0f) : s * r_s;
-                        e[i][j] = d * w_pre[i][j];
-                        a1 += e[i][j] * u[i][j];
-                        if (LAYER) a2 += e[i][j];
-                        sum_nw[i][j] += d * u[i][j];
-                        if (!PLAIN) sum_nc[i][j] += d;
+                    bh[i][j] = PLAIN ? rb[i][j] * r_b : (rb[i][j] - mean_b) * r_b;
+                    const float y = gw[i][j] * bh[i][j], d = rn[i][j], e = d * w_pre[i][j];
+                    if (PLAIN) u[i][j] = (p.alpha * rx[i][j] + y) * r_s;
+                    else u[i][j] = (p.alpha * rx[i][j] + y + gc[i][j] - mean_s) * r_s;
+                    z[i][j] = rs[i][j] + r_s * e;
+                    v[0] += e * u[i][j];
+                    v[1] += y * z[i][j];
+                    v[2] += y * u[i][j];
+                    sum_nw[i][j] += d * u[i][j];
+                    if (!PLAIN) {
+                        sum_nc[i][j] += d;
+                        v[3] += e;
+                        v[SUMS - 4] += y;
+                        v[SUMS - 3] += gw[i][j] * z[i][j];
+                        v[SUMS - 2] += gw[i][j] * u[i][j];
+                        v[SUMS - 1] += gw[i][j];
                     }
                 }
-            }
             if (AHEAD && m + 1 < end) request(m + 1);
-            float m1 = 0.0f, m2 = 0.0f;
-            if (inner) {
-                const float2 t = block_sum2<LAYER>(a1, a2, buf[turn], warps, warp, lane);
-                m1 = t.x * p.inv_d; m2 = p.layer ? t.y * p.inv_d : 0.0f;
-            }
-            float b1 = 0.0f, b2 = 0.0f;
+            block_sums<SUMS>(v, buf[turn], warps, warp, lane);
+            const float rm1 = inner ? r_s * (v[0] * p.inv_d) : 0.0f, rm2 = !PLAIN && inner && p.layer ? r_s * (v[3] * p.inv_d) : 0.0f;
+            float b1 = v[1] - rm1 * v[2], b2 = 0.0f;
+            if (!PLAIN) { b1 -= rm2 * v[SUMS - 4]; b2 = v[SUMS - 3] - rm1 * v[SUMS - 2] - rm2 * v[SUMS - 1]; }
+            b1 = p.post ? r_b * (b1 * p.inv_d) : 0.0f;
+            b2 = !PLAIN && p.post && p.layer ? r_b * (b2 * p.inv_d) : 0.0f;
 #pragma unroll
             for (int i = 0; i < SLOTS; ++i) {
                 float d[8];
-                Eight<T> c;
-                if (pc) c = read8<T, VEC>(pc, i, tid, team, p.D);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const bool in = VEC || inside<VEC>(i, j, tid, team, p.D);
-                    float t = ds[i][j];
-                    if (inner) t += r_s * (e[i][j] - u[i][j] * m1 - (LAYER ? m2 : 0.0f));
+                    float t = z[i][j];
+                    if (inner) t -= PLAIN ? rm1 * u[i][j] : rm1 * u[i][j] + rm2;
+                    z[i][j] = t;
                     d[j] = p.alpha * t;
-                    if (B) {
-                        const float w = w_post[i][j];
-                        float q = bh[i][j] * w;
-                        if (pc) q += c[j];
-                        sum_g[i][j] += t * q;
-                        const float dp = gates[i][j] * t;
-                        e[i][j] = in ? dp * w : 0.0f;
-                        if (LAYER && VEC && !inside<VEC>(i, j, tid, team, p.D)) e[i][j] = 0.0f;
-                        sum_pw[i][j] += dp * bh[i][j];
-                        if (!PLAIN) sum_pc[i][j] += dp;
-                        b1 += e[i][j] * bh[i][j];
-                        if (LAYER) b2 += e[i][j];
-                    }
+                    sum_tb[i][j] += t * bh[i][j];
+                    if (!PLAIN) sum_t[i][j] += t;
                 }
                 if (p.dx) write8<T, VEC>(static_cast<T *>(p.dx) + m * p.lddx, i, tid, team, p.D, d);
-            }
-            if (B && p.db) {
-                m1 = m2 = 0.0f;
-                if (p.post) {
-                    const float2 t = block_sum2<LAYER>(b1, b2, buf[2 + turn], warps, warp, lane);
-                    m1 = t.x * p.inv_d; m2 = p.layer ? t.y * p.inv_d : 0.0f;
-                }
+                if (B && p.db) {
 #pragma unroll
-                for (int i = 0; i < SLOTS; ++i) {
-                    float d[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) d[j] = p.post ? r_b * (e[i][j] - bh[i][j] * m1 - (LAYER ? m2 : 0.0f)) : e[i][j];
+                    for (int j = 0; j < 8; ++j) {
+                        d[j] = r_b * (gw[i][j] * z[i][j]);
+                        if (p.post) d[j] -= PLAIN ? b1 * bh[i][j] : b1 * bh[i][j] + b2;
+                    }
                     write8<T, VEC>(static_cast<T *>(p.db) + m * p.lddb, i, tid, team, p.D, d);
                 }
             }
         }
-        if (p.dgate) {
 #pragma unroll
-            for (int i = 0; i < SLOTS; ++i) {
-                if (p.chunks == 1) write8<T, VEC>(static_cast<T *>(p.dgate) + group * p.ld_dgate, i, tid, team, p.D, sum_g[i]);
-                else {
+        for (int i = 0; i < SLOTS; ++i) {
+            Eight<T> w, c, g;
+            parameters(i, w, c, g);
+            float d[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int c = column<VEC>(i, j, tid, team);
-                        if (c < p.D) p.part_gate[unit * p.D + c] = sum_g[i][j];
-                    }
+            for (int j = 0; j < 8; ++j) {
+                sum_pw[i][j] += g[j] * sum_tb[i][j];
+                if (!PLAIN) sum_pc[i][j] += g[j] * sum_t[i][j];
+                d[j] = w[j] * sum_tb[i][j];
+                if (!PLAIN) d[j] += c[j] * sum_t[i][j];
+            }
+            if (!p.dgate) continue;
+            if (p.chunks == 1) write8<T, VEC>(static_cast<T *>(p.dgate) + group * p.ld_dgate, i, tid, team, p.D, d);
+            else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int at = column<VEC>(i, j, tid, team);
+                    if (at < p.D) p.part_gate[unit * p.D + at] = d[j];
                 }
             }
         }
@@ -472,10 +505,14 @@ template <typename T, bool VEC> int launch_forward(bnn_ctx *ctx, const NormArgs 
     const int slots = groups > 1024 ? 4 : (few || groups <= 32) ? 1 : groups <= 64 ? 2 : 4;
     const int team = ((groups + slots - 1) / slots + 31) & ~31;
     const dim3 grid((unsigned)a.M), block(team);
-    if (slots == 1) BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_block_norm<T, 1, 1024, VEC>, grid, block, 0, ctx->stream, a));
-    else if (slots == 2) BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_block_norm<T, 2, 256, VEC>, grid, block, 0, ctx->stream, a));
-    else if (team <= 256) BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_block_norm<T, 4, 256, VEC>, grid, block, 0, ctx->stream, a));
-    else BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_block_norm<T, 4, 1024, VEC>, grid, block, 0, ctx->stream, a));
+    const bool plain = VEC && !a.layer && !a.post_c && !a.pre_c;
+#define BNN_FORWARD(SLOTS, THREADS) BNN_CUDA_TRY(ctx, bnn_launch_dependent(plain ? k_block_norm<T, SLOTS, THREADS, VEC, VEC> : k_block_norm<T, SLOTS, THREADS, VEC, false>, \
+                                                                           grid, block, 0, ctx->stream, a))
+    if (slots == 1) BNN_FORWARD(1, 1024);
+    else if (slots == 2) BNN_FORWARD(2, 256);
+    else if (team <= 256) BNN_FORWARD(4, 256);
+    else BNN_FORWARD(4, 1024);
+#undef BNN_FORWARD
     return bnn_check_launch(ctx);
 }
 int backward_slots(int64_t D) { return D <= 8192 ? 1 : D <= 16384 ? 2 : 4; }
