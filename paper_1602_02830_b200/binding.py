@@ -101,6 +101,8 @@ class BnnError(RuntimeError):
 
 
 _lib = None
+_raw_stream = torch._C._cuda_getCurrentRawStream if torch.cuda._is_compiled() else None
+_empty_strided = torch.empty_strided
 
 
 def lib() -> ctypes.CDLL:
@@ -221,7 +223,7 @@ class Context:
             raise BnnError(st, "bnn_create")
         self._h = h
         self._ws = None
-        self._device = torch.device("cuda", device)
+        self._device, self._raw = torch.device("cuda", device), self.stream.cuda_stream
         self._destroy = lib().bnn_destroy      # kept here: module globals may be gone when __del__ runs at interpreter exit
 
     def close(self):
@@ -489,29 +491,29 @@ class Context:
             raise ValueError(f"{what}: expected contiguous {dtype} [{n}] on cuda:{self.device}, got {t.dtype} {list(t.shape)} on {t.device}")
         return t.data_ptr()
 
-    def _elsewhere(self):
-        """Whether torch's current stream is another one than the context's."""
-        return torch._C._cuda_getCurrentRawStream(self.device) != self.stream.cuda_stream
+    def _here(self):
+        """Whether torch's current stream is the context's: then memory needs no care across streams."""
+        return _raw_stream(self.device) == self._raw
 
-    def _new(self, *shape, dtype):
-        """Memory for a result, from the pool of the stream that the library writes it on."""
-        if not self._elsewhere():
-            return torch.empty(shape, dtype=dtype, device=self._device)
+    def _new(self, rows, cols, dtype, here):
+        """A row-major matrix for a result, from the pool of the stream that the library writes it on."""
+        if here:
+            return _empty_strided((rows, cols), (cols, 1), dtype=dtype, device=self._device)
         with torch.cuda.stream(self.stream):
-            t = torch.empty(shape, dtype=dtype, device=self._device)
+            t = _empty_strided((rows, cols), (cols, 1), dtype=dtype, device=self._device)
         t.record_stream(torch.cuda.current_stream(self.device))
         return t
 
-    def _like(self, x):
-        """A contiguous tensor of x's shape and type."""
-        return torch.empty_like(x) if x.is_contiguous() and not self._elsewhere() else self._new(*x.shape, dtype=x.dtype)
+    def _new_vector(self, n, dtype, here):
+        if here:
+            return _empty_strided((n,), (1,), dtype=dtype, device=self._device)
+        return self._new(1, n, dtype, here).view(n)
 
     def _used(self, *tensors):
         """Keeps the memory of tensors of another stream until the work queued on the context's stream is done with it."""
-        if self._elsewhere():
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(self.stream)
+        for t in tensors:
+            if t is not None:
+                t.record_stream(self.stream)
 
     def make_linear(self, W, bias=None, act: str = "none") -> Layer:
         """Dense layer y = residual + act(x W^T + bias): W [N, K] float16 or bfloat16, bias [N] or None."""
@@ -555,7 +557,9 @@ class Context:
                                                        (pre_shift, "pre_shift"))]
         d = BlockNormDesc(_REAL_TYPES[dtype], NORMS[kind], D, eps, alpha, int(post), int(pre), *v, gp, gl, rows_per_gate or 1)
         layer = Layer(d, dtype, self.device, D, D, (post_weight, post_shift, pre_weight, pre_shift, gate))
-        layer.gates, layer.pre = gate.shape[0] if gate is not None else 0, bool(pre)
+        layer.gates, layer.rows_per_gate, layer.pre = gate.shape[0] if gate is not None else 0, d.rows_per_gate, bool(pre)
+        layer.grads = [n for n, t, on in (("dpost_weight", post_weight, post), ("dpost_shift", post_shift, post),
+                                          ("dpre_weight", pre_weight, pre), ("dpre_shift", pre_shift, pre)) if on and t is not None]
         return layer
 
     @staticmethod
@@ -575,148 +579,180 @@ class Context:
 
     def linear(self, layer: Layer, x, residual=None, out=None, pre=None):
         """bnn_linear.  pre: float32 [M, N] that receives x W^T + bias for linear_backward.  out may be residual."""
-        M, N = x.shape[0], layer.outer
-        xp, ldx = self._fit(x, M, layer.inner, layer.dtype, "x")
-        rp, ldr = self._fit(residual, M, N, layer.dtype, "residual")
-        pp, ldp = self._fit(pre, M, N, torch.float32, "pre")
+        M, N, dtype, here = x.shape[0], layer.outer, layer.dtype, self._here()
+        xp, ldx = self._fit(x, M, layer.inner, dtype, "x")
+        rp = pp = None
+        ldr = ldp = 0
+        if residual is not None:
+            rp, ldr = self._fit(residual, M, N, dtype, "residual")
+        if pre is not None:
+            pp, ldp = self._fit(pre, M, N, torch.float32, "pre")
         if out is None:
-            out = self._new(M, N, dtype=layer.dtype)
+            out = self._new(M, N, dtype, here)
             op, ldo = out.data_ptr(), N
         else:
-            op, ldo = self._fit(out, M, N, layer.dtype, "out")
-        self._ck(lib().bnn_linear(self._h, layer.ref, xp, ldx, M, rp, ldr, op, ldo, pp, ldp), "bnn_linear")
-        self._used(x, residual, out, pre, *layer.tensors)
+            op, ldo = self._fit(out, M, N, dtype, "out")
+        st = lib().bnn_linear(self._h, layer.ref, xp, ldx, M, rp, ldr, op, ldo, pp, ldp)
+        if st:
+            self._ck(st, "bnn_linear")
+        if not here:
+            self._used(x, residual, out, pre, *layer.tensors)
         return out
 
     def linear_backward(self, layer: Layer, dy, x, pre=None, want_dx: bool = True, want_dW: bool = True, want_db: bool = True):
         """bnn_linear_backward -> (dx, dW, dbias); dbias is None for a layer without bias, what is not wanted is None."""
-        M, N, K = x.shape[0], layer.outer, layer.inner
-        gp, ldg = self._fit(dy, M, N, layer.dtype, "dy")
-        xp, ldx = self._fit(x, M, K, layer.dtype, "x")
-        pp, ldp = self._fit(pre, M, N, torch.float32, "pre")
-        W, bias = layer.tensors
-        dx = self._like(x) if want_dx else None
-        dW = self._like(W) if want_dW else None
-        db = self._like(bias) if want_db and bias is not None else None
-        self._ck(lib().bnn_linear_backward(self._h, layer.ref, gp, ldg, xp, ldx, M, pp, ldp, _ptr(dx), K, _ptr(dW), K, _ptr(db)),
-                 "bnn_linear_backward")
-        self._used(dy, x, pre, *layer.tensors)
+        M, N, K, dtype, here = x.shape[0], layer.outer, layer.inner, layer.dtype, self._here()
+        gp, ldg = self._fit(dy, M, N, dtype, "dy")
+        xp, ldx = self._fit(x, M, K, dtype, "x")
+        pp, ldp = self._fit(pre, M, N, torch.float32, "pre") if pre is not None else (None, 0)
+        dx = self._new(M, K, dtype, here) if want_dx else None
+        dW = self._new(N, K, dtype, here) if want_dW else None
+        db = self._new_vector(N, dtype, here) if want_db and layer.tensors[1] is not None else None
+        st = lib().bnn_linear_backward(self._h, layer.ref, gp, ldg, xp, ldx, M, pp, ldp, dx.data_ptr() if want_dx else None, K,
+                                       dW.data_ptr() if want_dW else None, K, db.data_ptr() if db is not None else None)
+        if st:
+            self._ck(st, "bnn_linear_backward")
+        if not here:
+            self._used(dy, x, pre, *layer.tensors)
         return dx, dW, db
-
-    def gated(self, layer: Layer, x, out=None, pre=None):
-        """bnn_gated.  pre: contiguous float32 [2, M, N] that receives x Wg^T and x Wu^T for gated_backward."""
-        M, N = x.shape[0], layer.outer
-        xp, ldx = self._fit(x, M, layer.inner, layer.dtype, "x")
-        pp, ldp = self._planes(pre, M, N)
-        if out is None:
-            out = self._new(M, N, dtype=layer.dtype)
-            op, ldo = out.data_ptr(), N
-        else:
-            op, ldo = self._fit(out, M, N, layer.dtype, "out")
-        self._ck(lib().bnn_gated(self._h, layer.ref, xp, ldx, M, op, ldo, pp, ldp), "bnn_gated")
-        self._used(x, out, pre, *layer.tensors)
-        return out
 
     def _planes(self, pre, M, N):
         if pre is None:
             return None, 0
-        if pre.shape != (2, M, N) or not pre.is_contiguous():
-            raise ValueError(f"pre: expected contiguous [2, {M}, {N}], got {list(pre.shape)} with strides {pre.stride()}")
-        return self._fit(pre.view(2 * M, N), 2 * M, N, torch.float32, "pre")
+        if pre.shape != (2, M, N) or pre.dtype is not torch.float32 or pre.get_device() != self.device or not pre.is_contiguous():
+            raise ValueError(f"pre: expected contiguous torch.float32 [2, {M}, {N}] on cuda:{self.device}, got {pre.dtype} {list(pre.shape)} "
+                             f"with strides {pre.stride()} on {pre.device}")
+        return pre.data_ptr(), N
+
+    def gated(self, layer: Layer, x, out=None, pre=None):
+        """bnn_gated.  pre: contiguous float32 [2, M, N] that receives x Wg^T and x Wu^T for gated_backward."""
+        M, N, dtype, here = x.shape[0], layer.outer, layer.dtype, self._here()
+        xp, ldx = self._fit(x, M, layer.inner, dtype, "x")
+        pp, ldp = self._planes(pre, M, N)
+        if out is None:
+            out = self._new(M, N, dtype, here)
+            op, ldo = out.data_ptr(), N
+        else:
+            op, ldo = self._fit(out, M, N, dtype, "out")
+        st = lib().bnn_gated(self._h, layer.ref, xp, ldx, M, op, ldo, pp, ldp)
+        if st:
+            self._ck(st, "bnn_gated")
+        if not here:
+            self._used(x, out, pre, *layer.tensors)
+        return out
 
     def gated_backward(self, layer: Layer, dh, x, pre=None, want_dx: bool = True, want_dW: bool = True):
         """bnn_gated_backward -> (dx, dWg, dWu); what is not wanted is None.  Without pre both products are computed again."""
-        M, N, K = x.shape[0], layer.outer, layer.inner
-        gp, ldg = self._fit(dh, M, N, layer.dtype, "dh")
-        xp, ldx = self._fit(x, M, K, layer.dtype, "x")
+        M, N, K, dtype, here = x.shape[0], layer.outer, layer.inner, layer.dtype, self._here()
+        gp, ldg = self._fit(dh, M, N, dtype, "dh")
+        xp, ldx = self._fit(x, M, K, dtype, "x")
         pp, ldp = self._planes(pre, M, N)
-        dx = self._like(x) if want_dx else None
-        dWg, dWu = (self._like(layer.tensors[0]) if want_dW else None for _ in range(2))
-        self._ck(lib().bnn_gated_backward(self._h, layer.ref, gp, ldg, xp, ldx, M, pp, ldp, _ptr(dx), K, _ptr(dWg), K, _ptr(dWu), K),
-                 "bnn_gated_backward")
-        self._used(dh, x, pre, *layer.tensors)
+        dx = self._new(M, K, dtype, here) if want_dx else None
+        dWg = dWu = wgp = wup = None
+        if want_dW:
+            dWg, dWu = self._new(N, K, dtype, here), self._new(N, K, dtype, here)
+            wgp, wup = dWg.data_ptr(), dWu.data_ptr()
+        st = lib().bnn_gated_backward(self._h, layer.ref, gp, ldg, xp, ldx, M, pp, ldp, dx.data_ptr() if want_dx else None, K, wgp, K, wup, K)
+        if st:
+            self._ck(st, "bnn_gated_backward")
+        if not here:
+            self._used(dh, x, pre, *layer.tensors)
         return dx, dWg, dWu
 
     def _gate_rows(self, layer: Layer, M: int):
-        if layer.gates and layer.gates * layer.desc.rows_per_gate < M:
-            raise ValueError(f"gate: {layer.gates} rows of {layer.desc.rows_per_gate} cover fewer than {M}")
+        if layer.gates * layer.rows_per_gate < M:
+            raise ValueError(f"gate: {layer.gates} rows of {layer.rows_per_gate} cover fewer than {M}")
+
+    def _stats(self, stats, M):
+        if stats is None:
+            return None
+        tp, ldt = self._fit(stats, M, 4, torch.float32, "stats")
+        if M > 1 and ldt != 4:
+            raise ValueError("stats: expected a contiguous tensor")
+        return tp
 
     def block_norm(self, layer: Layer, x, block=None, stream=None, normed=None, stats=None):
         """bnn_block_norm -> (stream, normed); normed is None for a layer without pre.  stream may be x.
         stats: contiguous float32 [M, 4] kept for block_norm_backward."""
-        M, D = x.shape[0], layer.inner
-        self._gate_rows(layer, M)
-        xp, ldx = self._fit(x, M, D, layer.dtype, "x")
-        bp, ldb = self._fit(block, M, D, layer.dtype, "block")
-        tp, ldt = self._fit(stats, M, 4, torch.float32, "stats")
-        if stats is not None and M > 1 and ldt != 4:
-            raise ValueError("stats: expected a contiguous tensor")
+        M, D, dtype, here = x.shape[0], layer.inner, layer.dtype, self._here()
+        if layer.gates:
+            self._gate_rows(layer, M)
+        xp, ldx = self._fit(x, M, D, dtype, "x")
+        bp, ldb = self._fit(block, M, D, dtype, "block") if block is not None else (None, 0)
+        tp = self._stats(stats, M)
         if stream is None:
-            stream = self._like(x)
+            stream = self._new(M, D, dtype, here)
             sp, lds = stream.data_ptr(), D
         else:
-            sp, lds = self._fit(stream, M, D, layer.dtype, "stream")
+            sp, lds = self._fit(stream, M, D, dtype, "stream")
         if normed is None and layer.pre:
-            normed = self._like(x)
+            normed = self._new(M, D, dtype, here)
             np_, ldn = normed.data_ptr(), D
         else:
-            np_, ldn = self._fit(normed, M, D, layer.dtype, "normed")
-        self._ck(lib().bnn_block_norm(self._h, layer.ref, xp, ldx, bp, ldb, M, sp, lds, np_, ldn, tp), "bnn_block_norm")
-        self._used(x, block, stream, normed, stats, *layer.tensors)
+            np_, ldn = self._fit(normed, M, D, dtype, "normed")
+        st = lib().bnn_block_norm(self._h, layer.ref, xp, ldx, bp, ldb, M, sp, lds, np_, ldn, tp)
+        if st:
+            self._ck(st, "bnn_block_norm")
+        if not here:
+            self._used(x, block, stream, normed, stats, *layer.tensors)
         return stream, normed
 
     def block_norm_backward(self, layer: Layer, dstream, dnormed, x, block=None, stats=None):
         """bnn_block_norm_backward -> dict with dx, dblock and, as far as the layer has them, dgate, dpost_weight, dpost_shift,
         dpre_weight, dpre_shift (None otherwise)."""
-        M, D, d = x.shape[0], layer.inner, layer.desc
-        self._gate_rows(layer, M)
-        sp, lds = self._fit(dstream, M, D, layer.dtype, "dstream")
-        np_, ldn = self._fit(dnormed, M, D, layer.dtype, "dnormed")
-        xp, ldx = self._fit(x, M, D, layer.dtype, "x")
-        bp, ldb = self._fit(block, M, D, layer.dtype, "block")
-        tp, ldt = self._fit(stats, M, 4, torch.float32, "stats")
-        if stats is not None and M > 1 and ldt != 4:
-            raise ValueError("stats: expected a contiguous tensor")
-        post_w, post_c, pre_w, pre_c, gate = layer.tensors
-
-        def like(t, wanted=True):
-            return self._like(t) if t is not None and wanted else None
-
-        out = {"dx": self._like(x), "dblock": self._like(x) if block is not None else None,
-               "dgate": None, "dpost_weight": like(post_w, d.post), "dpost_shift": like(post_c, d.post),
-               "dpre_weight": like(pre_w, d.pre), "dpre_shift": like(pre_c, d.pre)}
-        if gate is not None and block is not None:
-            out["dgate"] = self._like(gate)
-            used = -(-M // d.rows_per_gate)
-            if used < layer.gates:                    # gate rows that no row of the stream uses
-                with torch.cuda.stream(self.stream):
-                    out["dgate"][used:].zero_()
-        g = BlockNormGrads(out["dx"].data_ptr(), D, *((out["dblock"].data_ptr(), D) if block is not None else (None, 0)),
-                           *(None if out[k] is None else out[k].data_ptr() for k in ("dpost_weight", "dpost_shift", "dpre_weight",
-                                                                                     "dpre_shift", "dgate")), D)
-        self._ck(lib().bnn_block_norm_backward(self._h, layer.ref, sp, lds, np_, ldn, xp, ldx, bp, ldb, tp, M, ctypes.byref(g)),
-                 "bnn_block_norm_backward")
-        self._used(dstream, dnormed, x, block, stats, *layer.tensors)
+        M, D, dtype, here = x.shape[0], layer.inner, layer.dtype, self._here()
+        if layer.gates:
+            self._gate_rows(layer, M)
+        sp, lds = self._fit(dstream, M, D, dtype, "dstream")
+        np_, ldn = self._fit(dnormed, M, D, dtype, "dnormed")
+        xp, ldx = self._fit(x, M, D, dtype, "x")
+        bp, ldb = self._fit(block, M, D, dtype, "block")
+        tp = self._stats(stats, M)
+        out = dict.fromkeys(("dx", "dblock", "dgate", "dpost_weight", "dpost_shift", "dpre_weight", "dpre_shift"))
+        dx = out["dx"] = self._new(M, D, dtype, here)
+        g = BlockNormGrads(dx.data_ptr(), D)
+        if block is not None:
+            t = out["dblock"] = self._new(M, D, dtype, here)
+            g.dblock, g.lddb = t.data_ptr(), D
+            if layer.gates:
+                t = out["dgate"] = self._new(layer.gates, D, dtype, here)
+                g.dgate, g.ld_dgate = t.data_ptr(), D
+                used = -(-M // layer.rows_per_gate)
+                if used < layer.gates:                    # gate rows that no row of the stream uses
+                    with torch.cuda.stream(self.stream):
+                        t[used:].zero_()
+        for name in layer.grads:
+            t = out[name] = self._new_vector(D, dtype, here)
+            setattr(g, name, t.data_ptr())
+        st = lib().bnn_block_norm_backward(self._h, layer.ref, sp, lds, np_, ldn, xp, ldx, bp, ldb, tp, M, ctypes.byref(g))
+        if st:
+            self._ck(st, "bnn_block_norm_backward")
+        if not here:
+            self._used(dstream, dnormed, x, block, stats, *layer.tensors)
         return out
 
     def dropout(self, x, p: float, seed: int, offset: int = 0, residual=None, out=None):
         """bnn_dropout: residual + (kept ? x / (1 - p) : 0); the backward pass is the same call on the gradient.  out may be x."""
-        if x.dtype not in _REAL_TYPES:
-            raise ValueError(f"x: expected float32, float16 or bfloat16, got {x.dtype}")
+        dtype, here = x.dtype, self._here()
+        if dtype not in _REAL_TYPES:
+            raise ValueError(f"x: expected float32, float16 or bfloat16, got {dtype}")
         if not 0.0 <= p <= 1.0:
             raise ValueError(f"p: expected 0 to 1, got {p}")
         if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
             raise ValueError("seed, offset: expected 64-bit unsigned numbers")
         M, D = x.shape
-        xp, ldx = self._fit(x, M, D, x.dtype, "x")
-        rp, ldr = self._fit(residual, M, D, x.dtype, "residual")
+        xp, ldx = self._fit(x, M, D, dtype, "x")
+        rp, ldr = self._fit(residual, M, D, dtype, "residual") if residual is not None else (None, 0)
         if out is None:
-            out = self._like(x)
+            out = self._new(M, D, dtype, here)
             op, ldo = out.data_ptr(), D
         else:
-            op, ldo = self._fit(out, M, D, x.dtype, "out")
-        self._ck(lib().bnn_dropout(self._h, _REAL_TYPES[x.dtype], xp, ldx, rp, ldr, op, ldo, M, D, p, seed, offset), "bnn_dropout")
-        self._used(x, residual, out)
+            op, ldo = self._fit(out, M, D, dtype, "out")
+        st = lib().bnn_dropout(self._h, _REAL_TYPES[dtype], xp, ldx, rp, ldr, op, ldo, M, D, p, seed, offset)
+        if st:
+            self._ck(st, "bnn_dropout")
+        if not here:
+            self._used(x, residual, out)
         return out
 
 

@@ -53,17 +53,20 @@ struct Problem {
     int vec_out;                         // widest access that every row allows: 2 = 32 bytes, 1 = 16 bytes, 0 = one element
 };
 constexpr int PROBLEMS = 3;              // a gated layer's gradients: dx, dWg, dWu
-struct ProductArgs {
-    Problem q[PROBLEMS];
-    int problems;
-    uint32_t tiles;
-    const void *bias, *add;              // of a single problem
+// What the epilogue of a single product needs beside the problem, and what every launch needs.
+struct Common {
+    const void *bias, *add;
     float *pre;
     int64_t ld_add, ldp;
     int act, f16;
     int vec_bias, vec_add, vec_pre;
     unsigned long long wait_ns;
     int drop_loads;                      // test hook: the producers request nothing, every consumer's wait runs out
+};
+template <int N> struct ProductArgs : Common {
+    Problem q[N];
+    int problems;
+    uint32_t tiles;
 };
 
 struct __align__(16) Control {
@@ -105,9 +108,10 @@ __device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr) {
 }
 
 struct Tile { int problem, m0, n0; };
-template <int WIDTH> __device__ __forceinline__ Tile tile_at(const ProductArgs &p, uint32_t t) {
+template <int WIDTH, int N> __device__ __forceinline__ Tile tile_at(const ProductArgs<N> &p, uint32_t t) {
     int i = 0;
-    while (i + 1 < p.problems && t >= p.q[i + 1].first) ++i;
+    if (N > 1)
+        while (i + 1 < p.problems && t >= p.q[i + 1].first) ++i;
     const Problem &q = p.q[i];
     t -= q.first;
     const uint32_t band = t / (BAND * q.tiles_n), w = t - band * BAND * q.tiles_n;
@@ -205,7 +209,7 @@ __device__ __forceinline__ void act_values(int act, float (&v)[32]) {
 
 // 32 rows x 32 columns of a warp, from accumulators to memory; m: the lane's row.  b: the second accumulator of the gated epilogues.
 template <int EPI, typename T>
-__device__ __forceinline__ void finish32(const ProductArgs &p, const Problem &q, int64_t m, int64_t n0, float *stage, float (&a)[32], float (&b)[32]) {
+__device__ __forceinline__ void finish32(const Common &p, const Problem &q, int64_t m, int64_t n0, float *stage, float (&a)[32], float (&b)[32]) {
     const int lane = threadIdx.x & 31;
     const int64_t below = q.M - (m - lane);
     const Block k{(int)(below < 32 ? below : 32), (int)(q.N - n0 < 32 ? q.N - n0 : 32), stage};
@@ -271,8 +275,8 @@ __device__ __forceinline__ void finish32(const ProductArgs &p, const Problem &q,
     }
 }
 
-template <int EPI, int BN>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_product_pair(const __grid_constant__ ProductArgs p) {
+template <int EPI, int BN, int N>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_product_pair(const __grid_constant__ ProductArgs<N> p) {
     constexpr bool GATED = EPI == BNN_EPI_GATED || EPI == BNN_EPI_GATED_BACK;
     constexpr int WIDTH = GATED ? BN / 2 : BN;                   // output columns of a tile
     constexpr int STAGES = Ring<BN>::STAGES;
@@ -435,8 +439,8 @@ constexpr int FEW_STAGES = 12;
 constexpr int FEW_TOKENS = 256;
 constexpr int64_t FEW_ROWS = 1024;         // beyond, the pair kernel's tiles fill the GPU
 
-struct FewArgs {
-    ProductArgs p;                      // a: weights (a[1]: up rows, or the second pair), b: tokens; M tokens, N outputs
+struct FewArgs : Common {
+    Problem q;                          // a: weights (a[1]: up rows, or the second pair), b: tokens; M tokens, N outputs
     uint32_t token_tiles;
     int tokens;                         // N of the MMA: tokens per tile, a multiple of 16
     int stages;
@@ -500,8 +504,7 @@ template <typename T> __device__ __forceinline__ void write4(T *p, int n, int ve
             if (j < n) p[j] = from_f32<T>(v[j]);
     }
 }
-template <int EPI, typename T> __device__ __forceinline__ void finish4(const ProductArgs &p, int64_t m, int64_t n0, float (&a)[4], float (&b)[4]) {
-    const Problem &q = p.q[0];
+template <int EPI, typename T> __device__ __forceinline__ void finish4(const Common &p, const Problem &q, int64_t m, int64_t n0, float (&a)[4], float (&b)[4]) {
     const int n = (int)(q.N - n0 < 4 ? q.N - n0 : 4);
     const T *add = static_cast<const T *>(p.add) + m * p.ld_add + n0;
     T *out = static_cast<T *>(q.out[0]) + m * q.ldo[0] + n0;
@@ -541,8 +544,8 @@ template <int EPI, typename T> __device__ __forceinline__ void finish4(const Pro
 template <bool W_MN, int EPI> __global__ void __launch_bounds__(FEW_THREADS, 2) k_product_few(const __grid_constant__ FewArgs f) {
     constexpr bool GATED = EPI == BNN_EPI_GATED || EPI == BNN_EPI_GATED_BACK;
     constexpr int ROWS = GATED ? 64 : 128;                        // outputs of a tile
-    const ProductArgs &p = f.p;
-    const Problem &q = p.q[0];
+    const Common &p = f;
+    const Problem &q = f.q;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *tiles = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ FewControl control;
@@ -657,8 +660,8 @@ template <bool W_MN, int EPI> __global__ void __launch_bounds__(FEW_THREADS, 2) 
             float a[4], b[4];
             sum_parts(part + t * 128 + row, split, a);
             if (GATED) sum_parts(part + t * 128 + 64 + row, split, b);
-            if (p.f16) finish4<EPI, __half>(p, t0 + t, n0 + row, a, b);
-            else finish4<EPI, __nv_bfloat16>(p, t0 + t, n0 + row, a, b);
+            if (p.f16) finish4<EPI, __half>(p, q, t0 + t, n0 + row, a, b);
+            else finish4<EPI, __nv_bfloat16>(p, q, t0 + t, n0 + row, a, b);
         }
     }
     __syncwarp();
@@ -672,13 +675,13 @@ template <int BN> constexpr size_t pair_smem() {
 static_assert(pair_smem<256>() <= 227 * 1024 && pair_smem<128>() <= 227 * 1024, "fits the shared memory of an SM");
 
 // Opts in to the shared memory and asks how many pairs fit the device, once per device and kernel; 0 = cannot run.
-template <int EPI, int BN> int pairs_of(int device, int sm_count) {
+template <int EPI, int BN, int N> int pairs_of(int device, int sm_count) {
     static std::mutex lock;
     static int cached[64];
     if (device < 0 || device >= 64) return 0;
     std::lock_guard<std::mutex> guard(lock);
     if (cached[device] == 0) {
-        auto kernel = k_product_pair<EPI, BN>;
+        auto kernel = k_product_pair<EPI, BN, N>;
         int pairs = 0;
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pair_smem<BN>()) == cudaSuccess) {
             cudaLaunchConfig_t cfg = {};
@@ -695,11 +698,11 @@ template <int EPI, int BN> int pairs_of(int device, int sm_count) {
     return cached[device] > 0 ? cached[device] : 0;
 }
 
-template <int EPI, int BN> int launch(bnn_ctx *ctx, const ProductArgs &a) {
-    const int pairs = pairs_of<EPI, BN>(ctx->device, ctx->sm_count);
+template <int EPI, int BN, int N> int launch(bnn_ctx *ctx, const ProductArgs<N> &a) {
+    const int pairs = pairs_of<EPI, BN, N>(ctx->device, ctx->sm_count);
     if (pairs == 0) return BNN_ERR_CUDA;
     const unsigned n = a.tiles < (uint32_t)pairs ? a.tiles : (unsigned)pairs;
-    BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_product_pair<EPI, BN>, dim3(2 * n), dim3(THREADS), pair_smem<BN>(), ctx->stream, a));
+    BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_product_pair<EPI, BN, N>, dim3(2 * n), dim3(THREADS), pair_smem<BN>(), ctx->stream, a));
     return bnn_check_launch(ctx);
 }
 
@@ -747,12 +750,9 @@ int bnn_product_status(bnn_ctx *ctx, int *code) {
 namespace {
 bool is_gated(const BnnProduct &q) { return q.epilogue == BNN_EPI_GATED || q.epilogue == BNN_EPI_GATED_BACK; }
 int64_t steps_of(const BnnProduct &q) { return (q.K + BK - 1) / BK * (is_gated(q) ? 1 : q.pairs); }
-ProductArgs common_args(bnn_ctx *ctx, const BnnProduct &q) {
-    ProductArgs a{};
+void common_args(Common &a, bnn_ctx *ctx, const BnnProduct &q) {
     a.bias = q.bias; a.add = q.add; a.ld_add = q.ld_add; a.pre = q.pre; a.ldp = q.ldp; a.act = q.act; a.f16 = q.dtype == BNN_F16;
     a.wait_ns = ctx->wait_limit_ns; a.drop_loads = ctx->drop_loads;
-    a.problems = 1;
-    return a;
 }
 void common_problem(Problem &w, const BnnProduct &q) {
     w.M = q.M; w.N = q.N;
@@ -819,11 +819,11 @@ int product_few(bnn_ctx *ctx, const BnnProduct &q) {
     const FewPlan plan = few_plan(q);
     if (plan.tiles * plan.split > 0x7fffffff) return BNN_ERR_INVALID_ARG;
     FewArgs f{};
-    f.p = common_args(ctx, q);
-    Problem &w = f.p.q[0];
+    common_args(f, ctx, q);
+    Problem &w = f.q;
     common_problem(w, q);
     const auto fours = [](const void *at, int64_t ld, int64_t n, int size) { return reinterpret_cast<uintptr_t>(at) % (4 * size) == 0 && (n <= 1 || ld % 4 == 0); };
-    f.p.vec_bias = fours(q.bias, 0, 1, 2); f.p.vec_add = fours(q.add, q.ld_add, q.M, 2); f.p.vec_pre = fours(q.pre, q.ldp, 2 * q.M, 4);
+    f.vec_bias = fours(q.bias, 0, 1, 2); f.vec_add = fours(q.add, q.ld_add, q.M, 2); f.vec_pre = fours(q.pre, q.ldp, 2 * q.M, 4);
     w.vec_out = fours(q.out[0], q.ldo[0], q.M, 2) && fours(q.out[1], q.ldo[1], q.M, 2);
     const int rows = is_gated(q) ? 64 : 128;
     f.tokens = plan.tokens; f.token_tiles = (uint32_t)plan.token_tiles;
@@ -869,16 +869,16 @@ bool bnn_product_few(const bnn_ctx *ctx, const BnnProduct &q, const BnnProduct *
     const double apart = few_plan(q).cost + 5.0 + 0.30 * (double)steps * (double)((others + pairs - 1) / pairs);
     return apart < 5.0 + 0.30 * (double)longest * (double)((tiles + others + pairs - 1) / pairs);
 }
-int bnn_product(bnn_ctx *ctx, const BnnProduct *list, int count) {
-    if (count < 1 || count > PROBLEMS) return BNN_ERR_INVALID_ARG;
-    if (count == 1 && !list[0].whole && bnn_product_few(ctx, list[0], nullptr, 0)) return product_few(ctx, list[0]);
+namespace {
+template <int N> int product_pair(bnn_ctx *ctx, const BnnProduct *list, int count) {
     // Half-width tiles where whole ones would leave half of the pairs without work.
     int64_t whole = 0, tiles = 0;
     for (int i = 0; i < count; ++i) whole += pair_tiles(list[i], 256);
     const int bn = 2 * whole <= ctx->sm_count / 2 ? 128 : 256;
-    ProductArgs a = common_args(ctx, list[0]);
+    ProductArgs<N> a{};
+    common_args(a, ctx, list[0]);
     a.problems = count;
-    const BnnProduct *order[PROBLEMS];
+    const BnnProduct *order[N];
     for (int i = 0; i < count; ++i) order[i] = &list[i];
     for (int i = 1; i < count; ++i)                      // the longest sums first: short tiles fill the end of the launch
         for (int j = i; j > 0 && steps_of(*order[j]) > steps_of(*order[j - 1]); --j) { const BnnProduct *t = order[j]; order[j] = order[j - 1]; order[j - 1] = t; }
@@ -905,11 +905,19 @@ int bnn_product(bnn_ctx *ctx, const BnnProduct *list, int count) {
     const BnnProduct &q = list[0];
     a.vec_bias = width_of(q.bias, 0, 1, 2); a.vec_add = width_of(q.add, q.ld_add, q.M, 2); a.vec_pre = width_of(q.pre, q.ldp, 2 * q.M, 4);
 #define BNN_LAUNCH(EPI) (bn == 256 ? launch<EPI, 256>(ctx, a) : launch<EPI, 128>(ctx, a))
-    switch (q.epilogue) {
-        case BNN_EPI_LINEAR: return BNN_LAUNCH(BNN_EPI_LINEAR);
-        case BNN_EPI_LINEAR_BACK: return BNN_LAUNCH(BNN_EPI_LINEAR_BACK);
-        case BNN_EPI_GATED: return BNN_LAUNCH(BNN_EPI_GATED);
-        default: return BNN_LAUNCH(BNN_EPI_GATED_BACK);
+    if constexpr (N == 1) {
+        if (q.epilogue == BNN_EPI_LINEAR_BACK) return BNN_LAUNCH(BNN_EPI_LINEAR_BACK);
+        if (q.epilogue == BNN_EPI_GATED) return BNN_LAUNCH(BNN_EPI_GATED);
+        if (q.epilogue == BNN_EPI_GATED_BACK) return BNN_LAUNCH(BNN_EPI_GATED_BACK);
     }
+    return BNN_LAUNCH(BNN_EPI_LINEAR);
 #undef BNN_LAUNCH
+}
+}  // namespace
+
+int bnn_product(bnn_ctx *ctx, const BnnProduct *list, int count) {
+    if (count < 1 || count > PROBLEMS) return BNN_ERR_INVALID_ARG;
+    if (count > 1) return product_pair<PROBLEMS>(ctx, list, count);
+    if (!list[0].whole && bnn_product_few(ctx, list[0], nullptr, 0)) return product_few(ctx, list[0]);
+    return product_pair<1>(ctx, list, 1);
 }
