@@ -89,30 +89,48 @@ __global__ void __launch_bounds__(256) k_act_backward(const SlopeArgs p) {
     bnn_pdl_wait();
     bnn_pdl_launch_next();
     float s[8] = {};
-    if (c0 < p.N) {
-#pragma unroll 2
+    if (c0 < p.N && p.vec) {
+        constexpr int AT_ONCE = 4;               // rows on their way
+        for (int64_t m0 = first + ry; m0 < end; m0 += SUM_ROWS * AT_ONCE) {
+            uint4 dw[AT_ONCE], zw[AT_ONCE][2];
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) {
+                const int64_t m = m0 + i * SUM_ROWS;
+                if (m >= end) break;
+                dw[i] = *reinterpret_cast<const uint4 *>(dy + m * p.lddy + c0);
+                if (p.pre) {
+                    zw[i][0] = __ldcs(reinterpret_cast<const uint4 *>(p.pre + m * p.ldp + c0));
+                    zw[i][1] = __ldcs(reinterpret_cast<const uint4 *>(p.pre + m * p.ldp + c0) + 1);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) {
+                const int64_t m = m0 + i * SUM_ROWS;
+                if (m >= end) break;
+                float d[8], z[8];
+                unpack8<T>(&dw[i], d);
+                if (p.pre) {
+                    unpack8<float>(zw[i], z);
+                    slopes8(p.act, z, d);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s[j] += d[j];
+                if (dz) store8(dz + m * p.lddz + c0, d);
+            }
+        }
+    } else if (c0 < p.N) {
         for (int64_t m = first + ry; m < end; m += SUM_ROWS) {
             float d[8], z[8];
-            if (p.vec) {
-                load8(dy + m * p.lddy + c0, d);
-                if (p.pre) load8(p.pre + m * p.ldp + c0, z);
-            } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    d[j] = c0 + j < p.N ? to_f32(dy[m * p.lddy + c0 + j]) : 0.0f;
-                    z[j] = p.pre && c0 + j < p.N ? p.pre[m * p.ldp + c0 + j] : 0.0f;
-                }
+            for (int j = 0; j < 8; ++j) {
+                d[j] = c0 + j < p.N ? to_f32(dy[m * p.lddy + c0 + j]) : 0.0f;
+                z[j] = p.pre && c0 + j < p.N ? p.pre[m * p.ldp + c0 + j] : 0.0f;
             }
             if (p.pre) slopes8(p.act, z, d);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[j] += d[j];
-            if (dz) {
-                if (p.vec) store8(dz + m * p.lddz + c0, d);
-                else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (c0 + j < p.N) dz[m * p.lddz + c0 + j] = from_f32<T>(d[j]);
-                }
+            for (int j = 0; j < 8; ++j) {
+                s[j] += d[j];
+                if (dz && c0 + j < p.N) dz[m * p.lddz + c0 + j] = from_f32<T>(d[j]);
             }
         }
     }
@@ -227,20 +245,21 @@ struct Readable {
     }
 };
 
-// The gradients of a layer (dx first, if there is one) in one launch, so that the tiles of all of them fill the GPU together, or dx of
-// few rows on the kernel for those.  The choice is made for all of them and then what is not wanted (out[0] NULL) is left out, so that
-// a gradient has the same bits whatever is asked for beside it.
+// The gradients of a layer: in one launch, so that the tiles of all of them fill the GPU together, or some of them on the kernel for few
+// rows.  The choice is made for all of them and then what is not wanted (out[0] NULL) is left out, so that a gradient has the same
+// bits whatever is asked for beside it.
 int gradients(bnn_ctx *ctx, int dtype, BnnProduct *g, int n) {
-    for (int i = 0; i < n; ++i) { g[i].dtype = dtype; g[i].epilogue = BNN_EPI_LINEAR; g[i].whole = 1; if (!g[i].pairs) g[i].pairs = 1; }
-    if (n > 1 && !g[0].a_mn && bnn_product_few(ctx, g[0], g + 1, n - 1)) {
-        g[0].whole = 0;
-        if (g[0].out[0])
-            if (int st = bnn_product(ctx, g, 1)) return st;
-        ++g; --n;
-    }
+    if (n == 0) return BNN_OK;
+    for (int i = 0; i < n; ++i) { g[i].dtype = dtype; g[i].epilogue = BNN_EPI_LINEAR; if (!g[i].pairs) g[i].pairs = 1; }
+    bool few[3] = {};
+    if (!bnn_product_apart(ctx, g, n, few)) few[0] = few[1] = few[2] = false;
     int kept = 0;
-    for (int i = 0; i < n; ++i)
-        if (g[i].out[0]) g[kept++] = g[i];
+    for (int i = 0; i < n; ++i) {
+        if (!g[i].out[0]) continue;
+        g[i].kernel = few[i] ? BNN_FEW : BNN_PAIR;
+        if (few[i]) { if (int st = bnn_product(ctx, g + i, 1)) return st; }
+        else g[kept++] = g[i];
+    }
     return kept ? bnn_product(ctx, g, kept) : BNN_OK;
 }
 

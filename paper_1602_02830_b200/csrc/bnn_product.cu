@@ -154,8 +154,9 @@ template <typename T> __device__ __forceinline__ void read32(const T *row, int64
         __syncwarp();
     }
 }
+// Results are written past the operands that the tiles in flight share in L2 (.cs: first to be evicted).
 __device__ __forceinline__ void st256(void *p, const uint32_t *w) {
-    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+    asm volatile("st.global.cs.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
                  ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
 }
 template <typename T> __device__ __forceinline__ void write32(T *row, int64_t ld, int vec, const Block &k, const float (&v)[32]) {
@@ -174,7 +175,7 @@ template <typename T> __device__ __forceinline__ void write32(T *row, int64_t ld
                 for (int i = 0; i < WORDS / 8; ++i) st256(reinterpret_cast<uint32_t *>(row) + 8 * i, w + 8 * i);
             } else {
 #pragma unroll
-                for (int i = 0; i < WORDS / 4; ++i) reinterpret_cast<uint4 *>(row)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                for (int i = 0; i < WORDS / 4; ++i) __stcs(reinterpret_cast<uint4 *>(row) + i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
             }
         }
     } else {
@@ -437,7 +438,7 @@ constexpr int FEW_SMEM = 200 * 1024;
 constexpr int FEW_THREADS = 384;
 constexpr int FEW_STAGES = 12;
 constexpr int FEW_TOKENS = 256;
-constexpr int64_t FEW_ROWS = 1024;         // beyond, the pair kernel's tiles fill the GPU
+constexpr int64_t FEW_TILES = 128;         // from so many whole tiles on the pair kernel fills the GPU
 
 struct FewArgs : Common {
     Problem q;                          // a: weights (a[1]: up rows, or the second pair), b: tokens; M tokens, N outputs
@@ -541,7 +542,7 @@ template <int EPI, typename T> __device__ __forceinline__ void finish4(const Com
     if constexpr (EPI == BNN_EPI_GATED_BACK) write4(static_cast<T *>(q.out[1]) + m * q.ldo[1] + n0, n, q.vec_out, b);
 }
 
-template <bool W_MN, int EPI> __global__ void __launch_bounds__(FEW_THREADS, 2) k_product_few(const __grid_constant__ FewArgs f) {
+template <bool W_MN, bool T_MN, int EPI> __global__ void __launch_bounds__(FEW_THREADS, 2) k_product_few(const __grid_constant__ FewArgs f) {
     constexpr bool GATED = EPI == BNN_EPI_GATED || EPI == BNN_EPI_GATED_BACK;
     constexpr int ROWS = GATED ? 64 : 128;                        // outputs of a tile
     const Common &p = f;
@@ -591,7 +592,9 @@ template <bool W_MN, int EPI> __global__ void __launch_bounds__(FEW_THREADS, 2) 
                     tma_load_2d(dst, &q.a[second], (int)n0, k, bar);
                     tma_load_2d(dst + 8192, &q.a[second], (int)n0 + 64, k, bar);
                 } else tma_load_2d(dst, &q.a[second], k, (int)n0, bar);
-                tma_load_2d(dst + A_STAGE, &q.b[second], k, (int)t0, bar);
+                if constexpr (T_MN) {
+                    for (int i = 0; i < f.tokens; i += 64) tma_load_2d(dst + A_STAGE + i * 128, &q.b[second], (int)t0 + i, k, bar);
+                } else tma_load_2d(dst + A_STAGE, &q.b[second], k, (int)t0, bar);
                 stage += 2;
                 while (stage >= f.stages) { stage -= f.stages; ++lap; }
             }
@@ -605,7 +608,8 @@ template <bool W_MN, int EPI> __global__ void __launch_bounds__(FEW_THREADS, 2) 
     } else if (warp == 1) {
         if (lane == 0) {
             constexpr uint64_t A_STEP = W_MN ? 2048 >> 4 : 32 >> 4;
-            const uint64_t a0 = W_MN ? smem_desc_mn(smem_u32(tiles)) : smem_desc_sw128(smem_u32(tiles)), b0 = smem_desc_sw128(smem_u32(tiles + A_STAGE));
+            const uint64_t a0 = W_MN ? smem_desc_mn(smem_u32(tiles)) : smem_desc_sw128(smem_u32(tiles)), b0 = T_MN ? smem_desc_mn(smem_u32(tiles + A_STAGE)) : smem_desc_sw128(smem_u32(tiles + A_STAGE));
+            constexpr uint64_t B_STEP = T_MN ? 2048 >> 4 : 32 >> 4;
             int stage = 0;
             uint32_t phase = 0;
             for (int kit = first; kit < last; ++kit) {
@@ -613,7 +617,7 @@ template <bool W_MN, int EPI> __global__ void __launch_bounds__(FEW_THREADS, 2) 
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint64_t at = (uint64_t)(stage * (f.stage_bytes >> 4));
 #pragma unroll
-                for (int k = 0; k < BK / 16; ++k) mma_f16(tmem_base, a0 + at + k * A_STEP, b0 + at + k * (32 >> 4), q.idesc, (kit > first || k) ? 1u : 0u);
+                for (int k = 0; k < BK / 16; ++k) mma_f16(tmem_base, a0 + at + k * A_STEP, b0 + at + k * B_STEP, q.idesc, (kit > first || k) ? 1u : 0u);
                 mma_commit(&ctl->empty[stage]);
                 if (++stage == f.stages) { stage = 0; phase ^= 1; }
             }
@@ -706,8 +710,8 @@ template <int EPI, int BN, int N> int launch(bnn_ctx *ctx, const ProductArgs<N> 
     return bnn_check_launch(ctx);
 }
 
-template <bool W_MN, int EPI> int launch_few(bnn_ctx *ctx, const FewArgs &f, unsigned tiles, unsigned split) {
-    auto kernel = k_product_few<W_MN, EPI>;
+template <bool W_MN, bool T_MN, int EPI> int launch_few(bnn_ctx *ctx, const FewArgs &f, unsigned tiles, unsigned split) {
+    auto kernel = k_product_few<W_MN, T_MN, EPI>;
     static std::mutex lock;
     static bool ready[64];
     if (ctx->device < 0 || ctx->device >= 64) return BNN_ERR_INVALID_ARG;
@@ -793,12 +797,13 @@ FewPlan few_plan(const BnnProduct &q) {
     FewPlan best{};
     best.cost = 1e30;
     int last = 0;
-    for (int most = FEW_TOKENS; most >= 16; most /= 2) {
+    const int unit = q.a_mn ? 64 : 16;                     // boxes of 64 when the token operand lies against the sum
+    for (int most = FEW_TOKENS; most >= unit; most /= 2) {
         FewPlan f{};
         f.token_tiles = (int)((q.M + most - 1) / most);
         if (f.token_tiles == last) continue;
         last = f.token_tiles;
-        f.tokens = (int)(((q.M + f.token_tiles - 1) / f.token_tiles + 15) & ~int64_t(15));
+        f.tokens = (int)(((q.M + f.token_tiles - 1) / f.token_tiles + unit - 1) / unit * unit);
         f.tiles = weight_tiles * f.token_tiles;
         for (int log = 0; log < 4; ++log) {
             f.split = 1 << log;
@@ -828,7 +833,7 @@ int product_few(bnn_ctx *ctx, const BnnProduct &q) {
     const int rows = is_gated(q) ? 64 : 128;
     f.tokens = plan.tokens; f.token_tiles = (uint32_t)plan.token_tiles;
     w.tiles_n = (uint32_t)((q.N + rows - 1) / rows);
-    w.idesc = instruction(q.dtype, q.b_mn, 0, f.tokens, 128);
+    w.idesc = instruction(q.dtype, q.b_mn, q.a_mn, f.tokens, 128);
     f.stage_bytes = A_STAGE + (uint32_t)f.tokens * BK * 2;
     f.tmem_cols = 32;
     while ((int)f.tmem_cols < f.tokens) f.tmem_cols *= 2;
@@ -842,33 +847,45 @@ int product_few(bnn_ctx *ctx, const BnnProduct &q) {
             if (q.b[i].p)
                 if (int st = q.b_mn ? map16(ctx, &w.a[i], q.b[i].p, q.b[i].ld, q.K, q.N, BK) : map16(ctx, &w.a[i], q.b[i].p, q.b[i].ld, q.N, q.K, rows)) return st;
             if (q.a[i].p)
-                if (int st = map16(ctx, &w.b[i], q.a[i].p, q.a[i].ld, q.M, q.K, f.tokens)) return st;
+                if (int st = q.a_mn ? map16(ctx, &w.b[i], q.a[i].p, q.a[i].ld, q.K, q.M, BK) : map16(ctx, &w.b[i], q.a[i].p, q.a[i].ld, q.M, q.K, f.tokens)) return st;
         }
     }
     const unsigned tiles = (unsigned)plan.tiles, split = (unsigned)plan.split;
-    if (q.b_mn) return launch_few<true, BNN_EPI_LINEAR>(ctx, f, tiles, split);
+    if (q.a_mn) return launch_few<true, true, BNN_EPI_LINEAR>(ctx, f, tiles, split);          // a weight gradient: both against the sum
+    if (q.b_mn) return launch_few<true, false, BNN_EPI_LINEAR>(ctx, f, tiles, split);
     switch (q.epilogue) {
-        case BNN_EPI_LINEAR: return launch_few<false, BNN_EPI_LINEAR>(ctx, f, tiles, split);
-        case BNN_EPI_LINEAR_BACK: return launch_few<false, BNN_EPI_LINEAR_BACK>(ctx, f, tiles, split);
-        case BNN_EPI_GATED: return launch_few<false, BNN_EPI_GATED>(ctx, f, tiles, split);
-        default: return launch_few<false, BNN_EPI_GATED_BACK>(ctx, f, tiles, split);
+        case BNN_EPI_LINEAR: return launch_few<false, false, BNN_EPI_LINEAR>(ctx, f, tiles, split);
+        case BNN_EPI_LINEAR_BACK: return launch_few<false, false, BNN_EPI_LINEAR_BACK>(ctx, f, tiles, split);
+        case BNN_EPI_GATED: return launch_few<false, false, BNN_EPI_GATED>(ctx, f, tiles, split);
+        default: return launch_few<false, false, BNN_EPI_GATED_BACK>(ctx, f, tiles, split);
     }
 }
 }  // namespace
 
-bool bnn_product_few(const bnn_ctx *ctx, const BnnProduct &q, const BnnProduct *more, int n) {
-    if (q.a_mn || q.M > FEW_ROWS) return false;
-    if (n == 0) return few_plan(q).cost < pair_cost(ctx, q);
-    // beside others: alone and then the others, against all of them in one launch
-    int64_t tiles = pair_tiles(q, 256), others = 0, steps = 0;
+// The cheapest way to make several products: each alone on either kernel, or all of them in one launch of the pair kernel.
+// few[i]: product i runs on k_product_few.
+bool bnn_product_apart(const bnn_ctx *ctx, const BnnProduct *list, int n, bool *few) {
+    struct Load { int64_t longest = 0, total = 0; } rest, all;       // K steps: of one tile, of all tiles
+    const auto add = [](Load &l, const BnnProduct &q) {
+        const int64_t steps = steps_of(q);
+        if (steps > l.longest) l.longest = steps;
+        l.total += steps * pair_tiles(q, 256);
+    };
+    const auto cost = [&](const Load &l) {
+        const int64_t even = (l.total + ctx->sm_count / 2 - 1) / (ctx->sm_count / 2);
+        return l.longest ? 5.0 + 0.30 * (double)(even > l.longest ? even : l.longest) : 0.0;
+    };
+    double apart = 0.0;
     for (int i = 0; i < n; ++i) {
-        others += pair_tiles(more[i], 256);
-        if (steps_of(more[i]) > steps) steps = steps_of(more[i]);
+        const double f = pair_tiles(list[i], 256) <= FEW_TILES ? few_plan(list[i]).cost : 1e30;
+        few[i] = f < pair_cost(ctx, list[i]);
+        if (few[i]) apart += f;
+        else add(rest, list[i]);
+        add(all, list[i]);
     }
-    const int64_t pairs = ctx->sm_count / 2, longest = steps_of(q) > steps ? steps_of(q) : steps;
-    const double apart = few_plan(q).cost + 5.0 + 0.30 * (double)steps * (double)((others + pairs - 1) / pairs);
-    return apart < 5.0 + 0.30 * (double)longest * (double)((tiles + others + pairs - 1) / pairs);
+    return n == 1 || apart + cost(rest) < cost(all);
 }
+
 namespace {
 template <int N> int product_pair(bnn_ctx *ctx, const BnnProduct *list, int count) {
     // Half-width tiles where whole ones would leave half of the pairs without work.
@@ -918,6 +935,8 @@ template <int N> int product_pair(bnn_ctx *ctx, const BnnProduct *list, int coun
 int bnn_product(bnn_ctx *ctx, const BnnProduct *list, int count) {
     if (count < 1 || count > PROBLEMS) return BNN_ERR_INVALID_ARG;
     if (count > 1) return product_pair<PROBLEMS>(ctx, list, count);
-    if (!list[0].whole && bnn_product_few(ctx, list[0], nullptr, 0)) return product_few(ctx, list[0]);
+    bool few = list[0].kernel == BNN_FEW;
+    if (list[0].kernel == BNN_CHEAPEST) bnn_product_apart(ctx, list, 1, &few);
+    if (few) return product_few(ctx, list[0]);
     return product_pair<1>(ctx, list, 1);
 }

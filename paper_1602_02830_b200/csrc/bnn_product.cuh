@@ -8,6 +8,7 @@ enum BnnEpilogue {
     BNN_EPI_GATED,        // g, u: pre = (g, u); out0 = act(g) u
     BNN_EPI_GATED_BACK    // out0 = add u act'(g), out1 = add act(g)
 };
+enum { BNN_CHEAPEST = 0, BNN_PAIR = 1, BNN_FEW = 2 };
 // One operand: rows of `ld` elements.  Its rows run along the output's rows (columns) and its columns along the sum, or, with
 // BnnProduct::a_mn / b_mn, the other way round.
 struct BnnOperand { const void *p; int64_t ld; };
@@ -23,10 +24,10 @@ struct BnnProduct {
     void *out[2]; int64_t ldo[2];
     float *pre; int64_t ldp;      // EPI_GATED: [2][M][ldp]
     int act;
-    int whole;                    // 1: on the pair kernel, however few rows
+    int kernel;                   // BNN_CHEAPEST, or the one to use
 };
 // Up to three products in one launch (several: linear epilogue without bias, add or pre).  Every operand must satisfy bnn_rows16.
 // M, N > 0; K = 0 is the empty sum.
 int bnn_product(bnn_ctx *ctx, const BnnProduct *list, int count);
-// Whether a product of few rows is better off on the kernel for those, alone in its launch, than with `more` in one launch of the other.
-bool bnn_product_few(const bnn_ctx *ctx, const BnnProduct &p, const BnnProduct *more, int n);
+// Whether several products are made faster apart than in one launch of the pair kernel; few[i]: product i on the kernel for few rows.
+bool bnn_product_apart(const bnn_ctx *ctx, const BnnProduct *list, int n, bool *few);
