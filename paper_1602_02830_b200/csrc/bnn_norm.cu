@@ -62,11 +62,13 @@ template <typename T, bool VEC> __device__ __forceinline__ Eight<T> read8(const 
     Eight<T> e;
     if constexpr (VEC) {
         const int c = column<true>(slot, 0, tid, team);
+        // a predicated load instead of a branch: the branches around 28 accesses a row were a sixth of the instructions
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-            const uint4 q = c < D ? reinterpret_cast<const uint4 *>(row + c)[i] : make_uint4(0u, 0u, 0u, 0u);
-            e.w[4 * i] = q.x; e.w[4 * i + 1] = q.y; e.w[4 * i + 2] = q.z; e.w[4 * i + 3] = q.w;
-        }
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t"
+                         "@p ld.global.v4.u32 {%0,%1,%2,%3}, [%4];\n\t}"
+                         : "=&r"(e.w[4 * i]), "=&r"(e.w[4 * i + 1]), "=&r"(e.w[4 * i + 2]), "=&r"(e.w[4 * i + 3])
+                         : "l"(reinterpret_cast<const uint4 *>(row + c) + i), "r"((uint32_t)(c < D)) : "memory");
     } else {
 #pragma unroll
         for (int j = 0; j < 8; j += 8 / (2 * (int)sizeof(T))) {
@@ -84,7 +86,19 @@ template <typename T, bool VEC>
 __device__ __forceinline__ void write8(T *row, int slot, int tid, int team, int D, const float (&v)[8]) {
     if constexpr (VEC) {
         const int c = column<true>(slot, 0, tid, team);
-        if (c < D) store8(row + c, v);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+            uint32_t w[4];
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = __float_as_uint(v[4 * i + k]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = pack2<T>(v[2 * k], v[2 * k + 1]);
+            }
+            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\t@p st.global.v4.u32 [%4], {%0,%1,%2,%3};\n\t}"
+                         ::"r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "l"(reinterpret_cast<uint4 *>(row + c) + i), "r"((uint32_t)(c < D)) : "memory");
+        }
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -136,18 +150,63 @@ template <int N> __device__ __forceinline__ void block_sums(float (&v)[N], float
 }
 
 // One row per CTA: both rows are requested before anything is computed from them.
-// PLAIN: BNN_NORM_RMS without shifts.  Columns beyond D read as zero, which adds nothing to the sums of squares; around a mean
+// PLAIN: BNN_NORM_RMS without shifts, with a block, both outputs wanted.  Columns beyond D read as zero, which adds nothing to the sums of squares; around a mean
 // (layer norm) they have to be left out.
 template <typename T, int SLOTS, int THREADS, bool VEC, bool PLAIN>
-__global__ void __launch_bounds__(THREADS, 1) k_block_norm(const NormArgs p) {
+__global__ void __launch_bounds__(THREADS, THREADS <= 256 ? 3 : 1) k_block_norm(const NormArgs p) {
     __shared__ float buf[4][32];
     const int tid = threadIdx.x, team = blockDim.x, warps = team >> 5, warp = tid >> 5, lane = tid & 31;
-    const T *pw = static_cast<const T *>(p.post_w), *pc = PLAIN ? nullptr : static_cast<const T *>(p.post_c);
-    const T *nw = static_cast<const T *>(p.pre_w), *nc = PLAIN ? nullptr : static_cast<const T *>(p.pre_c);
-    const bool layer = !PLAIN && p.layer;
+    const T *pw = static_cast<const T *>(p.post_w), *pc = static_cast<const T *>(p.post_c);
+    const T *nw = static_cast<const T *>(p.pre_w), *nc = static_cast<const T *>(p.pre_c);
+    const bool layer = p.layer;
     const int64_t m = blockIdx.x;
     bnn_pdl_wait();
     bnn_pdl_launch_next();
+    if constexpr (PLAIN) {
+        // everything is there and nothing is optional inside the loops: weights that are not given are ones
+        Eight<T> rx[SLOTS], rb[SLOTS];
+        const T *X = static_cast<const T *>(p.x) + m * p.ldx, *B = static_cast<const T *>(p.block) + m * p.ldb;
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) { rx[i] = read8<T, VEC>(X, i, tid, team, p.D); rb[i] = read8<T, VEC>(B, i, tid, team, p.D); }
+        const T *gate = p.gate ? static_cast<const T *>(p.gate) + (m / p.rows_per_gate) * p.ld_gate : nullptr;
+        float r = 1.0f, q = 0.0f;
+        if (p.post) {
+#pragma unroll
+            for (int i = 0; i < SLOTS; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) q += rb[i][j] * rb[i][j];
+            r = 1.0f / sqrtf(block_sum(q, buf[1], warps, warp, lane) * p.inv_d + p.eps);
+        }
+        float s[SLOTS][8];
+        q = 0.0f;
+        T *out = static_cast<T *>(p.stream) + m * p.lds;
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) {
+            Eight<T> w, g;
+            w.fill(1.0f); g.fill(1.0f);
+            if (pw) w = read8<T, VEC>(pw, i, tid, team, p.D);
+            if (gate) g = read8<T, VEC>(gate, i, tid, team, p.D);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                s[i][j] = p.alpha * rx[i][j] + rb[i][j] * r * (w[j] * g[j]);
+                q += s[i][j] * s[i][j];
+            }
+            write8<T, VEC>(out, i, tid, team, p.D, s[i]);
+        }
+        const float r_s = 1.0f / sqrtf(block_sum(q, buf[3], warps, warp, lane) * p.inv_d + p.eps);
+        if (p.stats && tid == 0) { p.stats[4 * m] = 0.0f; p.stats[4 * m + 1] = r; p.stats[4 * m + 2] = 0.0f; p.stats[4 * m + 3] = r_s; }
+        out = static_cast<T *>(p.normed) + m * p.ldn;
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) {
+            Eight<T> w;
+            w.fill(1.0f);
+            if (nw) w = read8<T, VEC>(nw, i, tid, team, p.D);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[i][j] *= r_s * w[j];
+            write8<T, VEC>(out, i, tid, team, p.D, s[i]);
+        }
+        return;
+    }
     Eight<T> rx[SLOTS], rb[SLOTS];
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
@@ -168,11 +227,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_block_norm(const NormArgs p) {
         float q = 0.0f;
 #pragma unroll
         for (int i = 0; i < SLOTS; ++i) {
-            if (VEC && !PLAIN && column<VEC>(i, 0, tid, team) >= p.D) continue;
+            if (VEC && column<VEC>(i, 0, tid, team) >= p.D) continue;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 float v = rb[i][j];
-                if (!PLAIN) v = VEC || column<VEC>(i, j, tid, team) < p.D ? v - mean : 0.0f;
+                v = VEC || column<VEC>(i, j, tid, team) < p.D ? v - mean : 0.0f;
                 q += v * v;
             }
         }
@@ -189,7 +248,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_block_norm(const NormArgs p) {
             if (pc) c = read8<T, VEC>(pc, i, tid, team, p.D);
             if (gate) g = read8<T, VEC>(gate, i, tid, team, p.D);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = PLAIN ? rb[i][j] * r : (rb[i][j] - mean) * r;
+            for (int j = 0; j < 8; ++j) v[j] = (rb[i][j] - mean) * r;
             if (pw)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] *= w[j];
@@ -221,11 +280,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_block_norm(const NormArgs p) {
     float q = 0.0f;
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
-        if (VEC && !PLAIN && column<VEC>(i, 0, tid, team) >= p.D) continue;
+        if (VEC && column<VEC>(i, 0, tid, team) >= p.D) continue;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             float v = s[i][j];
-            if (!PLAIN) v = VEC || column<VEC>(i, j, tid, team) < p.D ? v - mean : 0.0f;
+            v = VEC || column<VEC>(i, j, tid, team) < p.D ? v - mean : 0.0f;
             q += v * v;
         }
     }
@@ -238,7 +297,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_block_norm(const NormArgs p) {
         if (nw) w = read8<T, VEC>(nw, i, tid, team, p.D);
         if (nc) c = read8<T, VEC>(nc, i, tid, team, p.D);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s[i][j] = PLAIN ? s[i][j] * r : (s[i][j] - mean) * r;
+        for (int j = 0; j < 8; ++j) s[i][j] = (s[i][j] - mean) * r;
         if (nw)
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[i][j] *= w[j];
@@ -250,33 +309,42 @@ __global__ void __launch_bounds__(THREADS, 1) k_block_norm(const NormArgs p) {
 }
 
 // A CTA takes whole units (a unit: chunk_rows rows that share one gate row), so every thread keeps the column sums of its own
-// columns in registers from row to row.  The next row is requested before the current one is worked on (SLOTS = 1; wider rows
-// leave no registers for it).
+// columns in registers from row to row.  STAGES > 0 (VEC): the rows ahead are on their way to shared memory by cp.async, each thread's
+// sixteen bytes to its own place, so that no register waits for memory; otherwise a row is read when it is its turn.
 // One reduction per row: with y = gate w_post bh and z = ds + r_s e, the row's T is z - r_s (m1 u + m2), linear in the means m1 = mean(e u) and
 // m2 = mean(e) of the stream's norm, so the two sums that the block's norm needs, of T y and of T gate w_post, follow from sums that
 // are taken together with those of e u and e.  Of the parameter sums only sum T bh (and sum T) is kept per unit: the gate's gradient is
 // w_post times it, the post weight's the gate times it.
-// PLAIN: no means and no shifts (BNN_NORM_RMS without shift vectors or their gradients).
-template <typename T, int SLOTS, int THREADS, bool VEC, bool PLAIN>
-__global__ void __launch_bounds__(THREADS, 1) k_block_norm_backward(const NormArgs p) {
-    constexpr bool AHEAD = SLOTS == 1;
-    constexpr int SUMS = PLAIN ? 4 : 8;
+// PLAIN: no means and no shifts (BNN_NORM_RMS without shift vectors or their gradients), and all four inputs and both row gradients are there,
+// so that nothing is optional inside the row loop.
+// Sixteen bytes, or zeros without an access where `bytes` is 0.
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, uint32_t bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+template <typename T, int SLOTS, int THREADS, int CTAS, bool VEC, bool PLAIN, int STAGES>
+__global__ void __launch_bounds__(THREADS, CTAS) k_block_norm_backward(const NormArgs p) {
+    constexpr int SUMS = PLAIN ? 4 : 8, PIECES = (int)sizeof(T) / 2;        // 16-byte pieces of eight values
+    extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float buf[2][32 * SUMS];
     const int tid = threadIdx.x, team = blockDim.x, warps = team >> 5, warp = tid >> 5, lane = tid & 31;
     const T *pw = static_cast<const T *>(p.post_w), *pc = PLAIN ? nullptr : static_cast<const T *>(p.post_c), *nw = static_cast<const T *>(p.pre_w);
     const T *X = static_cast<const T *>(p.x), *B = static_cast<const T *>(p.block), *S = static_cast<const T *>(p.ds), *N = static_cast<const T *>(p.dn);
-    const bool inner = p.pre && p.dn;
+    const bool inner = PLAIN || (p.pre && p.dn), has_b = PLAIN || B, has_s = PLAIN || S;
     bnn_pdl_wait();
     bnn_pdl_launch_next();
-    float w_pre[SLOTS][8], sum_nw[SLOTS][8], sum_nc[SLOTS][8], sum_pw[SLOTS][8], sum_pc[SLOTS][8];
+    Eight<T> w_pre[SLOTS];
+    float sum_nw[SLOTS][8], sum_nc[SLOTS][8];
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
-        Eight<T> w;
-        w.fill(1.0f);
-        if (nw) w = read8<T, VEC>(nw, i, tid, team, p.D);
+        w_pre[i].fill(1.0f);
+        if (nw) w_pre[i] = read8<T, VEC>(nw, i, tid, team, p.D);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) { w_pre[i][j] = w[j]; sum_nw[i][j] = 0.0f; sum_nc[i][j] = 0.0f; sum_pw[i][j] = 0.0f; sum_pc[i][j] = 0.0f; }
+        for (int j = 0; j < 8; ++j) { sum_nw[i][j] = 0.0f; sum_nc[i][j] = 0.0f; }
     }
+    float *part = p.part + (int64_t)blockIdx.x * 4 * p.D;
+    // this thread's place in a stage: [array][slot][piece], a team's width apart
+    const uint32_t place = STAGES ? (uint32_t)__cvta_generic_to_shared(ring) + (uint32_t)tid * 16 : 0;
+    const uint32_t step = (uint32_t)team * 16, stage_bytes = step * 4 * SLOTS * PIECES;
     uint32_t turn = 0;                     // rows done: alternates the buffers of the sums
     for (int64_t unit = blockIdx.x; unit < p.units; unit += gridDim.x) {
         const int64_t group = unit / p.chunks, chunk = unit - group * p.chunks;
@@ -302,38 +370,76 @@ __global__ void __launch_bounds__(THREADS, 1) k_block_norm_backward(const NormAr
                 sum_tb[i][j] = 0.0f; sum_t[i][j] = 0.0f;
             }
         }
-        Eight<T> rx[SLOTS], rb[SLOTS], rs[SLOTS], rn[SLOTS];
-        float4 st = make_float4(0.0f, 1.0f, 0.0f, 1.0f);
+        // a row's four arrays in the order block, x, dn, ds
+        auto ahead = [&](int64_t m, uint32_t stage) {
+            if (m < end) {
+                const T *const rows[4] = {B + m * p.ldb, X + m * p.ldx, N + m * p.lddn, S + m * p.ldds};
+                const bool has[4] = {has_b, inner, inner, has_s};
 #pragma unroll
-        for (int i = 0; i < SLOTS; ++i) { rx[i].fill(0.0f); rb[i].fill(0.0f); rs[i].fill(0.0f); rn[i].fill(0.0f); }
-        auto request = [&](int64_t m) {
+                for (int k = 0; k < 4; ++k) {
+                    if (!has[k]) continue;
 #pragma unroll
-            for (int i = 0; i < SLOTS; ++i) {
-                if (B) rb[i] = read8<T, VEC>(B + m * p.ldb, i, tid, team, p.D);
-                if (inner) {
-                    rx[i] = read8<T, VEC>(X + m * p.ldx, i, tid, team, p.D);
-                    rn[i] = read8<T, VEC>(N + m * p.lddn, i, tid, team, p.D);
+                    for (int i = 0; i < SLOTS; ++i) {
+                        const int c = column<VEC>(i, 0, tid, team);
+#pragma unroll
+                        for (int h = 0; h < PIECES; ++h)
+                            copy16(place + stage * stage_bytes + ((k * SLOTS + i) * PIECES + h) * step,
+                                   reinterpret_cast<const uint4 *>(rows[k] + (c < p.D ? c : 0)) + h, c < p.D ? 16u : 0u);
+                    }
                 }
-                if (S) rs[i] = read8<T, VEC>(S + m * p.ldds, i, tid, team, p.D);
             }
-            if (p.stats) st = make_float4(p.stats[4 * m], p.stats[4 * m + 1], p.stats[4 * m + 2], p.stats[4 * m + 3]);
+            asm volatile("cp.async.commit_group;" ::: "memory");
         };
-        if (AHEAD && first < end) request(first);
+        auto arrived = [&](uint32_t stage, int k, int i) {
+            Eight<T> e;                       // columns beyond D arrive as zeros
+#pragma unroll
+            for (int h = 0; h < PIECES; ++h)
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(e.w[4 * h]), "=r"(e.w[4 * h + 1]), "=r"(e.w[4 * h + 2]), "=r"(e.w[4 * h + 3])
+                             : "r"(place + stage * stage_bytes + ((k * SLOTS + i) * PIECES + h) * step) : "memory");
+            return e;
+        };
+        auto statistics = [&](int64_t m) {          // read a row ahead
+            if (!p.stats || m >= end) return make_float4(0.0f, 1.0f, 0.0f, 1.0f);
+            const float *at = p.stats + 4 * m;
+            return make_float4(__ldg(at), __ldg(at + 1), __ldg(at + 2), __ldg(at + 3));
+        };
+        float4 next = statistics(first);
+        uint32_t stage = 0, fill = 0;
+        if (STAGES) {
+#pragma unroll
+            for (int k = 0; k < STAGES - 1; ++k) ahead(first + k, (uint32_t)k);
+            fill = (uint32_t)(STAGES > 0 ? STAGES - 1 : 0);
+        }
         for (int64_t m = first; m < end; ++m, turn ^= 1u) {
-            if (!AHEAD) request(m);
+            const float4 st = next;
+            next = statistics(m + 1);
+            if (STAGES) {
+                ahead(m + STAGES - 1, fill);
+                fill = fill + 1 == STAGES ? 0 : fill + 1;
+                asm volatile("cp.async.wait_group %0;" ::"n"(STAGES > 0 ? STAGES - 1 : 0) : "memory");
+            }
             const float mean_b = p.post ? st.x : 0.0f, r_b = p.post ? st.y : 1.0f, mean_s = p.pre ? st.z : 0.0f, r_s = p.pre ? st.w : 1.0f;
-            float u[SLOTS][8], z[SLOTS][8], bh[SLOTS][8], v[SUMS];
+            Eight<T> rb[SLOTS];
+            float u[SLOTS][8], z[SLOTS][8], v[SUMS];
 #pragma unroll
             for (int k = 0; k < SUMS; ++k) v[k] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < SLOTS; ++i)
+            for (int i = 0; i < SLOTS; ++i) {
+                Eight<T> rx, rn, rs;
+                if (!PLAIN) { rb[i].fill(0.0f); rx.fill(0.0f); rn.fill(0.0f); rs.fill(0.0f); }
+                if (has_b) rb[i] = STAGES ? arrived(stage, 0, i) : read8<T, VEC>(B + m * p.ldb, i, tid, team, p.D);
+                if (inner) {
+                    rx = STAGES ? arrived(stage, 1, i) : read8<T, VEC>(X + m * p.ldx, i, tid, team, p.D);
+                    rn = STAGES ? arrived(stage, 2, i) : read8<T, VEC>(N + m * p.lddn, i, tid, team, p.D);
+                }
+                if (has_s) rs = STAGES ? arrived(stage, 3, i) : read8<T, VEC>(S + m * p.ldds, i, tid, team, p.D);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    bh[i][j] = PLAIN ? rb[i][j] * r_b : (rb[i][j] - mean_b) * r_b;
-                    const float y = gw[i][j] * bh[i][j], d = rn[i][j], e = d * w_pre[i][j];
-                    if (PLAIN) u[i][j] = (p.alpha * rx[i][j] + y) * r_s;
-                    else u[i][j] = (p.alpha * rx[i][j] + y + gc[i][j] - mean_s) * r_s;
-                    z[i][j] = rs[i][j] + r_s * e;
+                    const float bh = PLAIN ? rb[i][j] * r_b : (rb[i][j] - mean_b) * r_b;
+                    const float y = gw[i][j] * bh, d = rn[j], e = d * w_pre[i][j];
+                    if (PLAIN) u[i][j] = (p.alpha * rx[j] + y) * r_s;
+                    else u[i][j] = (p.alpha * rx[j] + y + gc[i][j] - mean_s) * r_s;
+                    z[i][j] = rs[j] + r_s * e;
                     v[0] += e * u[i][j];
                     v[1] += y * z[i][j];
                     v[2] += y * u[i][j];
@@ -347,7 +453,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_block_norm_backward(const NormAr
                         v[SUMS - 1] += gw[i][j];
                     }
                 }
-            if (AHEAD && m + 1 < end) request(m + 1);
+            }
+            if (STAGES) stage = stage + 1 == STAGES ? 0 : stage + 1;
             block_sums<SUMS>(v, buf[turn], warps, warp, lane);
             const float rm1 = inner ? r_s * (v[0] * p.inv_d) : 0.0f, rm2 = !PLAIN && inner && p.layer ? r_s * (v[3] * p.inv_d) : 0.0f;
             float b1 = v[1] - rm1 * v[2], b2 = 0.0f;
@@ -356,27 +463,31 @@ __global__ void __launch_bounds__(THREADS, 1) k_block_norm_backward(const NormAr
             b2 = !PLAIN && p.post && p.layer ? r_b * (b2 * p.inv_d) : 0.0f;
 #pragma unroll
             for (int i = 0; i < SLOTS; ++i) {
-                float d[8];
+                float d[8], bh[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
+                    bh[j] = PLAIN ? rb[i][j] * r_b : (rb[i][j] - mean_b) * r_b;
                     float t = z[i][j];
                     if (inner) t -= PLAIN ? rm1 * u[i][j] : rm1 * u[i][j] + rm2;
                     z[i][j] = t;
                     d[j] = p.alpha * t;
-                    sum_tb[i][j] += t * bh[i][j];
+                    sum_tb[i][j] += t * bh[j];
                     if (!PLAIN) sum_t[i][j] += t;
                 }
-                if (p.dx) write8<T, VEC>(static_cast<T *>(p.dx) + m * p.lddx, i, tid, team, p.D, d);
-                if (B && p.db) {
+                if (PLAIN || p.dx) write8<T, VEC>(static_cast<T *>(p.dx) + m * p.lddx, i, tid, team, p.D, d);
+                if (PLAIN || (B && p.db)) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         d[j] = r_b * (gw[i][j] * z[i][j]);
-                        if (p.post) d[j] -= PLAIN ? b1 * bh[i][j] : b1 * bh[i][j] + b2;
+                        if (PLAIN) d[j] -= b1 * bh[j];          // b1 = 0 without a post norm
+                        else if (p.post) d[j] -= b1 * bh[j] + b2;
                     }
                     write8<T, VEC>(static_cast<T *>(p.db) + m * p.lddb, i, tid, team, p.D, d);
                 }
             }
         }
+        if (STAGES) asm volatile("cp.async.wait_group 0;" ::: "memory");
+        // the unit's sums: the gate's gradient, and the post norm's parameters added to what earlier units of this CTA left
 #pragma unroll
         for (int i = 0; i < SLOTS; ++i) {
             Eight<T> w, c, g;
@@ -384,23 +495,17 @@ __global__ void __launch_bounds__(THREADS, 1) k_block_norm_backward(const NormAr
             float d[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                sum_pw[i][j] += g[j] * sum_tb[i][j];
-                if (!PLAIN) sum_pc[i][j] += g[j] * sum_t[i][j];
                 d[j] = w[j] * sum_tb[i][j];
                 if (!PLAIN) d[j] += c[j] * sum_t[i][j];
+                const int at = column<VEC>(i, j, tid, team);
+                if (at >= p.D) continue;
+                if (p.want & POST_W) part[2 * p.D + at] = g[j] * sum_tb[i][j] + (unit == blockIdx.x ? 0.0f : part[2 * p.D + at]);
+                if (!PLAIN && (p.want & POST_C)) part[3 * p.D + at] = g[j] * sum_t[i][j] + (unit == blockIdx.x ? 0.0f : part[3 * p.D + at]);
+                if (p.dgate && p.chunks > 1) p.part_gate[unit * p.D + at] = d[j];
             }
-            if (!p.dgate) continue;
-            if (p.chunks == 1) write8<T, VEC>(static_cast<T *>(p.dgate) + group * p.ld_dgate, i, tid, team, p.D, d);
-            else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int at = column<VEC>(i, j, tid, team);
-                    if (at < p.D) p.part_gate[unit * p.D + at] = d[j];
-                }
-            }
+            if (p.dgate && p.chunks == 1) write8<T, VEC>(static_cast<T *>(p.dgate) + group * p.ld_dgate, i, tid, team, p.D, d);
         }
     }
-    float *part = p.part + (int64_t)blockIdx.x * 4 * p.D;
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i)
 #pragma unroll
@@ -409,8 +514,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_block_norm_backward(const NormAr
             if (c >= p.D) continue;
             if (p.want & PRE_W) part[c] = sum_nw[i][j];
             if (!PLAIN && (p.want & PRE_C)) part[p.D + c] = sum_nc[i][j];
-            if (p.want & POST_W) part[2 * p.D + c] = sum_pw[i][j];
-            if (!PLAIN && (p.want & POST_C)) part[3 * p.D + c] = sum_pc[i][j];
         }
 }
 
@@ -422,7 +525,7 @@ struct JoinArgs {
     int outs[5];             // rows of out (gate rows; 1 for the parameters)
     int D;
 };
-constexpr int JOIN_LANES = 32;      // partial sums read at a time per column
+constexpr int JOIN_LANES = 8, JOIN_AHEAD = 16;      // threads per column; loads a thread has on their way
 template <typename T>
 __global__ void __launch_bounds__(32 * JOIN_LANES) k_join_columns(const JoinArgs p) {
     __shared__ float sum[JOIN_LANES][33];
@@ -436,8 +539,13 @@ __global__ void __launch_bounds__(32 * JOIN_LANES) k_join_columns(const JoinArgs
         float t = 0.0f;
         if (c < p.D) {
             const float *part = p.part[which] + o * count * pitch + c;
-#pragma unroll 4
-            for (int64_t i = ry; i < count; i += JOIN_LANES) t += part[i * pitch];
+            for (int64_t i = ry; i < count; i += JOIN_LANES * JOIN_AHEAD) {
+                float v[JOIN_AHEAD];
+#pragma unroll
+                for (int k = 0; k < JOIN_AHEAD; ++k) v[k] = i + k * JOIN_LANES < count ? part[(i + k * JOIN_LANES) * pitch] : 0.0f;
+#pragma unroll
+                for (int k = 0; k < JOIN_AHEAD; ++k) t += v[k];
+            }
         }
         sum[ry][cx] = t;
         __syncthreads();
@@ -505,7 +613,7 @@ template <typename T, bool VEC> int launch_forward(bnn_ctx *ctx, const NormArgs 
     const int slots = groups > 1024 ? 4 : (few || groups <= 32) ? 1 : groups <= 64 ? 2 : 4;
     const int team = ((groups + slots - 1) / slots + 31) & ~31;
     const dim3 grid((unsigned)a.M), block(team);
-    const bool plain = VEC && !a.layer && !a.post_c && !a.pre_c;
+    const bool plain = VEC && !a.layer && !a.post_c && !a.pre_c && a.block && a.stream && a.pre && a.normed;
 #define BNN_FORWARD(SLOTS, THREADS) BNN_CUDA_TRY(ctx, bnn_launch_dependent(plain ? k_block_norm<T, SLOTS, THREADS, VEC, VEC> : k_block_norm<T, SLOTS, THREADS, VEC, false>, \
                                                                            grid, block, 0, ctx->stream, a))
     if (slots == 1) BNN_FORWARD(1, 1024);
@@ -515,21 +623,46 @@ template <typename T, bool VEC> int launch_forward(bnn_ctx *ctx, const NormArgs 
 #undef BNN_FORWARD
     return bnn_check_launch(ctx);
 }
-int backward_slots(int64_t D) { return D <= 8192 ? 1 : D <= 16384 ? 2 : 4; }
-int backward_team(int64_t D) {
-    const int groups = (int)((D + 7) / 8), slots = backward_slots(D);
+// Backward, rows of 16-byte groups: two slots a thread (one below 257 columns), at most 256 threads up to 4096 columns, so that two
+// CTAs share an SM and one computes while the other waits at its barrier.  Other rows: one slot, more threads; their single
+// elements are not fetched ahead, and more warps cover the wait (1000 x 1011: 34 us for the whole step, 52 with two slots).
+int backward_slots(int64_t D, bool vec) {
+    if (!vec) return D <= 8192 ? 1 : D <= 16384 ? 2 : 4;
+    return D <= 256 ? 1 : D <= 16384 ? 2 : 4;
+}
+int backward_team(int64_t D, bool vec) {
+    const int groups = (int)((D + 7) / 8), slots = backward_slots(D, vec);
     return ((groups + slots - 1) / slots + 31) & ~31;
 }
 template <typename T, bool VEC> int launch_backward(bnn_ctx *ctx, const NormArgs &a, unsigned ctas) {
-    const int slots = backward_slots(a.D), team = backward_team(a.D);
-    const bool plain = VEC && !a.layer && !a.post_c && !(a.want & (PRE_C | POST_C));
+    const int slots = backward_slots(a.D, VEC), team = backward_team(a.D, VEC);
+    const bool plain = VEC && !a.layer && !a.post_c && !(a.want & (PRE_C | POST_C)) && a.block && a.pre && a.dn && a.ds && a.dx && a.db;
+    constexpr int STAGES = VEC ? (sizeof(T) == 4 ? 2 : 3) : 0, WIDE = VEC && sizeof(T) == 2 ? 2 : 0;      // rows of all four arrays that fit
     const dim3 grid(ctas), block(team);
-    if (slots == 1 && team <= 512 && plain) BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_block_norm_backward<T, 1, 512, VEC, VEC>, grid, block, 0, ctx->stream, a));
-    else if (slots == 1 && team <= 512) BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_block_norm_backward<T, 1, 512, VEC, false>, grid, block, 0, ctx->stream, a));
-    else if (slots == 1 && plain) BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_block_norm_backward<T, 1, 1024, VEC, VEC>, grid, block, 0, ctx->stream, a));
-    else if (slots == 1) BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_block_norm_backward<T, 1, 1024, VEC, false>, grid, block, 0, ctx->stream, a));
-    else if (slots == 2) BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_block_norm_backward<T, 2, 1024, VEC, false>, grid, block, 0, ctx->stream, a));
-    else BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_block_norm_backward<T, 4, 1024, VEC, false>, grid, block, 0, ctx->stream, a));
+#define BNN_BACKWARD(SLOTS, THREADS, CTAS, PLAIN, DEEP)                                                                              \
+    do {                                                                                                                             \
+        auto kernel = k_block_norm_backward<T, SLOTS, THREADS, CTAS, VEC, PLAIN, DEEP>;                                              \
+        const size_t smem = (size_t)DEEP * team * 64 * SLOTS * (sizeof(T) / 2);                                                      \
+        if (smem > 48 * 1024)                                                                                                        \
+            BNN_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));                 \
+        BNN_CUDA_TRY(ctx, bnn_launch_dependent(kernel, grid, block, smem, ctx->stream, a));                                          \
+    } while (0)
+    if constexpr (VEC) {
+        if (slots == 1 && plain) BNN_BACKWARD(1, 32, 1, true, STAGES);
+        else if (slots == 1) BNN_BACKWARD(1, 32, 1, false, STAGES);
+        else if (team <= 256 && plain) BNN_BACKWARD(2, 256, (sizeof(T) == 4 ? 1 : 2), true, STAGES);
+        else if (team <= 256) BNN_BACKWARD(2, 256, 1, false, STAGES);
+        else if (team <= 512 && plain) BNN_BACKWARD(2, 512, 1, true, WIDE);
+        else if (team <= 512) BNN_BACKWARD(2, 512, 1, false, WIDE);
+        else if (slots == 2) BNN_BACKWARD(2, 1024, 1, false, 0);
+        else BNN_BACKWARD(4, 1024, 1, false, 0);
+    } else {
+        if (slots == 1 && team <= 512) BNN_BACKWARD(1, 512, 1, false, 0);
+        else if (slots == 1) BNN_BACKWARD(1, 1024, 1, false, 0);
+        else if (slots == 2) BNN_BACKWARD(2, 1024, 1, false, 0);
+        else BNN_BACKWARD(4, 1024, 1, false, 0);
+    }
+#undef BNN_BACKWARD
     return bnn_check_launch(ctx);
 }
 
@@ -547,10 +680,12 @@ Division divide_rows(int64_t M, int64_t rows_per_gate, int64_t ctas) {
     d.ctas = d.units < ctas ? d.units : ctas;
     return d;
 }
-// CTAs of the backward pass: 512 threads per SM (their registers hold the column sums), at most eight CTAs.
-int64_t norm_ctas(int64_t D) {
-    const int per = 512 / backward_team(D);
-    return 148 * (per < 1 ? 1 : per > 8 ? 8 : per);
+// CTAs of the backward pass: 512 threads per SM (their registers hold the column sums), at most sixteen CTAs; at least two rows
+// each, or joining the partial sums takes longer than making them.
+int64_t norm_ctas(int64_t D, int64_t M, bool vec) {
+    const int per = 512 / backward_team(D, vec);
+    const int64_t most = 148 * (per < 1 ? 1 : per > 16 ? 16 : per), rows = (M + 1) / 2;
+    return rows < most ? rows : most;
 }
 size_t norm_part_floats(const Division &d, int64_t D) { return (size_t)d.ctas * 4 * D + (d.chunks > 1 ? (size_t)d.units * D : 0); }
 
@@ -587,7 +722,12 @@ extern "C" int bnn_block_norm(bnn_ctx *ctx, const bnn_block_norm_desc *norm, con
 
 extern "C" size_t bnn_block_norm_workspace_bytes(const bnn_block_norm_desc *norm, int64_t M) {
     if (check_norm(norm, M) || M == 0) return 0;
-    return (norm_part_floats(divide_rows(M, norm->gate ? norm->rows_per_gate : M, norm_ctas(norm->D)), norm->D) * 4 + 255) & ~size_t(255);
+    size_t most = 0;                         // of both kinds of rows
+    for (int vec = 0; vec < 2; ++vec) {
+        const size_t n = norm_part_floats(divide_rows(M, norm->gate ? norm->rows_per_gate : M, norm_ctas(norm->D, M, vec != 0)), norm->D);
+        if (n > most) most = n;
+    }
+    return (most * 4 + 255) & ~size_t(255);
 }
 
 extern "C" int bnn_block_norm_backward(bnn_ctx *ctx, const bnn_block_norm_desc *norm, const void *dstream, int64_t ldds, const void *dnormed,
@@ -624,13 +764,13 @@ extern "C" int bnn_block_norm_backward(bnn_ctx *ctx, const bnn_block_norm_desc *
     a.ds = dstream; a.ldds = ldds; a.dn = dnormed; a.lddn = lddn;
     a.dx = g->dx; a.lddx = g->lddx; a.db = g->dblock; a.lddb = g->lddb; a.dgate = g->dgate; a.ld_dgate = g->ld_dgate;
     for (int k = 0; k < 4; ++k) a.want |= sums[k] ? (1 << k) : 0;
-    const Division d = divide_rows(M, a.rows_per_gate, norm_ctas(norm->D));
+    const bool vec = norm_vec(norm, M, a);
+    const Division d = divide_rows(M, a.rows_per_gate, norm_ctas(norm->D, M, vec));
     a.groups = d.groups; a.chunks = d.chunks; a.chunk_rows = d.chunk_rows; a.units = d.units;
     const bool joins = a.want || (a.dgate && d.chunks > 1);
     if (joins && (!ctx->ws || ctx->ws_bytes < norm_part_floats(d, norm->D) * 4)) return BNN_ERR_WORKSPACE;
     a.part = static_cast<float *>(ctx->ws);
     a.part_gate = a.part + (size_t)d.ctas * 4 * norm->D;
-    const bool vec = norm_vec(norm, M, a);
     const unsigned ctas = (unsigned)d.ctas;
     int st;
     if (norm->dtype == BNN_F32) st = vec ? launch_backward<float, true>(ctx, a, ctas) : launch_backward<float, false>(ctx, a, ctas);
