@@ -50,18 +50,50 @@ __device__ __forceinline__ void gated8(int act, const float (&d)[8], float (&a)[
     }
 }
 
-// Copies a matrix whose rows are not whole 16-byte groups to one whose rows are: what TMA can read.  Streaming, both sides coalesced.
-__global__ void __launch_bounds__(256) k_repitch(const uint16_t *__restrict__ src, int64_t ld, uint16_t *__restrict__ dst, int64_t pitch,
-                                                 int64_t rows, int64_t cols) {
+// Copies matrices whose rows are not whole 16-byte groups to ones whose rows are: what TMA can read.  Bound: HBM.  One thread per 16
+// bytes written: it reads the one or two aligned 16-byte groups that hold them and shifts (single elements at the very ends of the
+// matrix, where a group would reach outside).  The copied row's padding up to a whole group is written as zero.
+struct RepitchArgs {
+    const uint16_t *src[3];
+    uint16_t *dst[3];
+    int64_t ld[3], pitch[3], rows[3], cols[3];
+    int64_t groups[3];            // per row
+    int64_t first[4];             // first group of each matrix in the launch's numbering
+    int count;
+};
+__global__ void __launch_bounds__(256) k_repitch(const __grid_constant__ RepitchArgs p) {
     bnn_pdl_wait();
     bnn_pdl_launch_next();
-    for (int64_t m = blockIdx.y; m < rows; m += gridDim.y) {
-        const int64_t c0 = (int64_t)blockIdx.x * 2048 + threadIdx.x;
+    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < p.first[p.count]; t += (int64_t)gridDim.x * 256) {
+        int i = 0;
+        while (i + 1 < p.count && t >= p.first[i + 1]) ++i;
+        const int64_t at = t - p.first[i], gpr = p.groups[i];
+        const int64_t m = p.first[p.count] <= 0xffffffffll ? (int64_t)((uint32_t)at / (uint32_t)gpr) : at / gpr, c = (at - m * gpr) * 8;
+        const uint16_t *from = p.src[i] + m * p.ld[i] + c;
+        const int n = (int)(p.cols[i] - c < 8 ? p.cols[i] - c : 8);
+        const uintptr_t begin = reinterpret_cast<uintptr_t>(from), low = begin & ~uintptr_t(15), high = (begin + 2 * n - 1) & ~uintptr_t(15);
+        const uintptr_t matrix = reinterpret_cast<uintptr_t>(p.src[i]), limit = reinterpret_cast<uintptr_t>(p.src[i] + (p.rows[i] - 1) * p.ld[i] + p.cols[i]);
+        uint32_t w[4] = {0u, 0u, 0u, 0u};
+        if (low >= matrix && high + 16 <= limit) {
+            const uint4 a = *reinterpret_cast<const uint4 *>(low), b = high > low ? *reinterpret_cast<const uint4 *>(high) : make_uint4(0u, 0u, 0u, 0u);
+            const uint32_t v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            const uint32_t skip = (uint32_t)(begin - low) >> 1, word = skip >> 1, half = (skip & 1) * 16;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int64_t c = c0 + i * 256;
-            if (c < cols) dst[m * pitch + c] = src[m * ld + c];
+            for (int k = 0; k < 4; ++k) {
+                uint32_t lo = 0u, hi = 0u;
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+                    if (word == (uint32_t)s) { lo = v[k + s]; hi = k + s + 1 < 8 ? v[k + s + 1] : 0u; }
+                w[k] = __funnelshift_r(lo, hi, half);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] &= 2 * k + 1 < n ? 0xffffffffu : 2 * k < n ? 0xffffu : 0u;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k < n) w[k >> 1] |= (uint32_t)from[k] << (16 * (k & 1));
         }
+        *reinterpret_cast<uint4 *>(p.dst[i] + m * p.pitch[i] + c) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 
@@ -226,21 +258,24 @@ struct Scratch {
     }
     bool ok() const { return used == 0 || (ctx->ws && ctx->ws_bytes >= used); }
 };
-// An operand as TMA can read it: itself, or room for its copy (made by `copy` once the scratch is known to suffice).
+// Operands as TMA can read them: themselves, or copies in the scratch (made by `copy`, in one launch, once the scratch is known to suffice).
 struct Readable {
-    BnnOperand use;
-    const void *src = nullptr;
-    int64_t ld = 0, rows = 0, cols = 0;
-    Readable(Scratch &s, const void *p, int64_t ld_, int64_t rows_, int64_t cols_) : use{p, ld_} {
-        if (rows_ == 0 || cols_ == 0 || bnn_rows16(p, ld_, rows_, 2)) return;
-        src = p; ld = ld_; rows = rows_; cols = cols_;
-        use = {s.take(dz_bytes(rows, cols)), pitch16(cols)};
+    Scratch &scratch;
+    RepitchArgs r{};
+    explicit Readable(Scratch &s) : scratch(s) {}
+    BnnOperand operator()(const void *p, int64_t ld, int64_t rows, int64_t cols) {
+        if (rows == 0 || cols == 0 || bnn_rows16(p, ld, rows, 2)) return {p, ld};
+        const int i = r.count++;
+        r.src[i] = static_cast<const uint16_t *>(p); r.ld[i] = rows > 1 ? ld : cols; r.rows[i] = rows; r.cols[i] = cols;
+        r.dst[i] = reinterpret_cast<uint16_t *>(scratch.take(dz_bytes(rows, cols))); r.pitch[i] = pitch16(cols);
+        r.groups[i] = r.pitch[i] / 8;
+        r.first[i + 1] = r.first[i] + rows * r.groups[i];
+        return {r.dst[i], r.pitch[i]};
     }
-    int copy(bnn_ctx *ctx) const {
-        if (!src) return BNN_OK;
-        const dim3 grid((unsigned)((cols + 2047) / 2048), (unsigned)(rows < 65535 ? rows : 65535));
-        BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_repitch, grid, dim3(256), 0, ctx->stream, static_cast<const uint16_t *>(src), ld,
-                                               static_cast<uint16_t *>(const_cast<void *>(use.p)), use.ld, rows, cols));
+    int copy(bnn_ctx *ctx) {
+        if (!r.count) return BNN_OK;
+        const int64_t blocks = (r.first[r.count] + 255) / 256, most = 148 * 8 * 4;
+        BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_repitch, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, ctx->stream, r));
         return bnn_check_launch(ctx);
     }
 };
@@ -284,13 +319,13 @@ extern "C" int bnn_linear(bnn_ctx *ctx, const bnn_linear_desc *l, const void *x,
     bnn_device_guard guard(ctx);
     if (!guard.ok) return BNN_ERR_CUDA;
     Scratch scratch(ctx);
-    const Readable rx(scratch, x, ldx, M, l->K), rw(scratch, l->W, l->ldw, l->N, l->K);
+    Readable readable(scratch);
+    const BnnOperand rx = readable(x, ldx, M, l->K), rw = readable(l->W, l->ldw, l->N, l->K);
     if (!scratch.ok()) return BNN_ERR_WORKSPACE;
-    if (int st = rx.copy(ctx)) return st;
-    if (int st = rw.copy(ctx)) return st;
+    if (int st = readable.copy(ctx)) return st;
     BnnProduct p{};
     p.dtype = l->dtype; p.epilogue = BNN_EPI_LINEAR; p.pairs = 1;
-    p.a[0] = rx.use; p.b[0] = rw.use; p.M = M; p.N = l->N; p.K = l->K;
+    p.a[0] = rx; p.b[0] = rw; p.M = M; p.N = l->N; p.K = l->K;
     p.bias = l->bias; p.add = residual; p.ld_add = ldr; p.out[0] = y; p.ldo[0] = ldy; p.pre = pre; p.ldp = ldp; p.act = l->act;
     return bnn_product(ctx, &p, 1);
 }
@@ -315,18 +350,18 @@ extern "C" int bnn_linear_backward(bnn_ctx *ctx, const bnn_linear_desc *l, const
     Scratch scratch(ctx);
     BnnOperand dz{dy, lddy};
     if (slopes) dz = {scratch.take(dz_bytes(M, l->N)), pitch16(l->N)};
-    const Readable rz(scratch, dz.p, dz.ld, products && !slopes ? M : 0, l->N);
-    const Readable rx(scratch, x, ldx, dW || again ? M : 0, l->K), rw(scratch, l->W, l->ldw, dx || again ? l->N : 0, l->K);
+    Readable readable(scratch);
+    const BnnOperand rz = readable(dz.p, dz.ld, products && !slopes ? M : 0, l->N), rx = readable(x, ldx, dW || again ? M : 0, l->K),
+                     rw = readable(l->W, l->ldw, dx || again ? l->N : 0, l->K);
     const int64_t chunks = sums ? sum_chunks(M, l->N) : 0;
     float *part = chunks > 1 ? reinterpret_cast<float *>(scratch.take(sums_bytes(M, l->N))) : nullptr;
     if (!scratch.ok()) return BNN_ERR_WORKSPACE;
-    for (const Readable *r : {&rz, &rx, &rw})
-        if (int st = r->copy(ctx)) return st;
+    if (int st = readable.copy(ctx)) return st;
     BnnProduct p{};
     p.dtype = l->dtype; p.pairs = 1;
     if (again) {
         p.epilogue = BNN_EPI_LINEAR_BACK;
-        p.a[0] = rx.use; p.b[0] = rw.use; p.M = M; p.N = l->N; p.K = l->K;
+        p.a[0] = rx; p.b[0] = rw; p.M = M; p.N = l->N; p.K = l->K;
         p.bias = l->bias; p.add = dy; p.ld_add = lddy; p.out[0] = const_cast<void *>(dz.p); p.ldo[0] = dz.ld; p.act = l->act;
         if (int st = bnn_product(ctx, &p, 1)) return st;
     }
@@ -346,17 +381,17 @@ extern "C" int bnn_linear_backward(bnn_ctx *ctx, const bnn_linear_desc *l, const
         if (part)
             if (int st = bnn_join_columns(ctx, l->dtype, part, l->N, chunks, dbias, l->N)) return st;
     }
-    const BnnOperand z = slopes ? dz : rz.use;
+    const BnnOperand z = slopes ? dz : rz;
     BnnProduct g[2] = {};
     int n = 0;
     if (M > 0 && l->K > 0) {
         BnnProduct &d = g[n++];
-        d.a[0] = z; d.b[0] = rw.use; d.b_mn = 1;
+        d.a[0] = z; d.b[0] = rw; d.b_mn = 1;
         d.M = M; d.N = l->K; d.K = l->N; d.out[0] = dx; d.ldo[0] = lddx;
     }
     if (l->N > 0 && l->K > 0) {
         BnnProduct &d = g[n++];
-        d.a[0] = z; d.b[0] = rx.use; d.a_mn = d.b_mn = 1;
+        d.a[0] = z; d.b[0] = rx; d.a_mn = d.b_mn = 1;
         d.M = l->N; d.N = l->K; d.K = M; d.out[0] = dW; d.ldo[0] = lddw;
     }
     return gradients(ctx, l->dtype, g, n);
@@ -378,13 +413,13 @@ extern "C" int bnn_gated(bnn_ctx *ctx, const bnn_gated_desc *l, const void *x, i
     bnn_device_guard guard(ctx);
     if (!guard.ok) return BNN_ERR_CUDA;
     Scratch scratch(ctx);
-    const Readable rx(scratch, x, ldx, M, l->K), rg(scratch, l->Wg, l->ldg, l->N, l->K), ru(scratch, l->Wu, l->ldu, l->N, l->K);
+    Readable readable(scratch);
+    const BnnOperand rx = readable(x, ldx, M, l->K), rg = readable(l->Wg, l->ldg, l->N, l->K), ru = readable(l->Wu, l->ldu, l->N, l->K);
     if (!scratch.ok()) return BNN_ERR_WORKSPACE;
-    for (const Readable *r : {&rx, &rg, &ru})
-        if (int st = r->copy(ctx)) return st;
+    if (int st = readable.copy(ctx)) return st;
     BnnProduct p{};
     p.dtype = l->dtype; p.epilogue = BNN_EPI_GATED; p.pairs = 1;
-    p.a[0] = rx.use; p.b[0] = rg.use; p.b[1] = ru.use; p.M = M; p.N = l->N; p.K = l->K;
+    p.a[0] = rx; p.b[0] = rg; p.b[1] = ru; p.M = M; p.N = l->N; p.K = l->K;
     p.out[0] = h; p.ldo[0] = ldh; p.pre = pre; p.ldp = ldp; p.act = l->act;
     return bnn_product(ctx, &p, 1);
 }
@@ -406,16 +441,16 @@ extern "C" int bnn_gated_backward(bnn_ctx *ctx, const bnn_gated_desc *l, const v
     Scratch scratch(ctx);
     const int64_t ldd = pitch16(l->N);
     void *dg = scratch.take(dz_bytes(M, l->N)), *du = scratch.take(dz_bytes(M, l->N));
-    const Readable rx(scratch, x, ldx, dWg || dWu || again ? M : 0, l->K);
-    const Readable rg(scratch, l->Wg, l->ldg, dx || again ? l->N : 0, l->K), ru(scratch, l->Wu, l->ldu, dx || again ? l->N : 0, l->K);
+    Readable readable(scratch);
+    const BnnOperand rx = readable(x, ldx, dWg || dWu || again ? M : 0, l->K), rg = readable(l->Wg, l->ldg, dx || again ? l->N : 0, l->K),
+                     ru = readable(l->Wu, l->ldu, dx || again ? l->N : 0, l->K);
     if (!scratch.ok()) return BNN_ERR_WORKSPACE;
-    for (const Readable *r : {&rx, &rg, &ru})
-        if (int st = r->copy(ctx)) return st;
+    if (int st = readable.copy(ctx)) return st;
     BnnProduct p{};
     p.dtype = l->dtype; p.pairs = 1;
     if (again) {
         p.epilogue = BNN_EPI_GATED_BACK;
-        p.a[0] = rx.use; p.b[0] = rg.use; p.b[1] = ru.use; p.M = M; p.N = l->N; p.K = l->K;
+        p.a[0] = rx; p.b[0] = rg; p.b[1] = ru; p.M = M; p.N = l->N; p.K = l->K;
         p.add = dh; p.ld_add = lddh; p.out[0] = dg; p.out[1] = du; p.ldo[0] = p.ldo[1] = ldd; p.act = l->act;
         if (int st = bnn_product(ctx, &p, 1)) return st;
     } else if (some) {
@@ -432,7 +467,7 @@ extern "C" int bnn_gated_backward(bnn_ctx *ctx, const bnn_gated_desc *l, const v
     int n = 0;
     if (M > 0 && l->K > 0) {
         BnnProduct &d = g[n++];
-        d.a[0] = {dg, ldd}; d.a[1] = {du, ldd}; d.b[0] = rg.use; d.b[1] = ru.use; d.b_mn = 1; d.pairs = 2;
+        d.a[0] = {dg, ldd}; d.a[1] = {du, ldd}; d.b[0] = rg; d.b[1] = ru; d.b_mn = 1; d.pairs = 2;
         d.M = M; d.N = l->K; d.K = l->N; d.out[0] = dx; d.ldo[0] = lddx;
     }
     void *const dw[2] = {dWg, dWu};
@@ -440,7 +475,7 @@ extern "C" int bnn_gated_backward(bnn_ctx *ctx, const bnn_gated_desc *l, const v
     for (int k = 0; k < 2; ++k) {
         if (l->N == 0 || l->K == 0) continue;
         BnnProduct &d = g[n++];
-        d.a[0] = {k ? du : dg, ldd}; d.b[0] = rx.use; d.a_mn = d.b_mn = 1;
+        d.a[0] = {k ? du : dg, ldd}; d.b[0] = rx; d.a_mn = d.b_mn = 1;
         d.M = l->N; d.N = l->K; d.K = M; d.out[0] = dw[k]; d.ldo[0] = ldw[k];
     }
     return gradients(ctx, l->dtype, g, n);

@@ -624,6 +624,14 @@ template <bool W_MN, bool T_MN, int EPI> __global__ void __launch_bounds__(FEW_T
             mma_commit(&ctl->acc_full);
         }
     }
+    if (warp >= 2) {                                              // what this thread's first outputs will need from memory is brought to L2 meanwhile
+        const int i = (int)threadIdx.x + FEW_THREADS * (int)rank, t = i / (ROWS / 4), row = (i - t * (ROWS / 4)) * 4;
+        if (t0 + t < q.M && n0 + row < q.N && t < f.tokens) {
+            const uint16_t *add = static_cast<const uint16_t *>(p.add) + (t0 + t) * p.ld_add + n0 + row;
+            if (EPI != BNN_EPI_GATED && p.add) asm volatile("prefetch.global.L2 [%0];" ::"l"(add));
+            if (!GATED && p.bias) asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint16_t *>(p.bias) + n0 + row));
+        }
+    }
     // The partial tile as part[token][row]: the ring is drained by now and its memory is free.  The MMAs issued before a failure end
     // before tensor memory is given back, hence a wait that does not look at the failure word.
     float *part = reinterpret_cast<float *>(tiles);
