@@ -429,11 +429,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_produc
 // Few output rows (tokens): k_product_few.  The roles are swapped -- 128 weight rows are the M side of the tensor-core tile and the
 // tokens, 16 to 256 of them, its N side -- so a single token costs a tile of 16 columns and not of 256 rows, and every SM streams
 // weights.  Bound: the weights' bytes (HBM).  The sum is split over the CTAs of a cluster when there are too few tiles of
-// weight rows to keep every SM loading: each takes a share of the K steps, leaves its partial tile in its shared memory, and after a
-// cluster barrier every CTA adds up and finishes its part of the tile through distributed shared memory, in the order of the ranks:
-// one launch, no workspace, the same bits every time.
+// weight rows to keep every SM loading: each takes a share of the K steps, stores its partial tile into the shared memory of the CTAs
+// that finish it (distributed shared memory, a share of the rows each), and after a cluster barrier every CTA adds up the parts of its
+// share in the order of the ranks: one launch, no workspace, the same bits every time.  (Reading the parts from the other CTAs
+// instead cost a remote access's latency per pass: 4096 x 4096, 256 rows, 17.9 us.)
 // Gated projections: 64 gate rows and the up rows of the same 64 hidden units form the 128 rows of a tile.
-//   warps 0 and 11  TMA producers, warp 1  MMA issuer (cta_group::1), warps 2 .. 9  tensor memory -> shared memory, all warps  sum and epilogue
+//   warps 0 and 11  TMA producers, warp 1  MMA issuer (cta_group::1), warps 2 .. 9  partial tile to its finishers, all warps  sum and epilogue
 constexpr int FEW_SMEM = 200 * 1024;
 constexpr int FEW_THREADS = 384;
 constexpr int FEW_STAGES = 12;
@@ -462,26 +463,19 @@ __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint
 __device__ __forceinline__ void mma_commit(uint64_t *bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
-__device__ __forceinline__ float4 cluster_load4(uint32_t addr, uint32_t rank) {
+__device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {
     uint32_t remote;
-    float4 v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(remote) : "memory");
-    return v;
+    return remote;
 }
-// The sum of four neighbouring values of all partial tiles, in the order of the ranks; every load is on its way before the first is used.
-__device__ __forceinline__ void sum_parts(const float *at, uint32_t split, float (&v)[4]) {
-    float4 r[8];
-    if (split == 1) r[0] = *reinterpret_cast<const float4 *>(at);
-    else {
-#pragma unroll
-        for (uint32_t i = 0; i < 8; ++i)
-            if (i < split) r[i] = cluster_load4(smem_u32(at), i);
+// The sum of four neighbouring values over the ranks' parts, in the order of the ranks, `pitch` floats apart.
+__device__ __forceinline__ void sum_parts(const float *at, int split, int pitch, float (&v)[4]) {
+    float4 t = *reinterpret_cast<const float4 *>(at);
+    for (int i = 1; i < split; ++i) {
+        const float4 r = *reinterpret_cast<const float4 *>(at + i * pitch);
+        t.x += r.x; t.y += r.y; t.z += r.z; t.w += r.w;
     }
-    v[0] = r[0].x; v[1] = r[0].y; v[2] = r[0].z; v[3] = r[0].w;
-#pragma unroll
-    for (uint32_t i = 1; i < 8; ++i)
-        if (i < split) { v[0] += r[i].x; v[1] += r[i].y; v[2] += r[i].z; v[3] += r[i].w; }
+    v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
 }
 
 // Four neighbouring outputs of one token, n of them inside; vec: on 8-byte (pre: 16-byte) boundaries.
@@ -624,60 +618,70 @@ template <bool W_MN, bool T_MN, int EPI> __global__ void __launch_bounds__(FEW_T
             mma_commit(&ctl->acc_full);
         }
     }
-    if (warp >= 2) {                                              // what this thread's first outputs will need from memory is brought to L2 meanwhile
-        const int i = (int)threadIdx.x + FEW_THREADS * (int)rank, t = i / (ROWS / 4), row = (i - t * (ROWS / 4)) * 4;
-        if (t0 + t < q.M && n0 + row < q.N && t < f.tokens) {
-            const uint16_t *add = static_cast<const uint16_t *>(p.add) + (t0 + t) * p.ld_add + n0 + row;
+    // Rank r finishes the tile's outputs r * OUT .. r * OUT + OUT - 1 of every token.  A lane of warps 2 .. 9 holds one weight row of the
+    // partial tile and stores it where it is needed: parts[rank it comes from][token][row of the finishing rank's share], the gate rows of
+    // a share before its up rows, in the finishing CTA's ring, which is free once all MMAs of the cluster are done (first barrier).
+    const int log = split == 8 ? 3 : (int)split >> 1, out = ROWS >> log, share = 128 >> log, pitch = f.tokens * share;
+    float *parts = reinterpret_cast<float *>(tiles);
+    const int valid = (int)(q.M - t0 < f.tokens ? q.M - t0 : f.tokens);
+    {                                                             // what this thread's first outputs will need from memory is brought to L2
+        const int t = (int)threadIdx.x / (out / 4);
+        const int64_t n = n0 + (int)rank * out + ((int)threadIdx.x - t * (out / 4)) * 4;
+        if (t < valid && n < q.N) {
+            const uint16_t *add = static_cast<const uint16_t *>(p.add) + (t0 + t) * p.ld_add + n;
             if (EPI != BNN_EPI_GATED && p.add) asm volatile("prefetch.global.L2 [%0];" ::"l"(add));
-            if (!GATED && p.bias) asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint16_t *>(p.bias) + n0 + row));
+            if (!GATED && p.bias) asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint16_t *>(p.bias) + n));
         }
     }
-    // The partial tile as part[token][row]: the ring is drained by now and its memory is free.  The MMAs issued before a failure end
-    // before tensor memory is given back, hence a wait that does not look at the failure word.
-    float *part = reinterpret_cast<float *>(tiles);
+    bool done = false;
     if (warp >= 2 && warp < 10) {
-        const bool done = wait(ctl, 2 * p.wait_ns, &ctl->acc_full, 0, false);
+        // the MMAs issued before a failure end before tensor memory is given back: a wait that does not look at the failure word
+        done = wait(ctl, 2 * p.wait_ns, &ctl->acc_full, 0, false);
         if (!done) few_fail(ctl, 23);
+    }
+    __syncwarp();
+    if (split > 1) cluster_sync_all();
+    else __syncthreads();
+    if (done && *reinterpret_cast<volatile uint32_t *>(&ctl->failed) == 0u) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        if (done && *reinterpret_cast<volatile uint32_t *>(&ctl->failed) == 0u) {
-            const int quad = warp & 3, row = 32 * quad + lane;
-            for (int c = warp < 6 ? 0 : 16; c < f.tokens; c += 32) {
-                if (t0 + c >= q.M) break;
-                uint32_t r[16];
-                asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                             : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-                               "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-                             : "r"(tmem_base + ((uint32_t)(32 * quad) << 16) + c) : "memory");
-                asm volatile("tcgen05.wait::ld.sync.aligned;"
-                             : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
-                               "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
+        const int quad = warp & 3, row = 32 * quad + lane, unit = GATED ? row & 63 : row, owner = unit / out;
+        const int place = unit - owner * out + (GATED && row >= 64 ? out : 0);
+        const uint32_t to = in_cta(smem_u32(parts + (int)rank * pitch + place), (uint32_t)owner);
+        for (int c = warp < 6 ? 0 : 16; c < f.tokens; c += 32) {
+            if (c >= valid) break;
+            uint32_t r[16];
+            asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                           "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                         : "r"(tmem_base + ((uint32_t)(32 * quad) << 16) + c) : "memory");
+            asm volatile("tcgen05.wait::ld.sync.aligned;"
+                         : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                           "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
 #pragma unroll
-                for (int j = 0; j < 16; ++j) part[(c + j) * 128 + row] = last > first ? __uint_as_float(r[j]) : 0.0f;
-            }
+            for (int j = 0; j < 16; ++j)
+                if (c + j < valid)
+                    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to + (uint32_t)((c + j) * share) * 4), "r"(last > first ? r[j] : 0u) : "memory");
         }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
+    __syncwarp();
+    if (split > 1) cluster_sync_all();
+    else __syncthreads();
     if (warp == 1) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(f.tmem_cols) : "memory");
     }
-    if (split > 1) cluster_sync_all();
-    const bool failed = *reinterpret_cast<volatile uint32_t *>(&ctl->failed) != 0u;
-    if (!failed) {
-        const int valid = (int)(q.M - t0 < f.tokens ? q.M - t0 : f.tokens), rows = (int)(q.N - n0 < ROWS ? q.N - n0 : ROWS);
-        for (int i = threadIdx.x + FEW_THREADS * (int)rank; i < valid * (ROWS / 4); i += FEW_THREADS * (int)split) {
-            const int t = i / (ROWS / 4), row = (i - t * (ROWS / 4)) * 4;
-            if (row >= rows) continue;
-            float a[4], b[4];
-            sum_parts(part + t * 128 + row, split, a);
-            if (GATED) sum_parts(part + t * 128 + 64 + row, split, b);
-            if (p.f16) finish4<EPI, __half>(p, q, t0 + t, n0 + row, a, b);
-            else finish4<EPI, __nv_bfloat16>(p, q, t0 + t, n0 + row, a, b);
-        }
+    if (*reinterpret_cast<volatile uint32_t *>(&ctl->failed) != 0u) return;
+    for (int i = threadIdx.x; i < valid * (out / 4); i += FEW_THREADS) {
+        const int t = i / (out / 4), row = (i - t * (out / 4)) * 4;
+        const int64_t n = n0 + (int)rank * out + row;
+        if (n >= q.N) continue;
+        float a[4], b[4];
+        sum_parts(parts + t * share + row, (int)split, pitch, a);
+        if (GATED) sum_parts(parts + t * share + out + row, (int)split, pitch, b);
+        if (p.f16) finish4<EPI, __half>(p, q, t0 + t, n, a, b);
+        else finish4<EPI, __nv_bfloat16>(p, q, t0 + t, n, a, b);
     }
-    __syncwarp();
-    if (split > 1) cluster_sync_all();                            // nobody leaves while others still read its partial tile
 }
 
 // ---------------------------------------------------------------------------------------------------------
