@@ -61,6 +61,11 @@ struct RepitchArgs {
     int64_t first[4];             // first group of each matrix in the launch's numbering
     int count;
 };
+template <int WORD> __device__ __forceinline__ void shifted(const uint4 &a, const uint4 &b, uint32_t half, uint32_t (&w)[4]) {
+    const uint32_t v[9] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, 0u};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(v[k + WORD], v[k + WORD + 1], half);
+}
 __global__ void __launch_bounds__(256) k_repitch(const __grid_constant__ RepitchArgs p) {
     bnn_pdl_wait();
     bnn_pdl_launch_next();
@@ -75,17 +80,15 @@ __global__ void __launch_bounds__(256) k_repitch(const __grid_constant__ Repitch
         const uintptr_t matrix = reinterpret_cast<uintptr_t>(p.src[i]), limit = reinterpret_cast<uintptr_t>(p.src[i] + (p.rows[i] - 1) * p.ld[i] + p.cols[i]);
         uint32_t w[4] = {0u, 0u, 0u, 0u};
         if (low >= matrix && high + 16 <= limit) {
-            const uint4 a = *reinterpret_cast<const uint4 *>(low), b = high > low ? *reinterpret_cast<const uint4 *>(high) : make_uint4(0u, 0u, 0u, 0u);
-            const uint32_t v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-            const uint32_t skip = (uint32_t)(begin - low) >> 1, word = skip >> 1, half = (skip & 1) * 16;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                uint32_t lo = 0u, hi = 0u;
-#pragma unroll
-                for (int s = 0; s < 4; ++s)
-                    if (word == (uint32_t)s) { lo = v[k + s]; hi = k + s + 1 < 8 ? v[k + s + 1] : 0u; }
-                w[k] = __funnelshift_r(lo, hi, half);
+            const uint4 a = *reinterpret_cast<const uint4 *>(low), b = *reinterpret_cast<const uint4 *>(high);
+            const uint32_t skip = (uint32_t)(begin - low) >> 1, half = (skip & 1) * 16;
+            switch (skip >> 1) {                      // the same for a whole row
+                case 0: shifted<0>(a, b, half, w); break;
+                case 1: shifted<1>(a, b, half, w); break;
+                case 2: shifted<2>(a, b, half, w); break;
+                default: shifted<3>(a, b, half, w); break;
             }
+            if (n < 8)
 #pragma unroll
             for (int k = 0; k < 4; ++k) w[k] &= 2 * k + 1 < n ? 0xffffffffu : 2 * k < n ? 0xffffu : 0u;
         } else {
