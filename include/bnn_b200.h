@@ -311,10 +311,10 @@ BNN_API int bnn_mlp_forward_host(bnn_ctx *ctx, const bnn_mlp_desc *m, const uint
  * Runs on the context's stream and synchronises it; the three results are host doubles. */
 BNN_API int bnn_measure_pipe_rates(bnn_ctx *ctx, void *scratch, size_t scratch_bytes, double *popc_per_clk_per_sm,
                                    double *lop3_per_clk_per_sm, double *xor_popc_add_per_clk_per_sm);
-/* Name and tile shape of the tensor-core kernel this context launched last ("" if none yet): lets a benchmark label its
+/* Name and tile shape of the binary engine's tensor-core kernel this context launched last ("" if none yet): lets a benchmark label its
  * numbers with what actually ran.  The string is owned by the context and valid until its next call. */
 BNN_API const char *bnn_last_tensor_kernel(const bnn_ctx *ctx);
-/* The SM clock the tensor-core kernel launched last on this device really ran at, and how long its first CTA lived:
+/* The SM clock the binary engine's tensor-core kernel launched last on this device really ran at, and how long its first CTA lived:
  * the kernel's CTA 0 reads the SM cycle counter and the nanosecond timer when it starts and when it ends.  (This part
  * holds tensor-heavy kernels well below the maximum SM clock that nvidia-smi samples around them.)  Synchronises the
  * context's stream.  sm_mhz, microseconds: host pointers, written.  0.0 MHz if no such kernel has run. */
@@ -378,8 +378,9 @@ BNN_API int bnn_fold_batchnorm(const float *gamma, const float *beta, const floa
  *    (BNN_ERR_WORKSPACE if less is lent).  Matrix products read their operands in 16-byte groups: an operand whose base
  *    or leading dimension is not a multiple of 16 bytes is first copied to the workspace, so `aligned` = 0 asks for room
  *    for those copies; `aligned` = 1 promises that x, dy (dh) and the weights all satisfy the rule.
- *  - An output may be the very matrix that a call adds to it (y = residual, dx = dy: same pointer, same ld) but must not
- *    overlap any other input.  */
+ *  - Outputs must not overlap inputs, except where a call names a matrix that an output may be (same pointer, same ld).
+ *  - The products run on the tensor cores; their waits are bounded like those of the binary engine (bnn_set_wait_limit_ns,
+ *    bnn_device_status). */
 
 /* Activations.  htanh(z) = max(-1, min(1, z)); its slope 1 for |z| <= 1, else 0, is the straight-through estimator of Sign
  * (Section 1.3, Eq. 4-5). */
@@ -397,7 +398,7 @@ typedef struct {
 } bnn_linear_desc;
 
 /* x M x K, residual M x N or NULL, y M x N.  pre: NULL, or M x N float32 (leading dimension ldp) that receives z for
- * bnn_linear_backward.  K = 0 gives z = bias. */
+ * bnn_linear_backward.  K = 0 gives z = bias.  y may be residual. */
 BNN_API size_t bnn_linear_workspace_bytes(const bnn_linear_desc *layer, int64_t M, int backward, int aligned);
 BNN_API int bnn_linear(bnn_ctx *ctx, const bnn_linear_desc *layer, const void *x, int64_t ldx, int64_t M, const void *residual,
                        int64_t ldr, void *y, int64_t ldy, float *pre, int64_t ldp);
@@ -452,7 +453,7 @@ typedef struct {
 
 /* block NULL: no block has run yet, stream = alpha * x (post must be 0 and gate NULL).  stream and normed may be NULL if not
  * wanted (normed must be NULL when pre is 0).  stats: NULL, or M x 4 float32 (mean and reciprocal deviation of the block's row,
- * then of the stream's) for the backward call. */
+ * then of the stream's) for the backward call.  stream may be x. */
 BNN_API int bnn_block_norm(bnn_ctx *ctx, const bnn_block_norm_desc *norm, const void *x, int64_t ldx, const void *block, int64_t ldb,
                            int64_t M, void *stream, int64_t lds, void *normed, int64_t ldn, float *stats);
 
@@ -468,7 +469,7 @@ typedef struct {
     int64_t ld_dgate;
 } bnn_block_norm_grads;
 /* dstream (gradient of the stream from later in the network) and dnormed may each be NULL (zero); x, block and stats as given to
- * and left by bnn_block_norm.  M = 0 gives zero sums. */
+ * and left by bnn_block_norm.  M = 0 gives zero sums.  dx may be dstream. */
 BNN_API size_t bnn_block_norm_workspace_bytes(const bnn_block_norm_desc *norm, int64_t M);
 BNN_API int bnn_block_norm_backward(bnn_ctx *ctx, const bnn_block_norm_desc *norm, const void *dstream, int64_t ldds, const void *dnormed,
                                     int64_t lddn, const void *x, int64_t ldx, const void *block, int64_t ldb, const float *stats,
@@ -478,7 +479,7 @@ BNN_API int bnn_block_norm_backward(bnn_ctx *ctx, const bnn_block_norm_desc *nor
  * e % 4 of Philox4x32-10 (Salmon, Moraes, Dror, Shaw, 2011) at counter (e / 4 low, e / 4 high, offset low, offset high), key
  * (seed low, seed high) is >= p * 2^32 rounded to the nearest whole number.  The same call on dy without a residual is the
  * backward pass.  The mask depends on rows, cols, seed and offset only, not on strides or alignment.  Dropped elements of x are
- * not looked at: NaN or infinity there does not reach y.  0 <= p <= 1; residual may be NULL; y may be x. */
+ * not looked at: NaN or infinity there does not reach y.  0 <= p <= 1; residual may be NULL; y may be x or residual. */
 BNN_API int bnn_dropout(bnn_ctx *ctx, int dtype, const void *x, int64_t ldx, const void *residual, int64_t ldr, void *y, int64_t ldy,
                         int64_t rows, int64_t cols, double p, uint64_t seed, uint64_t offset);
 

@@ -221,7 +221,9 @@ __global__ void __launch_bounds__(256) k_gated_slopes(const GatedSlopeArgs p) {
     }
 }
 
-int64_t pitch16(int64_t n) { return (n + 7) & ~int64_t(7); }            // 16-bit rows of whole 16-byte groups
+// Pitch of 16-bit rows in the scratch: whole 128-byte lines, what one row of a TMA box reads (1000 x 1008 x 4104 with rows of 8208 bytes
+// 21 us, of whole lines 17).
+int64_t pitch16(int64_t n) { return (n + 63) & ~int64_t(63); }
 size_t round256(size_t b) { return (b + 255) & ~size_t(255); }
 
 // Rows per chunk of the column sums: about four blocks per SM; up to 256 rows one chunk, which needs no second kernel to join
@@ -271,7 +273,7 @@ struct Readable {
         const int i = r.count++;
         r.src[i] = static_cast<const uint16_t *>(p); r.ld[i] = rows > 1 ? ld : cols; r.rows[i] = rows; r.cols[i] = cols;
         r.dst[i] = reinterpret_cast<uint16_t *>(scratch.take(dz_bytes(rows, cols))); r.pitch[i] = pitch16(cols);
-        r.groups[i] = r.pitch[i] / 8;
+        r.groups[i] = (cols + 7) / 8;
         r.first[i + 1] = r.first[i] + rows * r.groups[i];
         return {r.dst[i], r.pitch[i]};
     }

@@ -413,6 +413,65 @@ def test_another_stream():
     c.close()
 
 
+@pytest.mark.parametrize("M", (3, 700), ids=("few", "pairs"))
+def test_waits_that_run_out(M):
+    """With the producers switched off every wait of the products runs out: a status, no hang, and the context works afterwards."""
+    c = binding.Context(0)
+    mk = Maker(14)
+    x, W = mk(M, 512), mk(1000, 512, scale=0.05)
+    layer, glu, dy = c.make_linear(W), c.make_gated(W, W), mk(M, 1000)
+    ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    c.set_workspace(ws)
+    c.set_wait_limit_ns(20_000_000)
+    for call in (lambda: c.linear(layer, x), lambda: c.gated(glu, x), lambda: c.linear_backward(layer, dy, x)):
+        c.debug_drop_loads(True)
+        call()
+        with pytest.raises(binding.BnnError) as e:
+            c.device_status()
+        assert e.value.status == -5
+        c.debug_drop_loads(False)
+        call()
+        c.device_status()
+    ref.check(c.linear(layer, x), *ref.linear(x, W, None, None, "none")["y"], "y after failures")
+    c.close()
+
+
+def test_captured_in_a_graph():
+    """The calls of a training step replayed from a CUDA graph give the bits of the calls themselves."""
+    side = torch.cuda.Stream()
+    c = binding.Context(0, side)
+    mk = Maker(15)
+    x, W, Wg, dy = mk(130, 256), mk(256, 640, scale=0.05), mk(640, 256, scale=0.05), mk(130, 256)
+    layer, glu, norm = c.make_linear(W), c.make_gated(Wg, Wg), c.make_block_norm(256, BF, post=True, pre_weight=mk(256, shift=1.0))
+    ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    c.set_workspace(ws)
+
+    def step():
+        pre, stats = c.empty(2, 130, 640, dtype=FF), c.empty(130, 4, dtype=FF)
+        h = c.gated(glu, x, pre=pre)
+        b = c.dropout(c.linear(layer, h), 0.25, 5)
+        s, n = c.block_norm(norm, x, b, stats=stats)
+        back = c.block_norm_backward(norm, dy, dy, x, b, stats)
+        dh, dW, _ = c.linear_backward(layer, back["dblock"], h)
+        return [s, n, back["dx"], back["dpre_weight"], dW, *c.gated_backward(glu, dh, x, pre)]
+
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        want = [t.clone() for t in step()]
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            got = step()
+        for _ in range(3):
+            for t in got:
+                t.fill_(9.0)
+            graph.replay()
+    side.synchronize()
+    c.device_status()
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+    c.close()
+
+
 def test_refusals(ctx):
     mk = Maker(2)
     x, W, b = mk(4, 64), mk(32, 64), mk(32)
