@@ -33,6 +33,7 @@ struct bnn_ctx {
         cudaError_t e__ = (call);                            \
         if (e__ != cudaSuccess) {                            \
             if (ctx) (ctx)->last_cuda_error = (int)e__;      \
+            (void)cudaGetLastError(); /* reported here: the next call starts clean */ \
             return BNN_ERR_CUDA;                             \
         }                                                    \
     } while (0)

@@ -643,7 +643,7 @@ template <typename T, bool VEC> int launch_backward(bnn_ctx *ctx, const NormArgs
     do {                                                                                                                             \
         auto kernel = k_block_norm_backward<T, SLOTS, THREADS, CTAS, VEC, PLAIN, DEEP>;                                              \
         const size_t smem = (size_t)DEEP * team * 64 * SLOTS * (sizeof(T) / 2);                                                      \
-        if (smem > 48 * 1024)                                                                                                        \
+        if (smem > 40 * 1024)      /* with the kernel's own shared memory below the 48 KB that need no opting in */                  \
             BNN_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));                 \
         BNN_CUDA_TRY(ctx, bnn_launch_dependent(kernel, grid, block, smem, ctx->stream, a));                                          \
     } while (0)

@@ -295,6 +295,30 @@ def test_block_norm(ctx, M, D, dtype, kind, post, pre, gates, alpha, weights, sh
     intact(ws, n)
 
 
+@pytest.mark.parametrize("kind,shifts", [("rms", False), ("layer", True)])
+@pytest.mark.parametrize("dtype", (BF, FF))
+@pytest.mark.parametrize("D", (8, 248, 256, 264, 504, 1000, 1952, 2048, 2056, 4088, 4096, 4104, 8192, 8200, 16384))
+def test_block_norm_of_every_team(ctx, D, dtype, kind, shifts):
+    """Widths around every change of team, slots and stages."""
+    mk = Maker(D)
+    M = 11
+    x, b, ds, dn = mk(M, D, dtype=dtype, scale=2.0), mk(M, D, dtype=dtype), mk(M, D, dtype=dtype), mk(M, D, dtype=dtype)
+    par = {"kind": kind, "eps": 1e-5, "alpha": 1.0, "post": True, "pre": True, "rows_per_gate": 6, "gate": mk(2, D, dtype=dtype, shift=0.5)}
+    par |= {k: mk(D, dtype=dtype, scale=0.2, shift=1.0) for k in ("post_weight", "pre_weight")}
+    par |= {k: mk(D, dtype=dtype, scale=0.2) if shifts else None for k in ("post_shift", "pre_shift")}
+    layer = ctx.make_block_norm(D, dtype, **par)
+    n = ctx.block_norm_workspace_bytes(layer, M)
+    ws = lend(ctx, n)
+    stats = ctx.empty(M, 4, dtype=FF)
+    want = ref.block_norm(x, b, par, ds, dn)
+    for key, t in zip(("stream", "normed"), ctx.block_norm(layer, x, b, stats=stats)):
+        ref.check(t, *want[key], key)
+    for key, t in ctx.block_norm_backward(layer, ds, dn, x, b, stats).items():
+        if t is not None:
+            ref.check(t, *want[key], key)
+    intact(ws, n)
+
+
 def test_block_norm_gradients_against_differences(ctx):
     mk = Maker(8)
     M, D = 12, 40
