@@ -10,7 +10,7 @@
 // SM, tiles in bands of eight tile rows so that the operands of the tiles in flight stay in L2.
 //   warp 0, last warp  TMA producers, K steps in turn: 64-element K slices of both operands, 128-byte swizzle, a ring of stages
 //   warp 1             MMA issuer (CTA 0 of the pair): four K = 16 MMAs per stage; tcgen05.commit frees the stage
-//   warps 2 .. 9       epilogue: two per TMEM lane quadrant, each half of the columns, one output row per thread
+//   warps 2 .. 17      epilogue: four per TMEM lane quadrant, a quarter of the columns each, one output row per thread
 // Two accumulator buffers: the epilogue of a tile runs under the MMAs of the next one.
 // Gated projections: B's two halves are the gate rows (CTA 0) and the up rows (CTA 1), so columns 0 .. BN/2 - 1 of the
 // accumulator are g and the others u of the same hidden units, and one thread holds both when it forms act(g) u.
@@ -28,7 +28,7 @@ __device__ int g_product_error;          // 0 = fine; otherwise a code saying wh
 
 constexpr int BK = 64;                   // elements of K per stage: one 128-byte row
 constexpr int TM = 256;                  // tile rows of a pair
-constexpr int EPI_WARPS = 8;
+constexpr int EPI_WARPS = 16;
 constexpr int THREADS = (2 + EPI_WARPS + 1) * 32;
 constexpr uint32_t A_STAGE = 128 * BK * 2;
 template <int BN> struct Ring {
@@ -50,7 +50,7 @@ struct Problem {
     int a_mn, b_mn;
     void *out[2];
     int64_t ldo[2];
-    int vec_out;                         // widest access that every row allows: 2 = 32 bytes, 1 = 16 bytes, 0 = one element
+    int vec_out;                         // what every row is made of: 2 = 16-byte groups, 1 = 4-byte words, 0 = elements
 };
 constexpr int PROBLEMS = 3;              // a gated layer's gradients: dx, dWg, dWu
 // What the epilogue of a single product needs beside the problem, and what every launch needs.
@@ -59,7 +59,7 @@ struct Common {
     float *pre;
     int64_t ld_add, ldp;
     int act, f16;
-    int vec_bias, vec_add, vec_pre;
+    int vec_bias, vec_add, vec_pre;      // as vec_out; vec_pre 3 = 32-byte sectors
     unsigned long long wait_ns;
     int drop_loads;                      // test hook: the producers request nothing, every consumer's wait runs out
 };
@@ -120,163 +120,280 @@ template <int WIDTH, int N> __device__ __forceinline__ Tile tile_at(const Produc
     return {i, (int)((band * BAND + w - n * high) * TM), (int)(n * WIDTH)};
 }
 
-// A warp's 32 x 32 block in memory: the lane's row starts at `row` (element n0 of it), rows are `ld` apart, `rows` x n of it
-// exist.  Rows of whole 16-byte groups are accessed by their own lane, 64 (128) bytes each.  Others go through the warp's
-// piece of shared memory, one row at a time across the lanes, so that neighbouring lanes touch neighbouring elements:
-// lane-private rows of 2-byte accesses took 40 us for a 700 x 700 output, this takes one row's transaction per instruction.
-struct Block { int rows, n; float *stage; };          // stage: 32 x 33 floats
-constexpr int STAGE_PITCH = 33;
-template <typename T> __device__ __forceinline__ void read32(const T *row, int64_t ld, int vec, const Block &k, float (&v)[32]) {
+// A warp's block of 32 rows in memory passes through its piece of shared memory (32 rows of 64 bytes: 32 16-bit or 16 float columns), so that
+// a lane computes on its own row while neighbouring lanes touch neighbouring bytes of memory.  Sixteen-byte units of a row are
+// permuted by the row, which keeps both sides free of bank conflicts.
+// vec: 2 = rows of whole 16-byte groups, 1 = of whole 4-byte words, 0 = single elements (lane-private rows of 2-byte accesses took five
+// times as long: 3644 x 6417, K = 288, 281 us).
+constexpr int PIECE = 32 * 64, BLOCK = 32, CHUNK = 16;      // columns of a block; of one pass through the registers
+__device__ __forceinline__ uint4 *unit_of(uint8_t *piece, int row, int unit) { return reinterpret_cast<uint4 *>(piece + row * 64 + ((unit ^ ((row >> 1) & 3)) << 4)); }
+template <typename W> __device__ __forceinline__ W *word_of(uint8_t *piece, int row, int word) {
+    constexpr int PER = 16 / (int)sizeof(W);
+    return reinterpret_cast<W *>(unit_of(piece, row, word / PER)) + word % PER;
+}
+// Writes a block: rows x n of its 32 x COLS elements exist, `first` is its first element.
+template <typename T, int COLS> __device__ __forceinline__ void flush(T *first, int64_t ld, int vec, int rows, int n, uint8_t *piece) {
+    constexpr int PER = 16 / (int)sizeof(T), UNITS = COLS / PER;
     const int lane = threadIdx.x & 31;
-    if (vec && k.n >= 32) {
-        if (lane < k.rows) {
+    __syncwarp();
+    if (vec == 2) {
+        const int u = lane % UNITS;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint4 w = reinterpret_cast<const uint4 *>(row)[i];
-                const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float2 f = unpack2<T>(u[j]);
-                    v[8 * i + 2 * j] = f.x; v[8 * i + 2 * j + 1] = f.y;
-                }
-            }
+        for (int i = 0; i < UNITS; ++i) {
+            const int r = i * (32 / UNITS) + lane / UNITS;
+            if (r >= rows) continue;
+            const uint4 w = *unit_of(piece, r, u);
+            T *to = first + r * ld + u * PER;
+            if ((u + 1) * PER <= n) __stcs(reinterpret_cast<uint4 *>(to), w);
+            else
+                for (int k = 0; k < n - u * PER; ++k) to[k] = *word_of<T>(piece, r, u * PER + k);
         }
-    } else {
-        const T *first = row - (int64_t)lane * ld;
-        if (lane < k.n) {
+    } else if (vec == 1) {
+        constexpr int EACH = 4 / (int)sizeof(T), WORDS = COLS / EACH;                 // words of a row
+        const int c = lane % WORDS;
 #pragma unroll 8
-            for (int r = 0; r < 32; ++r)
-                if (r < k.rows) k.stage[r * STAGE_PITCH + lane] = to_f32(first[r * ld + lane]);
-        }
-        __syncwarp();
-#pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = k.stage[lane * STAGE_PITCH + j];
-        __syncwarp();
-    }
-}
-// Results are written past the operands that the tiles in flight share in L2 (.cs: first to be evicted).
-__device__ __forceinline__ void st256(void *p, const uint32_t *w) {
-    asm volatile("st.global.cs.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
-                 ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
-}
-template <typename T> __device__ __forceinline__ void write32(T *row, int64_t ld, int vec, const Block &k, const float (&v)[32]) {
-    const int lane = threadIdx.x & 31;
-    if (vec && k.n >= 32) {
-        if (lane < k.rows) {
-            constexpr int WORDS = 8 * (int)sizeof(T);
-            uint32_t w[WORDS];
-#pragma unroll
-            for (int j = 0; j < WORDS; ++j) {
-                if constexpr (sizeof(T) == 4) w[j] = __float_as_uint(v[j]);
-                else w[j] = pack2<T>(v[2 * j], v[2 * j + 1]);
-            }
-            if (vec == 2) {
-#pragma unroll
-                for (int i = 0; i < WORDS / 8; ++i) st256(reinterpret_cast<uint32_t *>(row) + 8 * i, w + 8 * i);
-            } else {
-#pragma unroll
-                for (int i = 0; i < WORDS / 4; ++i) __stcs(reinterpret_cast<uint4 *>(row) + i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+        for (int i = 0; i < WORDS; ++i) {
+            const int r = i * (32 / WORDS) + lane / WORDS;
+            T *to = first + r * ld + c * EACH;
+            if (r < rows) {
+                if ((c + 1) * EACH <= n) __stcs(reinterpret_cast<uint32_t *>(to), *word_of<uint32_t>(piece, r, c));
+                else if (c * EACH < n) *to = *word_of<T>(piece, r, c * EACH);
             }
         }
     } else {
-        T *first = row - (int64_t)lane * ld;
-#pragma unroll
-        for (int j = 0; j < 32; ++j) k.stage[lane * STAGE_PITCH + j] = v[j];
-        __syncwarp();
-        if (lane < k.n) {
+        constexpr int PASSES = COLS;                                                   // COLS x 32 elements, 32 at a time
+        const int c = lane % COLS;
 #pragma unroll 8
-            for (int r = 0; r < 32; ++r)
-                if (r < k.rows) first[r * ld + lane] = from_f32<T>(k.stage[r * STAGE_PITCH + lane]);
+        for (int i = 0; i < PASSES; ++i) {
+            const int r = i * (32 / COLS) + lane / COLS;
+            if (r < rows && c < n) first[r * ld + c] = *word_of<T>(piece, r, c);
         }
+    }
+    __syncwarp();
+}
+// A block of 16-bit elements comes in: `request` asks for its units, `land` puts them into the piece, from where each lane takes its row.
+struct Incoming { uint4 w[4]; };
+__device__ __forceinline__ void request(Incoming &in, const uint16_t *first, int64_t ld, int rows, int n) {
+    const int lane = threadIdx.x & 31, u = lane & 3;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = i * 8 + (lane >> 2);
+        const uint16_t *from = first + r * ld + u * 8;
+        in.w[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (r >= rows) continue;
+        if ((u + 1) * 8 <= n) in.w[i] = *reinterpret_cast<const uint4 *>(from);
+        else {
+            uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (u * 8 + k < n) w[k >> 1] |= (uint32_t)from[k] << (16 * (k & 1));
+            in.w[i] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+}
+__device__ __forceinline__ void land(const Incoming &in, const uint16_t *first, int64_t ld, int vec, int rows, int n, uint8_t *piece) {
+    const int lane = threadIdx.x & 31;
+    if (vec == 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *unit_of(piece, i * 8 + (lane >> 2), lane & 3) = in.w[i];
+    } else {
+        for (int i = 0; i < 32; i += 16) {                       // sixteen rows on their way
+            uint16_t v[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) v[k] = i + k < rows && lane < n ? first[(i + k) * ld + lane] : (uint16_t)0;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) *word_of<uint16_t>(piece, i + k, lane) = v[k];
+        }
+    }
+    __syncwarp();
+}
+// Sixteen columns of the lane's row into the piece (16-bit ones from column `at` on, or floats), and out of it.
+template <typename T> __device__ __forceinline__ void put16(uint8_t *piece, int at, const float (&v)[16]) {
+    constexpr int PER = 16 / (int)sizeof(T);
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < 16 / PER; ++i) {
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if constexpr (sizeof(T) == 4) w[k] = __float_as_uint(v[4 * i + k]);
+            else w[k] = pack2<T>(v[8 * i + 2 * k], v[8 * i + 2 * k + 1]);
+        }
+        *unit_of(piece, lane, at / PER + i) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+template <typename T> __device__ __forceinline__ void get16(uint8_t *piece, int at, float (&d)[16]) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint4 w = *unit_of(piece, lane, at / 8 + i);
+        float e[8];
+        unpack8<T>(&w, e);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) d[8 * i + j] = e[j];
+    }
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait16(uint32_t (&r)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                   "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
+}
+
+template <int ACT> __device__ __forceinline__ void act16(float (&v)[16]) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[j] = act_value(ACT, v[j]);
+}
+template <int ACT> __device__ __forceinline__ void back16(const float (&d)[16], float (&a)[16]) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        float value;
+        a[j] = d[j] * act_slope(ACT, a[j], value);
+    }
+}
+template <int ACT> __device__ __forceinline__ void gated_back16(const float (&d)[16], float (&a)[16], float (&b)[16]) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        float value;
+        const float slope = act_slope(ACT, a[j], value);
+        a[j] = d[j] * b[j] * slope;
+        b[j] = d[j] * value;
+    }
+}
+// The choice of the activation is made once for sixteen values.
+#define BNN_EACH_ACT(CALL)                                        \
+    switch (p.act) {                                              \
+        case BNN_ACT_RELU: CALL(BNN_ACT_RELU); break;             \
+        case BNN_ACT_GELU: CALL(BNN_ACT_GELU); break;             \
+        case BNN_ACT_GELU_TANH: CALL(BNN_ACT_GELU_TANH); break;   \
+        case BNN_ACT_SILU: CALL(BNN_ACT_SILU); break;             \
+        case BNN_ACT_SIGMOID: CALL(BNN_ACT_SIGMOID); break;       \
+        case BNN_ACT_HTANH: CALL(BNN_ACT_HTANH); break;           \
+        default: CALL(BNN_ACT_NONE); break;                       \
+    }
+// Sixteen bias values.
+struct Bias { uint4 w[2]; };
+__device__ __forceinline__ Bias bias_of(const Common &p, int64_t n0, int n) {
+    const uint16_t *bias = static_cast<const uint16_t *>(p.bias) + n0;
+    Bias b;
+    if (p.vec_bias == 2 && n >= 16) { b.w[0] = reinterpret_cast<const uint4 *>(bias)[0]; b.w[1] = reinterpret_cast<const uint4 *>(bias)[1]; }
+    else {
+        uint32_t w[8] = {};
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (j < n) w[j >> 1] |= (uint32_t)bias[j] << (16 * (j & 1));
+        b.w[0] = make_uint4(w[0], w[1], w[2], w[3]); b.w[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+    return b;
+}
+template <typename T> __device__ __forceinline__ void add_bias16(const Bias &bias, float (&a)[16]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        float c[8];
+        unpack8<T>(&bias.w[i], c);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) a[8 * i + j] += c[j];
+    }
+}
+// Sixteen pre-activations of the lane's row, 64 bytes: directly where rows are whole 32-byte sectors (3), else through the piece.
+__device__ __forceinline__ void keep16(float *first, int64_t ld, int vec, int rows, int n, uint8_t *piece, const float (&v)[16]) {
+    const int lane = threadIdx.x & 31;
+    if (vec == 3 && n >= 16) {
+        if (lane < rows) {
+            float *to = first + lane * ld;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                asm volatile("st.global.cs.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                             ::"l"(to + 8 * i), "r"(__float_as_uint(v[8 * i])), "r"(__float_as_uint(v[8 * i + 1])), "r"(__float_as_uint(v[8 * i + 2])),
+                               "r"(__float_as_uint(v[8 * i + 3])), "r"(__float_as_uint(v[8 * i + 4])), "r"(__float_as_uint(v[8 * i + 5])),
+                               "r"(__float_as_uint(v[8 * i + 6])), "r"(__float_as_uint(v[8 * i + 7])) : "memory");
+        }
+    } else {
+        put16<float>(piece, 0, v);
+        flush<float, 16>(first, ld, vec < 2 ? vec : 2, rows, n, piece);
+    }
+}
+
+// A warp's block: 32 rows from m0 on, 32 columns from n0 on, accumulators at `acc` (and `acc2`: gated).  What is added has landed in the
+// piece; a lane takes sixteen columns of it at a time and puts the result into their place, unless the piece has to pass something
+// else on in between: the kept pre-activations (PRE: as floats) or the first of two outputs, which are then written sixteen columns at a
+// time.  In those cases the incoming values are taken before.
+template <int EPI, typename T, bool PRE>
+__device__ __forceinline__ void finish_block(const Common &p, const Problem &q, int64_t m0, int64_t n0, uint32_t acc, uint32_t acc2, uint8_t *piece) {
+    constexpr bool GATED = EPI == BNN_EPI_GATED || EPI == BNN_EPI_GATED_BACK, APART = PRE || EPI == BNN_EPI_GATED_BACK;
+    const int rows = (int)(q.M - m0 < 32 ? q.M - m0 : 32), n = (int)(q.N - n0 < BLOCK ? q.N - n0 : BLOCK);
+    T *out = static_cast<T *>(q.out[0]) + m0 * q.ldo[0] + n0;
+    const bool adds = EPI != BNN_EPI_GATED && p.add;
+    uint4 held[4];                                           // APART: the lane's row of what is added
+    if (APART && adds) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) held[i] = *unit_of(piece, threadIdx.x & 31, i);
         __syncwarp();
     }
-}
-
-template <int ACT> __device__ __forceinline__ void act32(float (&v)[32]) {
 #pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] = act_value(ACT, v[j]);
-}
-__device__ __forceinline__ void act_values(int act, float (&v)[32]) {
-    switch (act) {               // the choice is made once for 32 values
-        case BNN_ACT_RELU: act32<BNN_ACT_RELU>(v); break;
-        case BNN_ACT_GELU: act32<BNN_ACT_GELU>(v); break;
-        case BNN_ACT_GELU_TANH: act32<BNN_ACT_GELU_TANH>(v); break;
-        case BNN_ACT_SILU: act32<BNN_ACT_SILU>(v); break;
-        case BNN_ACT_SIGMOID: act32<BNN_ACT_SIGMOID>(v); break;
-        case BNN_ACT_HTANH: act32<BNN_ACT_HTANH>(v); break;
-        default: break;
-    }
-}
-
-// 32 rows x 32 columns of a warp, from accumulators to memory; m: the lane's row.  b: the second accumulator of the gated epilogues.
-template <int EPI, typename T>
-__device__ __forceinline__ void finish32(const Common &p, const Problem &q, int64_t m, int64_t n0, float *stage, float (&a)[32], float (&b)[32]) {
-    const int lane = threadIdx.x & 31;
-    const int64_t below = q.M - (m - lane);
-    const Block k{(int)(below < 32 ? below : 32), (int)(q.N - n0 < 32 ? q.N - n0 : 32), stage};
-    if (k.rows <= 0) return;
-    float d[32];
-    if constexpr (EPI == BNN_EPI_LINEAR || EPI == BNN_EPI_LINEAR_BACK) {
-        if (p.bias) {
-            const T *bias = static_cast<const T *>(p.bias) + n0;
-            if (p.vec_bias && k.n >= 32) {
+    for (int c = 0; c < BLOCK; c += CHUNK) {
+        uint32_t ra[16], rb[16];
+        float a[16], b[16], d[16];
+        const int left = n - c < CHUNK ? n - c : CHUNK;
+        if (left <= 0) break;
+        tmem_ld16(acc + c, ra);
+        if (GATED) tmem_ld16(acc2 + c, rb);
+        tmem_ld_wait16(ra);
+        if (GATED) tmem_ld_wait16(rb);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float c[8];
-                    load8(bias + 8 * i, c);
+        for (int j = 0; j < 16; ++j) {
+            a[j] = q.k_iters ? __uint_as_float(ra[j]) : 0.0f;
+            if (GATED) b[j] = q.k_iters ? __uint_as_float(rb[j]) : 0.0f;
+        }
+        if (!GATED && p.bias) add_bias16<T>(bias_of(p, n0 + c, left), a);
+        if (adds) {
+            if constexpr (APART) {
+                float e[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) a[8 * i + j] += c[j];
+                for (int i = 0; i < 2; ++i) {
+                    unpack8<T>(&held[c / 8 + i], e);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) d[8 * i + j] = e[j];
                 }
-            } else {
+            } else get16<T>(piece, c, d);
+        }
+        if constexpr (PRE) {
+            keep16(p.pre + m0 * p.ldp + n0 + c, p.ldp, p.vec_pre, rows, left, piece, a);
+            if constexpr (GATED) keep16(p.pre + (q.M + m0) * p.ldp + n0 + c, p.ldp, p.vec_pre, rows, left, piece, b);
+        }
+        if constexpr (EPI == BNN_EPI_LINEAR || EPI == BNN_EPI_GATED) {
+#define BNN_CALL(ACT) act16<ACT>(a)
+            BNN_EACH_ACT(BNN_CALL)
+#undef BNN_CALL
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (j < k.n) a[j] += to_f32(bias[j]);
+            for (int j = 0; j < 16; ++j) {
+                if (GATED) a[j] *= b[j];
+                else if (adds) a[j] += d[j];
             }
+        } else if constexpr (EPI == BNN_EPI_LINEAR_BACK) {
+#define BNN_CALL(ACT) back16<ACT>(d, a)
+            BNN_EACH_ACT(BNN_CALL)
+#undef BNN_CALL
+        } else {
+#define BNN_CALL(ACT) gated_back16<ACT>(d, a, b)
+            BNN_EACH_ACT(BNN_CALL)
+#undef BNN_CALL
+        }
+        put16<T>(piece, APART ? 0 : c, a);
+        if constexpr (APART) flush<T, 16>(out + c, q.ldo[0], q.vec_out, rows, left, piece);
+        if constexpr (EPI == BNN_EPI_GATED_BACK) {
+            put16<T>(piece, 0, b);
+            flush<T, 16>(static_cast<T *>(q.out[1]) + m0 * q.ldo[1] + n0 + c, q.ldo[1], q.vec_out, rows, left, piece);
         }
     }
-    const T *add = static_cast<const T *>(p.add) + m * p.ld_add + n0;
-    T *out = static_cast<T *>(q.out[0]) + m * q.ldo[0] + n0;
-    if constexpr (EPI == BNN_EPI_LINEAR) {
-        if (p.pre) write32(p.pre + m * p.ldp + n0, p.ldp, p.vec_pre, k, a);
-        act_values(p.act, a);
-        if (p.add) {
-            read32(add, p.ld_add, p.vec_add, k, d);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) a[j] += d[j];
-        }
-        write32(out, q.ldo[0], q.vec_out, k, a);
-    } else if constexpr (EPI == BNN_EPI_LINEAR_BACK) {
-        read32(add, p.ld_add, p.vec_add, k, d);
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            float value;
-            d[j] *= act_slope(p.act, a[j], value);
-        }
-        write32(out, q.ldo[0], q.vec_out, k, d);
-    } else if constexpr (EPI == BNN_EPI_GATED) {
-        if (p.pre) {
-            write32(p.pre + m * p.ldp + n0, p.ldp, p.vec_pre, k, a);
-            write32(p.pre + (q.M + m) * p.ldp + n0, p.ldp, p.vec_pre, k, b);
-        }
-        act_values(p.act, a);
-#pragma unroll
-        for (int j = 0; j < 32; ++j) a[j] *= b[j];
-        write32(out, q.ldo[0], q.vec_out, k, a);
-    } else {
-        read32(add, p.ld_add, p.vec_add, k, d);
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            float value;
-            const float slope = act_slope(p.act, a[j], value);
-            a[j] = d[j] * b[j] * slope;
-            b[j] = d[j] * value;
-        }
-        write32(out, q.ldo[0], q.vec_out, k, a);
-        write32(static_cast<T *>(q.out[1]) + m * q.ldo[1] + n0, q.ldo[1], q.vec_out, k, b);
-    }
+    if constexpr (!APART) flush<T, BLOCK>(out, q.ldo[0], q.vec_out, rows, n, piece);
 }
 
-template <int EPI, int BN, int N>
+template <int EPI, int BN, int N, bool PRE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_product_pair(const __grid_constant__ ProductArgs<N> p) {
     constexpr bool GATED = EPI == BNN_EPI_GATED || EPI == BNN_EPI_GATED_BACK;
     constexpr int WIDTH = GATED ? BN / 2 : BN;                   // output columns of a tile
@@ -381,34 +498,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_produc
     } else if (warp < 2 + EPI_WARPS) {
         bnn_pdl_wait();
         bnn_pdl_launch_next();
-        const int quad = warp & 3, half = (warp - 2) >> 2;
+        const int quad = warp & 3, quarter = (warp - 2) >> 2;
         const uint32_t quadrant = (uint32_t)(32 * quad) << 16;
-        float *stage = reinterpret_cast<float *>(ctl + 1) + (warp - 2) * 32 * STAGE_PITCH;
+        uint8_t *piece = reinterpret_cast<uint8_t *>(ctl + 1) + (warp - 2) * PIECE;
         uint32_t count = 0;
         for (uint32_t t = pair; t < p.tiles; t += pairs, ++count) {
             const uint32_t buf = count & 1;
             const Tile tile = tile_at<WIDTH>(p, t);
             const Problem &q = p.q[tile.problem];
+            const int64_t m0 = tile.m0 + (int)rank * 128 + 32 * quad;
+            constexpr int SHARE = WIDTH / 4 < BLOCK ? BLOCK : WIDTH / 4;       // a warp's columns of a tile (gated 128-wide tiles: two warps of four)
+            const int first = quarter * SHARE < WIDTH ? quarter * SHARE : WIDTH, last = first + SHARE < WIDTH ? first + SHARE : WIDTH;
+            const int rows = (int)(q.M - m0 < 32 ? q.M - m0 : 32);
+            // what is added (the residual, an incoming gradient) is requested a block ahead, the first one while the tile is being multiplied
+            const bool adds = EPI != BNN_EPI_GATED && p.add != nullptr;
+            const uint16_t *add = static_cast<const uint16_t *>(p.add) + m0 * p.ld_add + tile.n0;
+            Incoming in;
+            if (adds && p.vec_add == 2 && rows > 0 && first < last) request(in, add + first, p.ld_add, rows, (int)(q.N - tile.n0 - first));
             if (!wait(ctl, p.wait_ns, &ctl->acc_full[buf], (count >> 1) & 1)) { fail(ctl, 3); break; }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const int64_t m = tile.m0 + (int)rank * 128 + 32 * quad + lane;
             const uint32_t acc = tmem_base + buf * BN + quadrant;
 #pragma unroll 1
-            for (int c = half * (WIDTH / 2); c < (half + 1) * (WIDTH / 2); c += 32) {
-                if (tile.n0 + c >= q.N) break;
-                uint32_t ra[32], rb[32];
-                float a[32], b[32];
-                tmem_ld32(acc + c, ra);
-                if (GATED) tmem_ld32(acc + WIDTH + c, rb);
-                tmem_ld_wait(ra);
-                if (GATED) tmem_ld_wait(rb);
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    a[j] = q.k_iters ? __uint_as_float(ra[j]) : 0.0f;
-                    if (GATED) b[j] = q.k_iters ? __uint_as_float(rb[j]) : 0.0f;
+            for (int c = first; c < last; c += BLOCK) {
+                const int n = (int)(q.N - tile.n0 - c);
+                if (n <= 0 || rows <= 0) break;
+                if (adds) {
+                    land(in, add + c, p.ld_add, p.vec_add, rows, n, piece);
+                    if (p.vec_add == 2 && c + BLOCK < last) request(in, add + c + BLOCK, p.ld_add, rows, n - BLOCK);
                 }
-                if (p.f16) finish32<EPI, __half>(p, q, m, tile.n0 + c, stage, a, b);
-                else finish32<EPI, __nv_bfloat16>(p, q, m, tile.n0 + c, stage, a, b);
+                if (p.f16) finish_block<EPI, __half, PRE>(p, q, m0, tile.n0 + c, acc + c, acc + WIDTH + c, piece);
+                else finish_block<EPI, __nv_bfloat16, PRE>(p, q, m0, tile.n0 + c, acc + c, acc + WIDTH + c, piece);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
@@ -650,13 +769,8 @@ template <bool W_MN, bool T_MN, int EPI> __global__ void __launch_bounds__(FEW_T
         for (int c = warp < 6 ? 0 : 16; c < f.tokens; c += 32) {
             if (c >= valid) break;
             uint32_t r[16];
-            asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-                           "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-                         : "r"(tmem_base + ((uint32_t)(32 * quad) << 16) + c) : "memory");
-            asm volatile("tcgen05.wait::ld.sync.aligned;"
-                         : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
-                           "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
+            tmem_ld16(tmem_base + ((uint32_t)(32 * quad) << 16) + c, r);
+            tmem_ld_wait16(r);
 #pragma unroll
             for (int j = 0; j < 16; ++j)
                 if (c + j < valid)
@@ -686,18 +800,18 @@ template <bool W_MN, bool T_MN, int EPI> __global__ void __launch_bounds__(FEW_T
 
 // ---------------------------------------------------------------------------------------------------------
 template <int BN> constexpr size_t pair_smem() {
-    return (size_t)Ring<BN>::STAGES * Ring<BN>::STAGE + sizeof(Control) + EPI_WARPS * 32 * STAGE_PITCH * 4 + 1024;
+    return (size_t)Ring<BN>::STAGES * Ring<BN>::STAGE + sizeof(Control) + EPI_WARPS * PIECE + 1024;
 }
 static_assert(pair_smem<256>() <= 227 * 1024 && pair_smem<128>() <= 227 * 1024, "fits the shared memory of an SM");
 
 // Opts in to the shared memory and asks how many pairs fit the device, once per device and kernel; 0 = cannot run.
-template <int EPI, int BN, int N> int pairs_of(int device, int sm_count) {
+template <int EPI, int BN, int N, bool PRE> int pairs_of(int device, int sm_count) {
     static std::mutex lock;
     static int cached[64];
     if (device < 0 || device >= 64) return 0;
     std::lock_guard<std::mutex> guard(lock);
     if (cached[device] == 0) {
-        auto kernel = k_product_pair<EPI, BN, N>;
+        auto kernel = k_product_pair<EPI, BN, N, PRE>;
         int pairs = 0;
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pair_smem<BN>()) == cudaSuccess) {
             cudaLaunchConfig_t cfg = {};
@@ -714,11 +828,11 @@ template <int EPI, int BN, int N> int pairs_of(int device, int sm_count) {
     return cached[device] > 0 ? cached[device] : 0;
 }
 
-template <int EPI, int BN, int N> int launch(bnn_ctx *ctx, const ProductArgs<N> &a) {
-    const int pairs = pairs_of<EPI, BN, N>(ctx->device, ctx->sm_count);
+template <int EPI, int BN, bool PRE, int N> int launch(bnn_ctx *ctx, const ProductArgs<N> &a) {
+    const int pairs = pairs_of<EPI, BN, N, PRE>(ctx->device, ctx->sm_count);
     if (pairs == 0) return BNN_ERR_CUDA;
     const unsigned n = a.tiles < (uint32_t)pairs ? a.tiles : (unsigned)pairs;
-    BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_product_pair<EPI, BN, N>, dim3(2 * n), dim3(THREADS), pair_smem<BN>(), ctx->stream, a));
+    BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_product_pair<EPI, BN, N, PRE>, dim3(2 * n), dim3(THREADS), pair_smem<BN>(), ctx->stream, a));
     return bnn_check_launch(ctx);
 }
 
@@ -751,7 +865,8 @@ int map16(bnn_ctx *ctx, CUtensorMap *map, const void *p, int64_t ld, int64_t row
 int width_of(const void *p, int64_t ld, int64_t rows, int size) {
     const uintptr_t at = reinterpret_cast<uintptr_t>(p);
     const uint64_t pitch = rows > 1 ? (uint64_t)ld * size : 0;
-    return (at | pitch) % 32 == 0 ? 2 : (at | pitch) % 16 == 0 ? 1 : 0;
+    if (size == 4 && (at | pitch) % 32 == 0) return 3;
+    return (at | pitch) % 16 == 0 ? 2 : (at | pitch) % 4 == 0 ? 1 : 0;
 }
 
 }  // namespace
@@ -933,13 +1048,14 @@ template <int N> int product_pair(bnn_ctx *ctx, const BnnProduct *list, int coun
     a.tiles = (uint32_t)tiles;
     const BnnProduct &q = list[0];
     a.vec_bias = width_of(q.bias, 0, 1, 2); a.vec_add = width_of(q.add, q.ld_add, q.M, 2); a.vec_pre = width_of(q.pre, q.ldp, 2 * q.M, 4);
-#define BNN_LAUNCH(EPI) (bn == 256 ? launch<EPI, 256>(ctx, a) : launch<EPI, 128>(ctx, a))
+#define BNN_LAUNCH(EPI, PRE) (bn == 256 ? launch<EPI, 256, PRE>(ctx, a) : launch<EPI, 128, PRE>(ctx, a))
     if constexpr (N == 1) {
-        if (q.epilogue == BNN_EPI_LINEAR_BACK) return BNN_LAUNCH(BNN_EPI_LINEAR_BACK);
-        if (q.epilogue == BNN_EPI_GATED) return BNN_LAUNCH(BNN_EPI_GATED);
-        if (q.epilogue == BNN_EPI_GATED_BACK) return BNN_LAUNCH(BNN_EPI_GATED_BACK);
+        if (q.epilogue == BNN_EPI_LINEAR_BACK) return BNN_LAUNCH(BNN_EPI_LINEAR_BACK, false);
+        if (q.epilogue == BNN_EPI_GATED_BACK) return BNN_LAUNCH(BNN_EPI_GATED_BACK, false);
+        if (q.epilogue == BNN_EPI_GATED) return q.pre ? BNN_LAUNCH(BNN_EPI_GATED, true) : BNN_LAUNCH(BNN_EPI_GATED, false);
+        if (q.pre) return BNN_LAUNCH(BNN_EPI_LINEAR, true);
     }
-    return BNN_LAUNCH(BNN_EPI_LINEAR);
+    return BNN_LAUNCH(BNN_EPI_LINEAR, false);
 #undef BNN_LAUNCH
 }
 }  // namespace
