@@ -10,7 +10,7 @@
 // SM, tiles in bands of eight tile rows so that the operands of the tiles in flight stay in L2.
 //   warp 0, last warp  TMA producers, K steps in turn: 64-element K slices of both operands, 128-byte swizzle, a ring of stages
 //   warp 1             MMA issuer (CTA 0 of the pair): four K = 16 MMAs per stage; tcgen05.commit frees the stage
-//   warps 2 .. 17      epilogue: four per TMEM lane quadrant, a quarter of the columns each, one output row per thread
+//   the others         epilogue: two or four per TMEM lane quadrant, a share of the columns each, one output row per thread
 // Two accumulator buffers: the epilogue of a tile runs under the MMAs of the next one.
 // Gated projections: B's two halves are the gate rows (CTA 0) and the up rows (CTA 1), so columns 0 .. BN/2 - 1 of the
 // accumulator are g and the others u of the same hidden units, and one thread holds both when it forms act(g) u.
@@ -28,8 +28,11 @@ __device__ int g_product_error;          // 0 = fine; otherwise a code saying wh
 
 constexpr int BK = 64;                   // elements of K per stage: one 128-byte row
 constexpr int TM = 256;                  // tile rows of a pair
-constexpr int EPI_WARPS = 16;
-constexpr int THREADS = (2 + EPI_WARPS + 1) * 32;
+// Epilogue warps: sixteen, or eight where a thread needs more than the 104 registers that sixteen leave (kept pre-activations, the gated
+// gradient).  8192 x 4096 x 4096 with GELU, residual and kept pre-activations: 281 us with sixteen, 259 with eight; its plain
+// short sums, which the epilogue bounds, want sixteen (7868 x 1000, K = 728: 27.2 us with eight, 22.9 with sixteen).
+template <int EPI, bool PRE> constexpr int epi_warps() { return PRE || EPI == BNN_EPI_GATED_BACK ? 8 : 16; }
+template <int EPI, bool PRE> constexpr int pair_threads() { return (2 + epi_warps<EPI, PRE>() + 1) * 32; }
 constexpr uint32_t A_STAGE = 128 * BK * 2;
 template <int BN> struct Ring {
     static constexpr uint32_t B_STAGE = (BN / 2) * BK * 2;
@@ -394,10 +397,10 @@ __device__ __forceinline__ void finish_block(const Common &p, const Problem &q, 
 }
 
 template <int EPI, int BN, int N, bool PRE>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_product_pair(const __grid_constant__ ProductArgs<N> p) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads<EPI, PRE>(), 1) k_product_pair(const __grid_constant__ ProductArgs<N> p) {
     constexpr bool GATED = EPI == BNN_EPI_GATED || EPI == BNN_EPI_GATED_BACK;
     constexpr int WIDTH = GATED ? BN / 2 : BN;                   // output columns of a tile
-    constexpr int STAGES = Ring<BN>::STAGES;
+    constexpr int STAGES = Ring<BN>::STAGES, EPI_WARPS = epi_warps<EPI, PRE>(), PARTS = EPI_WARPS / 4;
     constexpr uint32_t STAGE = Ring<BN>::STAGE, TMEM = Ring<BN>::TMEM;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *tiles = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -498,7 +501,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_produc
     } else if (warp < 2 + EPI_WARPS) {
         bnn_pdl_wait();
         bnn_pdl_launch_next();
-        const int quad = warp & 3, quarter = (warp - 2) >> 2;
+        const int quad = warp & 3, part = (warp - 2) >> 2;
         const uint32_t quadrant = (uint32_t)(32 * quad) << 16;
         uint8_t *piece = reinterpret_cast<uint8_t *>(ctl + 1) + (warp - 2) * PIECE;
         uint32_t count = 0;
@@ -507,8 +510,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_produc
             const Tile tile = tile_at<WIDTH>(p, t);
             const Problem &q = p.q[tile.problem];
             const int64_t m0 = tile.m0 + (int)rank * 128 + 32 * quad;
-            constexpr int SHARE = WIDTH / 4 < BLOCK ? BLOCK : WIDTH / 4;       // a warp's columns of a tile (gated 128-wide tiles: two warps of four)
-            const int first = quarter * SHARE < WIDTH ? quarter * SHARE : WIDTH, last = first + SHARE < WIDTH ? first + SHARE : WIDTH;
+            constexpr int SHARE = WIDTH / PARTS < BLOCK ? BLOCK : WIDTH / PARTS;       // a warp's columns of a tile (gated 128-wide tiles: two warps of four)
+            const int first = part * SHARE < WIDTH ? part * SHARE : WIDTH, last = first + SHARE < WIDTH ? first + SHARE : WIDTH;
             const int rows = (int)(q.M - m0 < 32 ? q.M - m0 : 32);
             // what is added (the residual, an incoming gradient) is requested a block ahead, the first one while the tile is being multiplied
             const bool adds = EPI != BNN_EPI_GATED && p.add != nullptr;
@@ -799,8 +802,8 @@ template <bool W_MN, bool T_MN, int EPI> __global__ void __launch_bounds__(FEW_T
 }
 
 // ---------------------------------------------------------------------------------------------------------
-template <int BN> constexpr size_t pair_smem() {
-    return (size_t)Ring<BN>::STAGES * Ring<BN>::STAGE + sizeof(Control) + EPI_WARPS * PIECE + 1024;
+template <int BN, int EPI = BNN_EPI_LINEAR, bool PRE = false> constexpr size_t pair_smem() {
+    return (size_t)Ring<BN>::STAGES * Ring<BN>::STAGE + sizeof(Control) + epi_warps<EPI, PRE>() * PIECE + 1024;
 }
 static_assert(pair_smem<256>() <= 227 * 1024 && pair_smem<128>() <= 227 * 1024, "fits the shared memory of an SM");
 
@@ -813,9 +816,9 @@ template <int EPI, int BN, int N, bool PRE> int pairs_of(int device, int sm_coun
     if (cached[device] == 0) {
         auto kernel = k_product_pair<EPI, BN, N, PRE>;
         int pairs = 0;
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pair_smem<BN>()) == cudaSuccess) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pair_smem<BN, EPI, PRE>()) == cudaSuccess) {
             cudaLaunchConfig_t cfg = {};
-            cfg.gridDim = dim3(2 * sm_count); cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = pair_smem<BN>();
+            cfg.gridDim = dim3(2 * sm_count); cfg.blockDim = dim3(pair_threads<EPI, PRE>()); cfg.dynamicSmemBytes = pair_smem<BN, EPI, PRE>();
             cudaLaunchAttribute attr;
             attr.id = cudaLaunchAttributeClusterDimension;
             attr.val.clusterDim.x = 2; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
@@ -832,7 +835,7 @@ template <int EPI, int BN, bool PRE, int N> int launch(bnn_ctx *ctx, const Produ
     const int pairs = pairs_of<EPI, BN, N, PRE>(ctx->device, ctx->sm_count);
     if (pairs == 0) return BNN_ERR_CUDA;
     const unsigned n = a.tiles < (uint32_t)pairs ? a.tiles : (unsigned)pairs;
-    BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_product_pair<EPI, BN, N, PRE>, dim3(2 * n), dim3(THREADS), pair_smem<BN>(), ctx->stream, a));
+    BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_product_pair<EPI, BN, N, PRE>, dim3(2 * n), dim3(pair_threads<EPI, PRE>()), pair_smem<BN, EPI, PRE>(), ctx->stream, a));
     return bnn_check_launch(ctx);
 }
 
