@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(256) k_repitch(const __grid_constant__ Repitch
 
 // dz = dy act'(pre) and/or the column sums of dz: a block takes 64 columns (8 per thread) of one chunk of rows, 32 rows at a time.  With
 // a single chunk (few rows) the sums are the bias gradient itself, otherwise partial sums.  Without `pre` dz is dy itself and only the
-// sums are taken.
+// sums are taken.  VEC: rows of dy, pre and dz in 16-byte groups, N % 8 == 0.
 struct SlopeArgs {
     const void *dy; int64_t lddy;
     const float *pre; int64_t ldp;
@@ -110,11 +110,11 @@ struct SlopeArgs {
     float *part;                       // [chunk][N] or NULL
     void *sum;                         // N or NULL
     int64_t M, N, chunk_rows;
-    int act, vec;                      // vec: rows of dy, pre and dz in 16-byte groups, N % 8 == 0
+    int act;
 };
 constexpr int SUM_COLS = 64, SUM_ROWS = 32;
-template <typename T>
-__global__ void __launch_bounds__(256) k_act_backward(const SlopeArgs p) {
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256, VEC ? 2 : 4) k_act_backward(const SlopeArgs p) {
     __shared__ float sums[SUM_ROWS][SUM_COLS + 1];
     const int cx = threadIdx.x & 7, ry = threadIdx.x >> 3;
     const int64_t c0 = (int64_t)blockIdx.x * SUM_COLS + cx * 8;
@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(256) k_act_backward(const SlopeArgs p) {
     bnn_pdl_wait();
     bnn_pdl_launch_next();
     float s[8] = {};
-    if (c0 < p.N && p.vec) {
+    if (VEC && c0 < p.N) {
         constexpr int AT_ONCE = 4;               // rows on their way
         for (int64_t m0 = first + ry; m0 < end; m0 += SUM_ROWS * AT_ONCE) {
             uint4 dw[AT_ONCE], zw[AT_ONCE][2];
@@ -153,43 +153,56 @@ __global__ void __launch_bounds__(256) k_act_backward(const SlopeArgs p) {
                 if (dz) store8(dz + m * p.lddz + c0, d);
             }
         }
-    } else if (c0 < p.N) {
-        for (int64_t m = first + ry; m < end; m += SUM_ROWS) {
-            float d[8], z[8];
+    } else if (!VEC) {                         // a warp takes half of the columns and every fourth row, a lane one column of eight rows at a time
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        const int64_t c = (int64_t)blockIdx.x * SUM_COLS + 32 * (warp & 1) + lane;
+        for (int64_t m0 = first + (warp >> 1); c < p.N && m0 < end; m0 += 32) {
+            T bits[8];
+            float d[8], z[8] = {};
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                d[j] = c0 + j < p.N ? to_f32(dy[m * p.lddy + c0 + j]) : 0.0f;
-                z[j] = p.pre && c0 + j < p.N ? p.pre[m * p.ldp + c0 + j] : 0.0f;
+            for (int j = 0; j < 8; ++j) {            // requests without a branch, which would wait for each: beyond the end the last row again
+                const int64_t m = m0 + 4 * j < end ? m0 + 4 * j : end - 1;
+                bits[j] = dy[m * p.lddy + c];
+                if (p.pre) z[j] = p.pre[m * p.ldp + c];
             }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) d[j] = m0 + 4 * j < end ? to_f32(bits[j]) : 0.0f;
             if (p.pre) slopes8(p.act, z, d);
+            T *to = dz + m0 * p.lddz + c;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                s[j] += d[j];
-                if (dz && c0 + j < p.N) dz[m * p.lddz + c0 + j] = from_f32<T>(d[j]);
+                s[0] += d[j];
+                if (dz && m0 + 4 * j < end) to[4 * j * p.lddz] = from_f32<T>(d[j]);
             }
         }
     }
     if (!p.part && !p.sum) return;
+    if (VEC) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sums[ry][cx * 8 + j] = s[j];
+        for (int j = 0; j < 8; ++j) sums[ry][cx * 8 + j] = s[j];
+    } else {
+        sums[threadIdx.x >> 6][threadIdx.x & 63] = s[0];
+    }
     __syncthreads();
     const int64_t c = (int64_t)blockIdx.x * SUM_COLS + threadIdx.x;
     if (threadIdx.x < SUM_COLS && c < p.N) {
         float t = 0.0f;
+        constexpr int rows = VEC ? SUM_ROWS : 4;
 #pragma unroll
-        for (int k = 0; k < SUM_ROWS; ++k) t += sums[k][threadIdx.x];
+        for (int k = 0; k < rows; ++k) t += sums[k][threadIdx.x];
         if (p.sum) static_cast<T *>(p.sum)[c] = from_f32<T>(t);
         else p.part[(int64_t)blockIdx.y * p.N + c] = t;
     }
 }
 
-// dg = dh u act'(g), du = dh act(g) from the kept g and u: one thread per 8 columns.
+// dg = dh u act'(g), du = dh act(g) from the kept g and u: one thread per 8 columns, neighbouring ones or (rows that are not whole 16-byte
+// groups) every eighth of 64, so that neighbouring lanes touch neighbouring elements.
 struct GatedSlopeArgs {
     const void *dh; int64_t lddh;
     const float *pre; int64_t ldp;
     void *dg, *du; int64_t ldd;
     int64_t M, N;
-    uint32_t groups;                   // of 8 columns in a row
+    uint32_t groups;                   // threads of a row
     int act, vec;
 };
 template <typename T>
@@ -198,25 +211,29 @@ __global__ void __launch_bounds__(256) k_gated_slopes(const GatedSlopeArgs p) {
     bnn_pdl_launch_next();
     const int64_t total = p.M * p.groups, stride = (int64_t)gridDim.x * 256;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += stride) {
-        const int64_t m = total <= 0xffffffffll ? (int64_t)((uint32_t)i / p.groups) : i / p.groups, c0 = (i - m * p.groups) * 8;
+        const int64_t m = total <= 0xffffffffll ? (int64_t)((uint32_t)i / p.groups) : i / p.groups, at = i - m * p.groups;
+        const int64_t c0 = p.vec ? at * 8 : at / 8 * 64 + at % 8;
         const T *dh = static_cast<const T *>(p.dh) + m * p.lddh + c0;
         const float *g = p.pre + m * p.ldp + c0, *u = p.pre + (p.M + m) * p.ldp + c0;
         T *dg = static_cast<T *>(p.dg) + m * p.ldd + c0, *du = static_cast<T *>(p.du) + m * p.ldd + c0;
         float d[8], a[8], b[8];
         if (p.vec) { load8(dh, d); load8(g, a); load8(u, b); }
         else {
+            T bits[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const bool in = c0 + j < p.N;
-                d[j] = in ? to_f32(dh[j]) : 0.0f; a[j] = in ? g[j] : 0.0f; b[j] = in ? u[j] : 0.0f;
+            for (int j = 0; j < 8; ++j) {            // requests without a branch, which would wait for each: beyond N the last column again
+                const int64_t c = c0 + 8 * j < p.N ? 8 * j : p.N - 1 - c0;
+                bits[j] = dh[c]; a[j] = g[c]; b[j] = u[c];
             }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) d[j] = to_f32(bits[j]);
         }
         gated8(p.act, d, a, b);
         if (p.vec) { store8(dg, a); store8(du, b); }
         else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (c0 + j < p.N) { dg[j] = from_f32<T>(a[j]); du[j] = from_f32<T>(b[j]); }
+                if (c0 + 8 * j < p.N) { dg[8 * j] = from_f32<T>(a[j]); du[8 * j] = from_f32<T>(b[j]); }
         }
     }
 }
@@ -230,7 +247,7 @@ size_t round256(size_t b) { return (b + 255) & ~size_t(255); }
 // the partial sums.
 int64_t sum_chunk_rows(int64_t M, int64_t N) {
     if (M <= 256) return M;
-    const int64_t blocks_n = (N + SUM_COLS - 1) / SUM_COLS, want = 592 / blocks_n + 1;
+    const int64_t blocks_n = (N + SUM_COLS - 1) / SUM_COLS, want = blocks_n < 592 ? 592 / blocks_n : 1;
     const int64_t rows = (M + want - 1) / want;
     return (rows + SUM_ROWS - 1) / SUM_ROWS * SUM_ROWS;
 }
@@ -378,9 +395,10 @@ extern "C" int bnn_linear_backward(bnn_ctx *ctx, const bnn_linear_desc *l, const
         s.dz = kept ? const_cast<void *>(dz.p) : nullptr; s.lddz = dz.ld;
         s.part = part; s.sum = chunks == 1 ? dbias : nullptr;
         s.M = M; s.N = l->N; s.chunk_rows = sum_chunk_rows(M, l->N); s.act = l->act;
-        s.vec = l->N % 8 == 0 && bnn_rows16(s.dy, s.lddy, M, 2) && (!kept || bnn_rows16(pre, ldp, M, 4));
+        const bool vec = l->N % 8 == 0 && bnn_rows16(s.dy, s.lddy, M, 2) && (!kept || bnn_rows16(pre, ldp, M, 4));
         const dim3 grid((unsigned)((l->N + SUM_COLS - 1) / SUM_COLS), (unsigned)sum_chunks(M, l->N));
-        auto kernel = l->dtype == BNN_F16 ? k_act_backward<__half> : k_act_backward<__nv_bfloat16>;
+        auto kernel = l->dtype == BNN_F16 ? (vec ? k_act_backward<__half, true> : k_act_backward<__half, false>)
+                                            : (vec ? k_act_backward<__nv_bfloat16, true> : k_act_backward<__nv_bfloat16, false>);
         BNN_CUDA_TRY(ctx, bnn_launch_dependent(kernel, grid, dim3(256), 0, ctx->stream, s));
         if (int st = bnn_check_launch(ctx)) return st;
         if (part)
@@ -462,7 +480,7 @@ extern "C" int bnn_gated_backward(bnn_ctx *ctx, const bnn_gated_desc *l, const v
         GatedSlopeArgs s{};
         s.dh = dh; s.lddh = lddh; s.pre = pre; s.ldp = ldp; s.dg = dg; s.du = du; s.ldd = ldd; s.M = M; s.N = l->N; s.act = l->act;
         s.vec = l->N % 8 == 0 && bnn_rows16(dh, lddh, M, 2) && bnn_rows16(pre, ldp, 2 * M, 4);
-        s.groups = (uint32_t)((l->N + 7) / 8);
+        s.groups = (uint32_t)(s.vec ? l->N / 8 : (l->N + 63) / 64 * 8);
         const int64_t blocks = (M * s.groups + 255) / 256, most = 8 * 148;
         auto kernel = l->dtype == BNN_F16 ? k_gated_slopes<__half> : k_gated_slopes<__nv_bfloat16>;
         BNN_CUDA_TRY(ctx, bnn_launch_dependent(kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, ctx->stream, s));
