@@ -72,11 +72,15 @@ template <typename T, bool VEC> __device__ __forceinline__ Eight<T> read8(const 
     } else {
 #pragma unroll
         for (int j = 0; j < 8; j += 8 / (2 * (int)sizeof(T))) {
+            // requests without a branch, which would wait for each: beyond D the last column again
             const int c = column<false>(slot, j, tid, team), c1 = c + team;
-            if constexpr (sizeof(T) == 4) e.w[j] = c < D ? __float_as_uint(row[c]) : 0u;
-            else {
+            if constexpr (sizeof(T) == 4) {
+                const uint32_t v = __float_as_uint(row[c < D ? c : D - 1]);
+                e.w[j] = c < D ? v : 0u;
+            } else {
                 const uint16_t *bits = reinterpret_cast<const uint16_t *>(row);
-                e.w[j >> 1] = (c < D ? bits[c] : 0u) | ((c1 < D ? (uint32_t)bits[c1] : 0u) << 16);
+                const uint32_t v = bits[c < D ? c : D - 1], v1 = bits[c1 < D ? c1 : D - 1];
+                e.w[j >> 1] = (c < D ? v : 0u) | (c1 < D ? v1 << 16 : 0u);
             }
         }
     }
@@ -419,6 +423,17 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_block_norm_backward(const Nor
                 asm volatile("cp.async.wait_group %0;" ::"n"(STAGES > 0 ? STAGES - 1 : 0) : "memory");
             }
             const float mean_b = p.post ? st.x : 0.0f, r_b = p.post ? st.y : 1.0f, mean_s = p.pre ? st.z : 0.0f, r_s = p.pre ? st.w : 1.0f;
+            if (!STAGES && m + 1 < end) {              // the next row comes to L2: a 128-byte line per thread and array
+                constexpr int LINE = 128 / (int)sizeof(T);
+                if (tid * LINE < p.D) {
+                    if (has_b) asm volatile("prefetch.global.L2 [%0];" ::"l"(B + (m + 1) * p.ldb + tid * LINE));
+                    if (inner) {
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(X + (m + 1) * p.ldx + tid * LINE));
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(N + (m + 1) * p.lddn + tid * LINE));
+                    }
+                    if (has_s) asm volatile("prefetch.global.L2 [%0];" ::"l"(S + (m + 1) * p.ldds + tid * LINE));
+                }
+            }
             Eight<T> rb[SLOTS];
             float u[SLOTS][8], z[SLOTS][8], v[SUMS];
 #pragma unroll
@@ -609,8 +624,8 @@ bool norm_vec(const bnn_block_norm_desc *n, int64_t M, const NormArgs &a) {
 // single elements, one slot (the shortest chain; 1000 x 1011 float32 forward: 21 us with four).  Backward: one slot up to 8192 columns, so that the column sums fit the registers.
 template <typename T, bool VEC> int launch_forward(bnn_ctx *ctx, const NormArgs &a) {
     const int groups = (a.D + 7) / 8;
-    const bool few = !VEC || a.M <= 2 * ctx->sm_count;
-    const int slots = groups > 1024 ? 4 : (few || groups <= 32) ? 1 : groups <= 64 ? 2 : 4;
+    const bool few = a.M <= 2 * ctx->sm_count || (!VEC && groups <= 256);
+    const int slots = groups > 1024 ? 4 : (few || groups <= 32) ? 1 : groups <= (VEC ? 64 : 512) ? 2 : 4;
     const int team = ((groups + slots - 1) / slots + 31) & ~31;
     const dim3 grid((unsigned)a.M), block(team);
     const bool plain = VEC && !a.layer && !a.post_c && !a.pre_c && a.block && a.stream && a.pre && a.normed;
