@@ -638,21 +638,26 @@ template <typename T, bool VEC> int launch_forward(bnn_ctx *ctx, const NormArgs 
 #undef BNN_FORWARD
     return bnn_check_launch(ctx);
 }
-// Backward, rows of 16-byte groups: two slots a thread (one below 257 columns), at most 256 threads up to 4096 columns, so that two
-// CTAs share an SM and one computes while the other waits at its barrier.  Other rows: one slot, more threads; their single
+// Backward.  TWICE, 16-bit rows of 16-byte groups without means and shifts: two slots a thread (one below 257 columns), at most 256 threads
+// up to 4096 columns, so that two CTAs share an SM and one computes while the other waits at its barrier.  ONCE, other rows of 16-byte
+// groups: their state and float32 rows fill the registers of two slots, so one slot up to 4096 columns (4096 rows, layer norm, 1016
+// columns of bf16: 29 us, 42 with two; RMS norm, 2048 columns of float32: 61 us, 69 with two).  ELEMENTS: one slot, more threads; single
 // elements are not fetched ahead, and more warps cover the wait (1000 x 1011: 34 us for the whole step, 52 with two slots).
-int backward_slots(int64_t D, bool vec) {
-    if (!vec) return D <= 8192 ? 1 : D <= 16384 ? 2 : 4;
-    return D <= 256 ? 1 : D <= 16384 ? 2 : 4;
+enum Rows { ELEMENTS, ONCE, TWICE, ROWS_KINDS };
+int backward_slots(int64_t D, int rows) {
+    if (D <= (rows == TWICE ? 256 : rows == ONCE ? 4096 : 8192)) return 1;
+    return D <= 16384 ? 2 : 4;
 }
-int backward_team(int64_t D, bool vec) {
-    const int groups = (int)((D + 7) / 8), slots = backward_slots(D, vec);
+int backward_team(int64_t D, int rows) {
+    const int groups = (int)((D + 7) / 8), slots = backward_slots(D, rows);
     return ((groups + slots - 1) / slots + 31) & ~31;
 }
+Rows backward_rows(const NormArgs &a, int size, bool vec) { return !vec ? ELEMENTS : size == 4 || a.layer || a.post_c || a.pre_c ? ONCE : TWICE; }
 template <typename T, bool VEC> int launch_backward(bnn_ctx *ctx, const NormArgs &a, unsigned ctas) {
-    const int slots = backward_slots(a.D, VEC), team = backward_team(a.D, VEC);
+    const Rows rows = backward_rows(a, (int)sizeof(T), VEC);
+    const int slots = backward_slots(a.D, rows), team = backward_team(a.D, rows);
     const bool plain = VEC && !a.layer && !a.post_c && !(a.want & (PRE_C | POST_C)) && a.block && a.pre && a.dn && a.ds && a.dx && a.db;
-    constexpr int STAGES = VEC ? (sizeof(T) == 4 ? 2 : 3) : 0, WIDE = VEC && sizeof(T) == 2 ? 2 : 0;      // rows of all four arrays that fit
+    constexpr int STAGES = VEC ? 3 : 0, WIDE = VEC && sizeof(T) == 2 ? 2 : 0;      // rows of all four arrays that fit
     const dim3 grid(ctas), block(team);
 #define BNN_BACKWARD(SLOTS, THREADS, CTAS, PLAIN, DEEP)                                                                              \
     do {                                                                                                                             \
@@ -663,10 +668,14 @@ template <typename T, bool VEC> int launch_backward(bnn_ctx *ctx, const NormArgs
         BNN_CUDA_TRY(ctx, bnn_launch_dependent(kernel, grid, block, smem, ctx->stream, a));                                          \
     } while (0)
     if constexpr (VEC) {
-        if (slots == 1 && plain) BNN_BACKWARD(1, 32, 1, true, STAGES);
-        else if (slots == 1) BNN_BACKWARD(1, 32, 1, false, STAGES);
-        else if (team <= 256 && plain) BNN_BACKWARD(2, 256, (sizeof(T) == 4 ? 1 : 2), true, STAGES);
-        else if (team <= 256) BNN_BACKWARD(2, 256, 1, false, STAGES);
+        if (slots == 1 && plain) BNN_BACKWARD(1, 512, 1, true, STAGES);
+        else if (slots == 1) BNN_BACKWARD(1, 512, 1, false, STAGES);
+        else if (team <= 256) {                                    // 16 bits
+            if constexpr (sizeof(T) == 2) {
+                if (plain) BNN_BACKWARD(2, 256, 2, true, STAGES);
+                else BNN_BACKWARD(2, 256, 1, false, STAGES);
+            }
+        }
         else if (team <= 512 && plain) BNN_BACKWARD(2, 512, 1, true, WIDE);
         else if (team <= 512) BNN_BACKWARD(2, 512, 1, false, WIDE);
         else if (slots == 2) BNN_BACKWARD(2, 1024, 1, false, 0);
@@ -697,8 +706,8 @@ Division divide_rows(int64_t M, int64_t rows_per_gate, int64_t ctas) {
 }
 // CTAs of the backward pass: 512 threads per SM (their registers hold the column sums), at most sixteen CTAs; at least two rows
 // each, or joining the partial sums takes longer than making them.
-int64_t norm_ctas(int64_t D, int64_t M, bool vec) {
-    const int per = 512 / backward_team(D, vec);
+int64_t norm_ctas(int64_t D, int64_t M, int rows_kind) {
+    const int per = 512 / backward_team(D, rows_kind);
     const int64_t most = 148 * (per < 1 ? 1 : per > 16 ? 16 : per), rows = (M + 1) / 2;
     return rows < most ? rows : most;
 }
@@ -737,9 +746,9 @@ extern "C" int bnn_block_norm(bnn_ctx *ctx, const bnn_block_norm_desc *norm, con
 
 extern "C" size_t bnn_block_norm_workspace_bytes(const bnn_block_norm_desc *norm, int64_t M) {
     if (check_norm(norm, M) || M == 0) return 0;
-    size_t most = 0;                         // of both kinds of rows
-    for (int vec = 0; vec < 2; ++vec) {
-        const size_t n = norm_part_floats(divide_rows(M, norm->gate ? norm->rows_per_gate : M, norm_ctas(norm->D, M, vec != 0)), norm->D);
+    size_t most = 0;                         // of all kinds of rows
+    for (int rows = 0; rows < ROWS_KINDS; ++rows) {
+        const size_t n = norm_part_floats(divide_rows(M, norm->gate ? norm->rows_per_gate : M, norm_ctas(norm->D, M, rows)), norm->D);
         if (n > most) most = n;
     }
     return (most * 4 + 255) & ~size_t(255);
@@ -780,7 +789,7 @@ extern "C" int bnn_block_norm_backward(bnn_ctx *ctx, const bnn_block_norm_desc *
     a.dx = g->dx; a.lddx = g->lddx; a.db = g->dblock; a.lddb = g->lddb; a.dgate = g->dgate; a.ld_dgate = g->ld_dgate;
     for (int k = 0; k < 4; ++k) a.want |= sums[k] ? (1 << k) : 0;
     const bool vec = norm_vec(norm, M, a);
-    const Division d = divide_rows(M, a.rows_per_gate, norm_ctas(norm->D, M, vec));
+    const Division d = divide_rows(M, a.rows_per_gate, norm_ctas(norm->D, M, backward_rows(a, size, vec)));
     a.groups = d.groups; a.chunks = d.chunks; a.chunk_rows = d.chunk_rows; a.units = d.units;
     const bool joins = a.want || (a.dgate && d.chunks > 1);
     if (joins && (!ctx->ws || ctx->ws_bytes < norm_part_floats(d, norm->D) * 4)) return BNN_ERR_WORKSPACE;
