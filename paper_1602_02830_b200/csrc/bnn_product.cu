@@ -28,11 +28,12 @@ __device__ int g_product_error;          // 0 = fine; otherwise a code saying wh
 
 constexpr int BK = 64;                   // elements of K per stage: one 128-byte row
 constexpr int TM = 256;                  // tile rows of a pair
-// Epilogue warps: sixteen, or eight where a thread needs more than the 104 registers that sixteen leave (kept pre-activations, the gated
-// gradient).  8192 x 4096 x 4096 with GELU, residual and kept pre-activations: 281 us with sixteen, 259 with eight; its plain
-// short sums, which the epilogue bounds, want sixteen (7868 x 1000, K = 728: 27.2 us with eight, 22.9 with sixteen).
-template <int EPI, bool PRE> constexpr int epi_warps() { return PRE || EPI == BNN_EPI_GATED_BACK ? 8 : 16; }
-template <int EPI, bool PRE> constexpr int pair_threads() { return (2 + epi_warps<EPI, PRE>() + 1) * 32; }
+// Epilogue warps: sixteen or eight.  Eight where a thread needs more than the 104 registers that sixteen leave (kept pre-activations, the
+// gated gradient: 8192 x 4096 x 4096 with GELU, residual and kept pre-activations 281 us with sixteen, 259 with eight) and, from LONG_SUM
+// K steps on, where the epilogue has time (2048 x 4096 x 8192 112 us with sixteen, 110 with eight; 4096 x 4096 x 4096, both gradients 220
+// and 216).  Shorter sums are bound by their epilogue (3584 x 6400 x 256 with residual and bias 42 with sixteen, 49 with eight; K = 1024 53 and 59, 2048 79 and 77).
+constexpr int LONG_SUM = 32;
+constexpr int pair_threads(int epi_warps) { return (2 + epi_warps + 1) * 32; }
 constexpr uint32_t A_STAGE = 128 * BK * 2;
 template <int BN> struct Ring {
     static constexpr uint32_t B_STAGE = (BN / 2) * BK * 2;
@@ -396,11 +397,11 @@ __device__ __forceinline__ void finish_block(const Common &p, const Problem &q, 
     if constexpr (!APART) flush<T, BLOCK>(out, q.ldo[0], q.vec_out, rows, n, piece);
 }
 
-template <int EPI, int BN, int N, bool PRE>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads<EPI, PRE>(), 1) k_product_pair(const __grid_constant__ ProductArgs<N> p) {
+template <int EPI, int BN, int N, bool PRE, int EPI_WARPS>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads(EPI_WARPS), 1) k_product_pair(const __grid_constant__ ProductArgs<N> p) {
     constexpr bool GATED = EPI == BNN_EPI_GATED || EPI == BNN_EPI_GATED_BACK;
     constexpr int WIDTH = GATED ? BN / 2 : BN;                   // output columns of a tile
-    constexpr int STAGES = Ring<BN>::STAGES, EPI_WARPS = epi_warps<EPI, PRE>(), PARTS = EPI_WARPS / 4;
+    constexpr int STAGES = Ring<BN>::STAGES, PARTS = EPI_WARPS / 4;
     constexpr uint32_t STAGE = Ring<BN>::STAGE, TMEM = Ring<BN>::TMEM;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *tiles = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -802,23 +803,23 @@ template <bool W_MN, bool T_MN, int EPI> __global__ void __launch_bounds__(FEW_T
 }
 
 // ---------------------------------------------------------------------------------------------------------
-template <int BN, int EPI = BNN_EPI_LINEAR, bool PRE = false> constexpr size_t pair_smem() {
-    return (size_t)Ring<BN>::STAGES * Ring<BN>::STAGE + sizeof(Control) + epi_warps<EPI, PRE>() * PIECE + 1024;
+template <int BN> constexpr size_t pair_smem(int epi_warps) {
+    return (size_t)Ring<BN>::STAGES * Ring<BN>::STAGE + sizeof(Control) + epi_warps * PIECE + 1024;
 }
-static_assert(pair_smem<256>() <= 227 * 1024 && pair_smem<128>() <= 227 * 1024, "fits the shared memory of an SM");
+static_assert(pair_smem<256>(16) <= 227 * 1024 && pair_smem<128>(16) <= 227 * 1024, "fits the shared memory of an SM");
 
 // Opts in to the shared memory and asks how many pairs fit the device, once per device and kernel; 0 = cannot run.
-template <int EPI, int BN, int N, bool PRE> int pairs_of(int device, int sm_count) {
+template <int EPI, int BN, int N, bool PRE, int WARPS> int pairs_of(int device, int sm_count) {
     static std::mutex lock;
     static int cached[64];
     if (device < 0 || device >= 64) return 0;
     std::lock_guard<std::mutex> guard(lock);
     if (cached[device] == 0) {
-        auto kernel = k_product_pair<EPI, BN, N, PRE>;
+        auto kernel = k_product_pair<EPI, BN, N, PRE, WARPS>;
         int pairs = 0;
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pair_smem<BN, EPI, PRE>()) == cudaSuccess) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pair_smem<BN>(WARPS)) == cudaSuccess) {
             cudaLaunchConfig_t cfg = {};
-            cfg.gridDim = dim3(2 * sm_count); cfg.blockDim = dim3(pair_threads<EPI, PRE>()); cfg.dynamicSmemBytes = pair_smem<BN, EPI, PRE>();
+            cfg.gridDim = dim3(2 * sm_count); cfg.blockDim = dim3(pair_threads(WARPS)); cfg.dynamicSmemBytes = pair_smem<BN>(WARPS);
             cudaLaunchAttribute attr;
             attr.id = cudaLaunchAttributeClusterDimension;
             attr.val.clusterDim.x = 2; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
@@ -831,12 +832,17 @@ template <int EPI, int BN, int N, bool PRE> int pairs_of(int device, int sm_coun
     return cached[device] > 0 ? cached[device] : 0;
 }
 
-template <int EPI, int BN, bool PRE, int N> int launch(bnn_ctx *ctx, const ProductArgs<N> &a) {
-    const int pairs = pairs_of<EPI, BN, N, PRE>(ctx->device, ctx->sm_count);
+template <int EPI, int BN, bool PRE, int WARPS, int N> int launch_warps(bnn_ctx *ctx, const ProductArgs<N> &a) {
+    const int pairs = pairs_of<EPI, BN, N, PRE, WARPS>(ctx->device, ctx->sm_count);
     if (pairs == 0) return BNN_ERR_CUDA;
     const unsigned n = a.tiles < (uint32_t)pairs ? a.tiles : (unsigned)pairs;
-    BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_product_pair<EPI, BN, N, PRE>, dim3(2 * n), dim3(pair_threads<EPI, PRE>()), pair_smem<BN, EPI, PRE>(), ctx->stream, a));
+    BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_product_pair<EPI, BN, N, PRE, WARPS>, dim3(2 * n), dim3(pair_threads(WARPS)), pair_smem<BN>(WARPS), ctx->stream, a));
     return bnn_check_launch(ctx);
+}
+template <int EPI, int BN, bool PRE, int N> int launch(bnn_ctx *ctx, const ProductArgs<N> &a) {      // q[0] has the longest sum
+    if constexpr (!PRE && EPI != BNN_EPI_GATED_BACK)
+        if (a.q[0].k_iters < LONG_SUM) return launch_warps<EPI, BN, PRE, 16>(ctx, a);
+    return launch_warps<EPI, BN, PRE, 8>(ctx, a);
 }
 
 template <bool W_MN, bool T_MN, int EPI> int launch_few(bnn_ctx *ctx, const FewArgs &f, unsigned tiles, unsigned split) {
