@@ -102,7 +102,8 @@ __global__ void __launch_bounds__(256) k_repitch(const __grid_constant__ Repitch
 
 // dz = dy act'(pre) and/or the column sums of dz: a block takes 64 columns (8 per thread) of one chunk of rows, 32 rows at a time.  With
 // a single chunk (few rows) the sums are the bias gradient itself, otherwise partial sums.  Without `pre` dz is dy itself and only the
-// sums are taken.  VEC: rows of dy, pre and dz in 16-byte groups, N % 8 == 0.
+// sums are taken.  Bound: HBM.  8192 x 4096 bf16 with GELU and the sums 56 us = 4.8 TB/s (blocks in whole rounds of two per SM; a
+// round more took 67), the sums alone 13 us = 5.2 TB/s; 4096 x 5393 (rows off the 16-byte rule) 69 us.  VEC: rows of dy, pre and dz in 16-byte groups, N % 8 == 0.
 struct SlopeArgs {
     const void *dy; int64_t lddy;
     const float *pre; int64_t ldp;

@@ -15,6 +15,11 @@
 // Gated projections: B's two halves are the gate rows (CTA 0) and the up rows (CTA 1), so columns 0 .. BN/2 - 1 of the
 // accumulator are g and the others u of the same hidden units, and one thread holds both when it forms act(g) u.
 // One issuing thread keeps the order of the additions fixed: the same call gives the same bits.
+// Bound: the tensor pipe and, for seconds on end, the part's power limit.  Measured (bf16): 8192 x 4096 x 4096 213 us = 1.29 PFLOP/s, with a
+// residual 227; 2048 x 4096 x 8192 109 us = 1.26 PFLOP/s; gated, 8192 rows, 4096 to 8192 twice, SiLU 800 us = 1.37 PFLOP/s; gradients
+// of 8192 x 4096 x 4096 440 us = 1.25 PFLOP/s.  256 x 256 tiles read (256 + 256) x K of operands from L2 for 256 x 256 x K products, half
+// of what 128 x 128 tiles of single CTAs read.  Short sums are bound by the epilogue and by writing: 3644 x 6416, K = 64, 25 us for 47 MB
+// (a plain fill of as much takes 14).
 // Every wait is bounded, as in the binary engine: a failure ends the kernel and shows in bnn_device_status.
 #include "bnn_product.cuh"
 #include "bnn_internal.cuh"
@@ -551,7 +556,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads(EPI_WAR
 // ---------------------------------------------------------------------------------------------------------
 // Few output rows (tokens): k_product_few.  The roles are swapped -- 128 weight rows are the M side of the tensor-core tile and the
 // tokens, 16 to 256 of them, its N side -- so a single token costs a tile of 16 columns and not of 256 rows, and every SM streams
-// weights.  Bound: the weights' bytes (HBM).  The sum is split over the CTAs of a cluster when there are too few tiles of
+// weights.  Bound: the weights' bytes (HBM): one row by 4096 x 4096 bf16 9.4 us for 33.6 MB, by two 8192 x 4096 24.3 us = 5.5 TB/s; 48 rows by
+// two 5500 x 2048 14.8 us.  The sum is split over the CTAs of a cluster when there are too few tiles of
 // weight rows to keep every SM loading: each takes a share of the K steps, stores its partial tile into the shared memory of the CTAs
 // that finish it (distributed shared memory, a share of the rows each), and after a cluster barrier every CTA adds up the parts of its
 // share in the order of the ranks: one launch, no workspace, the same bits every time.  (Reading the parts from the other CTAs
