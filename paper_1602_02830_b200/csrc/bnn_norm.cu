@@ -158,61 +158,57 @@ template <int N> __device__ __forceinline__ void block_sums(float (&v)[N], float
 // One row per CTA: both rows are requested before anything is computed from them.
 // PLAIN: BNN_NORM_RMS without shifts, with a block, both outputs wanted.  Columns beyond D read as zero, which adds nothing to the sums of squares; around a mean
 // (layer norm) they have to be left out.
-template <typename T, int SLOTS, int THREADS, bool VEC, bool PLAIN>
-__global__ void __launch_bounds__(THREADS, THREADS <= 256 ? 3 : 1) k_block_norm(const NormArgs p) {
-    __shared__ float buf[4][32];
+template <typename T, int SLOTS, bool VEC> __device__ __forceinline__ void plain_row(const NormArgs &p, int64_t m, float (&buf)[4][32]) {
+    const int tid = threadIdx.x, team = blockDim.x, warps = team >> 5, warp = tid >> 5, lane = tid & 31;
+    const T *pw = static_cast<const T *>(p.post_w), *nw = static_cast<const T *>(p.pre_w);
+    // everything is there and nothing is optional inside the loops: weights that are not given are ones
+    Eight<T> rx[SLOTS], rb[SLOTS];
+    const T *X = static_cast<const T *>(p.x) + m * p.ldx, *B = static_cast<const T *>(p.block) + m * p.ldb;
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) { rx[i] = read8<T, VEC>(X, i, tid, team, p.D); rb[i] = read8<T, VEC>(B, i, tid, team, p.D); }
+    const T *gate = p.gate ? static_cast<const T *>(p.gate) + (m / p.rows_per_gate) * p.ld_gate : nullptr;
+    float r = 1.0f, q = 0.0f;
+    if (p.post) {
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q += rb[i][j] * rb[i][j];
+        r = 1.0f / sqrtf(block_sum(q, buf[1], warps, warp, lane) * p.inv_d + p.eps);
+    }
+    float s[SLOTS][8];
+    q = 0.0f;
+    T *out = static_cast<T *>(p.stream) + m * p.lds;
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+        Eight<T> w, g;
+        w.fill(1.0f); g.fill(1.0f);
+        if (pw) w = read8<T, VEC>(pw, i, tid, team, p.D);
+        if (gate) g = read8<T, VEC>(gate, i, tid, team, p.D);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            s[i][j] = p.alpha * rx[i][j] + rb[i][j] * r * (w[j] * g[j]);
+            q += s[i][j] * s[i][j];
+        }
+        write8<T, VEC>(out, i, tid, team, p.D, s[i]);
+    }
+    const float r_s = 1.0f / sqrtf(block_sum(q, buf[3], warps, warp, lane) * p.inv_d + p.eps);
+    if (p.stats && tid == 0) { p.stats[4 * m] = 0.0f; p.stats[4 * m + 1] = r; p.stats[4 * m + 2] = 0.0f; p.stats[4 * m + 3] = r_s; }
+    out = static_cast<T *>(p.normed) + m * p.ldn;
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+        Eight<T> w;
+        w.fill(1.0f);
+        if (nw) w = read8<T, VEC>(nw, i, tid, team, p.D);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[i][j] *= r_s * w[j];
+        write8<T, VEC>(out, i, tid, team, p.D, s[i]);
+    }
+}
+template <typename T, int SLOTS, bool VEC> __device__ __forceinline__ void any_row(const NormArgs &p, int64_t m, float (&buf)[4][32]) {
     const int tid = threadIdx.x, team = blockDim.x, warps = team >> 5, warp = tid >> 5, lane = tid & 31;
     const T *pw = static_cast<const T *>(p.post_w), *pc = static_cast<const T *>(p.post_c);
     const T *nw = static_cast<const T *>(p.pre_w), *nc = static_cast<const T *>(p.pre_c);
     const bool layer = p.layer;
-    const int64_t m = blockIdx.x;
-    bnn_pdl_wait();
-    bnn_pdl_launch_next();
-    if constexpr (PLAIN) {
-        // everything is there and nothing is optional inside the loops: weights that are not given are ones
-        Eight<T> rx[SLOTS], rb[SLOTS];
-        const T *X = static_cast<const T *>(p.x) + m * p.ldx, *B = static_cast<const T *>(p.block) + m * p.ldb;
-#pragma unroll
-        for (int i = 0; i < SLOTS; ++i) { rx[i] = read8<T, VEC>(X, i, tid, team, p.D); rb[i] = read8<T, VEC>(B, i, tid, team, p.D); }
-        const T *gate = p.gate ? static_cast<const T *>(p.gate) + (m / p.rows_per_gate) * p.ld_gate : nullptr;
-        float r = 1.0f, q = 0.0f;
-        if (p.post) {
-#pragma unroll
-            for (int i = 0; i < SLOTS; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) q += rb[i][j] * rb[i][j];
-            r = 1.0f / sqrtf(block_sum(q, buf[1], warps, warp, lane) * p.inv_d + p.eps);
-        }
-        float s[SLOTS][8];
-        q = 0.0f;
-        T *out = static_cast<T *>(p.stream) + m * p.lds;
-#pragma unroll
-        for (int i = 0; i < SLOTS; ++i) {
-            Eight<T> w, g;
-            w.fill(1.0f); g.fill(1.0f);
-            if (pw) w = read8<T, VEC>(pw, i, tid, team, p.D);
-            if (gate) g = read8<T, VEC>(gate, i, tid, team, p.D);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                s[i][j] = p.alpha * rx[i][j] + rb[i][j] * r * (w[j] * g[j]);
-                q += s[i][j] * s[i][j];
-            }
-            write8<T, VEC>(out, i, tid, team, p.D, s[i]);
-        }
-        const float r_s = 1.0f / sqrtf(block_sum(q, buf[3], warps, warp, lane) * p.inv_d + p.eps);
-        if (p.stats && tid == 0) { p.stats[4 * m] = 0.0f; p.stats[4 * m + 1] = r; p.stats[4 * m + 2] = 0.0f; p.stats[4 * m + 3] = r_s; }
-        out = static_cast<T *>(p.normed) + m * p.ldn;
-#pragma unroll
-        for (int i = 0; i < SLOTS; ++i) {
-            Eight<T> w;
-            w.fill(1.0f);
-            if (nw) w = read8<T, VEC>(nw, i, tid, team, p.D);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) s[i][j] *= r_s * w[j];
-            write8<T, VEC>(out, i, tid, team, p.D, s[i]);
-        }
-        return;
-    }
     Eight<T> rx[SLOTS], rb[SLOTS];
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
@@ -312,6 +308,14 @@ __global__ void __launch_bounds__(THREADS, THREADS <= 256 ? 3 : 1) k_block_norm(
             for (int j = 0; j < 8; ++j) s[i][j] += c[j];
         write8<T, VEC>(static_cast<T *>(p.normed) + m * p.ldn, i, tid, team, p.D, s[i]);
     }
+}
+template <typename T, int SLOTS, int THREADS, bool VEC, bool PLAIN>
+__global__ void __launch_bounds__(THREADS, THREADS <= 256 ? 3 : 1) k_block_norm(const NormArgs p) {
+    __shared__ float buf[4][32];
+    bnn_pdl_wait();
+    bnn_pdl_launch_next();
+    if constexpr (PLAIN) plain_row<T, SLOTS, VEC>(p, blockIdx.x, buf);
+    else any_row<T, SLOTS, VEC>(p, blockIdx.x, buf);
 }
 
 // A CTA takes whole units (a unit: chunk_rows rows that share one gate row), so every thread keeps the column sums of its own
