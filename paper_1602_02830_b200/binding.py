@@ -567,8 +567,12 @@ class Context:
         return all(t is None or (t.data_ptr() % 16 == 0 and (t.shape[0] <= 1 or t.stride(0) * t.element_size() % 16 == 0)) for t in tensors)
 
     def linear_workspace_bytes(self, layer: Layer, x, backward: bool = False, dy=None) -> int:
-        """Workspace of linear / linear_backward for inputs laid out like x (and dy)."""
-        return int(lib().bnn_linear_workspace_bytes(layer.ref, x.shape[0], int(backward), int(self._rows16(x, dy, layer.tensors[0]))))
+        """Workspace of linear / linear_backward for inputs laid out like x and dy (None: contiguous rows).  A layer without
+        activation multiplies dy itself, so its rows count like those of x and W."""
+        rows16 = self._rows16(x, dy, layer.tensors[0])
+        if backward and dy is None and layer.desc.act == ACTIVATIONS["none"] and x.shape[0] > 1:
+            rows16 = rows16 and layer.outer * x.element_size() % 16 == 0
+        return int(lib().bnn_linear_workspace_bytes(layer.ref, x.shape[0], int(backward), int(rows16)))
 
     def gated_workspace_bytes(self, layer: Layer, x, backward: bool = False) -> int:
         """Workspace of gated / gated_backward for inputs laid out like x."""
