@@ -14,6 +14,7 @@
 // the variance is taken around the mean (two reductions), not as a difference of squares.
 #include "bnn_real.cuh"
 #include "bnn_internal.cuh"
+#include <mutex>
 
 namespace {
 
@@ -660,41 +661,39 @@ int backward_team(int64_t D, int rows) {
     return ((groups + slots - 1) / slots + 31) & ~31;
 }
 Rows backward_rows(const NormArgs &a, int size, bool vec) { return !vec ? ELEMENTS : size == 4 || a.layer || a.post_c || a.pre_c ? ONCE : TWICE; }
+// Shared memory past 48 KB has to be opted in to.  The setting belongs to the kernel and not to a call, and contexts of several host threads
+// launch the same kernel at different widths: it is made once per device, for the widest team.
+template <typename T, int SLOTS, int THREADS, int CTAS, bool VEC, bool PLAIN, int DEEP>
+int launch_rows(bnn_ctx *ctx, const NormArgs &a, unsigned ctas, int team) {
+    auto kernel = k_block_norm_backward<T, SLOTS, THREADS, CTAS, VEC, PLAIN, DEEP>;
+    constexpr size_t PER_THREAD = (size_t)DEEP * 64 * SLOTS * (sizeof(T) / 2);
+    if constexpr (PER_THREAD * THREADS > 40 * 1024) {     // with the kernel's own shared memory below the 48 KB that need no opting in
+        static std::mutex lock;
+        static bool ready[64];
+        if (ctx->device < 0 || ctx->device >= 64) return BNN_ERR_INVALID_ARG;
+        std::lock_guard<std::mutex> guard(lock);
+        if (!ready[ctx->device]) BNN_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(PER_THREAD * THREADS)));
+        ready[ctx->device] = true;
+    }
+    BNN_CUDA_TRY(ctx, bnn_launch_dependent(kernel, dim3(ctas), dim3(team), PER_THREAD * team, ctx->stream, a));
+    return bnn_check_launch(ctx);
+}
 template <typename T, bool VEC> int launch_backward(bnn_ctx *ctx, const NormArgs &a, unsigned ctas) {
     const Rows rows = backward_rows(a, (int)sizeof(T), VEC);
     const int slots = backward_slots(a.D, rows), team = backward_team(a.D, rows);
     const bool plain = VEC && !a.layer && !a.post_c && !(a.want & (PRE_C | POST_C)) && a.block && a.pre && a.dn && a.ds && a.dx && a.db;
     constexpr int STAGES = VEC ? 3 : 0, WIDE = VEC && sizeof(T) == 2 ? 2 : 0;      // rows of all four arrays that fit
-    const dim3 grid(ctas), block(team);
-#define BNN_BACKWARD(SLOTS, THREADS, CTAS, PLAIN, DEEP)                                                                              \
-    do {                                                                                                                             \
-        auto kernel = k_block_norm_backward<T, SLOTS, THREADS, CTAS, VEC, PLAIN, DEEP>;                                              \
-        const size_t smem = (size_t)DEEP * team * 64 * SLOTS * (sizeof(T) / 2);                                                      \
-        if (smem > 40 * 1024)      /* with the kernel's own shared memory below the 48 KB that need no opting in */                  \
-            BNN_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));                 \
-        BNN_CUDA_TRY(ctx, bnn_launch_dependent(kernel, grid, block, smem, ctx->stream, a));                                          \
-    } while (0)
+#define BNN_BACKWARD(SLOTS, THREADS, CTAS, PLAIN, DEEP) launch_rows<T, SLOTS, THREADS, CTAS, VEC, PLAIN, DEEP>(ctx, a, ctas, team)
     if constexpr (VEC) {
-        if (slots == 1 && plain) BNN_BACKWARD(1, 512, 1, true, STAGES);
-        else if (slots == 1) BNN_BACKWARD(1, 512, 1, false, STAGES);
-        else if (team <= 256) {                                    // 16 bits
-            if constexpr (sizeof(T) == 2) {
-                if (plain) BNN_BACKWARD(2, 256, 2, true, STAGES);
-                else BNN_BACKWARD(2, 256, 1, false, STAGES);
-            }
-        }
-        else if (team <= 512 && plain) BNN_BACKWARD(2, 512, 1, true, WIDE);
-        else if (team <= 512) BNN_BACKWARD(2, 512, 1, false, WIDE);
-        else if (slots == 2) BNN_BACKWARD(2, 1024, 1, false, 0);
-        else BNN_BACKWARD(4, 1024, 1, false, 0);
-    } else {
-        if (slots == 1 && team <= 512) BNN_BACKWARD(1, 512, 1, false, 0);
-        else if (slots == 1) BNN_BACKWARD(1, 1024, 1, false, 0);
-        else if (slots == 2) BNN_BACKWARD(2, 1024, 1, false, 0);
-        else BNN_BACKWARD(4, 1024, 1, false, 0);
-    }
+        if (slots == 1) return plain ? BNN_BACKWARD(1, 512, 1, true, STAGES) : BNN_BACKWARD(1, 512, 1, false, STAGES);
+        if constexpr (sizeof(T) == 2)
+            if (team <= 256) return plain ? BNN_BACKWARD(2, 256, 2, true, STAGES) : BNN_BACKWARD(2, 256, 1, false, STAGES);
+        if (team <= 512) return plain ? BNN_BACKWARD(2, 512, 1, true, WIDE) : BNN_BACKWARD(2, 512, 1, false, WIDE);
+    } else if (slots == 1 && team <= 512) return BNN_BACKWARD(1, 512, 1, false, 0);
+    else if (slots == 1) return BNN_BACKWARD(1, 1024, 1, false, 0);
+    if (slots == 2) return BNN_BACKWARD(2, 1024, 1, false, 0);
+    return BNN_BACKWARD(4, 1024, 1, false, 0);
 #undef BNN_BACKWARD
-    return bnn_check_launch(ctx);
 }
 
 // How the rows of the backward pass are divided: units of rows that share a gate row, at least `ctas` of them if the rows allow.

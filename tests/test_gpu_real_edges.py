@@ -1,4 +1,6 @@
 """Edges of the real-valued operators on the GPU."""
+import threading
+
 import pytest
 import torch
 
@@ -40,3 +42,41 @@ def test_linear_backward_in_the_workspace_asked_for(ctx, M, N, K, bias):
     ctx.device_status()
     assert (ws[n:] == 0x7F).all(), "written beyond the workspace"
     ctx.set_workspace(None)
+
+
+def test_contexts_of_two_threads_at_different_widths():
+    """A context per host thread is allowed: what one thread's launches need must not depend on the other's.  Both widths run the same
+    kernel with different amounts of shared memory."""
+    widths, failures, results = (2048, 4096), [], {}
+
+    def steps(D, start):
+        try:
+            stream = torch.cuda.Stream()
+            c = binding.Context(0, stream)
+            with torch.cuda.stream(stream):
+                x, b, ds, dn, w = (normal(k, 4, D) for k in range(5))
+                layer = c.make_block_norm(D, BF, kind="layer", post=True, pre_weight=w[0])
+                ws = torch.empty(c.block_norm_workspace_bytes(layer, 4), dtype=torch.uint8, device="cuda")
+                c.set_workspace(ws)
+                stats = c.empty(4, 4, dtype=FF)
+                c.block_norm(layer, x, b, stats=stats)
+                start.wait()
+                for _ in range(3000):
+                    results[D] = c.block_norm_backward(layer, ds, dn, x, b, stats)["dblock"]
+            stream.synchronize()
+            c.close()
+        except Exception as e:                    # raised in the test's own thread below
+            failures.append(e)
+
+    build.build()
+    start = threading.Barrier(len(widths), timeout=60)
+    threads = [threading.Thread(target=steps, args=(D, start)) for D in widths]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failures, failures
+    for D in widths:
+        x, b, ds, dn, w = (normal(k, 4, D) for k in range(5))
+        par = {"kind": "layer", "eps": 1e-6, "alpha": 1.0, "post": True, "pre": True, "pre_weight": w[0]}
+        ref.check(results[D], *ref.block_norm(x, b, par, ds, dn)["dblock"], "dblock")
