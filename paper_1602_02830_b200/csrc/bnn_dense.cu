@@ -374,8 +374,9 @@ extern "C" int bnn_linear_backward(bnn_ctx *ctx, const bnn_linear_desc *l, const
     BnnOperand dz{dy, lddy};
     if (slopes) dz = {scratch.take(dz_bytes(M, l->N)), pitch16(l->N)};
     Readable readable(scratch);
-    const BnnOperand rz = readable(dz.p, dz.ld, products && !slopes ? M : 0, l->N), rx = readable(x, ldx, dW || again ? M : 0, l->K),
-                     rw = readable(l->W, l->ldw, dx || again ? l->N : 0, l->K);
+    // an empty product reads neither operand, and bnn_linear_workspace_bytes counts no copies for it
+    const BnnOperand rz = readable(dz.p, dz.ld, products && !slopes ? M : 0, l->N), rx = readable(x, ldx, some && (dW || again) ? M : 0, l->K),
+                     rw = readable(l->W, l->ldw, some && (dx || again) ? l->N : 0, l->K);
     const int64_t chunks = sums ? sum_chunks(M, l->N) : 0;
     float *part = chunks > 1 ? reinterpret_cast<float *>(scratch.take(sums_bytes(M, l->N))) : nullptr;
     if (!scratch.ok()) return BNN_ERR_WORKSPACE;
@@ -466,8 +467,8 @@ extern "C" int bnn_gated_backward(bnn_ctx *ctx, const bnn_gated_desc *l, const v
     const int64_t ldd = pitch16(l->N);
     void *dg = scratch.take(dz_bytes(M, l->N)), *du = scratch.take(dz_bytes(M, l->N));
     Readable readable(scratch);
-    const BnnOperand rx = readable(x, ldx, dWg || dWu || again ? M : 0, l->K), rg = readable(l->Wg, l->ldg, dx || again ? l->N : 0, l->K),
-                     ru = readable(l->Wu, l->ldu, dx || again ? l->N : 0, l->K);
+    const BnnOperand rx = readable(x, ldx, some && (dWg || dWu || again) ? M : 0, l->K), rg = readable(l->Wg, l->ldg, some && (dx || again) ? l->N : 0, l->K),
+                     ru = readable(l->Wu, l->ldu, some && (dx || again) ? l->N : 0, l->K);     // an empty product reads no operand
     if (!scratch.ok()) return BNN_ERR_WORKSPACE;
     if (int st = readable.copy(ctx)) return st;
     BnnProduct p{};

@@ -80,3 +80,27 @@ def test_contexts_of_two_threads_at_different_widths():
         x, b, ds, dn, w = (normal(k, 4, D) for k in range(5))
         par = {"kind": "layer", "eps": 1e-6, "alpha": 1.0, "post": True, "pre": True, "pre_weight": w[0]}
         ref.check(results[D], *ref.block_norm(x, b, par, ds, dn)["dblock"], "dblock")
+
+
+@pytest.mark.parametrize("M,N", [(0, 8), (4, 0)])
+@pytest.mark.parametrize("act", ("none", "silu"))
+def test_empty_backward_with_every_pointer_given(ctx, M, N, act):
+    """The C entry points with operands off the 16-byte rule and no workspace, which is what the size functions ask for."""
+    K, L = 9, binding.lib()
+    x, W, dy, room = normal(1, 4, K), normal(2, 8, K), normal(3, 4, 8), normal(4, 8, 8, dtype=FF)
+    b = normal(5, 8)
+    code = binding.ACTIVATIONS[act]
+    lin = binding.LinearDesc(binding.BNN_BF16, code, K, N, W.data_ptr(), K, b.data_ptr())
+    glu = binding.GatedDesc(binding.BNN_BF16, code, K, N, W.data_ptr(), K, W.data_ptr(), K)
+    assert L.bnn_linear_workspace_bytes(lin, M, 1, 0) == L.bnn_gated_workspace_bytes(glu, M, 1, 0) == 0
+    ctx.set_workspace(None)
+    dx, dW, dU, db = (torch.full(s, 5.0, dtype=BF, device="cuda") for s in ((4, K), (8, K), (8, K), (8,)))
+    for pre in (None, room.data_ptr()):
+        for t in (dx, dW, dU, db):
+            t.fill_(5.0)
+        assert L.bnn_linear_backward(ctx._h, lin, dy.data_ptr(), 8, x.data_ptr(), K, M, pre, 8, dx.data_ptr(), K, dW.data_ptr(), K, db.data_ptr()) == 0
+        assert (dx[:M] == 0).all() and (dx[M:] == 5).all() and (dW[:N] == 0).all() and (dW[N:] == 5).all() and (db[:N] == 0).all() and (db[N:] == 5).all()
+        dx.fill_(5.0), dW.fill_(5.0)
+        assert L.bnn_gated_backward(ctx._h, glu, dy.data_ptr(), 8, x.data_ptr(), K, M, pre, 8, dx.data_ptr(), K, dW.data_ptr(), K, dU.data_ptr(), K) == 0
+        assert (dx[:M] == 0).all() and (dx[M:] == 5).all() and (dW[:N] == 0).all() and (dU[:N] == 0).all() and (dU[N:] == 5).all()
+    ctx.device_status()
