@@ -591,6 +591,13 @@ int launch_join(bnn_ctx *ctx, int dtype, const JoinArgs &j, int sums) {
 
 constexpr int NORM_MAX_D = 32768;
 
+// Rows of the stream that share a gate row, and gate rows.  Any number from M on means one gate row: it is brought down to M, so that nothing
+// computed from it overflows.
+int64_t rows_per_gate(const bnn_block_norm_desc *n, int64_t M) {
+    const int64_t most = M > 0 ? M : 1;
+    return n->gate && n->rows_per_gate < most ? n->rows_per_gate : most;
+}
+int64_t gate_rows(const bnn_block_norm_desc *n, int64_t M) { return n->gate ? (M + rows_per_gate(n, M) - 1) / rows_per_gate(n, M) : 0; }
 int check_norm(const bnn_block_norm_desc *n, int64_t M) {
     if (!n || !bnn_real_size(n->dtype) || (n->kind != BNN_NORM_RMS && n->kind != BNN_NORM_LAYER)) return BNN_ERR_INVALID_ARG;
     if (n->D < 1 || n->D > NORM_MAX_D || !bnn_real_dim(M) || !(n->eps >= 0.0f)) return BNN_ERR_INVALID_ARG;
@@ -600,8 +607,7 @@ int check_norm(const bnn_block_norm_desc *n, int64_t M) {
     const void *vectors[] = {n->post_weight, n->post_shift, n->pre_weight, n->pre_shift};
     for (const void *v : vectors)
         if (int st = bnn_check_real_opt(v, n->D, 1, n->D, size)) return st;
-    const int64_t gates = n->gate ? (M + n->rows_per_gate - 1) / n->rows_per_gate : 0;
-    return bnn_check_real_opt(n->gate, n->ld_gate, gates, n->D, size);
+    return bnn_check_real_opt(n->gate, n->ld_gate, gate_rows(n, M), n->D, size);
 }
 NormArgs norm_args(const bnn_block_norm_desc *n, int64_t M) {
     NormArgs a{};
@@ -610,7 +616,7 @@ NormArgs norm_args(const bnn_block_norm_desc *n, int64_t M) {
     a.post_w = n->post ? n->post_weight : nullptr; a.post_c = n->post ? n->post_shift : nullptr;
     a.pre_w = n->pre ? n->pre_weight : nullptr; a.pre_c = n->pre ? n->pre_shift : nullptr;
     a.gate = n->gate; a.ld_gate = n->ld_gate;
-    a.rows_per_gate = n->gate ? n->rows_per_gate : (M > 0 ? M : 1);
+    a.rows_per_gate = rows_per_gate(n, M);
     return a;
 }
 // Whole 16-byte groups everywhere a row is touched.
@@ -698,10 +704,9 @@ template <typename T, bool VEC> int launch_backward(bnn_ctx *ctx, const NormArgs
 
 // How the rows of the backward pass are divided: units of rows that share a gate row, at least `ctas` of them if the rows allow.
 struct Division { int64_t groups, chunks, chunk_rows, units, ctas; };
-Division divide_rows(int64_t M, int64_t rows_per_gate, int64_t ctas) {
+Division divide_rows(int64_t M, int64_t rows, int64_t ctas) {             // rows of one group
     Division d{};
-    d.groups = (M + rows_per_gate - 1) / rows_per_gate;
-    const int64_t rows = rows_per_gate < M ? rows_per_gate : M;           // of one group
+    d.groups = (M + rows - 1) / rows;
     d.chunks = d.groups >= ctas ? 1 : (ctas + d.groups - 1) / d.groups;
     if (d.chunks > rows) d.chunks = rows;
     d.chunk_rows = (rows + d.chunks - 1) / d.chunks;
@@ -754,7 +759,7 @@ extern "C" size_t bnn_block_norm_workspace_bytes(const bnn_block_norm_desc *norm
     if (check_norm(norm, M) || M == 0) return 0;
     size_t most = 0;                         // of all kinds of rows
     for (int rows = 0; rows < ROWS_KINDS; ++rows) {
-        const size_t n = norm_part_floats(divide_rows(M, norm->gate ? norm->rows_per_gate : M, norm_ctas(norm->D, M, rows)), norm->D);
+        const size_t n = norm_part_floats(divide_rows(M, rows_per_gate(norm, M), norm_ctas(norm->D, M, rows)), norm->D);
         if (n > most) most = n;
     }
     return (most * 4 + 255) & ~size_t(255);
@@ -777,8 +782,7 @@ extern "C" int bnn_block_norm_backward(bnn_ctx *ctx, const bnn_block_norm_desc *
     const void *vectors[] = {g->dpost_weight, g->dpost_shift, g->dpre_weight, g->dpre_shift};
     for (const void *v : vectors)
         if (int st = bnn_check_real_opt(v, norm->D, 1, norm->D, size)) return st;
-    const int64_t gates = norm->gate ? (M + norm->rows_per_gate - 1) / norm->rows_per_gate : 0;
-    if (int st = bnn_check_real_opt(g->dgate, g->ld_dgate, gates, norm->D, size)) return st;
+    if (int st = bnn_check_real_opt(g->dgate, g->ld_dgate, gate_rows(norm, M), norm->D, size)) return st;
     if (int st = bnn_check_real_opt(stats, 4, M, 4, 4)) return st;
     if (!ctx) return BNN_ERR_INVALID_ARG;
     bnn_device_guard guard(ctx);

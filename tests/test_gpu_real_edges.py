@@ -104,3 +104,21 @@ def test_empty_backward_with_every_pointer_given(ctx, M, N, act):
         assert L.bnn_gated_backward(ctx._h, glu, dy.data_ptr(), 8, x.data_ptr(), K, M, pre, 8, dx.data_ptr(), K, dW.data_ptr(), K, dU.data_ptr(), K) == 0
         assert (dx[:M] == 0).all() and (dx[M:] == 5).all() and (dW[:N] == 0).all() and (dU[:N] == 0).all() and (dU[N:] == 5).all()
     ctx.device_status()
+
+
+@pytest.mark.parametrize("rows_per_gate", (9, 0x7fffffff, (1 << 63) - 1))
+def test_one_gate_row_that_covers_more_rows_than_there_are(ctx, rows_per_gate):
+    M, D = 9, 72
+    x, b, ds, dn, gate = normal(1, M, D), normal(2, M, D), normal(3, M, D), normal(4, M, D), normal(5, 1, D)
+    layer = ctx.make_block_norm(D, BF, post=True, gate=gate, rows_per_gate=rows_per_gate)
+    ws = torch.empty(ctx.block_norm_workspace_bytes(layer, M), dtype=torch.uint8, device="cuda")
+    ctx.set_workspace(ws)
+    par = {"kind": "rms", "eps": 1e-6, "alpha": 1.0, "post": True, "pre": True, "gate": gate, "rows_per_gate": M}
+    want = ref.block_norm(x, b, par, ds, dn)
+    stats = ctx.empty(M, 4, dtype=FF)
+    for key, t in zip(("stream", "normed"), ctx.block_norm(layer, x, b, stats=stats)):
+        ref.check(t, *want[key], key)
+    for key, t in ctx.block_norm_backward(layer, ds, dn, x, b, stats).items():
+        if t is not None:
+            ref.check(t, *want[key], key)
+    ctx.set_workspace(None)

@@ -1,4 +1,8 @@
 """CPU-side checks of what the real-valued operators ask for before they launch anything."""
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -27,3 +31,26 @@ def test_linear_workspace_without_dy_is_that_of_contiguous_rows(host, M, N, K, a
     if act == "none":
         assert host.linear_workspace_bytes(layer, x, backward=True) == host.linear_workspace_bytes(layer, x, backward=True, dy=dy)
     assert host.linear_workspace_bytes(layer, x) == int(binding.lib().bnn_linear_workspace_bytes(layer.ref, M, 0, 1))
+
+
+FAR = r"""
+import ctypes
+from paper_1602_02830_b200 import binding
+P = 0x1000
+for M in (1, 2, 7, 300, 0x7fff0000):
+    for far in (M, 0x7fffffff, (1 << 62) + 1, (1 << 63) - 2, (1 << 63) - 1):
+        d = ctypes.byref(binding.BlockNormDesc(3, 0, 64, 1e-6, 1.0, 0, 1, None, None, None, None, P, 64, far))
+        print(M, far, binding.lib().bnn_block_norm_workspace_bytes(d, M), binding.lib().bnn_block_norm(None, d, P, 64, P, 64, M, P, 64, None, 0, None), flush=True)
+"""
+
+
+def test_one_gate_row_may_cover_more_rows_than_there_are():
+    """rows_per_gate >= M means one gate row, whatever the number; in a process of its own, which an overflow would end."""
+    build.build()
+    run = subprocess.run([sys.executable, "-c", FAR], capture_output=True, text=True, cwd=os.path.dirname(build.HERE))
+    assert run.returncode == 0, f"ended by {run.returncode} after\n{run.stdout}{run.stderr}"
+    seen = {}
+    for line in run.stdout.splitlines():
+        M, far, *answer = line.split()
+        assert seen.setdefault(M, answer) == answer, line
+    assert len(seen) == 5
