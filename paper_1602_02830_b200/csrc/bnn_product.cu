@@ -107,6 +107,11 @@ template <typename C> __device__ __forceinline__ bool wait(const C *ctl, unsigne
         }
     }
 }
+// The same by a whole warp, with one answer for all lanes: what follows (tcgen05.ld, __syncwarp) needs them together, and a lane that looked
+// a moment earlier than another could have given up alone.
+template <typename C> __device__ __forceinline__ bool warp_wait(const C *ctl, unsigned long long limit, const uint64_t *barrier, uint32_t parity, bool look = true) {
+    return __all_sync(0xffffffffu, wait(ctl, limit, barrier, parity, look));
+}
 __device__ __forceinline__ void mma_f16_2sm(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                  ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
@@ -524,7 +529,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads(EPI_WAR
             const uint16_t *add = static_cast<const uint16_t *>(p.add) + m0 * p.ld_add + tile.n0;
             Incoming in;
             if (adds && p.vec_add == 2 && rows > 0 && first < last) request(in, add + first, p.ld_add, rows, (int)(q.N - tile.n0 - first));
-            if (!wait(ctl, p.wait_ns, &ctl->acc_full[buf], (count >> 1) & 1)) { fail(ctl, 3); break; }
+            if (!warp_wait(ctl, p.wait_ns, &ctl->acc_full[buf], (count >> 1) & 1)) { fail(ctl, 3); break; }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t acc = tmem_base + buf * BN + quadrant;
 #pragma unroll 1
@@ -765,7 +770,7 @@ template <bool W_MN, bool T_MN, int EPI> __global__ void __launch_bounds__(FEW_T
     bool done = false;
     if (warp >= 2 && warp < 10) {
         // the MMAs issued before a failure end before tensor memory is given back: a wait that does not look at the failure word
-        done = wait(ctl, 2 * p.wait_ns, &ctl->acc_full, 0, false);
+        done = warp_wait(ctl, 2 * p.wait_ns, &ctl->acc_full, 0, false);
         if (!done) few_fail(ctl, 23);
     }
     __syncwarp();

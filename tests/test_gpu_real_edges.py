@@ -122,3 +122,27 @@ def test_one_gate_row_that_covers_more_rows_than_there_are(ctx, rows_per_gate):
         if t is not None:
             ref.check(t, *want[key], key)
     ctx.set_workspace(None)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 300, 4096), (130, 1000, 64), (700, 8192, 512)], ids=("split", "few", "tiles in turn"))
+def test_waits_that_run_out_in_every_epilogue(M, N, K):
+    """Nothing is loaded, so that every warp of an epilogue gives up, as one: statuses, and right results afterwards."""
+    c = binding.Context(0)
+    x, W, U, dy = normal(1, M, K), normal(2, N, K, scale=K ** -0.5), normal(3, N, K, scale=K ** -0.5), normal(4, M, N)
+    layer, glu, pre = c.make_linear(W, None, "silu"), c.make_gated(W, U), c.empty(2, M, N, dtype=FF)
+    ws = torch.empty(max(c.linear_workspace_bytes(layer, x, backward=True), c.gated_workspace_bytes(glu, x, backward=True)), dtype=torch.uint8, device="cuda")
+    c.set_workspace(ws)
+    c.set_wait_limit_ns(5_000_000)
+    for call in (lambda: c.linear(layer, x, pre=pre[0]), lambda: c.gated(glu, x, pre=pre), lambda: c.linear_backward(layer, dy, x),
+                 lambda: c.gated_backward(glu, dy, x)):
+        c.debug_drop_loads(True)
+        call()
+        with pytest.raises(binding.BnnError) as e:
+            c.device_status()
+        assert e.value.status == -5
+        c.debug_drop_loads(False)
+    ref.check(c.linear(layer, x), *ref.linear(x, W, None, None, "silu")["y"], "y after failures")
+    ref.check(c.gated(glu, x), *ref.gated(x, W, U, "silu")["h"], "h after failures")
+    c.device_status()
+    c.set_workspace(None)
+    c.close()
