@@ -78,6 +78,10 @@ template <int N> struct ProductArgs : Common {
     uint32_t tiles;
 };
 
+// How long a kernel waits at its end for copies and MMAs that it has issued, whatever the limit of its other waits; and for copies that no
+// barrier of its own counts.
+constexpr unsigned long long DRAIN_NS = 1000000000ull, SETTLE_NS = 2000000ull;
+
 struct __align__(16) Control {
     uint64_t full[STAGES_MAX], empty[STAGES_MAX], acc_full[2], acc_empty[2], drain;
     uint32_t tmem_base, failed;
@@ -470,12 +474,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads(EPI_WAR
                 }
                 step += (uint32_t)k_iters;
             }
-            // after a failure: the copies still in flight land before the CTA gives its shared memory up
-            if (rank == 0 && *reinterpret_cast<volatile uint32_t *>(&ctl->failed) != 0u)
+            // The copies in flight land before the CTA gives its shared memory up.  Waited for in every case: whether one of the other waits gives up
+            // may be decided after this thread has requested everything.
+            if (rank == 0)
                 for (uint32_t i = 0, s = stage, l = lap; i < (uint32_t)STAGES; i += 2) {      // this thread's last uses, newest first
                     if (s < 2) { if (l == 0) break; s += STAGES; --l; }
                     s -= 2;
-                    if (!wait(ctl, p.wait_ns, &ctl->full[s], l & 1, false)) break;
+                    if (!wait(ctl, DRAIN_NS, &ctl->full[s], l & 1, false)) break;
                 }
         }
     } else if (warp == 1) {
@@ -504,10 +509,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads(EPI_WAR
                 }
                 umma_commit_2sm(smem_u32(&ctl->acc_full[buf]));
             }
-            if (!ok) {                               // the MMAs issued so far end before tensor memory is given back
-                umma_commit_2sm(smem_u32(&ctl->drain));
-                wait(ctl, p.wait_ns, &ctl->drain, 0, false);
-            }
+            umma_commit_2sm(smem_u32(&ctl->drain));  // the MMAs issued end before tensor memory is given back, also where nobody waits for them any more
+            wait(ctl, DRAIN_NS, &ctl->drain, 0, false);
         }
     } else if (warp < 2 + EPI_WARPS) {
         bnn_pdl_wait();
@@ -551,7 +554,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads(EPI_WAR
 
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if (rank != 0 && threadIdx.x == 0) wait(ctl, DRAIN_NS, &ctl->drain, 0, false);       // the issuer's signals have reached this CTA as well
+    __syncwarp();
     cluster_sync_all();                                          // nobody leaves while the peer may still reach its shared memory
+    if (threadIdx.x == 0 && *reinterpret_cast<volatile uint32_t *>(&ctl->failed) != 0u) {
+        // After a failure one CTA may have requested a step that the other has not, whose barrier then never completes: both stay until such
+        // copies have landed.
+        const unsigned long long t0 = global_ns();
+        while (global_ns() - t0 < SETTLE_NS) {}
+    }
+    __syncwarp();
     if (warp == 1) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM) : "memory");
@@ -726,12 +738,11 @@ template <bool W_MN, bool T_MN, int EPI> __global__ void __launch_bounds__(FEW_T
                 stage += 2;
                 while (stage >= f.stages) { stage -= f.stages; ++lap; }
             }
-            if (*reinterpret_cast<volatile uint32_t *>(&ctl->failed) != 0u)        // copies in flight land before the shared memory is given up
-                for (int i = 0, s = stage, l = lap; i < f.stages; i += 2) {
-                    s -= 2;
-                    while (s < 0) { s += f.stages; --l; }
-                    if (l < 0 || !wait(ctl, p.wait_ns, &ctl->full[s], l & 1, false)) break;
-                }
+            for (int i = 0, s = stage, l = lap; i < f.stages; i += 2) {            // copies in flight land before the shared memory is given up, as above
+                s -= 2;
+                while (s < 0) { s += f.stages; --l; }
+                if (l < 0 || !wait(ctl, DRAIN_NS, &ctl->full[s], l & 1, false)) break;
+            }
         }
     } else if (warp == 1) {
         if (lane == 0) {
@@ -750,6 +761,7 @@ template <bool W_MN, bool T_MN, int EPI> __global__ void __launch_bounds__(FEW_T
                 if (++stage == f.stages) { stage = 0; phase ^= 1; }
             }
             mma_commit(&ctl->acc_full);
+            wait(ctl, DRAIN_NS, &ctl->acc_full, 0, false);       // the MMAs issued end before tensor memory is given back, also where the epilogue has given up
         }
     }
     // Rank r finishes the tile's outputs r * OUT .. r * OUT + OUT - 1 of every token.  A lane of warps 2 .. 9 holds one weight row of the
@@ -769,7 +781,6 @@ template <bool W_MN, bool T_MN, int EPI> __global__ void __launch_bounds__(FEW_T
     }
     bool done = false;
     if (warp >= 2 && warp < 10) {
-        // the MMAs issued before a failure end before tensor memory is given back: a wait that does not look at the failure word
         done = warp_wait(ctl, 2 * p.wait_ns, &ctl->acc_full, 0, false);
         if (!done) few_fail(ctl, 23);
     }

@@ -146,3 +146,36 @@ def test_waits_that_run_out_in_every_epilogue(M, N, K):
     c.device_status()
     c.set_workspace(None)
     c.close()
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 300, 4096), (130, 1000, 64), (700, 1000, 128), (700, 8192, 1024)], ids=("split", "few", "pairs", "tiles in turn"))
+def test_waits_that_run_out_with_copies_in_flight(M, N, K):
+    """The shortest limit that can be set, with the loads on: waits may give up at any point while copies and products are under way.  Either
+    a status or a right result, nothing beyond the output written, and right results afterwards."""
+    c = binding.Context(0)
+    x, W, U, dy = normal(1, M, K), normal(2, N, K, scale=K ** -0.5), normal(3, N, K, scale=K ** -0.5), normal(4, M, N)
+    layer, glu = c.make_linear(W, None, "silu"), c.make_gated(W, U)
+    n = max(c.linear_workspace_bytes(layer, x, backward=True), c.gated_workspace_bytes(glu, x, backward=True))
+    ws = torch.full((n + 256,), 0x7F, dtype=torch.uint8, device="cuda")
+    c.set_workspace(ws[:n])
+    want = {"y": ref.linear(x, W, None, None, "silu")["y"], "h": ref.gated(x, W, U, "silu")["h"]}
+    room = torch.full((M + 2, N), 5.0, dtype=BF, device="cuda")
+    for key, call in (("y", lambda out: c.linear(layer, x, out=out)), ("h", lambda out: c.gated(glu, x, out=out)),
+                      (None, lambda out: c.linear_backward(layer, dy, x)), (None, lambda out: c.gated_backward(glu, dy, x))):
+        for _ in range(4):
+            c.set_wait_limit_ns(1)
+            call(room[1:-1])
+            try:
+                c.device_status()
+                if key:
+                    ref.check(room[1:-1], *want[key], key)
+            except binding.BnnError as e:
+                assert e.status == -5
+            assert (room[0] == 5).all() and (room[-1] == 5).all() and (ws[n:] == 0x7F).all()
+        c.set_wait_limit_ns(2_000_000_000)
+        call(room[1:-1])
+        c.device_status()
+        if key:
+            ref.check(room[1:-1], *want[key], key + " afterwards")
+    c.set_workspace(None)
+    c.close()
