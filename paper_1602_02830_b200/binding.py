@@ -491,6 +491,11 @@ class Context:
             raise ValueError(f"{what}: expected contiguous {dtype} [{n}] on cuda:{self.device}, got {t.dtype} {list(t.shape)} on {t.device}")
         return t.data_ptr()
 
+    def _on(self, layer: Layer):
+        """Refuses a layer whose tensors are on another device: their addresses mean nothing on this one."""
+        if layer.device != self.device:
+            raise ValueError(f"layer: its tensors are on cuda:{layer.device}, the context is on cuda:{self.device}")
+
     def _here(self):
         """Whether torch's current stream is the context's: then memory needs no care across streams."""
         return _raw_stream(self.device) == self._raw
@@ -583,6 +588,7 @@ class Context:
 
     def linear(self, layer: Layer, x, residual=None, out=None, pre=None):
         """bnn_linear.  pre: float32 [M, N] that receives x W^T + bias for linear_backward.  out may be residual."""
+        self._on(layer)
         M, N, dtype, here = x.shape[0], layer.outer, layer.dtype, self._here()
         xp, ldx = self._fit(x, M, layer.inner, dtype, "x")
         rp = pp = None
@@ -605,6 +611,7 @@ class Context:
 
     def linear_backward(self, layer: Layer, dy, x, pre=None, want_dx: bool = True, want_dW: bool = True, want_db: bool = True):
         """bnn_linear_backward -> (dx, dW, dbias); dbias is None for a layer without bias, what is not wanted is None."""
+        self._on(layer)
         M, N, K, dtype, here = x.shape[0], layer.outer, layer.inner, layer.dtype, self._here()
         gp, ldg = self._fit(dy, M, N, dtype, "dy")
         xp, ldx = self._fit(x, M, K, dtype, "x")
@@ -630,6 +637,7 @@ class Context:
 
     def gated(self, layer: Layer, x, out=None, pre=None):
         """bnn_gated.  pre: contiguous float32 [2, M, N] that receives x Wg^T and x Wu^T for gated_backward."""
+        self._on(layer)
         M, N, dtype, here = x.shape[0], layer.outer, layer.dtype, self._here()
         xp, ldx = self._fit(x, M, layer.inner, dtype, "x")
         pp, ldp = self._planes(pre, M, N)
@@ -647,6 +655,7 @@ class Context:
 
     def gated_backward(self, layer: Layer, dh, x, pre=None, want_dx: bool = True, want_dW: bool = True):
         """bnn_gated_backward -> (dx, dWg, dWu); what is not wanted is None.  Without pre both products are computed again."""
+        self._on(layer)
         M, N, K, dtype, here = x.shape[0], layer.outer, layer.inner, layer.dtype, self._here()
         gp, ldg = self._fit(dh, M, N, dtype, "dh")
         xp, ldx = self._fit(x, M, K, dtype, "x")
@@ -678,6 +687,7 @@ class Context:
     def block_norm(self, layer: Layer, x, block=None, stream=None, normed=None, stats=None):
         """bnn_block_norm -> (stream, normed); normed is None for a layer without pre.  stream may be x.
         stats: contiguous float32 [M, 4] kept for block_norm_backward."""
+        self._on(layer)
         M, D, dtype, here = x.shape[0], layer.inner, layer.dtype, self._here()
         if layer.gates:
             self._gate_rows(layer, M)
@@ -704,6 +714,7 @@ class Context:
     def block_norm_backward(self, layer: Layer, dstream, dnormed, x, block=None, stats=None):
         """bnn_block_norm_backward -> dict with dx, dblock and, as far as the layer has them, dgate, dpost_weight, dpost_shift,
         dpre_weight, dpre_shift (None otherwise)."""
+        self._on(layer)
         M, D, dtype, here = x.shape[0], layer.inner, layer.dtype, self._here()
         if layer.gates:
             self._gate_rows(layer, M)

@@ -54,3 +54,15 @@ def test_one_gate_row_may_cover_more_rows_than_there_are():
         M, far, *answer = line.split()
         assert seen.setdefault(M, answer) == answer, line
     assert len(seen) == 5
+
+
+def test_layers_of_another_device_are_refused(host):
+    """Only the addresses of a layer's tensors reach the library: on another device they would be read as that device's memory."""
+    other = object.__new__(binding.Context)
+    other.device = 0
+    t = torch.zeros(4, 8, dtype=BF)
+    linear, gated, norm = host.make_linear(t), host.make_gated(t, t), host.make_block_norm(8, BF, pre_weight=t[0])
+    for call in (lambda: other.linear(linear, t), lambda: other.linear_backward(linear, t[:, :4], t), lambda: other.gated(gated, t),
+                 lambda: other.gated_backward(gated, t[:, :4], t), lambda: other.block_norm(norm, t), lambda: other.block_norm_backward(norm, t, t, t)):
+        with pytest.raises(ValueError, match="layer: its tensors are on"):
+            call()
