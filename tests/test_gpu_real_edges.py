@@ -179,3 +179,60 @@ def test_waits_that_run_out_with_copies_in_flight(M, N, K):
             ref.check(room[1:-1], *want[key], key + " afterwards")
     c.set_workspace(None)
     c.close()
+
+
+# act(z) and act'(z) in 64 bits, each without a difference that cancels far out, the lowest z whose results are normal numbers of bfloat16, and
+# how far the exponent may be off: |exponent| times a few 2^-24.
+def phi64(z):
+    return 0.5 * torch.special.erfc(-z / 2 ** 0.5), torch.exp(-0.5 * z * z) / (2 * torch.pi) ** 0.5
+
+
+def gelu64(z):
+    cdf, density = phi64(z)
+    return z * cdf, cdf + z * density, cdf + z.abs() * density
+
+
+def silu64(z):
+    s = torch.sigmoid(z)
+    return z * s, s * (1 + z * torch.sigmoid(-z)), s * (1 + z.abs())
+
+
+def sigmoid64(z):
+    s = torch.sigmoid(z)
+    return s, s * torch.sigmoid(-z), s
+
+
+TAILS = {"gelu": (gelu64, -12.5, lambda z: 0.5 * z * z), "silu": (silu64, -80.0, torch.abs), "sigmoid": (sigmoid64, -80.0, torch.abs)}
+
+
+@pytest.mark.parametrize("dtype", (BF, HF))
+@pytest.mark.parametrize("act", TAILS)
+def test_activation_tails_are_relatively_exact(ctx, act, dtype):
+    """z = x (one input, weight 1), from far out to 4: values and slopes to a unit of the result's type and what a float32 evaluation may
+    lose of the magnitude form, wherever z is."""
+    form, low, exponent = TAILS[act]
+    x = torch.linspace(low, 4.0, 4096, device="cuda").to(dtype)[:, None]
+    layer = ctx.make_linear(torch.ones(1, 1, dtype=dtype, device="cuda"), None, act)
+    ws = torch.empty(max(256, ctx.linear_workspace_bytes(layer, x, backward=True)), dtype=torch.uint8, device="cuda")
+    ctx.set_workspace(ws)
+    z = x.double()
+    value, slope, magnitude = form(z)
+    rel = 2.0 ** -18 + 2.0 ** -21 * exponent(z)
+    unit, tiny = ref.UNIT[dtype], {BF: 2.0 ** -133, HF: 2.0 ** -25}[dtype]
+    pre = ctx.empty(4096, 1, dtype=FF)
+    ref.check(ctx.linear(layer, x, pre=pre), value, (unit + rel) * value.abs() + tiny, "value")
+    # h = act(g) u with u = 1, and its product's u goes through untouched
+    one = torch.ones(1, 2, dtype=dtype, device="cuda")
+    glu, pair = ctx.make_gated(one * torch.tensor([1, 0], device="cuda"), one * torch.tensor([0, 1], device="cuda"), act), torch.cat((x, torch.ones_like(x)), 1)
+    ws2 = torch.empty(ctx.gated_workspace_bytes(glu, pair, backward=True), dtype=torch.uint8, device="cuda")
+    ctx.set_workspace(ws2)
+    ref.check(ctx.gated(glu, pair), value, (unit + rel) * value.abs() + tiny, "gated value")
+    dh = torch.ones_like(x)
+    ref.check(ctx.gated_backward(glu, dh, pair)[0], torch.cat((slope, value), 1),
+              torch.cat((unit * slope.abs() + rel * magnitude, (unit + rel) * value.abs()), 1) + 2 * tiny, "gated slope and value")
+    ctx.set_workspace(ws)
+    for kept in (pre, None):
+        dx = ctx.linear_backward(layer, dh, x, kept)[0]       # the rounded dz itself
+        ref.check(dx, slope, unit * slope.abs() + rel * magnitude + 2 * tiny, "slope")
+    ctx.device_status()
+    ctx.set_workspace(None)
