@@ -80,7 +80,6 @@ template <typename T> __device__ __forceinline__ void store8(T *p, const float (
 // act(z).  exp and the division are the fast forms (relative error a few 2^-23): results are rounded to 8 or 11 bits.
 // A NaN stays a NaN in every branch.
 __device__ __forceinline__ float sigmoid_f(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
-__device__ __forceinline__ float tanh_f(float u) { return 1.0f - __fdividef(2.0f, 1.0f + __expf(2.0f * u)); }
 // The normal distribution: cdf Phi(z) and density phi(z).  Phi(-|z|) = e^(-z^2 / 2) t P(t), t = 1 / (1 + 0.375 |z| / sqrt 2), the form of Hastings (1955); P of
 // degree 6 is a least-squares fit of 0 <= |z| <= 14.5, reweighted until the largest RELATIVE error is smallest (Lawson 1961): 6.4e-7, 1.0e-6 in float32.  bfloat16
 // has float32's range, so that a tail like gelu(-8) = -5e-15 is a result like any other; Hastings' own coefficients are for the absolute error and were
@@ -92,12 +91,15 @@ __device__ __forceinline__ float normal_cdf(float z, float &density) {
     density = 0.3989422804014327f * e;
     return z < 0.0f ? half : 1.0f - half;
 }
-constexpr float GELU_C = 0.7978845608028654f /* sqrt(2 / pi) */, GELU_A = 0.044715f;
+// The tanh form of gelu, z (1 + tanh u) / 2 with u = sqrt(2 / pi) (z + 0.044715 z^3), as z sigmoid(2 u): the same function without the difference that
+// cancels below z = -3 (20 % off at -5).
+constexpr float GELU_2C = 1.5957691216057308f /* 2 sqrt(2 / pi) */, GELU_A = 0.044715f;
+__device__ __forceinline__ float gelu_tanh_share(float z) { return sigmoid_f(GELU_2C * (z + GELU_A * z * z * z)); }
 __device__ __forceinline__ float act_value(int act, float z) {
     switch (act) {
         case BNN_ACT_RELU: return z < 0.0f ? 0.0f : z;
         case BNN_ACT_GELU: { float density; return z * normal_cdf(z, density); }
-        case BNN_ACT_GELU_TANH: return 0.5f * z * (1.0f + tanh_f(GELU_C * (z + GELU_A * z * z * z)));
+        case BNN_ACT_GELU_TANH: return z * gelu_tanh_share(z);
         case BNN_ACT_SILU: return z * sigmoid_f(z);
         case BNN_ACT_SIGMOID: return sigmoid_f(z);
         case BNN_ACT_HTANH: return z > 1.0f ? 1.0f : (z < -1.0f ? -1.0f : z);
@@ -115,10 +117,10 @@ __device__ __forceinline__ float act_slope(int act, float z, float &value) {
             return cdf + z * density;
         }
         case BNN_ACT_GELU_TANH: {
-            const float t = tanh_f(GELU_C * (z + GELU_A * z * z * z));
-            value = 0.5f * z * (1.0f + t);
+            const float p = gelu_tanh_share(z);
+            value = z * p;
             if (fabsf(z) > 100.0f) return z > 0.0f ? 1.0f : 0.0f;
-            return 0.5f * (1.0f + t) + 0.5f * z * (1.0f - t * t) * GELU_C * (1.0f + 3.0f * GELU_A * z * z);
+            return p * (1.0f + z * (1.0f - p) * GELU_2C * (1.0f + 3.0f * GELU_A * z * z));
         }
         case BNN_ACT_SILU: {
             const float p = sigmoid_f(z);

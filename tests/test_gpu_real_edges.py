@@ -192,6 +192,16 @@ def gelu64(z):
     return z * cdf, cdf + z * density, cdf + z.abs() * density
 
 
+def gelu_tanh_exponent(z):
+    return (8 / torch.pi) ** 0.5 * (z + 0.044715 * z ** 3)
+
+
+def gelu_tanh64(z):
+    w = gelu_tanh_exponent(z)
+    s, steep = torch.sigmoid(w), torch.sigmoid(-w) * (8 / torch.pi) ** 0.5 * (1 + 3 * 0.044715 * z * z)
+    return z * s, s * (1 + z * steep), s * (1 + z.abs() * steep)
+
+
 def silu64(z):
     s = torch.sigmoid(z)
     return z * s, s * (1 + z * torch.sigmoid(-z)), s * (1 + z.abs())
@@ -202,7 +212,8 @@ def sigmoid64(z):
     return s, s * torch.sigmoid(-z), s
 
 
-TAILS = {"gelu": (gelu64, -12.5, lambda z: 0.5 * z * z), "silu": (silu64, -80.0, torch.abs), "sigmoid": (sigmoid64, -80.0, torch.abs)}
+TAILS = {"gelu": (gelu64, -12.5, lambda z: 0.5 * z * z), "gelu_tanh": (gelu_tanh64, -9.5, lambda z: gelu_tanh_exponent(z).abs()),
+         "silu": (silu64, -80.0, torch.abs), "sigmoid": (sigmoid64, -80.0, torch.abs)}
 
 
 @pytest.mark.parametrize("dtype", (BF, HF))
