@@ -247,3 +247,54 @@ def test_activation_tails_are_relatively_exact(ctx, act, dtype):
         ref.check(dx, slope, unit * slope.abs() + rel * magnitude + 2 * tiny, "slope")
     ctx.device_status()
     ctx.set_workspace(None)
+
+
+def padded(t, pad):
+    """The same values in rows with `pad` more columns of NaN between them."""
+    wide = torch.full((t.shape[0], t.shape[1] + pad), float("nan"), dtype=t.dtype, device="cuda")
+    wide[:, :t.shape[1]] = t
+    return wide[:, :t.shape[1]]
+
+
+# Several tiles a pair (a GPU has 74 pairs, a tile 256 x 256 outputs, of gated projections 256 x 128): the ring of stages runs on from tile to tile and the
+# two accumulators alternate.  Sums on both sides of the 32 K steps where the number of epilogue warps changes.
+@pytest.mark.parametrize("M,N,K,dtype,act,pad", [(2560, 2560, 520, HF, "silu", 0), (2560, 2560, 2056, BF, "gelu", 0), (2600, 2500, 520, BF, "none", 3)])
+def test_linear_of_many_tiles(ctx, M, N, K, dtype, act, pad):
+    x, W, b = normal(1, M, K, dtype=dtype), normal(2, N, K, dtype=dtype, scale=K ** -0.5), normal(3, N, dtype=dtype)
+    r, dy = (padded(normal(k, M, N, dtype=dtype), pad) for k in (4, 5))
+    layer = ctx.make_linear(W, b, act)
+    n = ctx.linear_workspace_bytes(layer, x, backward=True, dy=dy)
+    ws = torch.full((n + 256,), 0x7F, dtype=torch.uint8, device="cuda")
+    ctx.set_workspace(ws[:n])
+    want, pre = ref.linear(x, W, b, r, act, dy), ctx.empty(M, N, dtype=FF)
+    ref.check(ctx.linear(layer, x, r), *want["y"], "y")
+    ref.check(ctx.linear(layer, x, r, pre=pre), *want["y"], "y with pre")
+    ref.check(pre, *want["pre"], "pre")
+    got = [ctx.linear_backward(layer, dy, x, kept) for kept in (pre, None)]
+    ctx.device_status()
+    for grads in got:
+        for key, t in zip(("dx", "dW", "db"), grads):
+            ref.check(t, *want[key], key)
+    assert all(torch.equal(p, q) for p, q in zip(got[0][:2], got[1][:2])), "kept and recomputed pre-activations give other products"
+    assert (ws[n:] == 0x7F).all(), "written beyond the workspace"
+    ctx.set_workspace(None)
+
+
+@pytest.mark.parametrize("M,N,K,dtype,act", [(2560, 2000, 520, BF, "silu"), (2560, 2000, 2056, HF, "gelu_tanh")])
+def test_gated_of_many_tiles(ctx, M, N, K, dtype, act):
+    x, dh = normal(1, M, K, dtype=dtype), normal(4, M, N, dtype=dtype)
+    Wg, Wu = (normal(k, N, K, dtype=dtype, scale=K ** -0.5) for k in (2, 3))
+    layer = ctx.make_gated(Wg, Wu, act)
+    n = ctx.gated_workspace_bytes(layer, x, backward=True)
+    ws = torch.full((n + 256,), 0x7F, dtype=torch.uint8, device="cuda")
+    ctx.set_workspace(ws[:n])
+    want, pre = ref.gated(x, Wg, Wu, act, dh), ctx.empty(2, M, N, dtype=FF)
+    ref.check(ctx.gated(layer, x), *want["h"], "h")
+    ref.check(ctx.gated(layer, x, pre=pre), *want["h"], "h with pre")
+    ref.check(pre[0], *want["g"], "g"), ref.check(pre[1], *want["u"], "u")
+    for kept in (pre, None):
+        for key, t in zip(("dx", "dWg", "dWu"), ctx.gated_backward(layer, dh, x, kept)):
+            ref.check(t, *want[key], key)
+    ctx.device_status()
+    assert (ws[n:] == 0x7F).all(), "written beyond the workspace"
+    ctx.set_workspace(None)
