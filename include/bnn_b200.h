@@ -374,6 +374,7 @@ BNN_API int bnn_fold_batchnorm(const float *gamma, const float *beta, const floa
  *  - `dtype` is the type of every matrix and vector of a call unless it says float: BNN_BF16 or BNN_F16 for the products,
  *    also BNN_F32 for norms and dropout.  Sums, statistics and activations are computed in float32 and every result is
  *    rounded once to `dtype`.
+ *  - float32 and float16 results are sources of bnn_pack_signs, so a binary layer can follow; bfloat16 is not.
  *  - Where a call needs scratch, bnn_*_workspace_bytes says how much of the context's workspace it takes
  *    (BNN_ERR_WORKSPACE if less is lent).  Matrix products read their operands in 16-byte groups: an operand whose base
  *    or leading dimension is not a multiple of 16 bytes is first copied to the workspace, so `aligned` = 0 asks for room
@@ -404,6 +405,7 @@ BNN_API int bnn_linear(bnn_ctx *ctx, const bnn_linear_desc *layer, const void *x
                        int64_t ldr, void *y, int64_t ldy, float *pre, int64_t ldp);
 /* Gradients of bnn_linear from dy (M x N, the gradient of y; the residual's gradient is dy itself):
  *   dz = dy * act'(z) (rounded to dtype, the operand of both products);  dx = dz W,  dW = dz^T x,  dbias = column sums of dz.
+ * dbias sums dz before that rounding where pre is given, and the rounded dz where z is computed again: its last bits depend on pre.
  * pre: z as bnn_linear left it, or NULL: z is computed again (one more product, no M x N float32 kept).  dx (M x K),
  * dW (N x K, ld lddw) and dbias (N) may each be NULL if not wanted.  M = 0 gives zero dW and dbias. */
 BNN_API int bnn_linear_backward(bnn_ctx *ctx, const bnn_linear_desc *layer, const void *dy, int64_t lddy, const void *x, int64_t ldx,

@@ -101,8 +101,8 @@ __global__ void __launch_bounds__(256) k_repitch(const __grid_constant__ Repitch
 }
 
 // dz = dy act'(pre) and/or the column sums of dz: a block takes 64 columns (8 per thread) of one chunk of rows, 32 rows at a time.  With
-// a single chunk (few rows) the sums are the bias gradient itself, otherwise partial sums.  Without `pre` dz is dy itself and only the
-// sums are taken.  Bound: HBM.  8192 x 4096 bf16 with GELU and the sums 56 us = 4.8 TB/s (blocks in whole rounds of two per SM; a
+// a single chunk the sums are the bias gradient itself, otherwise partial sums.  With `pre` the sums take dz
+// before it is rounded; without, dz is given (dy itself, or recomputed and rounded) and only the sums are taken.  Bound: HBM.  8192 x 4096 bf16 with GELU and the sums 56 us = 4.8 TB/s (blocks in whole rounds of two per SM; a
 // round more took 67), the sums alone 13 us = 5.2 TB/s; 4096 x 5393 (rows off the 16-byte rule) 69 us.  VEC: rows of dy, pre and dz in 16-byte groups, N % 8 == 0.
 struct SlopeArgs {
     const void *dy; int64_t lddy;
@@ -244,8 +244,9 @@ __global__ void __launch_bounds__(256) k_gated_slopes(const GatedSlopeArgs p) {
 int64_t pitch16(int64_t n) { return (n + 63) & ~int64_t(63); }
 size_t round256(size_t b) { return (b + 255) & ~size_t(255); }
 
-// Rows per chunk of the column sums: about four blocks per SM; up to 256 rows one chunk, which needs no second kernel to join
-// the partial sums.
+// Rows per chunk of the column sums: about four blocks per SM, whole rounds of two, while there are at most 296 blocks of columns (18944 outputs); above, one
+// chunk, whose last round may be nearly empty (2048 rows: 18944 outputs 70 us, 22016 103, 37888 118).  Up to 256 rows one chunk as well, which needs no
+// second kernel to join the partial sums.
 int64_t sum_chunk_rows(int64_t M, int64_t N) {
     if (M <= 256) return M;
     const int64_t blocks_n = (N + SUM_COLS - 1) / SUM_COLS, want = blocks_n < 592 ? 592 / blocks_n : 1;

@@ -573,8 +573,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads(EPI_WAR
 // ---------------------------------------------------------------------------------------------------------
 // Few output rows (tokens): k_product_few.  The roles are swapped -- 128 weight rows are the M side of the tensor-core tile and the
 // tokens, 16 to 256 of them, its N side -- so a single token costs a tile of 16 columns and not of 256 rows, and every SM streams
-// weights.  Bound: the weights' bytes (HBM): one row by 4096 x 4096 bf16 9.4 us for 33.6 MB, by two 8192 x 4096 24.3 us = 5.5 TB/s; 48 rows by
-// two 5500 x 2048 14.8 us.  The sum is split over the CTAs of a cluster when there are too few tiles of
+// weights.  Bound: the weights' bytes (HBM) where they are more than L2 holds: one row by two 8192 x 4096 bf16 24.3 us for 134 MB = 5.5 TB/s.  Smaller weights stay in
+// L2 between calls that repeat them, and launch and fill show: one row by 4096 x 4096, 33.6 MB, 9.4 us; 48 rows by two 5500 x 2048, 45 MB, 14.8 us.  With
+// the weights rotated through 20 layers and the calls in a graph: 11.3 us = 3.0 TB/s and 14.5 us = 3.1 TB/s.  The sum is split over the CTAs of a cluster when there are too few tiles of
 // weight rows to keep every SM loading: each takes a share of the K steps, stores its partial tile into the shared memory of the CTAs
 // that finish it (distributed shared memory, a share of the rows each), and after a cluster barrier every CTA adds up the parts of its
 // share in the order of the ranks: one launch, no workspace, the same bits every time.  (Reading the parts from the other CTAs
@@ -585,7 +586,10 @@ constexpr int FEW_SMEM = 200 * 1024;
 constexpr int FEW_THREADS = 384;
 constexpr int FEW_STAGES = 12;
 constexpr int FEW_TOKENS = 256;
-constexpr int64_t FEW_TILES = 128;         // from so many whole tiles on the pair kernel fills the GPU
+// Above so many 256 x 256 tiles the pair kernel is taken without a comparison.  That is right for many rows, whose tiles fill the GPU.  The tiles are counted
+// whatever their rows, though, so it also holds for few tokens and more than 32768 outputs (gated: 16384), whose tiles are mostly padding: one token, 4096 inputs,
+// 32768 outputs 46 us = 5.8 TB/s of weights on this kernel, 40960 outputs 86 us = 3.9 TB/s on the pair kernel.
+constexpr int64_t FEW_TILES = 128;
 
 struct FewArgs : Common {
     Problem q;                          // a: weights (a[1]: up rows, or the second pair), b: tokens; M tokens, N outputs
@@ -932,8 +936,8 @@ int64_t pair_tiles(const BnnProduct &q, int bn) {
     const int64_t width = is_gated(q) ? bn / 2 : bn;
     return (q.M + TM - 1) / TM * ((q.N + width - 1) / width);
 }
-// Which kernel, and how k_product_few divides the work, by estimates of both in microseconds.  Fitted to measured times (N x K, rows,
-// few / pair): 4096 x 4096, 1: 10.7 / 27.8, 128: 14.2 / 25.8, 384: 22.5 / 26.8, 768: 37.5 / 30.4; 512 x 8192, 512: 16.0 / 44.1; 8192 x 1024,
+// Which kernel, and how k_product_few divides the work, by estimates of both in microseconds.  Fitted to times of calls that repeat the same weights, from L2
+// as far as it holds them (N x K, rows, few / pair): 4096 x 4096, 1: 10.7 / 27.8, 128: 14.2 / 25.8, 384: 22.5 / 26.8, 768: 37.5 / 30.4; 512 x 8192, 512: 16.0 / 44.1; 8192 x 1024,
 // 64: 9.5 / 10.6, 192: 14.1 / 11.3; 256 x 256, 1: 3.9 / 5.3, 128: 9.0 / 5.9.
 //   pair: 5 + 0.30 per K step and round of tiles, or the weights at 3.3 TB/s (gated, 5500 x 2048 twice: 20.9) if that takes longer.
 //   few:  3 for every round of CTAs, + per K step of an SM's CTAs 0.12 + 0.0012 per token of a tile, at least 0.28 (0.26 with

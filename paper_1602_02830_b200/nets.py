@@ -137,7 +137,8 @@ def feed_forward_workspace_bytes(ctx, net, x, backward: bool = False) -> int:
 
 
 def feed_forward(ctx, net, x, seed: int | None = None, keep: list | None = None):
-    """x [M, D] through the stack: (stream, normed) after the last layer; one row is the form for a single token.
+    """x [M, D] through the stack: (stream, normed) after the last layer; one row is the form for a single token.  A layer is three or
+    four calls (gated, linear, dropout, block_norm) of 5 to 10 us on the host each, more than a small layer takes for one row: capture the calls in a CUDA graph there.
     seed: trains with dropout (one offset per layer); keep: a list that receives what feed_forward_backward needs."""
     def stats():
         return ctx.empty(x.shape[0], 4, dtype=torch.float32) if keep is not None else None
