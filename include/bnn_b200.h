@@ -485,6 +485,71 @@ BNN_API int bnn_block_norm_backward(bnn_ctx *ctx, const bnn_block_norm_desc *nor
 BNN_API int bnn_dropout(bnn_ctx *ctx, int dtype, const void *x, int64_t ldx, const void *residual, int64_t ldr, void *y, int64_t ldy,
                         int64_t rows, int64_t cols, double p, uint64_t seed, uint64_t offset);
 
+/* ---------------------------------------------------------------------------------------------
+ * Microscaled operands: the same sublayer in 8 and 4 bits, between the +-1 values of the binary layers and 16 bits.
+ *
+ * A microscaled matrix (OCP Microscaling Formats 1.0) has one power of two for each 32 neighbours of a row and elements e4m3 or e2m1:
+ *   X = floor(log2 max|v|) - emax, held to -127 .. 127 (one byte, X + 127);  element = v 2^-X rounded to nearest, ties to even, magnitudes
+ *   above the format's largest (448, 6) to the largest;  emax = 8 (e4m3), 2 (e2m1).  A block of zeros has X = -127.  A block that holds an infinity or a
+ *   NaN is NaN as a whole (scale byte 255).  The last block of a row may be short.  Quantising represented values again changes nothing.
+ *   values: rows of bnn_mx_ld(format, cols) bytes, base 32-byte aligned; element 2 i of an e2m1 row is the low half of byte i; zeros behind cols.
+ *   scales: bnn_mx_scale_bytes(rows, cols) bytes, base 16-byte aligned, 512 for each 128 rows x 128 columns: row r, block b of such a tile at
+ *   16 (r % 32) + 4 (r / 32) + b; tiles of the same rows next to each other.  Bytes of rows that do not exist are neither written nor looked at.
+ * Only the calls below write and read this form.  float32 statistics, sums and pre-activations as above. */
+enum { BNN_MX_E4M3 = 0, BNN_MX_E2M1 = 1 };
+typedef struct {
+    int32_t format;
+    int64_t rows, cols;
+    void *values, *scales; /* device */
+} bnn_mx_matrix;
+BNN_API int64_t bnn_mx_ld(int format, int64_t cols);
+BNN_API size_t bnn_mx_scale_bytes(int64_t rows, int64_t cols);
+
+/* x (q->rows x q->cols of dtype) into q.  represented: NULL, or a matrix of dtype that receives the values q stands for (rounded to dtype where
+ * it has fewer bits or less range), the operands of a straight-through backward pass.  represented may be x. */
+BNN_API int bnn_mx_quantize(bnn_ctx *ctx, int dtype, const void *x, int64_t ldx, const bnn_mx_matrix *q, void *represented, int64_t ldv);
+/* The values q stands for, as dtype. */
+BNN_API int bnn_mx_values(bnn_ctx *ctx, const bnn_mx_matrix *q, int dtype, void *out, int64_t ldo);
+/* bnn_block_norm with the norm of the stream microscaled (M x D, from the unrounded row); pre must be 1.  represented: NULL, or M x D of the norm's type, the
+ * values that normed stands for.  bnn_block_norm_backward takes the same stats: the gradient goes straight through the rounding. */
+BNN_API int bnn_block_norm_mx(bnn_ctx *ctx, const bnn_block_norm_desc *norm, const void *x, int64_t ldx, const void *block, int64_t ldb, int64_t M,
+                              void *stream, int64_t lds, const bnn_mx_matrix *normed, void *represented, int64_t ldv, float *stats);
+
+/* Dense layer of microscaled operands  z = x W^T + bias, y = residual + act(z):  x M x K, W N x K.  x e4m3: W e4m3 or e2m1; x e2m1: W e2m1.
+ * The tensor cores multiply elements and scales and add up in float32.  dtype (BNN_BF16 or BNN_F16) is the type of bias, residual and y. */
+typedef struct {
+    int32_t dtype, act;
+    bnn_mx_matrix W;
+    const void *bias; /* N or NULL (device) */
+} bnn_mx_linear_desc;
+/* pre: NULL, or M x N float32 that receives z for bnn_linear_backward, given the represented values of x and W: the gradients straight through the rounding.
+ * y_mx: NULL, or y microscaled (M x N, from the unrounded values) instead of y; y, residual and pre are NULL then.  y may be residual. */
+BNN_API int bnn_mx_linear(bnn_ctx *ctx, const bnn_mx_linear_desc *layer, const bnn_mx_matrix *x, const void *residual, int64_t ldr, void *y,
+                          int64_t ldy, float *pre, int64_t ldp, const bnn_mx_matrix *y_mx);
+/* Gated projections of microscaled operands  h = act(x Wg^T) * (x Wu^T), Wg and Wu of one format.  pre: NULL, or float32 [2][M][ldp] for bnn_gated_backward
+ * (as above).  h_mx: NULL, or h microscaled instead of h, the operand of the projection that follows. */
+typedef struct {
+    int32_t dtype, act;
+    bnn_mx_matrix Wg, Wu;
+} bnn_mx_gated_desc;
+BNN_API int bnn_mx_gated(bnn_ctx *ctx, const bnn_mx_gated_desc *layer, const bnn_mx_matrix *x, void *h, int64_t ldh, float *pre, int64_t ldp,
+                         const bnn_mx_matrix *h_mx);
+
+/* ---------------------------------------------------------------------------------------------
+ * The norm of all gradients together, and clipping:  n = sqrt(sum g^2),  f = min(1, max_norm / (n + eps)),  out = f g  for every tensor.
+ * g, out: n contiguous values of dtype each, aligned to their element (out may be g; tensors do not overlap otherwise).  norm: one float (device),
+ * receives n.  Formula as it stands: a NaN makes n and every out NaN, an infinity makes n infinite and f zero.  Sums are float64 over float32
+ * sums of 32 squares, in a fixed order: the same call gives the same bits.  Needs bnn_clip_workspace_bytes(count) of workspace. */
+typedef struct {
+    const void *g;
+    void *out;
+    int64_t n;
+    int32_t dtype; /* BNN_F32, BNN_F16 or BNN_BF16 */
+} bnn_gradient;
+BNN_API size_t bnn_clip_workspace_bytes(int64_t count);
+/* list: host array of `count` entries, read during the call only. */
+BNN_API int bnn_clip_gradients(bnn_ctx *ctx, const bnn_gradient *list, int64_t count, double max_norm, double eps, float *norm);
+
 #ifdef __cplusplus
 }
 #endif

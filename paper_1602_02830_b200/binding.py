@@ -19,6 +19,7 @@ LIB_PATH = os.path.join(_HERE, "libbnn_b200.so")
 BNN_F32, BNN_F16, BNN_I8, BNN_BF16 = 0, 1, 2, 3
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4, "sigmoid": 5, "htanh": 6}
 NORMS = {"rms": 0, "layer": 1}
+MX_FORMATS = {"e4m3": 0, "e2m1": 1}
 _REAL_TYPES = {torch.float32: BNN_F32, torch.float16: BNN_F16, torch.bfloat16: BNN_BF16}
 _PRODUCT_TYPES = (torch.float16, torch.bfloat16)
 VARIANT_AUTO, VARIANT_PLAIN, VARIANT_CSA = 0, 1, 2
@@ -37,6 +38,8 @@ EXPORTS = (
     "bnn_filter_repetition_workspace_bytes", "bnn_filter_repetition_count",
     "bnn_linear_workspace_bytes", "bnn_linear", "bnn_linear_backward", "bnn_gated_workspace_bytes", "bnn_gated",
     "bnn_gated_backward", "bnn_block_norm", "bnn_block_norm_workspace_bytes", "bnn_block_norm_backward", "bnn_dropout",
+    "bnn_mx_ld", "bnn_mx_scale_bytes", "bnn_mx_quantize", "bnn_mx_values", "bnn_block_norm_mx", "bnn_mx_linear", "bnn_mx_gated",
+    "bnn_clip_workspace_bytes", "bnn_clip_gradients",
 )
 
 
@@ -79,6 +82,44 @@ class BlockNormGrads(Structure):
     _fields_ = [("dx", c_void_p), ("lddx", c_int64), ("dblock", c_void_p), ("lddb", c_int64), ("dpost_weight", c_void_p),
                 ("dpost_shift", c_void_p), ("dpre_weight", c_void_p), ("dpre_shift", c_void_p), ("dgate", c_void_p),
                 ("ld_dgate", c_int64)]
+
+
+class MxDesc(Structure):
+    _fields_ = [("format", c_int32), ("rows", c_int64), ("cols", c_int64), ("values", c_void_p), ("scales", c_void_p)]
+
+
+class MxLinearDesc(Structure):
+    _fields_ = [("dtype", c_int32), ("act", c_int32), ("W", MxDesc), ("bias", c_void_p)]
+
+
+class MxGatedDesc(Structure):
+    _fields_ = [("dtype", c_int32), ("act", c_int32), ("Wg", MxDesc), ("Wu", MxDesc)]
+
+
+class Gradient(Structure):
+    _fields_ = [("g", c_void_p), ("out", c_void_p), ("n", c_int64), ("dtype", c_int32)]
+
+
+class MxMatrix:
+    """A microscaled matrix (made by Context.make_mx): rows x cols elements of `format` ("e4m3" or "e2m1") with a power of two for each 32
+    neighbours of a row.  values [rows, pitch] and scales are bytes in the library's layout (bnn_mx_matrix); Context.mx_values reads them back."""
+
+    def __init__(self, format, rows, cols, values, scales, device):
+        self.format, self.rows, self.cols, self.values, self.scales, self.device = format, rows, cols, values, scales, device
+        self.desc = MxDesc(MX_FORMATS[format], rows, cols, values.data_ptr(), scales.data_ptr())
+        self.ref = ctypes.byref(self.desc)
+
+    @property
+    def shape(self):
+        return self.rows, self.cols
+
+
+class Gradients:
+    """The tensors whose norm is taken together (made by Context.make_gradients), and where their clipped values go."""
+
+    def __init__(self, tensors, out, device):
+        self.tensors, self.out, self.device = tensors, out, device
+        self.list = (Gradient * max(1, len(tensors)))(*[Gradient(g.data_ptr(), o.data_ptr(), g.numel(), _REAL_TYPES[g.dtype]) for g, o in zip(tensors, out)])
 
 
 class Layer:
@@ -182,6 +223,18 @@ def lib() -> ctypes.CDLL:
         L.bnn_block_norm_backward.argtypes = [vp, POINTER(BlockNormDesc), vp, i64, vp, i64, vp, i64, vp, i64, vp, i64,
                                               POINTER(BlockNormGrads)]
         L.bnn_dropout.argtypes = [vp, c_int, vp, i64, vp, i64, vp, i64, i64, i64, c_double, c_uint64, c_uint64]
+        L.bnn_mx_ld.argtypes = [c_int, i64]
+        L.bnn_mx_ld.restype = i64
+        L.bnn_mx_scale_bytes.argtypes = [i64, i64]
+        L.bnn_mx_scale_bytes.restype = c_size_t
+        L.bnn_mx_quantize.argtypes = [vp, c_int, vp, i64, POINTER(MxDesc), vp, i64]
+        L.bnn_mx_values.argtypes = [vp, POINTER(MxDesc), c_int, vp, i64]
+        L.bnn_block_norm_mx.argtypes = [vp, POINTER(BlockNormDesc), vp, i64, vp, i64, i64, vp, i64, POINTER(MxDesc), vp, i64, vp]
+        L.bnn_mx_linear.argtypes = [vp, POINTER(MxLinearDesc), POINTER(MxDesc), vp, i64, vp, i64, vp, i64, POINTER(MxDesc)]
+        L.bnn_mx_gated.argtypes = [vp, POINTER(MxGatedDesc), POINTER(MxDesc), vp, i64, vp, i64, POINTER(MxDesc)]
+        L.bnn_clip_workspace_bytes.argtypes = [i64]
+        L.bnn_clip_workspace_bytes.restype = c_size_t
+        L.bnn_clip_gradients.argtypes = [vp, POINTER(Gradient), i64, c_double, c_double, vp]
         L.bnn_mlp_noalloc_max_bytes.argtypes = []
         L.bnn_mlp_noalloc_max_bytes.restype = c_size_t
         L.bnn_mlp_forward_noalloc.argtypes = [vp, POINTER(MlpDesc), vp, i64, i64, vp, i64]
@@ -745,6 +798,220 @@ class Context:
         if not here:
             self._used(dstream, dnormed, x, block, stats, *layer.tensors)
         return out
+
+    # -- microscaled operands ----------------------------------------------------------------------------
+    def make_mx(self, rows: int, cols: int, format: str = "e4m3") -> MxMatrix:
+        """Room for a microscaled matrix; its contents are whatever the memory held."""
+        if format not in MX_FORMATS:
+            raise ValueError(f"format: one of {', '.join(MX_FORMATS)}, got {format!r}")
+        if rows < 0 or cols < 0:
+            raise ValueError(f"rows, cols: expected sizes, got {rows}, {cols}")
+        L, here = lib(), self._here()
+        values = self._new(rows, int(L.bnn_mx_ld(MX_FORMATS[format], cols)), torch.uint8, here)
+        scales = self._new_vector(int(L.bnn_mx_scale_bytes(rows, cols)), torch.uint8, here)
+        return MxMatrix(format, rows, cols, values, scales, self.device)
+
+    def _mx(self, q, rows, cols, what):
+        if not isinstance(q, MxMatrix):
+            raise ValueError(f"{what}: expected a microscaled matrix (make_mx, mx_quantize), got {type(q).__name__}")
+        if (q.rows, q.cols) != (rows, cols) or q.device != self.device:
+            raise ValueError(f"{what}: expected [{rows}, {cols}] on cuda:{self.device}, got [{q.rows}, {q.cols}] on cuda:{q.device}")
+        return q.ref
+
+    def mx_quantize(self, x, format: str | None = None, out: MxMatrix | None = None, values=None) -> MxMatrix:
+        """bnn_mx_quantize: x [M, K] float32, float16 or bfloat16 to `format` ("e4m3" if nothing says otherwise) or into out.  values: a matrix like x that receives
+        what the elements stand for; may be x."""
+        dtype, here = x.dtype, self._here()
+        if dtype not in _REAL_TYPES:
+            raise ValueError(f"x: expected float32, float16 or bfloat16, got {dtype}")
+        if out is not None and format is not None and format != out.format:
+            raise ValueError(f"format: out is {out.format}, got {format!r}")
+        M, K = x.shape
+        xp, ldx = self._fit(x, M, K, dtype, "x")
+        vp, ldv = self._fit(values, M, K, dtype, "values")
+        if out is None:
+            out = self.make_mx(M, K, format or "e4m3")
+        st = lib().bnn_mx_quantize(self._h, _REAL_TYPES[dtype], xp, ldx, self._mx(out, M, K, "out"), vp, ldv)
+        if st:
+            self._ck(st, "bnn_mx_quantize")
+        if not here:
+            self._used(x, values, out.values, out.scales)
+        return out
+
+    def mx_values(self, q: MxMatrix, dtype=torch.float32, out=None):
+        """bnn_mx_values: what the elements of q stand for, [rows, cols] of dtype."""
+        here = self._here()
+        if dtype not in _REAL_TYPES:
+            raise ValueError(f"dtype: expected float32, float16 or bfloat16, got {dtype}")
+        ref = self._mx(q, q.rows, q.cols, "q") if isinstance(q, MxMatrix) else self._mx(q, 0, 0, "q")
+        if out is None:
+            out = self._new(q.rows, q.cols, dtype, here)
+        op, ldo = self._fit(out, q.rows, q.cols, dtype, "out")
+        st = lib().bnn_mx_values(self._h, ref, _REAL_TYPES[dtype], op, ldo)
+        if st:
+            self._ck(st, "bnn_mx_values")
+        if not here:
+            self._used(q.values, q.scales, out)
+        return out
+
+    def block_norm_mx(self, layer: Layer, x, block=None, format: str | None = None, out: MxMatrix | None = None, stream=None, values=None, stats=None):
+        """bnn_block_norm_mx -> (stream, normed microscaled).  layer: make_block_norm with pre; format as in mx_quantize; values: a matrix like x
+        that receives what the normed elements stand for; stream may be x; stats as in block_norm."""
+        self._on(layer)
+        M, D, dtype, here = x.shape[0], layer.inner, layer.dtype, self._here()
+        if out is not None and format is not None and format != out.format:
+            raise ValueError(f"format: out is {out.format}, got {format!r}")
+        if not layer.pre:
+            raise ValueError("layer: has no norm of the stream (pre)")
+        if layer.gates:
+            self._gate_rows(layer, M)
+        xp, ldx = self._fit(x, M, D, dtype, "x")
+        bp, ldb = self._fit(block, M, D, dtype, "block")
+        vp, ldv = self._fit(values, M, D, dtype, "values")
+        tp = self._stats(stats, M)
+        if stream is None:
+            stream = self._new(M, D, dtype, here)
+        sp, lds = self._fit(stream, M, D, dtype, "stream")
+        if out is None:
+            out = self.make_mx(M, D, format or "e4m3")
+        st = lib().bnn_block_norm_mx(self._h, layer.ref, xp, ldx, bp, ldb, M, sp, lds, self._mx(out, M, D, "out"), vp, ldv, tp)
+        if st:
+            self._ck(st, "bnn_block_norm_mx")
+        if not here:
+            self._used(x, block, stream, values, stats, out.values, out.scales, *layer.tensors)
+        return stream, out
+
+    def _mx_layer(self, W, act, dtype, *weights):
+        for q in weights:
+            if not isinstance(q, MxMatrix):
+                raise ValueError(f"weights: expected microscaled matrices (make_mx, mx_quantize), got {type(q).__name__}")
+            if q.shape != W.shape or q.format != W.format or q.device != self.device:
+                raise ValueError(f"weights: expected {W.format} {list(W.shape)} on cuda:{self.device}, got {q.format} {list(q.shape)} on cuda:{q.device}")
+        if dtype not in _PRODUCT_TYPES:
+            raise ValueError(f"dtype: expected float16 or bfloat16, got {dtype}")
+        if act not in ACTIVATIONS:
+            raise ValueError(f"act: one of {', '.join(ACTIVATIONS)}, got {act!r}")
+
+    def make_mx_linear(self, W: MxMatrix, bias=None, act: str = "none", dtype=torch.bfloat16) -> Layer:
+        """Dense layer of microscaled operands y = residual + act(x W^T + bias): W [N, K], bias [N] of dtype or None; residual and y are of dtype."""
+        self._mx_layer(W, act, dtype, W)
+        N, K = W.shape
+        d = MxLinearDesc(_REAL_TYPES[dtype], ACTIVATIONS[act], W.desc, self._vector(bias, N, dtype, "bias"))
+        layer = Layer(d, dtype, self.device, K, N, (W.values, W.scales, bias))
+        layer.format = W.format
+        return layer
+
+    def make_mx_gated(self, Wg: MxMatrix, Wu: MxMatrix, act: str = "silu", dtype=torch.bfloat16) -> Layer:
+        """Gated projections of microscaled operands h = act(x Wg^T) * (x Wu^T): Wg, Wu [N, K] of one format; h is of dtype."""
+        self._mx_layer(Wg, act, dtype, Wg, Wu)
+        N, K = Wg.shape
+        layer = Layer(MxGatedDesc(_REAL_TYPES[dtype], ACTIVATIONS[act], Wg.desc, Wu.desc), dtype, self.device, K, N,
+                      (Wg.values, Wg.scales, Wu.values, Wu.scales))
+        layer.format = Wg.format
+        return layer
+
+    def _mx_inputs(self, layer, x):
+        if getattr(layer, "format", None) is None:
+            raise ValueError("layer: expected one of microscaled weights (make_mx_linear, make_mx_gated)")
+        self._on(layer)
+        if not isinstance(x, MxMatrix):
+            raise ValueError(f"x: expected a microscaled matrix (mx_quantize, block_norm_mx), got {type(x).__name__}")
+        if x.format == "e2m1" and layer.format != "e2m1":
+            raise ValueError("x: e2m1 inputs go with e2m1 weights")
+        return self._mx(x, x.rows, layer.inner, "x"), x.rows, layer.outer
+
+    def mx_linear(self, layer: Layer, x: MxMatrix, residual=None, out=None, pre=None):
+        """bnn_mx_linear.  x: e4m3 (weights of either format) or e2m1 (weights too).  out: a matrix of the layer's type (may be residual), or an MxMatrix
+        that receives y microscaled (without residual and pre).  pre: float32 [M, N] that receives x W^T + bias for linear_backward."""
+        ref, M, N = self._mx_inputs(layer, x)
+        if not isinstance(layer.desc, MxLinearDesc):
+            raise ValueError("layer: expected one made by make_mx_linear")
+        dtype, here = layer.dtype, self._here()
+        rp, ldr = self._fit(residual, M, N, dtype, "residual")
+        pp, ldp = self._fit(pre, M, N, torch.float32, "pre")
+        op, ldo, qp = self._mx_out(out, M, N, dtype, here, residual is not None or pre is not None)
+        if out is None:
+            out, op, ldo = op, op.data_ptr(), ldo
+        st = lib().bnn_mx_linear(self._h, layer.ref, ref, rp, ldr, op, ldo, pp, ldp, qp)
+        if st:
+            self._ck(st, "bnn_mx_linear")
+        if not here:
+            self._used(x.values, x.scales, residual, pre, *self._memory(out), *layer.tensors)
+        return out
+
+    def mx_gated(self, layer: Layer, x: MxMatrix, out=None, pre=None):
+        """bnn_mx_gated.  x and out as in mx_linear.  pre: contiguous float32 [2, M, N] for gated_backward."""
+        ref, M, N = self._mx_inputs(layer, x)
+        if not isinstance(layer.desc, MxGatedDesc):
+            raise ValueError("layer: expected one made by make_mx_gated")
+        dtype, here = layer.dtype, self._here()
+        pp, ldp = self._planes(pre, M, N)
+        op, ldo, qp = self._mx_out(out, M, N, dtype, here, pre is not None)
+        if out is None:
+            out, op, ldo = op, op.data_ptr(), ldo
+        st = lib().bnn_mx_gated(self._h, layer.ref, ref, op, ldo, pp, ldp, qp)
+        if st:
+            self._ck(st, "bnn_mx_gated")
+        if not here:
+            self._used(x.values, x.scales, pre, *self._memory(out), *layer.tensors)
+        return out
+
+    def _mx_out(self, out, M, N, dtype, here, more):
+        """(address or, for no out, a new matrix; leading dimension; microscaled matrix)."""
+        if out is None:
+            return self._new(M, N, dtype, here), N, None
+        if isinstance(out, MxMatrix):
+            if more:
+                raise ValueError("out: microscaled results come without residual and pre")
+            return None, 0, self._mx(out, M, N, "out")
+        return *self._fit(out, M, N, dtype, "out"), None
+
+    @staticmethod
+    def _memory(out):
+        return (out.values, out.scales) if isinstance(out, MxMatrix) else (out,)
+
+    # -- gradients of a model ----------------------------------------------------------------------------
+    def make_gradients(self, tensors, out=None) -> Gradients:
+        """The gradients whose norm is taken together: contiguous float32, float16 or bfloat16 tensors that share no memory.  out: where the clipped ones go,
+        tensors like them (None: in place).  Storage must stay where it is."""
+        tensors = list(tensors)
+        to = tensors if out is None else list(out)
+        if len(to) != len(tensors):
+            raise ValueError(f"out: expected {len(tensors)} tensors, got {len(to)}")
+        spans = []
+        for i, (g, o) in enumerate(zip(tensors, to)):
+            if g.dtype not in _REAL_TYPES or g.get_device() != self.device or not g.is_contiguous():
+                raise ValueError(f"tensors[{i}]: expected contiguous float32, float16 or bfloat16 on cuda:{self.device}, got {g.dtype} with strides {g.stride()} on {g.device}")
+            if o.dtype is not g.dtype or o.shape != g.shape or o.get_device() != self.device or not o.is_contiguous():
+                raise ValueError(f"out[{i}]: expected contiguous {g.dtype} {list(g.shape)} on cuda:{self.device}, got {o.dtype} {list(o.shape)} with strides {o.stride()} on {o.device}")
+            n = g.numel() * g.element_size()
+            if n:
+                spans.append((g.data_ptr(), n, i))
+                if o.data_ptr() != g.data_ptr():
+                    spans.append((o.data_ptr(), n, i))
+        spans.sort()
+        for (a, n, i), (b, _, j) in zip(spans, spans[1:]):
+            if a + n > b:
+                raise ValueError(f"tensors[{i}] and tensors[{j}] (or their out) share memory")
+        return Gradients(tensors, to, self.device)
+
+    def clip_workspace_bytes(self, gradients: Gradients) -> int:
+        return int(lib().bnn_clip_workspace_bytes(len(gradients.tensors)))
+
+    def clip_gradients(self, gradients: Gradients, max_norm: float, eps: float = 1e-6):
+        """bnn_clip_gradients: scales all tensors by min(1, max_norm / (n + eps)); returns n, their norm before that, as one float32 on the device."""
+        if gradients.device != self.device:
+            raise ValueError(f"gradients: on cuda:{gradients.device}, the context is on cuda:{self.device}")
+        if not (max_norm >= 0 and eps >= 0):
+            raise ValueError(f"max_norm, eps: expected numbers from 0 on, got {max_norm}, {eps}")
+        here = self._here()
+        norm = self._new_vector(1, torch.float32, here)
+        st = lib().bnn_clip_gradients(self._h, gradients.list, len(gradients.tensors), max_norm, eps, norm.data_ptr())
+        if st:
+            self._ck(st, "bnn_clip_gradients")
+        if not here:
+            self._used(*gradients.tensors, *gradients.out)
+        return norm[0]
 
     def dropout(self, x, p: float, seed: int, offset: int = 0, residual=None, out=None):
         """bnn_dropout: residual + (kept ? x / (1 - p) : 0); the backward pass is the same call on the gradient.  out may be x."""

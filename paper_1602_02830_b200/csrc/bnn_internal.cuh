@@ -64,3 +64,7 @@ int bnn_join_columns(bnn_ctx *ctx, int dtype, const float *part, int64_t pitch, 
 int bnn_tensor_map16(bnn_ctx *ctx, CUtensorMap *map, const void *base, int64_t rows, int64_t cols, int64_t ld, int box_rows, int box_cols);
 // The error word of the product kernels; read and cleared (bnn_product.cu)
 int bnn_product_status(bnn_ctx *ctx, int *code);
+int bnn_mx_product_status(bnn_ctx *ctx, int *code);     // the same of the microscaled products (bnn_mx_product.cu)
+// Tensor map of any type and rank (strides in bytes, of dimensions 1 ..), zeros outside (bnn_umma.cu)
+int bnn_tensor_map(bnn_ctx *ctx, CUtensorMap *map, CUtensorMapDataType type, int rank, const void *base, const uint64_t *dims, const uint64_t *strides,
+                   const uint32_t *box, CUtensorMapSwizzle swizzle);

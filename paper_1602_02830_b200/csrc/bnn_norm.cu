@@ -12,7 +12,7 @@
 //
 // A row lives in the registers of one team of threads: every value is read once and written once.  Sums are float32;
 // the variance is taken around the mean (two reductions), not as a difference of squares.
-#include "bnn_real.cuh"
+#include "bnn_mx.cuh"
 #include "bnn_internal.cuh"
 #include <mutex>
 
@@ -38,6 +38,9 @@ struct NormArgs {
     float *part, *part_gate;           // partial column sums: [CTA][4][D], [unit][D]
     int want;                          // which of the four parameter sums are wanted (bits: pre_w, pre_c, post_w, post_c)
     int64_t groups, chunks, chunk_rows, units;
+    // microscaled output: elements, scales, pitch in elements; normed receives the represented values
+    uint8_t *mx_values, *mx_scales;
+    int mx_limit, mx_four;
 };
 
 constexpr int PRE_W = 1, PRE_C = 2, POST_W = 4, POST_C = 8;
@@ -156,10 +159,36 @@ template <int N> __device__ __forceinline__ void block_sums(float (&v)[N], float
     for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xffffffffu, t, k * G);
 }
 
+// A slot of the normed row: written as it is, or microscaled (MX), where the thread's team has the row's blocks of 32 columns lane by lane in both orders of
+// columns and the values written are those that the elements stand for.  The team covers whole 256 columns, so it writes the padding too.
+template <typename T, bool VEC, bool MX> __device__ __forceinline__ void write_normed(const NormArgs &p, int64_t m, int slot, int tid, int team, float (&v)[8]) {
+    if constexpr (MX) {
+        if constexpr (VEC) {
+            const int c = column<true>(slot, 0, tid, team);
+            if (c >= p.D) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+            }
+            if (p.mx_four) mx_write8<true>(p.mx_values, p.mx_scales, m, c, p.mx_limit, v, p.normed != nullptr);
+            else mx_write8<false>(p.mx_values, p.mx_scales, m, c, p.mx_limit, v, p.normed != nullptr);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int c = column<false>(slot, j, tid, team);
+                if (c >= p.D) v[j] = 0.0f;
+                if (p.mx_four) mx_write1<true>(p.mx_values, p.mx_scales, m, c, p.mx_limit, v[j], p.normed != nullptr);
+                else mx_write1<false>(p.mx_values, p.mx_scales, m, c, p.mx_limit, v[j], p.normed != nullptr);
+            }
+        }
+        if (!p.normed) return;
+    }
+    write8<T, VEC>(static_cast<T *>(p.normed) + m * p.ldn, slot, tid, team, p.D, v);
+}
+
 // One row per CTA: both rows are requested before anything is computed from them.
 // PLAIN: BNN_NORM_RMS without shifts, with a block, both outputs wanted.  Columns beyond D read as zero, which adds nothing to the sums of squares; around a mean
 // (layer norm) they have to be left out.
-template <typename T, int SLOTS, bool VEC> __device__ __forceinline__ void plain_row(const NormArgs &p, int64_t m, float (&buf)[4][32]) {
+template <typename T, int SLOTS, bool VEC, bool MX> __device__ __forceinline__ void plain_row(const NormArgs &p, int64_t m, float (&buf)[4][32]) {
     const int tid = threadIdx.x, team = blockDim.x, warps = team >> 5, warp = tid >> 5, lane = tid & 31;
     const T *pw = static_cast<const T *>(p.post_w), *nw = static_cast<const T *>(p.pre_w);
     // everything is there and nothing is optional inside the loops: weights that are not given are ones
@@ -194,7 +223,6 @@ template <typename T, int SLOTS, bool VEC> __device__ __forceinline__ void plain
     }
     const float r_s = 1.0f / sqrtf(block_sum(q, buf[3], warps, warp, lane) * p.inv_d + p.eps);
     if (p.stats && tid == 0) { p.stats[4 * m] = 0.0f; p.stats[4 * m + 1] = r; p.stats[4 * m + 2] = 0.0f; p.stats[4 * m + 3] = r_s; }
-    out = static_cast<T *>(p.normed) + m * p.ldn;
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
         Eight<T> w;
@@ -202,10 +230,10 @@ template <typename T, int SLOTS, bool VEC> __device__ __forceinline__ void plain
         if (nw) w = read8<T, VEC>(nw, i, tid, team, p.D);
 #pragma unroll
         for (int j = 0; j < 8; ++j) s[i][j] *= r_s * w[j];
-        write8<T, VEC>(out, i, tid, team, p.D, s[i]);
+        write_normed<T, VEC, MX>(p, m, i, tid, team, s[i]);
     }
 }
-template <typename T, int SLOTS, bool VEC> __device__ __forceinline__ void any_row(const NormArgs &p, int64_t m, float (&buf)[4][32]) {
+template <typename T, int SLOTS, bool VEC, bool MX> __device__ __forceinline__ void any_row(const NormArgs &p, int64_t m, float (&buf)[4][32]) {
     const int tid = threadIdx.x, team = blockDim.x, warps = team >> 5, warp = tid >> 5, lane = tid & 31;
     const T *pw = static_cast<const T *>(p.post_w), *pc = static_cast<const T *>(p.post_c);
     const T *nw = static_cast<const T *>(p.pre_w), *nc = static_cast<const T *>(p.pre_c);
@@ -293,7 +321,7 @@ template <typename T, int SLOTS, bool VEC> __device__ __forceinline__ void any_r
     }
     r = 1.0f / sqrtf(block_sum(q, buf[3], warps, warp, lane) * p.inv_d + p.eps);
     if (p.stats && tid == 0) { p.stats[4 * m + 2] = mean; p.stats[4 * m + 3] = r; }
-    if (!p.normed) return;
+    if (!MX && !p.normed) return;
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
         Eight<T> w, c;
@@ -307,16 +335,16 @@ template <typename T, int SLOTS, bool VEC> __device__ __forceinline__ void any_r
         if (nc)
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[i][j] += c[j];
-        write8<T, VEC>(static_cast<T *>(p.normed) + m * p.ldn, i, tid, team, p.D, s[i]);
+        write_normed<T, VEC, MX>(p, m, i, tid, team, s[i]);
     }
 }
-template <typename T, int SLOTS, int THREADS, bool VEC, bool PLAIN>
+template <typename T, int SLOTS, int THREADS, bool VEC, bool PLAIN, bool MX>
 __global__ void __launch_bounds__(THREADS, THREADS <= 256 ? 3 : 1) k_block_norm(const NormArgs p) {
     __shared__ float buf[4][32];
     bnn_pdl_wait();
     bnn_pdl_launch_next();
-    if constexpr (PLAIN) plain_row<T, SLOTS, VEC>(p, blockIdx.x, buf);
-    else any_row<T, SLOTS, VEC>(p, blockIdx.x, buf);
+    if constexpr (PLAIN) plain_row<T, SLOTS, VEC, MX>(p, blockIdx.x, buf);
+    else any_row<T, SLOTS, VEC, MX>(p, blockIdx.x, buf);
 }
 
 // A CTA takes whole units (a unit: chunk_rows rows that share one gate row), so every thread keeps the column sums of its own
@@ -636,14 +664,14 @@ bool norm_vec(const bnn_block_norm_desc *n, int64_t M, const NormArgs &a) {
 // Teams.  Forward: many rows take four slots a thread (few warps per row, few barriers, many rows in flight); few rows one slot (the
 // shortest chain).  Rows of single elements: one slot up to 2048 columns (1000 x 1011 float32, both passes: 41 us with four, 34 with one), then two and four,
 // so that at most 256 threads wait at a barrier and several rows share an SM (4096 x 4097 bf16: 119 us with one, 93 with four).
-template <typename T, bool VEC> int launch_forward(bnn_ctx *ctx, const NormArgs &a) {
+template <typename T, bool VEC, bool MX> int launch_forward(bnn_ctx *ctx, const NormArgs &a) {
     const int groups = (a.D + 7) / 8;
     const bool few = a.M <= 2 * ctx->sm_count || (!VEC && groups <= 256);
     const int slots = groups > 1024 ? 4 : (few || groups <= 32) ? 1 : groups <= (VEC ? 64 : 512) ? 2 : 4;
     const int team = ((groups + slots - 1) / slots + 31) & ~31;
     const dim3 grid((unsigned)a.M), block(team);
-    const bool plain = VEC && !a.layer && !a.post_c && !a.pre_c && a.block && a.stream && a.pre && a.normed;
-#define BNN_FORWARD(SLOTS, THREADS) BNN_CUDA_TRY(ctx, bnn_launch_dependent(plain ? k_block_norm<T, SLOTS, THREADS, VEC, VEC> : k_block_norm<T, SLOTS, THREADS, VEC, false>, \
+    const bool plain = VEC && !a.layer && !a.post_c && !a.pre_c && a.block && a.stream && a.pre && (MX || a.normed);
+#define BNN_FORWARD(SLOTS, THREADS) BNN_CUDA_TRY(ctx, bnn_launch_dependent(plain ? k_block_norm<T, SLOTS, THREADS, VEC, VEC, MX> : k_block_norm<T, SLOTS, THREADS, VEC, false, MX>, \
                                                                            grid, block, 0, ctx->stream, a))
     if (slots == 1) BNN_FORWARD(1, 1024);
     else if (slots == 2) BNN_FORWARD(2, 256);
@@ -732,27 +760,47 @@ int bnn_join_columns(bnn_ctx *ctx, int dtype, const float *part, int64_t pitch, 
     return launch_join(ctx, dtype, j, 1);
 }
 
-extern "C" int bnn_block_norm(bnn_ctx *ctx, const bnn_block_norm_desc *norm, const void *x, int64_t ldx, const void *block, int64_t ldb,
-                              int64_t M, void *stream, int64_t lds, void *normed, int64_t ldn, float *stats) {
+namespace {
+// The forward pass of both entry points: normed as it is, or microscaled into q with normed for the represented values.
+template <bool MX> int block_norm(bnn_ctx *ctx, const bnn_block_norm_desc *norm, const void *x, int64_t ldx, const void *block, int64_t ldb, int64_t M, void *stream,
+                                  int64_t lds, const bnn_mx_matrix *q, void *normed, int64_t ldn, float *stats) {
     if (int st = check_norm(norm, M)) return st;
     const int size = bnn_real_size(norm->dtype);
     if (!block && M > 0 && (norm->post || norm->gate)) return BNN_ERR_INVALID_ARG;
-    if (normed && !norm->pre) return BNN_ERR_INVALID_ARG;
+    if ((MX || normed) && !norm->pre) return BNN_ERR_INVALID_ARG;
     if (int st = bnn_check_real(x, ldx, M, norm->D, size)) return st;
     if (int st = bnn_check_real_opt(block, ldb, M, norm->D, size)) return st;
     if (int st = bnn_check_real_opt(stream, lds, M, norm->D, size)) return st;
     if (int st = bnn_check_real_opt(normed, ldn, M, norm->D, size)) return st;
     if (int st = bnn_check_real_opt(stats, 4, M, 4, 4)) return st;
+    if (MX) {
+        if (int st = bnn_check_mx(q)) return st;
+        if (q->rows != M || q->cols != norm->D) return BNN_ERR_INVALID_ARG;
+    }
     if (!ctx) return BNN_ERR_INVALID_ARG;
     if (M == 0) return BNN_OK;
     bnn_device_guard guard(ctx);
     if (!guard.ok) return BNN_ERR_CUDA;
     NormArgs a = norm_args(norm, M);
     a.x = x; a.ldx = ldx; a.block = block; a.ldb = ldb; a.stream = stream; a.lds = lds; a.normed = normed; a.ldn = ldn; a.stats = stats;
+    if (MX) {
+        a.mx_values = static_cast<uint8_t *>(q->values); a.mx_scales = static_cast<uint8_t *>(q->scales);
+        a.mx_limit = (int)bnn_mx_groups(norm->D) * BNN_MX_GROUP; a.mx_four = q->format == BNN_MX_E2M1;
+    }
     const bool vec = norm_vec(norm, M, a);
-    if (norm->dtype == BNN_F32) return vec ? launch_forward<float, true>(ctx, a) : launch_forward<float, false>(ctx, a);
-    if (norm->dtype == BNN_F16) return vec ? launch_forward<__half, true>(ctx, a) : launch_forward<__half, false>(ctx, a);
-    return vec ? launch_forward<__nv_bfloat16, true>(ctx, a) : launch_forward<__nv_bfloat16, false>(ctx, a);
+    if (norm->dtype == BNN_F32) return vec ? launch_forward<float, true, MX>(ctx, a) : launch_forward<float, false, MX>(ctx, a);
+    if (norm->dtype == BNN_F16) return vec ? launch_forward<__half, true, MX>(ctx, a) : launch_forward<__half, false, MX>(ctx, a);
+    return vec ? launch_forward<__nv_bfloat16, true, MX>(ctx, a) : launch_forward<__nv_bfloat16, false, MX>(ctx, a);
+}
+}  // namespace
+
+extern "C" int bnn_block_norm(bnn_ctx *ctx, const bnn_block_norm_desc *norm, const void *x, int64_t ldx, const void *block, int64_t ldb,
+                              int64_t M, void *stream, int64_t lds, void *normed, int64_t ldn, float *stats) {
+    return block_norm<false>(ctx, norm, x, ldx, block, ldb, M, stream, lds, nullptr, normed, ldn, stats);
+}
+extern "C" int bnn_block_norm_mx(bnn_ctx *ctx, const bnn_block_norm_desc *norm, const void *x, int64_t ldx, const void *block, int64_t ldb, int64_t M,
+                                 void *stream, int64_t lds, const bnn_mx_matrix *normed, void *represented, int64_t ldv, float *stats) {
+    return block_norm<true>(ctx, norm, x, ldx, block, ldb, M, stream, lds, normed, represented, ldv, stats);
 }
 
 extern "C" size_t bnn_block_norm_workspace_bytes(const bnn_block_norm_desc *norm, int64_t M) {

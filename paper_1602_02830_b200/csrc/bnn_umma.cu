@@ -1734,6 +1734,17 @@ int bnn_tensor_map16(bnn_ctx *ctx, CUtensorMap *map, const void *base, int64_t r
     return BNN_OK;
 }
 
+int bnn_tensor_map(bnn_ctx *ctx, CUtensorMap *map, CUtensorMapDataType type, int rank, const void *base, const uint64_t *dims, const uint64_t *strides,
+                   const uint32_t *box, CUtensorMapSwizzle swizzle) {
+    encode_fn_t enc;
+    if (int st = get_encode(ctx, &enc)) return st;
+    const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+    const CUresult r = enc(map, type, (cuuint32_t)rank, const_cast<void *>(base), reinterpret_cast<const cuuint64_t *>(dims), reinterpret_cast<const cuuint64_t *>(strides),
+                           box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) { ctx->last_cuda_error = (int)r; return BNN_ERR_CUDA; }
+    return BNN_OK;
+}
+
 // Reads (and clears) the error word the tensor-core kernel sets when one of its bounded waits gives up.
 // Synchronises the context's stream.
 #ifdef BNN_TRACE
@@ -1786,5 +1797,7 @@ extern "C" int bnn_device_status(bnn_ctx *ctx) {
     if (code != 0) BNN_CUDA_TRY(ctx, cudaMemcpyToSymbol(g_umma_error, &zero, sizeof(int)));
     int product = 0;
     if (int st = bnn_product_status(ctx, &product)) return st;
-    return code != 0 || product != 0 ? BNN_ERR_DEVICE_STATUS : BNN_OK;
+    int mx = 0;
+    if (int st = bnn_mx_product_status(ctx, &mx)) return st;
+    return code != 0 || product != 0 || mx != 0 ? BNN_ERR_DEVICE_STATUS : BNN_OK;
 }
