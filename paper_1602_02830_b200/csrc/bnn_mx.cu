@@ -16,53 +16,75 @@ struct MxArgs {
 // A warp takes 256 columns of a row, ROWS rows one after another, all of which it requests before it computes.
 constexpr int WARPS = 8, ROWS = 2, CHUNK = 256;
 
+// Eight neighbouring elements of a row that begins at `row` and has `cols`, from column c on, packed as in memory; zeros behind the end.  Rows off the 16-byte rule are
+// read as aligned words of four bytes, shifted into place where they begin in the middle of one; the half words at both ends of a row are read alone.
+template <typename T> __device__ __forceinline__ void read_words(const T *row, int64_t c, int64_t cols, uint32_t (&w)[2 * sizeof(T)]) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = c + i < cols ? __float_as_uint(row[c + i]) : 0u;
+    } else {
+        const uintptr_t begin = reinterpret_cast<uintptr_t>(row), end = begin + 2 * (uintptr_t)cols, at = begin + 2 * (uintptr_t)c, from = at & ~uintptr_t(3);
+        const bool odd = at & 2;
+        uint32_t t[5];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) {
+            const uintptr_t p = from + 4 * i;
+            t[i] = 0u;
+            if (i == 4 && !odd) continue;
+            if (p >= begin && p + 4 <= end) t[i] = *reinterpret_cast<const uint32_t *>(p);
+            else if (p >= begin && p < end) t[i] = *reinterpret_cast<const uint16_t *>(p);
+            else if (p < begin && p + 2 < end) t[i] = (uint32_t)*reinterpret_cast<const uint16_t *>(p + 2) << 16;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = odd ? __funnelshift_r(t[i], t[i + 1], 16) : t[i];
+    }
+}
+
 template <typename T, bool VEC, bool FOUR>
 __global__ void __launch_bounds__(WARPS * 32) k_mx_quantize(const __grid_constant__ MxArgs p) {
+    constexpr int WORDS = (int)sizeof(T) / 2;
+    __shared__ __align__(16) uint4 stage[VEC ? 1 : WARPS][VEC ? 1 : 32 * WORDS];
     bnn_pdl_wait();
     bnn_pdl_launch_next();
     const int64_t group = blockIdx.x / p.chunks, c0 = (blockIdx.x - group * p.chunks) * CHUNK;
-    const int64_t first = (group * WARPS + (threadIdx.x >> 5)) * ROWS;
-    const int lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t first = (group * WARPS + warp) * ROWS, c = c0 + lane * 8;
     const T *x = static_cast<const T *>(p.x);
     T *out = static_cast<T *>(p.out);
-    if constexpr (VEC) {
-        constexpr int WORDS = (int)sizeof(T) / 2;
-        const int64_t c = c0 + lane * 8;
-        uint4 w[ROWS][WORDS];
+    uint4 w[ROWS][WORDS];
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r)
+    for (int r = 0; r < ROWS; ++r) {
 #pragma unroll
-            for (int i = 0; i < WORDS; ++i) {
-                w[r][i] = make_uint4(0u, 0u, 0u, 0u);
-                if (first + r < p.rows && c < p.cols) w[r][i] = reinterpret_cast<const uint4 *>(x + (first + r) * p.ldx + c)[i];
-            }
+        for (int i = 0; i < WORDS; ++i) w[r][i] = make_uint4(0u, 0u, 0u, 0u);
+        if (first + r >= p.rows || c >= p.cols) continue;
+        if constexpr (VEC) {
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            if (first + r >= p.rows) break;
-            float v[8];
-            unpack8<T>(w[r], v);
-            mx_write8<FOUR>(p.values, p.scales, first + r, c, p.limit, v, out != nullptr);
-            if (out && c < p.cols) store8(out + (first + r) * p.ldo + c, v);
+            for (int i = 0; i < WORDS; ++i) w[r][i] = reinterpret_cast<const uint4 *>(x + (first + r) * p.ldx + c)[i];
+        } else {
+            uint32_t t[4 * WORDS];
+            read_words<T>(x + (first + r) * p.ldx, c, p.cols, t);
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) w[r][i] = make_uint4(t[4 * i], t[4 * i + 1], t[4 * i + 2], t[4 * i + 3]);
         }
-    } else {
-        float v[ROWS][8];
+    }
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r)
+    for (int r = 0; r < ROWS; ++r) {
+        if (first + r >= p.rows) break;
+        float v[8];
+        unpack8<T>(w[r], v);
+        mx_write8<FOUR>(p.values, p.scales, first + r, c, p.limit, v, out != nullptr);
+        if (!out) continue;
+        if constexpr (VEC) {
+            if (c < p.cols) store8(out + (first + r) * p.ldo + c, v);
+        } else {
+            // neighbouring lanes write neighbouring elements
+            T *mine = reinterpret_cast<T *>(stage[warp]);
+            store8(mine + lane * 8, v);
+            __syncwarp();
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int64_t c = c0 + j * 32 + lane;
-                v[r][j] = first + r < p.rows && c < p.cols ? to_f32(x[(first + r) * p.ldx + c]) : 0.0f;
-            }
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            if (first + r >= p.rows) break;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int64_t c = c0 + j * 32 + lane;
-                if (c0 + j * 32 >= p.limit) break;
-                mx_write1<FOUR>(p.values, p.scales, first + r, c, p.limit, v[r][j], out != nullptr);
-                if (out && c < p.cols) out[(first + r) * p.ldo + c] = from_f32<T>(v[r][j]);
-            }
+            for (int j = 0; j < 8; ++j)
+                if (c0 + j * 32 + lane < p.cols) out[(first + r) * p.ldo + c0 + j * 32 + lane] = mine[j * 32 + lane];
+            __syncwarp();
         }
     }
 }

@@ -28,6 +28,13 @@ struct MxCommon : Common {
 
 constexpr uint32_t ROWS128 = 128 * 128;  // bytes of 128 rows of a stage
 
+// One lane of a warp that is together.  What leads the tensor cores and the copies runs warp-wide and lets one lane issue: descriptors, addresses and counters are then the
+// same for all lanes and stay in the registers that those instructions take them from.
+__device__ __forceinline__ bool elected() {
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
+}
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
@@ -65,48 +72,106 @@ template <int CTAS, bool FOUR> __device__ __forceinline__ void step_mx(uint32_t 
     }
 }
 
-// 32 columns of the lane's row, results of which are microscaled: one block a lane.  Columns behind the last are zeros whatever the accumulators hold (scales
-// of weight rows that do not exist may be NaN); the row's padding up to 128 columns is written too.
-template <int EPI, typename T>
-__device__ __forceinline__ void finish_mx_block(const MxCommon &p, const Output &q, int64_t m0, int64_t n0, uint32_t acc, uint32_t acc2) {
-    const int n = (int)(q.N - n0 < 32 ? q.N - n0 : 32), lane = threadIdx.x & 31;
-    float v[32];
+// Two float32 values in one instruction.
+__device__ __forceinline__ unsigned long long pair_of(float a, float b) {
+    unsigned long long w;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(w) : "f"(a), "f"(b));
+    return w;
+}
+__device__ __forceinline__ void pair_out(unsigned long long w, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(w)); }
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
+    unsigned long long d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
+    unsigned long long d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ unsigned long long both(float v) { return pair_of(v, v); }
+__device__ __forceinline__ float exp2_of(float v) { float r; asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
+__device__ __forceinline__ float inverse_of(float v) { float r; asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
+constexpr float LOG2E = 1.44269504f;
+// z sigmoid(u), u given as -u log2 e.
+__device__ __forceinline__ unsigned long long times_sigmoid(unsigned long long z, unsigned long long minus_u) {
+    float a, b;
+    pair_out(minus_u, a, b);
+    const unsigned long long d = add2(pair_of(exp2_of(a), exp2_of(b)), both(1.0f));
+    pair_out(d, a, b);
+    return mul2(z, pair_of(inverse_of(a), inverse_of(b)));
+}
+// gelu(z) = max(z, 0) - |z| Phi(-|z|), Phi as in normal_cdf (bnn_real.cuh).  Past |z| = 100 the second term is 0 and stays 0.
+__device__ __forceinline__ unsigned long long gelu2(unsigned long long z) {
+    float a, b;
+    pair_out(z, a, b);
+    const float ra = a < 0.0f ? 0.0f : a, rb = b < 0.0f ? 0.0f : b;
+    const unsigned long long size = pair_of(fminf(fabsf(a), 100.0f), fminf(fabsf(b), 100.0f));
+    pair_out(mul2(mul2(z, z), both(-0.5f * LOG2E)), a, b);
+    const unsigned long long e = pair_of(exp2_of(a), exp2_of(b));
+    pair_out(fma2(size, both(0.26516503f), both(1.0f)), a, b);
+    const unsigned long long t = pair_of(inverse_of(a), inverse_of(b));
+    unsigned long long s = fma2(t, both(-0.0675475374f), both(0.193967491f));
+    s = fma2(t, s, both(-0.0647966936f));
+    s = fma2(t, s, both(0.141529396f));
+    s = fma2(t, s, both(0.0833328068f));
+    s = fma2(t, s, both(0.107844487f));
+    s = fma2(t, s, both(0.105669729f));
+    s = mul2(mul2(mul2(t, s), e), size);
+    pair_out(s, a, b);
+    return pair_of(ra - a, rb - b);
+}
+// The activation of sixteen values.  Measured against one value an instruction (4096 x 4096 outputs, K = 128): gelu 36 us then.
+__device__ __forceinline__ void activate(int act, float (&v)[16]) {
+#define BNN_EACH_PAIR(EXPRESSION)                              \
+    _Pragma("unroll") for (int j = 0; j < 16; j += 2) {        \
+        const unsigned long long z = pair_of(v[j], v[j + 1]);  \
+        pair_out(EXPRESSION, v[j], v[j + 1]);                  \
+    }
+    switch (act) {
+        case BNN_ACT_NONE: break;
+        case BNN_ACT_GELU: BNN_EACH_PAIR(gelu2(z)); break;
+        case BNN_ACT_GELU_TANH:
+            BNN_EACH_PAIR(times_sigmoid(z, mul2(z, fma2(mul2(z, z), both(-GELU_2C * GELU_A * LOG2E), both(-GELU_2C * LOG2E)))));
+            break;
+        case BNN_ACT_SILU: BNN_EACH_PAIR(times_sigmoid(z, mul2(z, both(-LOG2E)))); break;
+        case BNN_ACT_SIGMOID: act16<BNN_ACT_SIGMOID>(v); break;
+        case BNN_ACT_RELU: act16<BNN_ACT_RELU>(v); break;
+        default: act16<BNN_ACT_HTANH>(v); break;
+    }
+#undef BNN_EACH_PAIR
+}
+
+// Results that are microscaled: a lane's 32 columns are a block.  Columns behind the last are zeros whatever the accumulators hold (scales of weight rows
+// that do not exist may be NaN); the row's padding up to 128 columns is written too.
+__device__ __forceinline__ void write_block(const MxCommon &p, const Output &q, int64_t m, int64_t n0, float (&v)[32]) {
+    const int n = (int)(q.N - n0 < 32 ? q.N - n0 : 32);
+    if (n < 32) {
 #pragma unroll
-    for (int c = 0; c < 32; c += 16) {
-        uint32_t ra[16], rb[16];
-        tmem_ld16(acc + c, ra);
-        if (EPI == BNN_EPI_GATED) tmem_ld16(acc2 + c, rb);
-        tmem_ld_wait16(ra);
-        if (EPI == BNN_EPI_GATED) tmem_ld_wait16(rb);
-        float a[16];
-#pragma unroll
-        for (int j = 0; j < 16; ++j) a[j] = q.k_iters ? __uint_as_float(ra[j]) : 0.0f;
-        if (EPI == BNN_EPI_LINEAR && p.bias && n > c) add_bias16<T>(bias_of(p, n0 + c, n - c < 16 ? n - c : 16), a);
-#define BNN_CALL(ACT) act16<ACT>(a)
-        BNN_EACH_ACT(BNN_CALL)
-#undef BNN_CALL
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            if (EPI == BNN_EPI_GATED) a[j] *= q.k_iters ? __uint_as_float(rb[j]) : 0.0f;
-            v[c + j] = c + j < n ? a[j] : 0.0f;
-        }
+        for (int j = 0; j < 32; ++j) v[j] = j < n ? v[j] : 0.0f;
     }
     uint32_t top = 0;
 #pragma unroll
     for (int j = 0; j < 32; ++j) top = max(top, mx_magnitude(v[j]));
     const uint32_t scale = p.q_four ? mx_scale<true>(top) : mx_scale<false>(top);
-    const float down = mx_down(scale);
+    const unsigned long long down = both(mx_down(scale));
+#pragma unroll
+    for (int j = 0; j < 32; j += 2) pair_out(mul2(pair_of(v[j], v[j + 1]), down), v[j], v[j + 1]);
     uint32_t w[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         float e[8];
         uint32_t t[2];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = v[8 * i + j] * down;
+        for (int j = 0; j < 8; ++j) e[j] = v[8 * i + j];
         if (p.q_four) { mx_encode8<true>(e, t); w[i] = t[0]; }
         else { mx_encode8<false>(e, t); w[2 * i] = t[0]; w[2 * i + 1] = t[1]; }
     }
-    const int64_t m = m0 + lane;
     if (m >= q.M || n0 >= p.q_limit) return;
     if (p.q_four) *reinterpret_cast<uint4 *>(p.q_values + m * (p.q_limit / 2) + n0 / 2) = make_uint4(w[0], w[1], w[2], w[3]);
     else {
@@ -115,6 +180,122 @@ __device__ __forceinline__ void finish_mx_block(const MxCommon &p, const Output 
         to[1] = make_uint4(w[4], w[5], w[6], w[7]);
     }
     p.q_scales[mx_scale_at(m, n0 >> 5, p.q_limit >> 7)] = (uint8_t)scale;
+}
+
+// 32 bytes, one sector of memory.
+__device__ __forceinline__ void read_sector(const void *from, uint32_t (&w)[8]) {
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(from) : "memory");
+}
+__device__ __forceinline__ void write_sector(void *to, const uint32_t (&w)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+// What is added to a warp's 32 rows x 16 columns: the lane's row, 32 bytes.  Where rows are not whole sectors (vec below 3) or the piece of the matrix is not whole,
+// it passes through the warp's piece of shared memory, neighbouring lanes at neighbouring elements.
+__device__ __forceinline__ void read_added(uint32_t (&in)[8], const uint16_t *first, int64_t ld, int rows) {
+    const int lane = threadIdx.x & 31;
+    if (lane < rows) read_sector(first + lane * ld, in);
+}
+// (The functions that are not inlined take no arrays, which would have to be in memory, and none of these kernels may spill registers around them: with twelve
+// bytes spilled, a warp's first piece of the residual came from the columns of another.)
+__device__ __noinline__ void land16(const uint16_t *first, int64_t ld, int rows, int n, uint8_t *piece) {
+    const int lane = threadIdx.x & 31, c = lane & 15;
+    uint16_t v[16];                                              // two rows a pass, all on their way
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v[k] = 2 * k + (lane >> 4) < rows && c < n ? first[(2 * k + (lane >> 4)) * ld + c] : (uint16_t)0;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) *word_of<uint16_t>(piece, 2 * k + (lane >> 4), c) = v[k];
+    __syncwarp();
+}
+__device__ __forceinline__ void pass_added(uint32_t (&in)[8], const uint16_t *first, int64_t ld, int rows, int n, uint8_t *piece) {
+    land16(first, ld, rows, n, piece);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint4 w = *unit_of(piece, threadIdx.x & 31, i);
+        in[4 * i] = w.x; in[4 * i + 1] = w.y; in[4 * i + 2] = w.z; in[4 * i + 3] = w.w;
+    }
+    __syncwarp();
+}
+__device__ __noinline__ void flush_out(uint16_t *first, int64_t ld, int vec, int rows, int n, uint8_t *piece) { flush<uint16_t, 16>(first, ld, vec, rows, n, piece); }
+__device__ __forceinline__ void flush_pre(float *first, int64_t ld, int vec, int rows, int n, uint8_t *piece) { flush<float, 16>(first, ld, vec, rows, n, piece); }
+// Sixteen values of the lane's row, as words, to rows that are not whole sectors.
+__device__ __forceinline__ void pass_out(const uint32_t (&w)[8], uint16_t *first, int64_t ld, int vec, int rows, int n, uint8_t *piece) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) *unit_of(piece, threadIdx.x & 31, i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    flush_out(first, ld, vec, rows, n, piece);
+}
+__device__ __forceinline__ void keep(const MxCommon &p, int64_t row, int64_t n0, int rows, int n, uint8_t *piece, const float (&v)[16]) {
+    float *to = p.pre + row * p.ldp + n0;
+    if (p.vec_pre == 3 && n == 16) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            uint32_t w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[8 * i + j]);
+            if ((int)(threadIdx.x & 31) < rows) write_sector(to + (threadIdx.x & 31) * p.ldp + 8 * i, w);
+        }
+    } else {
+        put16<float>(piece, 0, v);
+        flush_pre(to, p.ldp, p.vec_pre < 2 ? p.vec_pre : 2, rows, n, piece);
+    }
+}
+
+// A warp's 32 rows from m0 on, sixteen columns from n0 on, one row a lane: accumulators a (and b: gated), what is added in `in`.  One short path that all
+// warps run through again and again: blocks of 32 columns and both halves unrolled waited for instructions a fifth of the time.
+enum { OUT_PLAIN, OUT_PRE, OUT_MX };
+template <int EPI, typename T, bool PRE>
+__device__ __forceinline__ void finish16(const MxCommon &p, const Output &q, int64_t m0, int64_t n0, bool adds, const uint32_t (&in)[8], uint8_t *piece, float (&a)[16], float (&b)[16]) {
+    constexpr bool GATED = EPI == BNN_EPI_GATED;
+    const int lane = threadIdx.x & 31, rows = (int)(q.M - m0 < 32 ? q.M - m0 : 32), n = (int)(q.N - n0 < 16 ? q.N - n0 : 16);
+    if (!GATED && p.bias) add_bias16<T>(bias_of(p, n0, n), a);
+    if constexpr (PRE) {
+        keep(p, m0, n0, rows, n, piece, a);
+        if constexpr (GATED) keep(p, q.M + m0, n0, rows, n, piece, b);
+    }
+    activate(p.act, a);
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if (GATED) { a[2 * j] *= b[2 * j]; a[2 * j + 1] *= b[2 * j + 1]; }
+        else if (adds) {
+            const float2 d = unpack2<T>(in[j]);
+            a[2 * j] += d.x; a[2 * j + 1] += d.y;
+        }
+        w[j] = pack2<T>(a[2 * j], a[2 * j + 1]);
+    }
+    uint16_t *to = static_cast<uint16_t *>(q.out[0]) + m0 * q.ldo[0] + n0;
+    if (q.vec_out == 3 && n == 16) {
+        if (lane < rows) write_sector(to + lane * q.ldo[0], w);
+    } else pass_out(w, to, q.ldo[0], q.vec_out < 2 ? q.vec_out : 2, rows, n, piece);
+}
+// 32 columns for a microscaled result.  held: its columns of the accumulator that has been taken out of tensor memory, the only one or, gated, the
+// gate's (UP false) or the other (UP true); the second comes from `acc`.
+template <int EPI, typename T, bool UP>
+__device__ __forceinline__ void finish_mx(const MxCommon &p, const Output &q, int64_t m0, int64_t n0, uint32_t acc, const uint32_t (&held)[32]) {
+    constexpr bool GATED = EPI == BNN_EPI_GATED;
+    const int n = (int)(q.N - n0 < BLOCK ? q.N - n0 : BLOCK);
+    float all[32];
+#pragma unroll
+    for (int c = 0; c < BLOCK; c += CHUNK) {
+        float a[16], b[16];
+        if constexpr (GATED) {
+            uint32_t r[16];
+            tmem_ld16(acc + c, r);
+            tmem_ld_wait16(r);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                a[j] = __uint_as_float(UP ? r[j] : held[c + j]);
+                b[j] = __uint_as_float(UP ? held[c + j] : r[j]);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) a[j] = __uint_as_float(held[c + j]);
+            if (p.bias && n > c) add_bias16<T>(bias_of(p, n0 + c, n - c < 16 ? n - c : 16), a);
+        }
+        activate(p.act, a);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) all[c + j] = GATED ? a[j] * b[j] : a[j];
+    }
+    write_block(p, q, m0 + (threadIdx.x & 31), n0, all);
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -126,11 +307,12 @@ __device__ __forceinline__ void finish_mx_block(const MxCommon &p, const Output 
 //   the others    epilogue
 // Each of the two producers makes every K step, so the ring may have any number of stages: a stage is full with the bytes of all four.
 // Tensor memory: two accumulators of 256 columns and 48 of scales are more than there is.  The accumulators overlap by 64 columns: the epilogue
-// takes the blocks that they share first, the first one from above and the second from below, and hands them over before it goes on with the rest.
-constexpr int STAGES = 5, BAND = 8;
+// takes the blocks that they share first, from above in the first one and from below in the second, and hands them over before it computes.
+constexpr int STAGES = 5, BAND = 8, EPI_WARPS = 16, PAIR_THREADS = (EPI_WARPS + 3) * 32;
 constexpr uint32_t STAGE = 35 * 1024, X_SCALES = 2 * ROWS128, W_SCALES = X_SCALES + 1024;       // x, weights, scales of x, scales of weights
 constexpr uint32_t ACC2 = 192, SCALES = 448, SCALE_SET = 32;      // columns: second accumulator, scales (two sets: 8 of x, 16 of weights)
-constexpr int SHARED_BLOCKS = 2;
+constexpr int SHARED = 64;               // columns that both accumulators have
+static_assert(ACC2 + SHARED == 256, "of 256 each");
 
 struct PairArgs : MxCommon {
     Output q;
@@ -163,36 +345,40 @@ template <bool FOUR> __device__ __forceinline__ void issue_pair(const PairArgs &
     const int k_iters = p.q.k_iters;
     constexpr int GROUPS = FOUR ? 2 : 1;
     for (uint32_t t = pair; t < p.tiles && ok; t += pairs, ++count) {
-        if (count > 0 && !wait(ctl, p.wait_ns, &ctl->acc_empty, (count - 1) & 1)) { fail(ctl, 4); ok = false; break; }
+        if (count > 0 && !warp_wait(ctl, p.wait_ns, &ctl->acc_empty, (count - 1) & 1)) { fail(ctl, 4); ok = false; break; }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t d = tmem + (count & 1) * ACC2;
         for (int kit = 0; kit < k_iters; ++kit) {
-            if (!wait(ctl, p.wait_ns, &ctl->full[stage], phase)) { fail(ctl, 2); ok = false; break; }
+            if (!warp_wait(ctl, p.wait_ns, &ctl->full[stage], phase)) { fail(ctl, 2); ok = false; break; }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint64_t at = (uint64_t)(stage * (STAGE >> 4));
             const uint32_t sx = tmem + SCALES + set * SCALE_SET, sw = sx + 8;
+            if (elected()) {
 #pragma unroll
-            for (int g = 0; g < GROUPS; ++g) {
-                copy_scales<2>(sx + 4 * g, xs0 + at + 32 * g);
-                copy_scales<2>(sw + 8 * g, ws0 + at + 32 * g);                        // columns 0 .. 127 of the tile
-                copy_scales<2>(sw + 8 * g + 4, ws0 + at + 32 * (GROUPS + g));         // and 128 .. 255
+                for (int g = 0; g < GROUPS; ++g) {
+                    copy_scales<2>(sx + 4 * g, xs0 + at + 32 * g);
+                    copy_scales<2>(sw + 8 * g, ws0 + at + 32 * g);                        // columns 0 .. 127 of the tile
+                    copy_scales<2>(sw + 8 * g + 4, ws0 + at + 32 * (GROUPS + g));         // and 128 .. 255
+                }
+                step_mx<2, FOUR>(d, a0 + at, b0 + at, p.idesc, sx, sw, 8, kit == k_iters - 1 ? p.last : 4, kit == 0);
+                umma_commit_2sm(smem_u32(&ctl->empty[stage]));
             }
-            step_mx<2, FOUR>(d, a0 + at, b0 + at, p.idesc, sx, sw, 8, kit == k_iters - 1 ? p.last : 4, kit == 0);
-            umma_commit_2sm(smem_u32(&ctl->empty[stage]));
+            __syncwarp();
             set ^= 1;
             if (++stage == STAGES) { stage = 0; phase ^= 1; }
         }
-        umma_commit_2sm(smem_u32(&ctl->acc_full[count & 1]));
+        if (elected()) umma_commit_2sm(smem_u32(&ctl->acc_full[count & 1]));
+        __syncwarp();
     }
-    umma_commit_2sm(smem_u32(&ctl->drain));      // the MMAs issued end before tensor memory is given back, also where nobody waits for them any more
-    wait(ctl, DRAIN_NS, &ctl->drain, 0, false);
+    if (elected()) umma_commit_2sm(smem_u32(&ctl->drain));      // the MMAs issued end before tensor memory is given back, also where nobody waits for them any more
+    __syncwarp();
+    warp_wait(ctl, DRAIN_NS, &ctl->drain, 0, false);
 }
 
-enum { OUT_PLAIN, OUT_PRE, OUT_MX };
-template <int EPI, int OUT, int EPI_WARPS>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__((EPI_WARPS + 3) * 32, 1) k_mx_pair(const __grid_constant__ PairArgs p) {
+template <int EPI, int OUT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1) k_mx_pair(const __grid_constant__ PairArgs p) {
     constexpr bool GATED = EPI == BNN_EPI_GATED;
-    constexpr int WIDTH = GATED ? 128 : 256, PARTS = EPI_WARPS / 4, BLOCKS = WIDTH / 32;
+    constexpr int WIDTH = GATED ? 128 : 256, PARTS = EPI_WARPS / 4;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *tiles = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     Control *ctl = reinterpret_cast<Control *>(tiles + STAGES * STAGE);
@@ -220,7 +406,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__((EPI_WARPS + 3) * 32
     if (warp == 0 || warp == 2 + EPI_WARPS) {
         // ---------------- producers.  The "full" barrier of a stage (in CTA 0) completes with the arrival of CTA 0's first producer and the bytes of both
         // producers of both CTAs.
-        if (lane == 0 && !p.drop_loads) {
+        if (!p.drop_loads) {
             const bool weights = warp != 0;
             const int groups = p.four ? 2 : 1;      // of 128 columns in a stage; the coordinate of the elements counts bytes, or nibbles on their way to bytes: 128 a stage
             bool ok = true;
@@ -231,9 +417,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__((EPI_WARPS + 3) * 32
                 tile_at<WIDTH>(p, t, m0, n0);
                 m0 += (int)rank * 128;
                 for (int kit = 0; kit < p.q.k_iters; ++kit) {
-                    if (lap > 0 && !wait(ctl, p.wait_ns, &ctl->empty[stage], (lap - 1) & 1)) { fail(ctl, 1); ok = false; break; }
+                    if (lap > 0 && !warp_wait(ctl, p.wait_ns, &ctl->empty[stage], (lap - 1) & 1)) { fail(ctl, 1); ok = false; break; }
                     const uint32_t dst = smem_u32(tiles + stage * STAGE), bar = smem_u32(&ctl->full[stage]) & PEER_MASK;
-                    if (!weights) {
+                    if (!elected()) {
+                    } else if (!weights) {
                         if (rank == 0) mbar_expect_tx(smem_u32(&ctl->full[stage]), 2 * (ROWS128 + p.w_bytes + 3 * groups * BNN_MX_TILE));
                         tma_load_2d_2sm(dst, &p.maps.x, kit * 128, m0, bar);
                         tma_load_3d_2sm(dst + X_SCALES, &p.maps.xs, 0, kit * groups, m0 >> 7, bar);
@@ -245,6 +432,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__((EPI_WARPS + 3) * 32
                         tma_load_2d_2sm(dst + ROWS128, &p.maps.w[0], kit * 128, n0 + (int)rank * 128, bar);
                         tma_load_3d_2sm(dst + W_SCALES, &p.maps.ws[0], 0, kit * groups, n0 >> 7, bar);
                     }
+                    __syncwarp();
                     if (++stage == STAGES) { stage = 0; ++lap; }
                 }
             }
@@ -254,11 +442,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__((EPI_WARPS + 3) * 32
                 for (uint32_t i = 0, s = stage, l = lap; i < (uint32_t)STAGES; ++i) {      // this thread's last uses, newest first
                     if (s == 0) { if (l == 0) break; s = STAGES; --l; }
                     --s;
-                    if (!wait(ctl, DRAIN_NS, &ctl->full[s], l & 1, false)) break;
+                    if (!warp_wait(ctl, DRAIN_NS, &ctl->full[s], l & 1, false)) break;
                 }
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
             if (p.four) issue_pair<true>(p, ctl, tiles, tmem_base, pair, pairs);
             else issue_pair<false>(p, ctl, tiles, tmem_base, pair, pairs);
         }
@@ -275,44 +463,64 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__((EPI_WARPS + 3) * 32
             tile_at<WIDTH>(p, t, tm0, tn0);
             const int64_t m0 = tm0 + (int)rank * 128 + 32 * quad;
             const int rows = (int)(q.M - m0 < 32 ? q.M - m0 : 32);
-            // the i-th block of this warp: from above in the first accumulator, from below in the second, so that what they share comes first
-            const auto block_at = [&](int i) { const int k = i * PARTS + part; return buf ? k : BLOCKS - 1 - k; };
-            // the residual is requested a block ahead, the first one while the tile is being multiplied
-            const bool adds = OUT != OUT_MX && EPI == BNN_EPI_LINEAR && p.add != nullptr;
+            const uint32_t acc = tmem_base + buf * ACC2 + ((uint32_t)(32 * quad) << 16);
+            // the i-th piece of this warp: from above in the first accumulator, from below in the second, so that what they share comes first
+            constexpr int EACH = OUT == OUT_MX ? BLOCK : CHUNK, PIECES = WIDTH / EACH, MINE = PIECES / PARTS;
+            constexpr int LAST_SHARED = SHARED / EACH <= PARTS ? 0 : SHARED / EACH / PARTS - 1;       // of this warp's pieces
+            static_assert(PIECES % PARTS == 0, "every warp has as many pieces");
+            const auto column_of = [&](int i) { const int k = i * PARTS + part; return (buf ? k : PIECES - 1 - k) * EACH; };
+            const bool adds = OUT != OUT_MX && !GATED && p.add != nullptr;
             const uint16_t *add = static_cast<const uint16_t *>(p.add) + m0 * p.ld_add + tn0;
-            Incoming in;
+            uint32_t in[8];
             const auto ask = [&](int i) {
-                const int c = block_at(i) * 32, n = (int)(q.N - tn0 - c);
-                if (adds && p.vec_add == 2 && rows > 0 && n > 0) request(in, add + c, p.ld_add, rows, n);
+                const int c = column_of(i);
+                if (adds && p.vec_add == 3 && rows > 0 && q.N - tn0 - c >= CHUNK) read_added(in, add + c, p.ld_add, rows);
             };
-            if (part < BLOCKS) ask(0);
+            // The residual is requested a piece ahead, the first one while the tile is being multiplied; with pre-activations to keep there are no registers for that.
+            constexpr bool AHEAD = OUT == OUT_PLAIN;
+            if (AHEAD) ask(0);
             if (!warp_wait(ctl, p.wait_ns, &ctl->acc_full[buf], (count >> 1) & 1)) { fail(ctl, 3); break; }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t acc = tmem_base + buf * ACC2 + ((uint32_t)(32 * quad) << 16);
-            const auto hand_over = [&]() {
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive_cta0(smem_u32(&ctl->acc_empty));
-            };
-            if (part >= SHARED_BLOCKS) hand_over();
+            // Gated: the accumulators share columns of the up rows of the first and of the gate rows of the second.
+            const uint32_t first = acc + (GATED && !buf ? WIDTH : 0), second = acc + (GATED && buf ? WIDTH : 0);
 #pragma unroll 1
-            for (int i = 0; i * PARTS + part < BLOCKS; ++i) {
-                const int c = block_at(i) * 32, n = (int)(q.N - tn0 - c);
+            for (int i = 0; i < MINE; ++i) {
+                const int c = column_of(i), n = (int)(q.N - tn0 - c);
+                uint32_t r[EACH], other[CHUNK];
                 if constexpr (OUT == OUT_MX) {
-                    if (rows > 0 && tn0 + c < p.q_limit) {
-                        if (p.f16) finish_mx_block<EPI, __half>(p, q, m0, tn0 + c, acc + c, acc + WIDTH + c);
-                        else finish_mx_block<EPI, __nv_bfloat16>(p, q, m0, tn0 + c, acc + c, acc + WIDTH + c);
-                    }
+                    tmem_ld32(first + c, r);
+                    tmem_ld_wait(r);
                 } else {
-                    const bool there = n > 0 && rows > 0;
-                    if (adds && there) land(in, add + c, p.ld_add, p.vec_add, rows, n, piece);
-                    if ((i + 1) * PARTS + part < BLOCKS) ask(i + 1);
-                    if (there) {
-                        if (p.f16) finish_block<EPI, __half, OUT == OUT_PRE>(p, q, m0, tn0 + c, acc + c, acc + WIDTH + c, piece);
-                        else finish_block<EPI, __nv_bfloat16, OUT == OUT_PRE>(p, q, m0, tn0 + c, acc + c, acc + WIDTH + c, piece);
-                    }
+                    tmem_ld16(acc + c, r);
+                    if (GATED) tmem_ld16(acc + WIDTH + c, other);
+                    tmem_ld_wait16(r);
+                    if (GATED) tmem_ld_wait16(other);
                 }
-                if (i == 0 && part < SHARED_BLOCKS) hand_over();
+                if (i == LAST_SHARED) {
+                    // this warp has read its share of the columns that the next tile's MMAs write
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cta0(smem_u32(&ctl->acc_empty));
+                }
+                const bool there = rows > 0 && (OUT == OUT_MX ? tn0 + c < p.q_limit : n > 0);
+                if constexpr (OUT == OUT_MX) {
+                    if (!there) continue;
+                    if (GATED && !buf) finish_mx<EPI, __nv_bfloat16, GATED>(p, q, m0, tn0 + c, second + c, r);      // without bias nothing is of the 16-bit type
+                    else if (!GATED && p.f16) finish_mx<EPI, __half, false>(p, q, m0, tn0 + c, second + c, r);
+                    else finish_mx<EPI, __nv_bfloat16, false>(p, q, m0, tn0 + c, second + c, r);
+                } else if (there) {
+                    if (!AHEAD) ask(i);
+                    if (adds && (p.vec_add != 3 || n < CHUNK)) pass_added(in, add + c, p.ld_add, rows, n < CHUNK ? n : CHUNK, piece);
+                    float a[CHUNK], b[CHUNK];
+#pragma unroll
+                    for (int j = 0; j < CHUNK; ++j) {
+                        a[j] = __uint_as_float(r[j]);
+                        if (GATED) b[j] = __uint_as_float(other[j]);
+                    }
+                    if (p.f16) finish16<EPI, __half, OUT == OUT_PRE>(p, q, m0, tn0 + c, adds, in, piece, a, b);
+                    else finish16<EPI, __nv_bfloat16, OUT == OUT_PRE>(p, q, m0, tn0 + c, adds, in, piece, a, b);
+                }
+                if (AHEAD && i + 1 < MINE) ask(i + 1);
             }
         }
     }
@@ -334,8 +542,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__((EPI_WARPS + 3) * 32
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
     }
 }
-constexpr size_t pair_smem(int epi_warps) { return (size_t)STAGES * STAGE + sizeof(Control) + epi_warps * PIECE + 1024; }
-static_assert(pair_smem(16) <= 227 * 1024, "fits the shared memory of an SM");
+constexpr size_t PAIR_SMEM = (size_t)STAGES * STAGE + sizeof(Control) + EPI_WARPS * PIECE + 1024;
+static_assert(PAIR_SMEM <= 227 * 1024, "fits the shared memory of an SM");
 static_assert(BNN_MX_TILE * 3 * 2 + 2 * ROWS128 <= STAGE && STAGE % 1024 == 0, "a stage holds both operands and their scales");
 
 // ---------------------------------------------------------------------------------------------------------
@@ -376,26 +584,30 @@ template <bool FOUR, bool GATED> __device__ __forceinline__ void issue_few(const
     int stage = 0;
     uint32_t phase = 0, set = 0;
     for (int kit = first; kit < last; ++kit) {
-        if (!wait(ctl, f.wait_ns, &ctl->full[stage], phase)) { few_fail(ctl, 22); break; }
+        if (!warp_wait(ctl, f.wait_ns, &ctl->full[stage], phase)) { few_fail(ctl, 22); break; }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint64_t at = (uint64_t)(stage * (f.stage_bytes >> 4));
         // a set: for each group of 128 of K four columns of each half's weights, then for each group those of the tokens
         const uint32_t sw = tmem + f.scales + set * f.scale_set, sx = sw + 4 * GROUPS * HALVES;
-#pragma unroll
-        for (int i = 0; i < GROUPS * HALVES; ++i) copy_scales<1>(sw + 4 * i, ws0 + at + 32 * i);
-        for (int i = 0; i < x_tiles; ++i)
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g) copy_scales<1>(sx + f.x_pitch * g + 4 * i, xs0 + at + 32 * (i * GROUPS + g));
         const int count = kit == f.q.k_iters - 1 ? f.last : 4;
+        if (elected()) {
 #pragma unroll
-        for (int h = 0; h < HALVES; ++h)
-            step_mx<1, FOUR>(tmem + h * f.acc_up, a0 + at + h * (ROWS128 >> 4), b0 + at, f.idesc, sw + 4 * GROUPS * h, sx + shift, f.x_pitch, count, kit == first);
-        mma_commit(&ctl->empty[stage]);
+            for (int i = 0; i < GROUPS * HALVES; ++i) copy_scales<1>(sw + 4 * i, ws0 + at + 32 * i);
+            for (int i = 0; i < x_tiles; ++i)
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g) copy_scales<1>(sx + f.x_pitch * g + 4 * i, xs0 + at + 32 * (i * GROUPS + g));
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h)
+                step_mx<1, FOUR>(tmem + h * f.acc_up, a0 + at + h * (ROWS128 >> 4), b0 + at, f.idesc, sw + 4 * GROUPS * h, sx + shift, f.x_pitch, count, kit == first);
+            mma_commit(&ctl->empty[stage]);
+        }
+        __syncwarp();
         set ^= 1;
         if (++stage == f.stages) { stage = 0; phase ^= 1; }
     }
-    mma_commit(&ctl->acc_full);
-    wait(ctl, DRAIN_NS, &ctl->acc_full, 0, false);       // the MMAs issued end before tensor memory is given back, also where the epilogue has given up
+    if (elected()) mma_commit(&ctl->acc_full);
+    __syncwarp();
+    warp_wait(ctl, DRAIN_NS, &ctl->acc_full, 0, false);       // the MMAs issued end before tensor memory is given back, also where the epilogue has given up
 }
 
 // Four neighbouring outputs of one token, microscaled: eight neighbouring lanes hold a block.  All lanes of the warp take part; `there`: the token exists.
@@ -456,35 +668,36 @@ template <int EPI, bool MX> __global__ void __launch_bounds__(FEW_THREADS, 2) k_
     bnn_pdl_launch_next();
 
     if (warp == 0 || warp == FEW_THREADS / 32 - 1) {
-        if (lane == 0 && !f.drop_loads) {
+        if (!f.drop_loads) {
             const int mine = warp == 0 ? 0 : 1, groups = f.four ? 2 : 1;
             int stage = mine % f.stages, lap = mine / f.stages;
             for (int kit = first + mine; kit < last; kit += 2) {
-                if (lap > 0 && !wait(ctl, f.wait_ns, &ctl->empty[stage], (lap - 1) & 1)) { few_fail(ctl, 21); break; }
+                if (lap > 0 && !warp_wait(ctl, f.wait_ns, &ctl->empty[stage], (lap - 1) & 1)) { few_fail(ctl, 21); break; }
                 const uint32_t dst = smem_u32(tiles) + stage * f.stage_bytes, bar = smem_u32(&ctl->full[stage]);
-                mbar_expect_tx(bar, f.loaded);
+                if (elected()) {
+                    mbar_expect_tx(bar, f.loaded);
 #pragma unroll
-                for (int h = 0; h < HALVES; ++h) {
-                    tma_load_2d(dst + h * ROWS128, &f.maps.w[h], kit * 128, (int)n0, bar);
-                    tma_load_3d(dst + f.ws_at + h * groups * BNN_MX_TILE, &f.maps.ws[h], 0, kit * groups, (int)(n0 >> 7), bar);
+                    for (int h = 0; h < HALVES; ++h) {
+                        tma_load_2d(dst + h * ROWS128, &f.maps.w[h], kit * 128, (int)n0, bar);
+                        tma_load_3d(dst + f.ws_at + h * groups * BNN_MX_TILE, &f.maps.ws[h], 0, kit * groups, (int)(n0 >> 7), bar);
+                    }
+                    tma_load_2d(dst + f.x_at, &f.maps.x, kit * 128, (int)t0, bar);
+                    tma_load_3d(dst + f.xs_at, &f.maps.xs, 0, kit * groups, (int)(t0 >> 7), bar);
                 }
-                tma_load_2d(dst + f.x_at, &f.maps.x, kit * 128, (int)t0, bar);
-                tma_load_3d(dst + f.xs_at, &f.maps.xs, 0, kit * groups, (int)(t0 >> 7), bar);
+                __syncwarp();
                 stage += 2;
                 while (stage >= f.stages) { stage -= f.stages; ++lap; }
             }
             for (int i = 0, s = stage, l = lap; i < f.stages; i += 2) {            // copies in flight land before the shared memory is given up, as above
                 s -= 2;
                 while (s < 0) { s += f.stages; --l; }
-                if (l < 0 || !wait(ctl, DRAIN_NS, &ctl->full[s], l & 1, false)) break;
+                if (l < 0 || !warp_wait(ctl, DRAIN_NS, &ctl->full[s], l & 1, false)) break;
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            const int shift = (int)(t0 >> 5) & 3;        // columns of the first token within its tile of scales
-            if (f.four) issue_few<true, GATED>(f, ctl, tiles, tmem_base, first, last, shift);
-            else issue_few<false, GATED>(f, ctl, tiles, tmem_base, first, last, shift);
-        }
+        const int shift = (int)(t0 >> 5) & 3;        // columns of the first token within its tile of scales
+        if (f.four) issue_few<true, GATED>(f, ctl, tiles, tmem_base, first, last, shift);
+        else issue_few<false, GATED>(f, ctl, tiles, tmem_base, first, last, shift);
     }
     // Rank r finishes the tile's outputs r * out .. r * out + out - 1 of every token.  A lane of warps 2 .. 9 holds one weight row of the
     // partial tile and stores it where it is needed: parts[rank it comes from][token][row of the finishing rank's share], the gate rows of
@@ -554,17 +767,17 @@ template <int EPI, bool MX> __global__ void __launch_bounds__(FEW_THREADS, 2) k_
 
 // ---------------------------------------------------------------------------------------------------------
 // Opts in to the shared memory and asks how many pairs fit the device, once per device and kernel; 0 = cannot run.
-template <int EPI, int OUT, int WARPS> int pairs_of(int device, int sm_count) {
+template <int EPI, int OUT> int pairs_of(int device, int sm_count) {
     static std::mutex lock;
     static int cached[64];
     if (device < 0 || device >= 64) return 0;
     std::lock_guard<std::mutex> guard(lock);
     if (cached[device] == 0) {
-        auto kernel = k_mx_pair<EPI, OUT, WARPS>;
+        auto kernel = k_mx_pair<EPI, OUT>;
         int pairs = 0;
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pair_smem(WARPS)) == cudaSuccess) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PAIR_SMEM) == cudaSuccess) {
             cudaLaunchConfig_t cfg = {};
-            cfg.gridDim = dim3(2 * sm_count); cfg.blockDim = dim3((WARPS + 3) * 32); cfg.dynamicSmemBytes = pair_smem(WARPS);
+            cfg.gridDim = dim3(2 * sm_count); cfg.blockDim = dim3(PAIR_THREADS); cfg.dynamicSmemBytes = PAIR_SMEM;
             cudaLaunchAttribute attr;
             attr.id = cudaLaunchAttributeClusterDimension;
             attr.val.clusterDim.x = 2; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
@@ -576,11 +789,11 @@ template <int EPI, int OUT, int WARPS> int pairs_of(int device, int sm_count) {
     }
     return cached[device] > 0 ? cached[device] : 0;
 }
-template <int EPI, int OUT, int WARPS> int launch_pair(bnn_ctx *ctx, const PairArgs &a) {
-    const int pairs = pairs_of<EPI, OUT, WARPS>(ctx->device, ctx->sm_count);
+template <int EPI, int OUT> int launch_pair(bnn_ctx *ctx, const PairArgs &a) {
+    const int pairs = pairs_of<EPI, OUT>(ctx->device, ctx->sm_count);
     if (pairs == 0) return BNN_ERR_CUDA;
     const unsigned n = a.tiles < (uint32_t)pairs ? a.tiles : (unsigned)pairs;
-    BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_mx_pair<EPI, OUT, WARPS>, dim3(2 * n), dim3((WARPS + 3) * 32), pair_smem(WARPS), ctx->stream, a));
+    BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_mx_pair<EPI, OUT>, dim3(2 * n), dim3(PAIR_THREADS), PAIR_SMEM, ctx->stream, a));
     return bnn_check_launch(ctx);
 }
 template <int EPI, bool MX> int launch_few(bnn_ctx *ctx, const FewArgs &f, unsigned tiles, unsigned split) {
@@ -670,7 +883,6 @@ int map_operands(bnn_ctx *ctx, MxMaps &m, const Call &c, int x_rows, int x_tiles
     return BNN_OK;
 }
 
-constexpr int LONG_SUM = 32;             // K steps from which eight epilogue warps do: bnn_product.cu
 int product_pair(bnn_ctx *ctx, const Call &c) {
     PairArgs a{};
     common_args(a, a.q, ctx, c);
@@ -679,18 +891,12 @@ int product_pair(bnn_ctx *ctx, const Call &c) {
     if (tiles_m * tiles_n > 0x7fffffff) return BNN_ERR_INVALID_ARG;
     a.tiles_m = (uint32_t)tiles_m; a.tiles_n = (uint32_t)tiles_n; a.tiles = (uint32_t)(tiles_m * tiles_n);
     a.idesc = instruction(a.four, c.x->format, c.w[0]->format, 256, 256);
-    a.q.vec_out = width_of(c.out, c.ldo, a.q.M, 2);
-    a.vec_bias = width_of(c.bias, 0, 1, 2); a.vec_add = width_of(c.add, c.ld_add, a.q.M, 2); a.vec_pre = width_of(c.pre, c.ldp, 2 * a.q.M, 4);
+    const auto sectors = [](const void *at, int64_t ld, int64_t rows) { return (reinterpret_cast<uintptr_t>(at) | (rows > 1 ? (uint64_t)ld * 2 : 0)) % 32 == 0 ? 3 : width_of(at, ld, rows, 2); };
+    a.q.vec_out = sectors(c.out, c.ldo, a.q.M); a.vec_add = sectors(c.add, c.ld_add, a.q.M);
+    a.vec_bias = width_of(c.bias, 0, 1, 2); a.vec_pre = width_of(c.pre, c.ldp, 2 * a.q.M, 4);
     if (int st = map_operands(ctx, a.maps, c, 128, 1, gated ? 1 : 2)) return st;
-    const bool lean = a.q.k_iters < LONG_SUM;
-    if (gated) {
-        if (c.pre) return launch_pair<BNN_EPI_GATED, OUT_PRE, 8>(ctx, a);
-        if (c.q) return lean ? launch_pair<BNN_EPI_GATED, OUT_MX, 16>(ctx, a) : launch_pair<BNN_EPI_GATED, OUT_MX, 8>(ctx, a);
-        return lean ? launch_pair<BNN_EPI_GATED, OUT_PLAIN, 16>(ctx, a) : launch_pair<BNN_EPI_GATED, OUT_PLAIN, 8>(ctx, a);
-    }
-    if (c.pre) return launch_pair<BNN_EPI_LINEAR, OUT_PRE, 8>(ctx, a);
-    if (c.q) return lean ? launch_pair<BNN_EPI_LINEAR, OUT_MX, 16>(ctx, a) : launch_pair<BNN_EPI_LINEAR, OUT_MX, 8>(ctx, a);
-    return lean ? launch_pair<BNN_EPI_LINEAR, OUT_PLAIN, 16>(ctx, a) : launch_pair<BNN_EPI_LINEAR, OUT_PLAIN, 8>(ctx, a);
+    if (gated) return c.pre ? launch_pair<BNN_EPI_GATED, OUT_PRE>(ctx, a) : c.q ? launch_pair<BNN_EPI_GATED, OUT_MX>(ctx, a) : launch_pair<BNN_EPI_GATED, OUT_PLAIN>(ctx, a);
+    return c.pre ? launch_pair<BNN_EPI_LINEAR, OUT_PRE>(ctx, a) : c.q ? launch_pair<BNN_EPI_LINEAR, OUT_MX>(ctx, a) : launch_pair<BNN_EPI_LINEAR, OUT_PLAIN>(ctx, a);
 }
 
 // Which kernel, and how k_mx_few divides the work: the estimates of the 16-bit products, whose K steps move and multiply as many bytes.
@@ -769,7 +975,7 @@ int product(bnn_ctx *ctx, const Call &c) {
     bnn_device_guard guard(ctx);
     if (!guard.ok) return BNN_ERR_CUDA;
     const FewPlan plan = few_plan(c);
-    return plan.cost < pair_cost(ctx, c) ? product_few(ctx, c, plan) : product_pair(ctx, c);
+    return c.x->cols == 0 || plan.cost < pair_cost(ctx, c) ? product_few(ctx, c, plan) : product_pair(ctx, c);
 }
 // x e2m1: weights e2m1; x e4m3: weights of either format.
 int check_operands(const bnn_mx_matrix *w, const bnn_mx_matrix *x) {
