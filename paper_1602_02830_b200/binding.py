@@ -292,7 +292,7 @@ class Context:
             raise BnnError(st, what, lib().bnn_last_cuda_error(self._h))
 
     def empty(self, *shape, dtype=torch.int32):
-        return torch.empty(*shape, dtype=dtype, device=f"cuda:{self.device}")
+        return torch.empty(*shape, dtype=dtype, device=self._device)
 
     # -- plumbing ------------------------------------------------------------------------------
     def set_workspace(self, ws: "torch.Tensor | None"):
@@ -871,7 +871,9 @@ class Context:
         tp = self._stats(stats, M)
         if stream is None:
             stream = self._new(M, D, dtype, here)
-        sp, lds = self._fit(stream, M, D, dtype, "stream")
+            sp, lds = stream.data_ptr(), D
+        else:
+            sp, lds = self._fit(stream, M, D, dtype, "stream")
         if out is None:
             out = self.make_mx(M, D, format or "e4m3")
         st = lib().bnn_block_norm_mx(self._h, layer.ref, xp, ldx, bp, ldb, M, sp, lds, self._mx(out, M, D, "out"), vp, ldv, tp)
@@ -910,28 +912,31 @@ class Context:
         layer.format = Wg.format
         return layer
 
-    def _mx_inputs(self, layer, x):
-        if getattr(layer, "format", None) is None:
-            raise ValueError("layer: expected one of microscaled weights (make_mx_linear, make_mx_gated)")
+    def _mx_inputs(self, layer, x, kind, made):
+        if type(layer.desc) is not kind:
+            raise ValueError(f"layer: expected one of microscaled weights, made by {made}")
         self._on(layer)
-        if not isinstance(x, MxMatrix):
+        if type(x) is not MxMatrix:
             raise ValueError(f"x: expected a microscaled matrix (mx_quantize, block_norm_mx), got {type(x).__name__}")
         if x.format == "e2m1" and layer.format != "e2m1":
             raise ValueError("x: e2m1 inputs go with e2m1 weights")
-        return self._mx(x, x.rows, layer.inner, "x"), x.rows, layer.outer
+        return self._mx(x, x.rows, layer.inner, "x")
 
     def mx_linear(self, layer: Layer, x: MxMatrix, residual=None, out=None, pre=None):
         """bnn_mx_linear.  x: e4m3 (weights of either format) or e2m1 (weights too).  out: a matrix of the layer's type (may be residual), or an MxMatrix
         that receives y microscaled (without residual and pre).  pre: float32 [M, N] that receives x W^T + bias for linear_backward."""
-        ref, M, N = self._mx_inputs(layer, x)
-        if not isinstance(layer.desc, MxLinearDesc):
-            raise ValueError("layer: expected one made by make_mx_linear")
-        dtype, here = layer.dtype, self._here()
+        ref = self._mx_inputs(layer, x, MxLinearDesc, "make_mx_linear")
+        M, N, dtype, here = x.rows, layer.outer, layer.dtype, self._here()
         rp, ldr = self._fit(residual, M, N, dtype, "residual")
         pp, ldp = self._fit(pre, M, N, torch.float32, "pre")
-        op, ldo, qp = self._mx_out(out, M, N, dtype, here, residual is not None or pre is not None)
+        qp = None
         if out is None:
-            out, op, ldo = op, op.data_ptr(), ldo
+            out = self._new(M, N, dtype, here)
+            op, ldo = out.data_ptr(), N
+        elif type(out) is MxMatrix:
+            op, ldo, qp = None, 0, self._mx_out(out, M, N, residual is not None or pre is not None)
+        else:
+            op, ldo = self._fit(out, M, N, dtype, "out")
         st = lib().bnn_mx_linear(self._h, layer.ref, ref, rp, ldr, op, ldo, pp, ldp, qp)
         if st:
             self._ck(st, "bnn_mx_linear")
@@ -941,14 +946,17 @@ class Context:
 
     def mx_gated(self, layer: Layer, x: MxMatrix, out=None, pre=None):
         """bnn_mx_gated.  x and out as in mx_linear.  pre: contiguous float32 [2, M, N] for gated_backward."""
-        ref, M, N = self._mx_inputs(layer, x)
-        if not isinstance(layer.desc, MxGatedDesc):
-            raise ValueError("layer: expected one made by make_mx_gated")
-        dtype, here = layer.dtype, self._here()
+        ref = self._mx_inputs(layer, x, MxGatedDesc, "make_mx_gated")
+        M, N, dtype, here = x.rows, layer.outer, layer.dtype, self._here()
         pp, ldp = self._planes(pre, M, N)
-        op, ldo, qp = self._mx_out(out, M, N, dtype, here, pre is not None)
+        qp = None
         if out is None:
-            out, op, ldo = op, op.data_ptr(), ldo
+            out = self._new(M, N, dtype, here)
+            op, ldo = out.data_ptr(), N
+        elif type(out) is MxMatrix:
+            op, ldo, qp = None, 0, self._mx_out(out, M, N, pre is not None)
+        else:
+            op, ldo = self._fit(out, M, N, dtype, "out")
         st = lib().bnn_mx_gated(self._h, layer.ref, ref, op, ldo, pp, ldp, qp)
         if st:
             self._ck(st, "bnn_mx_gated")
@@ -956,19 +964,14 @@ class Context:
             self._used(x.values, x.scales, pre, *self._memory(out), *layer.tensors)
         return out
 
-    def _mx_out(self, out, M, N, dtype, here, more):
-        """(address or, for no out, a new matrix; leading dimension; microscaled matrix)."""
-        if out is None:
-            return self._new(M, N, dtype, here), N, None
-        if isinstance(out, MxMatrix):
-            if more:
-                raise ValueError("out: microscaled results come without residual and pre")
-            return None, 0, self._mx(out, M, N, "out")
-        return *self._fit(out, M, N, dtype, "out"), None
+    def _mx_out(self, out, M, N, more):
+        if more:
+            raise ValueError("out: microscaled results come without residual and pre")
+        return self._mx(out, M, N, "out")
 
     @staticmethod
     def _memory(out):
-        return (out.values, out.scales) if isinstance(out, MxMatrix) else (out,)
+        return (out.values, out.scales) if type(out) is MxMatrix else (out,)
 
     # -- gradients of a model ----------------------------------------------------------------------------
     def make_gradients(self, tensors, out=None) -> Gradients:
@@ -1005,13 +1008,13 @@ class Context:
         if not (max_norm >= 0 and eps >= 0):
             raise ValueError(f"max_norm, eps: expected numbers from 0 on, got {max_norm}, {eps}")
         here = self._here()
-        norm = self._new_vector(1, torch.float32, here)
+        norm = _empty_strided((), (), dtype=torch.float32, device=self._device) if here else self._new(1, 1, torch.float32, here)[0, 0]
         st = lib().bnn_clip_gradients(self._h, gradients.list, len(gradients.tensors), max_norm, eps, norm.data_ptr())
         if st:
             self._ck(st, "bnn_clip_gradients")
         if not here:
             self._used(*gradients.tensors, *gradients.out)
-        return norm[0]
+        return norm
 
     def dropout(self, x, p: float, seed: int, offset: int = 0, residual=None, out=None):
         """bnn_dropout: residual + (kept ? x / (1 - p) : 0); the backward pass is the same call on the gradient.  out may be x."""

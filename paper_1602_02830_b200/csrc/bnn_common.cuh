@@ -89,7 +89,8 @@ struct bnn_device_guard {
     bool ok = true;
     explicit bnn_device_guard(bnn_ctx *ctx) {
         if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-        if (prev != ctx->device && cudaSetDevice(ctx->device) != cudaSuccess) ok = false;
+        if (prev == ctx->device) prev = -1;              // nothing to restore
+        else if (cudaSetDevice(ctx->device) != cudaSuccess) ok = false;
     }
     ~bnn_device_guard() { if (prev >= 0) cudaSetDevice(prev); }
 };

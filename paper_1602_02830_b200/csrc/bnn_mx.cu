@@ -16,30 +16,6 @@ struct MxArgs {
 // A warp takes 256 columns of a row, ROWS rows one after another, all of which it requests before it computes.
 constexpr int WARPS = 8, ROWS = 2, CHUNK = 256;
 
-// Eight neighbouring elements of a row that begins at `row` and has `cols`, from column c on, packed as in memory; zeros behind the end.  Rows off the 16-byte rule are
-// read as aligned words of four bytes, shifted into place where they begin in the middle of one; the half words at both ends of a row are read alone.
-template <typename T> __device__ __forceinline__ void read_words(const T *row, int64_t c, int64_t cols, uint32_t (&w)[2 * sizeof(T)]) {
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = c + i < cols ? __float_as_uint(row[c + i]) : 0u;
-    } else {
-        const uintptr_t begin = reinterpret_cast<uintptr_t>(row), end = begin + 2 * (uintptr_t)cols, at = begin + 2 * (uintptr_t)c, from = at & ~uintptr_t(3);
-        const bool odd = at & 2;
-        uint32_t t[5];
-#pragma unroll
-        for (int i = 0; i < 5; ++i) {
-            const uintptr_t p = from + 4 * i;
-            t[i] = 0u;
-            if (i == 4 && !odd) continue;
-            if (p >= begin && p + 4 <= end) t[i] = *reinterpret_cast<const uint32_t *>(p);
-            else if (p >= begin && p < end) t[i] = *reinterpret_cast<const uint16_t *>(p);
-            else if (p < begin && p + 2 < end) t[i] = (uint32_t)*reinterpret_cast<const uint16_t *>(p + 2) << 16;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = odd ? __funnelshift_r(t[i], t[i + 1], 16) : t[i];
-    }
-}
-
 template <typename T, bool VEC, bool FOUR>
 __global__ void __launch_bounds__(WARPS * 32) k_mx_quantize(const __grid_constant__ MxArgs p) {
     constexpr int WORDS = (int)sizeof(T) / 2;
@@ -62,7 +38,7 @@ __global__ void __launch_bounds__(WARPS * 32) k_mx_quantize(const __grid_constan
             for (int i = 0; i < WORDS; ++i) w[r][i] = reinterpret_cast<const uint4 *>(x + (first + r) * p.ldx + c)[i];
         } else {
             uint32_t t[4 * WORDS];
-            read_words<T>(x + (first + r) * p.ldx, c, p.cols, t);
+            mx_read_words<T>(x + (first + r) * p.ldx, c, p.cols, t);
 #pragma unroll
             for (int i = 0; i < WORDS; ++i) w[r][i] = make_uint4(t[4 * i], t[4 * i + 1], t[4 * i + 2], t[4 * i + 3]);
         }
@@ -72,19 +48,12 @@ __global__ void __launch_bounds__(WARPS * 32) k_mx_quantize(const __grid_constan
         if (first + r >= p.rows) break;
         float v[8];
         unpack8<T>(w[r], v);
-        mx_write8<FOUR>(p.values, p.scales, first + r, c, p.limit, v, out != nullptr);
+        mx_write8<FOUR>(p.values, p.scales, first + r, c, p.limit, v, out != nullptr, MxExact());
         if (!out) continue;
         if constexpr (VEC) {
             if (c < p.cols) store8(out + (first + r) * p.ldo + c, v);
         } else {
-            // neighbouring lanes write neighbouring elements
-            T *mine = reinterpret_cast<T *>(stage[warp]);
-            store8(mine + lane * 8, v);
-            __syncwarp();
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (c0 + j * 32 + lane < p.cols) out[(first + r) * p.ldo + c0 + j * 32 + lane] = mine[j * 32 + lane];
-            __syncwarp();
+            mx_spread8(out + (first + r) * p.ldo, c0, p.cols, v, reinterpret_cast<T *>(stage[warp]));
         }
     }
 }

@@ -24,6 +24,30 @@ static inline int bnn_check_mx(const bnn_mx_matrix *q) {
 }
 
 #ifdef __CUDACC__
+// Two float32 values in one instruction.
+__device__ __forceinline__ unsigned long long pair_of(float a, float b) {
+    unsigned long long w;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(w) : "f"(a), "f"(b));
+    return w;
+}
+__device__ __forceinline__ void pair_out(unsigned long long w, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(w)); }
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
+    unsigned long long d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
+    unsigned long long d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ unsigned long long both(float v) { return pair_of(v, v); }
+
 __device__ __forceinline__ int64_t mx_scale_at(int64_t row, int64_t block, int64_t groups) {
     return ((row >> 7) * groups + (block >> 2)) * BNN_MX_TILE + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (block & 3);
 }
@@ -76,19 +100,77 @@ template <bool FOUR> __device__ __forceinline__ void mx_decode8(const uint32_t (
 }
 __device__ __forceinline__ uint32_t mx_magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
+// Eight neighbouring elements of a row that begins at `row` and has `cols`, from column c on, packed as in memory; zeros behind the end.  Rows off the 16-byte rule are
+// read as aligned words of four bytes, shifted into place where they begin in the middle of one; the half words at both ends of a row are read alone.
+template <typename T> __device__ __forceinline__ void mx_read_words(const T *row, int64_t c, int64_t cols, uint32_t (&w)[2 * sizeof(T)]) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = c + i < cols ? __float_as_uint(row[c + i]) : 0u;
+    } else {
+        const uintptr_t begin = reinterpret_cast<uintptr_t>(row), end = begin + 2 * (uintptr_t)cols, at = begin + 2 * (uintptr_t)c, from = at & ~uintptr_t(3);
+        const bool odd = at & 2;
+        uint32_t t[5];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) {
+            const uintptr_t p = from + 4 * i;
+            t[i] = 0u;
+            if (i == 4 && !odd) continue;
+            if (p >= begin && p + 4 <= end) t[i] = *reinterpret_cast<const uint32_t *>(p);
+            else if (p >= begin && p < end) t[i] = *reinterpret_cast<const uint16_t *>(p);
+            else if (p < begin && p + 2 < end) t[i] = (uint32_t)*reinterpret_cast<const uint16_t *>(p + 2) << 16;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = odd ? __funnelshift_r(t[i], t[i + 1], 16) : t[i];
+    }
+}
+// Eight values of each lane, neighbouring lanes at neighbouring columns from c0 on, to a row off the 16-byte rule: through the warp's shared memory (256 elements), so that
+// neighbouring lanes write neighbouring elements.  The warp is together.
+template <typename T> __device__ __forceinline__ void mx_spread8(T *row, int64_t c0, int64_t cols, const float (&v)[8], T *stage) {
+    const int lane = threadIdx.x & 31;
+    store8(stage + lane * 8, v);
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (c0 + j * 32 + lane < cols) row[c0 + j * 32 + lane] = stage[j * 32 + lane];
+    __syncwarp();
+}
+
+// Values that are float32 as they stand; or float32 roundings of others: rest(j, v) is then what v lacks.  A value whose rounding lies on the border of two
+// elements, or beside it, goes to the side on which the exact one lies.  (One in 2^20 values rounds to a border: 20 elements of an 8192 x 4096 norm were a step off.)
+struct MxExact { static constexpr bool rounded = false; __device__ float operator()(int, float) const { return 0.0f; } };
+
 // One row's columns c .. c + 7 (c a multiple of 8; zeros behind the last column) of every lane of a warp, lanes next to each other: four neighbouring lanes
 // hold a block, sixteen a group.  All lanes take part; those with c >= limit (the row's pitch in elements, a multiple of 128) write nothing.
-// On return v holds the values that the elements stand for.
-template <bool FOUR> __device__ __forceinline__ void mx_write8(uint8_t *values, uint8_t *scales, int64_t row, int64_t c, int64_t limit, float (&v)[8], bool back) {
+// On return v holds the values that the elements stand for, where they are asked back.
+template <bool FOUR, typename F> __device__ __forceinline__ void mx_write8(uint8_t *values, uint8_t *scales, int64_t row, int64_t c, int64_t limit, float (&v)[8], bool back, const F &rest) {
     uint32_t top = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, mx_magnitude(v[j]));
+    for (int j = 0; j < 8; j += 2) top = __vimax3_u32(top, mx_magnitude(v[j]), mx_magnitude(v[j + 1]));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
     const uint32_t scale = mx_scale<FOUR>(top);
-    const float down = mx_down(scale);
+    const float down = mx_down(scale), up = mx_up(scale);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= down;
+    for (int j = 0; j < 8; j += 2) pair_out(mul2(pair_of(v[j], v[j + 1]), both(down)), v[j], v[j + 1]);
+    if constexpr (F::rounded) {
+        // The bits below an element's (20 of e4m3, 22 of e2m1), moved to the top: a border is the highest of them alone.  (Elements below the smallest normal
+        // one have their borders elsewhere; what is missed there is 2^-15 of the block's largest.)
+        constexpr uint32_t UNIT = FOUR ? 1u << 10 : 1u << 12;
+        uint32_t near = 0xffffffffu;
+#pragma unroll
+        for (int j = 0; j < 8; j += 2)
+            near = __vimin3_u32(near, __float_as_uint(v[j]) * UNIT + (0x80000000u + UNIT), __float_as_uint(v[j + 1]) * UNIT + (0x80000000u + UNIT));
+        if (__builtin_expect(near <= 2 * UNIT, 0)) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t bits = __float_as_uint(v[j]), at = bits * UNIT + (0x80000000u + UNIT);
+                if (at > 2 * UNIT) continue;
+                const uint32_t border = bits + 1 - at / UNIT;
+                const float edge = __uint_as_float(border), d = (v[j] - edge) + rest(j, v[j] * up) * down;
+                v[j] = d == 0.0f || !(fabsf(v[j]) > 0.0f) ? edge : __uint_as_float((d > 0.0f) == (v[j] > 0.0f) ? border + 1 : border - 1);
+            }
+        }
+    }
     uint32_t w[2];
     mx_encode8<FOUR>(v, w);
     const int lane = threadIdx.x & 31;
@@ -101,28 +183,9 @@ template <bool FOUR> __device__ __forceinline__ void mx_write8(uint8_t *values, 
         if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(scales + mx_scale_at(row, c >> 5, limit >> 7)) = four;
     }
     if (back) {
-        const float up = mx_up(scale);
         mx_decode8<FOUR>(w, v);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= up;
-    }
-}
-// The same for one column per lane: the warp's 32 columns c (c of lane 0 a multiple of 32) are a block.
-template <bool FOUR> __device__ __forceinline__ void mx_write1(uint8_t *values, uint8_t *scales, int64_t row, int64_t c, int64_t limit, float &v, bool back) {
-    const uint32_t scale = mx_scale<FOUR>(__reduce_max_sync(0xffffffffu, mx_magnitude(v)));
-    const float e[8] = {v * mx_down(scale), 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    uint32_t w[2];
-    mx_encode8<FOUR>(e, w);
-    const int lane = threadIdx.x & 31;
-    if constexpr (FOUR) {
-        const uint32_t next = __shfl_down_sync(0xffffffffu, w[0] & 15u, 1);
-        if (c < limit && !(lane & 1)) values[row * (limit / 2) + c / 2] = (uint8_t)((w[0] & 15u) | next << 4);
-    } else if (c < limit) values[row * limit + c] = (uint8_t)w[0];
-    if (c < limit && lane == 0) scales[mx_scale_at(row, c >> 5, limit >> 7)] = (uint8_t)scale;
-    if (back) {
-        float d[8];
-        mx_decode8<FOUR>(w, d);
-        v = d[0] * mx_up(scale);
+        for (int j = 0; j < 8; j += 2) pair_out(mul2(pair_of(v[j], v[j + 1]), both(up)), v[j], v[j + 1]);
     }
 }
 #endif

@@ -72,29 +72,6 @@ template <int CTAS, bool FOUR> __device__ __forceinline__ void step_mx(uint32_t 
     }
 }
 
-// Two float32 values in one instruction.
-__device__ __forceinline__ unsigned long long pair_of(float a, float b) {
-    unsigned long long w;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(w) : "f"(a), "f"(b));
-    return w;
-}
-__device__ __forceinline__ void pair_out(unsigned long long w, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(w)); }
-__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
-    unsigned long long d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
-    unsigned long long d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
-    unsigned long long d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ unsigned long long both(float v) { return pair_of(v, v); }
 __device__ __forceinline__ float exp2_of(float v) { float r; asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
 __device__ __forceinline__ float inverse_of(float v) { float r; asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
 constexpr float LOG2E = 1.44269504f;

@@ -41,6 +41,7 @@ struct NormArgs {
     // microscaled output: elements, scales, pitch in elements; normed receives the represented values
     uint8_t *mx_values, *mx_scales;
     int mx_limit, mx_four;
+    float inv_low;                     // 1 / D is inv_d + inv_low
 };
 
 constexpr int PRE_W = 1, PRE_C = 2, POST_W = 4, POST_C = 8;
@@ -159,36 +160,10 @@ template <int N> __device__ __forceinline__ void block_sums(float (&v)[N], float
     for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xffffffffu, t, k * G);
 }
 
-// A slot of the normed row: written as it is, or microscaled (MX), where the thread's team has the row's blocks of 32 columns lane by lane in both orders of
-// columns and the values written are those that the elements stand for.  The team covers whole 256 columns, so it writes the padding too.
-template <typename T, bool VEC, bool MX> __device__ __forceinline__ void write_normed(const NormArgs &p, int64_t m, int slot, int tid, int team, float (&v)[8]) {
-    if constexpr (MX) {
-        if constexpr (VEC) {
-            const int c = column<true>(slot, 0, tid, team);
-            if (c >= p.D) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-            }
-            if (p.mx_four) mx_write8<true>(p.mx_values, p.mx_scales, m, c, p.mx_limit, v, p.normed != nullptr);
-            else mx_write8<false>(p.mx_values, p.mx_scales, m, c, p.mx_limit, v, p.normed != nullptr);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int c = column<false>(slot, j, tid, team);
-                if (c >= p.D) v[j] = 0.0f;
-                if (p.mx_four) mx_write1<true>(p.mx_values, p.mx_scales, m, c, p.mx_limit, v[j], p.normed != nullptr);
-                else mx_write1<false>(p.mx_values, p.mx_scales, m, c, p.mx_limit, v[j], p.normed != nullptr);
-            }
-        }
-        if (!p.normed) return;
-    }
-    write8<T, VEC>(static_cast<T *>(p.normed) + m * p.ldn, slot, tid, team, p.D, v);
-}
-
 // One row per CTA: both rows are requested before anything is computed from them.
 // PLAIN: BNN_NORM_RMS without shifts, with a block, both outputs wanted.  Columns beyond D read as zero, which adds nothing to the sums of squares; around a mean
 // (layer norm) they have to be left out.
-template <typename T, int SLOTS, bool VEC, bool MX> __device__ __forceinline__ void plain_row(const NormArgs &p, int64_t m, float (&buf)[4][32]) {
+template <typename T, int SLOTS, bool VEC> __device__ __forceinline__ void plain_row(const NormArgs &p, int64_t m, float (&buf)[4][32]) {
     const int tid = threadIdx.x, team = blockDim.x, warps = team >> 5, warp = tid >> 5, lane = tid & 31;
     const T *pw = static_cast<const T *>(p.post_w), *nw = static_cast<const T *>(p.pre_w);
     // everything is there and nothing is optional inside the loops: weights that are not given are ones
@@ -223,6 +198,7 @@ template <typename T, int SLOTS, bool VEC, bool MX> __device__ __forceinline__ v
     }
     const float r_s = 1.0f / sqrtf(block_sum(q, buf[3], warps, warp, lane) * p.inv_d + p.eps);
     if (p.stats && tid == 0) { p.stats[4 * m] = 0.0f; p.stats[4 * m + 1] = r; p.stats[4 * m + 2] = 0.0f; p.stats[4 * m + 3] = r_s; }
+    out = static_cast<T *>(p.normed) + m * p.ldn;
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
         Eight<T> w;
@@ -230,10 +206,10 @@ template <typename T, int SLOTS, bool VEC, bool MX> __device__ __forceinline__ v
         if (nw) w = read8<T, VEC>(nw, i, tid, team, p.D);
 #pragma unroll
         for (int j = 0; j < 8; ++j) s[i][j] *= r_s * w[j];
-        write_normed<T, VEC, MX>(p, m, i, tid, team, s[i]);
+        write8<T, VEC>(out, i, tid, team, p.D, s[i]);
     }
 }
-template <typename T, int SLOTS, bool VEC, bool MX> __device__ __forceinline__ void any_row(const NormArgs &p, int64_t m, float (&buf)[4][32]) {
+template <typename T, int SLOTS, bool VEC> __device__ __forceinline__ void any_row(const NormArgs &p, int64_t m, float (&buf)[4][32]) {
     const int tid = threadIdx.x, team = blockDim.x, warps = team >> 5, warp = tid >> 5, lane = tid & 31;
     const T *pw = static_cast<const T *>(p.post_w), *pc = static_cast<const T *>(p.post_c);
     const T *nw = static_cast<const T *>(p.pre_w), *nc = static_cast<const T *>(p.pre_c);
@@ -321,7 +297,7 @@ template <typename T, int SLOTS, bool VEC, bool MX> __device__ __forceinline__ v
     }
     r = 1.0f / sqrtf(block_sum(q, buf[3], warps, warp, lane) * p.inv_d + p.eps);
     if (p.stats && tid == 0) { p.stats[4 * m + 2] = mean; p.stats[4 * m + 3] = r; }
-    if (!MX && !p.normed) return;
+    if (!p.normed) return;
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
         Eight<T> w, c;
@@ -335,16 +311,215 @@ template <typename T, int SLOTS, bool VEC, bool MX> __device__ __forceinline__ v
         if (nc)
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[i][j] += c[j];
-        write_normed<T, VEC, MX>(p, m, i, tid, team, s[i]);
+        write8<T, VEC>(static_cast<T *>(p.normed) + m * p.ldn, i, tid, team, p.D, s[i]);
     }
 }
-template <typename T, int SLOTS, int THREADS, bool VEC, bool PLAIN, bool MX>
+template <typename T, int SLOTS, int THREADS, bool VEC, bool PLAIN>
 __global__ void __launch_bounds__(THREADS, THREADS <= 256 ? 3 : 1) k_block_norm(const NormArgs p) {
     __shared__ float buf[4][32];
     bnn_pdl_wait();
     bnn_pdl_launch_next();
-    if constexpr (PLAIN) plain_row<T, SLOTS, VEC, MX>(p, blockIdx.x, buf);
-    else any_row<T, SLOTS, VEC, MX>(p, blockIdx.x, buf);
+    if constexpr (PLAIN) plain_row<T, SLOTS, VEC>(p, blockIdx.x, buf);
+    else any_row<T, SLOTS, VEC>(p, blockIdx.x, buf);
+}
+
+// The same with the stream's norm microscaled (bnn_mx.cuh).  Eight neighbouring columns a thread and slot whatever the alignment, so that four lanes hold a block.
+// Elements have three or one bits behind the point: what decides an element is on which side of a border its value lies.  So the sums of the warps, the mean square
+// and the reciprocal root are kept in two float32 each (a value and what it lacks), and what a value's float32 rounding lacks is known where it lies beside a border.
+struct Two { float high, low; };
+__device__ __forceinline__ Two two_sum(float a, float b) {       // a + b exactly (Knuth)
+    const float s = __fadd_rn(a, b), t = __fsub_rn(s, a);
+    return {s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t))};
+}
+__device__ __forceinline__ Two two_product(float a, float b) {
+    const float s = __fmul_rn(a, b);
+    return {s, fmaf(a, b, -s)};
+}
+// Mean over the row of the block's sum of `a`, with `add` (eps or 0); 1 / D is inv + inv_low.
+__device__ __forceinline__ Two block_mean(float a, float add, float inv, float inv_low, float *buf, int warps, int warp, int lane) {
+    a = warp_sum(a);
+    Two s{a, 0.0f};
+    if (warps > 1) {
+        if (lane == 0) buf[warp] = a;
+        __syncthreads();
+        s = {buf[0], 0.0f};
+        for (int w = 1; w < warps; ++w) {
+            const Two t = two_sum(s.high, buf[w]);
+            s = {t.high, s.low + t.low};
+        }
+    }
+    const Two t = two_product(s.high, inv), u = two_sum(t.high, add);
+    return {u.high, u.low + (t.low + (s.high * inv_low + s.low * inv))};
+}
+__device__ __forceinline__ Two inverse_root(Two v) {
+    if (!(v.high > 1e-30f && v.high < 1e30f)) return {1.0f / sqrtf(v.high), 0.0f};
+    // r (1 + e / 2), e = 1 - v r^2
+    const float r = rsqrtf(v.high);
+    const Two s = two_product(r, r), t = two_product(v.high, s.high);
+    const float e = ((1.0f - t.high) - t.low) - v.high * s.low - v.low * s.high, low = 0.5f * r * e, high = __fadd_rn(r, low);
+    return {high, __fsub_rn(low, __fsub_rn(high, r))};
+}
+template <typename T, bool VEC> __device__ __forceinline__ Eight<T> take8(const T *row, int slot, int tid, int team, int D) {
+    if constexpr (VEC) return read8<T, true>(row, slot, tid, team, D);
+    else {
+        Eight<T> e;
+        mx_read_words<T>(row, column<true>(slot, 0, tid, team), D, e.w);
+        return e;
+    }
+}
+template <typename T, bool VEC> __device__ __forceinline__ void give8(T *row, int slot, int tid, int team, int D, const float (&v)[8], T *stage) {
+    if constexpr (VEC) write8<T, true>(row, slot, tid, team, D, v);
+    else mx_spread8(row, column<true>(slot, 0, tid & ~31, team), D, v, stage + (tid >> 5) * 256);
+}
+// What u = round(t r + c), t = round(s w), lacks: s w is t and its own rest, r two parts.
+struct NormRest {
+    static constexpr bool rounded = true;
+    const float (&s)[8];
+    const float (&w)[8];
+    const float (&c)[8];
+    Two r;
+    __device__ __forceinline__ float operator()(int j, float u) const {
+        const float t = __fmul_rn(s[j], w[j]);
+        return fmaf(fmaf(s[j], w[j], -t), r.high, fmaf(t, r.low, fmaf(t, r.high, c[j] - u)));
+    }
+};
+template <typename T, bool VEC> __device__ __forceinline__ void spread(const Eight<T> &e, float (&v)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = e[j];
+}
+template <typename T, int SLOTS, int THREADS, bool VEC, bool PLAIN, bool FOUR>
+__global__ void __launch_bounds__(THREADS, THREADS <= 256 ? 3 : 1) k_block_norm_mx(const NormArgs p) {
+    __shared__ float buf[4][32];
+    __shared__ __align__(16) T stage[VEC ? 8 : THREADS * 8];
+    bnn_pdl_wait();
+    bnn_pdl_launch_next();
+    const int64_t m = blockIdx.x;
+    const int tid = threadIdx.x, team = blockDim.x, warps = team >> 5, warp = tid >> 5, lane = tid & 31;
+    const T *pw = static_cast<const T *>(p.post_w), *pc = PLAIN ? nullptr : static_cast<const T *>(p.post_c);
+    const T *nw = static_cast<const T *>(p.pre_w), *nc = PLAIN ? nullptr : static_cast<const T *>(p.pre_c);
+    const bool layer = !PLAIN && p.layer, blocks = PLAIN || p.block;
+    Eight<T> rx[SLOTS], rb[SLOTS];
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+        rx[i] = take8<T, VEC>(static_cast<const T *>(p.x) + m * p.ldx, i, tid, team, p.D);
+        if (blocks) rb[i] = take8<T, VEC>(static_cast<const T *>(p.block) + m * p.ldb, i, tid, team, p.D);
+    }
+    const T *gate = p.gate ? static_cast<const T *>(p.gate) + (m / p.rows_per_gate) * p.ld_gate : nullptr;
+    // the block's norm: mean and reciprocal deviation.  Columns behind D are zeros: around a mean they are left out of the sums.
+    float mean = 0.0f;
+    Two r{1.0f, 0.0f};
+    if (blocks && p.post) {
+        if (layer) {
+            float t = 0.0f;
+#pragma unroll
+            for (int i = 0; i < SLOTS; ++i) {
+                float v = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v += rb[i][j];
+                t += v;
+            }
+            mean = block_mean(t, 0.0f, p.inv_d, p.inv_low, buf[0], warps, warp, lane).high;
+        }
+        float q = 0.0f;
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) {
+            float v = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float d = !layer || column<true>(i, j, tid, team) < p.D ? rb[i][j] - mean : 0.0f;
+                v = fmaf(d, d, v);
+            }
+            q += v;
+        }
+        r = inverse_root(block_mean(q, p.eps, p.inv_d, p.inv_low, buf[1], warps, warp, lane));
+    }
+    if (p.stats && tid == 0) { p.stats[4 * m] = mean; p.stats[4 * m + 1] = r.high; }
+    float s[SLOTS][8], q = 0.0f;
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+        Eight<T> w, g, c;
+        w.fill(1.0f); g.fill(1.0f);
+        if (blocks && pw) w = take8<T, VEC>(pw, i, tid, team, p.D);
+        if (gate) g = take8<T, VEC>(gate, i, tid, team, p.D);
+        if (blocks && pc) c = take8<T, VEC>(pc, i, tid, team, p.D);
+        float v = 0.0f;
+        if constexpr (PLAIN) {
+            unsigned long long squares = both(0.0f);
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                unsigned long long add = mul2(pair_of(rb[i][j], rb[i][j + 1]), pair_of(w[j], w[j + 1]));
+                if (p.post) add = fma2(add, both(r.high), mul2(add, both(r.low)));
+                if (gate) add = mul2(add, pair_of(g[j], g[j + 1]));
+                const unsigned long long sum = fma2(both(p.alpha), pair_of(rx[i][j], rx[i][j + 1]), add);
+                squares = fma2(sum, sum, squares);
+                pair_out(sum, s[i][j], s[i][j + 1]);
+            }
+            float odd;
+            pair_out(squares, v, odd);
+            v += odd;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float add = 0.0f;
+                if (blocks) {
+                    const float t = (rb[i][j] - mean) * w[j];
+                    add = p.post ? fmaf(t, r.high, t * r.low) : t;
+                    if (pc) add += c[j];
+                    if (gate) add *= g[j];
+                }
+                s[i][j] = fmaf(p.alpha, rx[i][j], add);
+                if (layer && column<true>(i, j, tid, team) >= p.D) s[i][j] = 0.0f;      // the block's mean is taken off zeros there
+                v = layer ? v + s[i][j] : fmaf(s[i][j], s[i][j], v);
+            }
+        }
+        q += v;
+        if (PLAIN || p.stream) give8<T, VEC>(static_cast<T *>(p.stream) + m * p.lds, i, tid, team, p.D, s[i], stage);
+    }
+    // the stream's
+    mean = 0.0f;
+    Two of = block_mean(q, layer ? 0.0f : p.eps, p.inv_d, p.inv_low, buf[2], warps, warp, lane);
+    if (layer) {
+        mean = of.high;
+        q = 0.0f;
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) {
+            float v = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                s[i][j] = column<true>(i, j, tid, team) < p.D ? (s[i][j] - mean) - of.low : 0.0f;
+                v = fmaf(s[i][j], s[i][j], v);
+            }
+            q += v;
+        }
+        of = block_mean(q, p.eps, p.inv_d, p.inv_low, buf[3], warps, warp, lane);
+    }
+    r = inverse_root(of);
+    if (p.stats && tid == 0) { p.stats[4 * m + 2] = mean; p.stats[4 * m + 3] = r.high; }
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+        const int c0 = column<true>(i, 0, tid, team);
+        Eight<T> e;
+        e.fill(1.0f);
+        if (nw) e = take8<T, VEC>(nw, i, tid, team, p.D);
+        float w[8], c[8], u[8];
+        spread<T, VEC>(e, w);
+        e.fill(0.0f);
+        if (nc) e = take8<T, VEC>(nc, i, tid, team, p.D);
+        spread<T, VEC>(e, c);
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            const unsigned long long t = mul2(pair_of(s[i][j], s[i][j + 1]), pair_of(w[j], w[j + 1]));
+            pair_out(fma2(t, both(r.high), nc ? fma2(t, both(r.low), pair_of(c[j], c[j + 1])) : mul2(t, both(r.low))), u[j], u[j + 1]);
+        }
+        if (layer) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (c0 + j >= p.D) u[j] = 0.0f;
+        }
+        const NormRest rest{s[i], w, c, r};
+        mx_write8<FOUR>(p.mx_values, p.mx_scales, m, c0, p.mx_limit, u, p.normed != nullptr, rest);
+        if (p.normed) give8<T, VEC>(static_cast<T *>(p.normed) + m * p.ldn, i, tid, team, p.D, u, stage);
+    }
 }
 
 // A CTA takes whole units (a unit: chunk_rows rows that share one gate row), so every thread keeps the column sums of its own
@@ -664,14 +839,31 @@ bool norm_vec(const bnn_block_norm_desc *n, int64_t M, const NormArgs &a) {
 // Teams.  Forward: many rows take four slots a thread (few warps per row, few barriers, many rows in flight); few rows one slot (the
 // shortest chain).  Rows of single elements: one slot up to 2048 columns (1000 x 1011 float32, both passes: 41 us with four, 34 with one), then two and four,
 // so that at most 256 threads wait at a barrier and several rows share an SM (4096 x 4097 bf16: 119 us with one, 93 with four).
-template <typename T, bool VEC, bool MX> int launch_forward(bnn_ctx *ctx, const NormArgs &a) {
+template <typename T, bool VEC> int launch_forward(bnn_ctx *ctx, const NormArgs &a) {
     const int groups = (a.D + 7) / 8;
     const bool few = a.M <= 2 * ctx->sm_count || (!VEC && groups <= 256);
     const int slots = groups > 1024 ? 4 : (few || groups <= 32) ? 1 : groups <= (VEC ? 64 : 512) ? 2 : 4;
     const int team = ((groups + slots - 1) / slots + 31) & ~31;
     const dim3 grid((unsigned)a.M), block(team);
-    const bool plain = VEC && !a.layer && !a.post_c && !a.pre_c && a.block && a.stream && a.pre && (MX || a.normed);
-#define BNN_FORWARD(SLOTS, THREADS) BNN_CUDA_TRY(ctx, bnn_launch_dependent(plain ? k_block_norm<T, SLOTS, THREADS, VEC, VEC, MX> : k_block_norm<T, SLOTS, THREADS, VEC, false, MX>, \
+    const bool plain = VEC && !a.layer && !a.post_c && !a.pre_c && a.block && a.stream && a.pre && a.normed;
+#define BNN_FORWARD(SLOTS, THREADS) BNN_CUDA_TRY(ctx, bnn_launch_dependent(plain ? k_block_norm<T, SLOTS, THREADS, VEC, VEC> : k_block_norm<T, SLOTS, THREADS, VEC, false>, \
+                                                                           grid, block, 0, ctx->stream, a))
+    if (slots == 1) BNN_FORWARD(1, 1024);
+    else if (slots == 2) BNN_FORWARD(2, 256);
+    else if (team <= 256) BNN_FORWARD(4, 256);
+    else BNN_FORWARD(4, 1024);
+#undef BNN_FORWARD
+    return bnn_check_launch(ctx);
+}
+// The same for a microscaled norm; four slots of rows that are not whole 16-byte groups keep their piece of shared memory below 48 KB with 256 threads.
+template <typename T, bool VEC, bool FOUR> int launch_forward_mx(bnn_ctx *ctx, const NormArgs &a) {
+    const int groups = (a.D + 7) / 8;
+    const bool few = a.M <= 2 * ctx->sm_count;
+    const int slots = groups > 1024 ? 4 : (few || groups <= 32) ? 1 : groups <= 64 ? 2 : 4;
+    const int team = ((groups + slots - 1) / slots + 31) & ~31;
+    const dim3 grid((unsigned)a.M), block(team);
+    const bool plain = VEC && !a.layer && !a.post_c && !a.pre_c && a.block && a.stream;
+#define BNN_FORWARD(SLOTS, THREADS) BNN_CUDA_TRY(ctx, bnn_launch_dependent(plain ? k_block_norm_mx<T, SLOTS, THREADS, VEC, VEC, FOUR> : k_block_norm_mx<T, SLOTS, THREADS, VEC, false, FOUR>, \
                                                                            grid, block, 0, ctx->stream, a))
     if (slots == 1) BNN_FORWARD(1, 1024);
     else if (slots == 2) BNN_FORWARD(2, 256);
@@ -785,12 +977,19 @@ template <bool MX> int block_norm(bnn_ctx *ctx, const bnn_block_norm_desc *norm,
     a.x = x; a.ldx = ldx; a.block = block; a.ldb = ldb; a.stream = stream; a.lds = lds; a.normed = normed; a.ldn = ldn; a.stats = stats;
     if (MX) {
         a.mx_values = static_cast<uint8_t *>(q->values); a.mx_scales = static_cast<uint8_t *>(q->scales);
+        a.inv_low = (float)(1.0 / (double)norm->D - (double)a.inv_d);
         a.mx_limit = (int)bnn_mx_groups(norm->D) * BNN_MX_GROUP; a.mx_four = q->format == BNN_MX_E2M1;
     }
     const bool vec = norm_vec(norm, M, a);
-    if (norm->dtype == BNN_F32) return vec ? launch_forward<float, true, MX>(ctx, a) : launch_forward<float, false, MX>(ctx, a);
-    if (norm->dtype == BNN_F16) return vec ? launch_forward<__half, true, MX>(ctx, a) : launch_forward<__half, false, MX>(ctx, a);
-    return vec ? launch_forward<__nv_bfloat16, true, MX>(ctx, a) : launch_forward<__nv_bfloat16, false, MX>(ctx, a);
+    const auto launch = [&](auto zero) {
+        using T = decltype(zero);
+        if constexpr (MX) {
+            if (a.mx_four) return vec ? launch_forward_mx<T, true, true>(ctx, a) : launch_forward_mx<T, false, true>(ctx, a);
+            return vec ? launch_forward_mx<T, true, false>(ctx, a) : launch_forward_mx<T, false, false>(ctx, a);
+        }
+        else return vec ? launch_forward<T, true>(ctx, a) : launch_forward<T, false>(ctx, a);
+    };
+    return norm->dtype == BNN_F32 ? launch(0.0f) : norm->dtype == BNN_F16 ? launch(__half()) : launch(__nv_bfloat16());
 }
 }  // namespace
 
