@@ -176,3 +176,38 @@ def feed_forward_backward(ctx, net, keep, dstream=None, dnormed=None, seed: int 
     x, st = keep[0]
     first = ctx.block_norm_backward(net["first"], dstream, dnormed, x, stats=st)
     return first["dx"], first, grads
+
+
+def feed_forward_gradients(first, grads) -> list:
+    """The tensors of feed_forward_backward's parameter gradients, for Context.make_gradients: their norm is taken, and clipped, together."""
+    names = ("dWg", "dWu", "dWd", "dgate", "dpost_weight", "dpre_weight")
+    return [t for t in [first["dpre_weight"]] + [g[n] for g in grads for n in names] if t is not None]
+
+
+def prepare_feed_forward_mx(ctx, layers, first_weight=None, act: str = "silu", kind: str = "rms", eps: float = 1e-6, alpha: float = 1.0,
+                            weights: str = "e2m1", activations: str = "e4m3"):
+    """The stack of prepare_feed_forward (same dicts) for serving in few bits: weights microscaled once, norms and gated projections with
+    microscaled results.  weights, activations: formats; e2m1 activations go with e2m1 weights."""
+    D, dtype = layers[0]["Wd"].shape[0], layers[0]["Wd"].dtype
+    net = {"first": ctx.make_block_norm(D, dtype, kind=kind, eps=eps, pre_weight=first_weight), "layers": [], "format": activations}
+    for L in layers:
+        Wg, Wu, Wd = (ctx.mx_quantize(L[n], weights) for n in ("Wg", "Wu", "Wd"))
+        net["layers"].append({
+            "up": ctx.make_mx_gated(Wg, Wu, act, dtype=dtype), "down": ctx.make_mx_linear(Wd, dtype=dtype),
+            "norm": ctx.make_block_norm(D, dtype, kind=kind, eps=eps, alpha=alpha, gate=L.get("gate"), post=L.get("post_weight") is not None,
+                                        post_weight=L.get("post_weight"), pre_weight=L.get("next_weight"))})
+    return net
+
+
+def feed_forward_mx(ctx, net, x):
+    """x [M, D] through the stack: (stream, normed) after the last layer, both of x's type.  A layer is three calls: gated projections with a microscaled
+    result, the projection back, and the norms that tie it to the stream, whose result for the next layer is microscaled."""
+    stream, n = ctx.block_norm_mx(net["first"], x, format=net["format"])
+    for i, L in enumerate(net["layers"]):
+        h = ctx.mx_gated(L["up"], n, out=ctx.make_mx(x.shape[0], L["up"].outer, net["format"]))
+        block = ctx.mx_linear(L["down"], h)
+        if i + 1 < len(net["layers"]):
+            stream, n = ctx.block_norm_mx(L["norm"], stream, block, format=net["format"])
+        else:
+            stream, n = ctx.block_norm(L["norm"], stream, block)
+    return stream, n
