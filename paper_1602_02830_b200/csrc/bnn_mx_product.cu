@@ -290,6 +290,8 @@ constexpr uint32_t STAGE = 35 * 1024, X_SCALES = 2 * ROWS128, W_SCALES = X_SCALE
 constexpr uint32_t ACC2 = 192, SCALES = 448, SCALE_SET = 32;      // columns: second accumulator, scales (two sets: 8 of x, 16 of weights)
 constexpr int SHARED = 64;               // columns that both accumulators have
 static_assert(ACC2 + SHARED == 256, "of 256 each");
+// Half-width tiles (128 columns, dense layer only) where whole ones would leave half of the pairs without work: their accumulators share nothing.
+template <int BN> constexpr uint32_t second_acc() { return BN == 256 ? ACC2 : 128; }
 
 struct PairArgs : MxCommon {
     Output q;
@@ -314,7 +316,7 @@ template <int WIDTH> __device__ __forceinline__ void tile_at(const PairArgs &p, 
     n0 = (int)(n * WIDTH);
 }
 
-template <bool FOUR> __device__ __forceinline__ void issue_pair(const PairArgs &p, Control *ctl, uint8_t *tiles, uint32_t tmem, uint32_t pair, uint32_t pairs) {
+template <bool FOUR, int BN> __device__ __forceinline__ void issue_pair(const PairArgs &p, Control *ctl, uint8_t *tiles, uint32_t tmem, uint32_t pair, uint32_t pairs) {
     uint32_t stage = 0, phase = 0, count = 0, set = 0;
     bool ok = true;
     const uint64_t a0 = smem_desc_sw128(smem_u32(tiles)), b0 = smem_desc_sw128(smem_u32(tiles + ROWS128));
@@ -324,7 +326,7 @@ template <bool FOUR> __device__ __forceinline__ void issue_pair(const PairArgs &
     for (uint32_t t = pair; t < p.tiles && ok; t += pairs, ++count) {
         if (count > 0 && !warp_wait(ctl, p.wait_ns, &ctl->acc_empty, (count - 1) & 1)) { fail(ctl, 4); ok = false; break; }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t d = tmem + (count & 1) * ACC2;
+        const uint32_t d = tmem + (count & 1) * second_acc<BN>();
         for (int kit = 0; kit < k_iters; ++kit) {
             if (!warp_wait(ctl, p.wait_ns, &ctl->full[stage], phase)) { fail(ctl, 2); ok = false; break; }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -335,7 +337,7 @@ template <bool FOUR> __device__ __forceinline__ void issue_pair(const PairArgs &
                 for (int g = 0; g < GROUPS; ++g) {
                     copy_scales<2>(sx + 4 * g, xs0 + at + 32 * g);
                     copy_scales<2>(sw + 8 * g, ws0 + at + 32 * g);                        // columns 0 .. 127 of the tile
-                    copy_scales<2>(sw + 8 * g + 4, ws0 + at + 32 * (GROUPS + g));         // and 128 .. 255
+                    if (BN == 256) copy_scales<2>(sw + 8 * g + 4, ws0 + at + 32 * (GROUPS + g));         // and 128 .. 255
                 }
                 step_mx<2, FOUR>(d, a0 + at, b0 + at, p.idesc, sx, sw, 8, kit == k_iters - 1 ? p.last : 4, kit == 0);
                 umma_commit_2sm(smem_u32(&ctl->empty[stage]));
@@ -352,10 +354,11 @@ template <bool FOUR> __device__ __forceinline__ void issue_pair(const PairArgs &
     warp_wait(ctl, DRAIN_NS, &ctl->drain, 0, false);
 }
 
-template <int EPI, int OUT>
+template <int EPI, int OUT, int BN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1) k_mx_pair(const __grid_constant__ PairArgs p) {
     constexpr bool GATED = EPI == BNN_EPI_GATED;
-    constexpr int WIDTH = GATED ? 128 : 256, PARTS = EPI_WARPS / 4;
+    constexpr int WIDTH = GATED ? BN / 2 : BN, PARTS = EPI_WARPS / 4;
+    static_assert(BN == 256 || (BN == 128 && !GATED), "gate and up rows of a tile are whole tiles of scales");
     extern __shared__ uint8_t smem_raw[];
     uint8_t *tiles = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     Control *ctl = reinterpret_cast<Control *>(tiles + STAGES * STAGE);
@@ -398,7 +401,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1) k_m
                     const uint32_t dst = smem_u32(tiles + stage * STAGE), bar = smem_u32(&ctl->full[stage]) & PEER_MASK;
                     if (!elected()) {
                     } else if (!weights) {
-                        if (rank == 0) mbar_expect_tx(smem_u32(&ctl->full[stage]), 2 * (ROWS128 + p.w_bytes + 3 * groups * BNN_MX_TILE));
+                        if (rank == 0) mbar_expect_tx(smem_u32(&ctl->full[stage]), 2 * (ROWS128 + p.w_bytes * (BN / 2) / 128 + (1 + BN / 128) * groups * BNN_MX_TILE));
                         tma_load_2d_2sm(dst, &p.maps.x, kit * 128, m0, bar);
                         tma_load_3d_2sm(dst + X_SCALES, &p.maps.xs, 0, kit * groups, m0 >> 7, bar);
                     } else if (GATED) {
@@ -406,7 +409,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1) k_m
                         tma_load_3d_2sm(dst + W_SCALES, &p.maps.ws[0], 0, kit * groups, n0 >> 7, bar);
                         tma_load_3d_2sm(dst + W_SCALES + groups * BNN_MX_TILE, &p.maps.ws[1], 0, kit * groups, n0 >> 7, bar);
                     } else {
-                        tma_load_2d_2sm(dst + ROWS128, &p.maps.w[0], kit * 128, n0 + (int)rank * 128, bar);
+                        tma_load_2d_2sm(dst + ROWS128, &p.maps.w[0], kit * 128, n0 + (int)rank * (BN / 2), bar);
                         tma_load_3d_2sm(dst + W_SCALES, &p.maps.ws[0], 0, kit * groups, n0 >> 7, bar);
                     }
                     __syncwarp();
@@ -424,8 +427,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1) k_m
         }
     } else if (warp == 1) {
         if (rank == 0) {
-            if (p.four) issue_pair<true>(p, ctl, tiles, tmem_base, pair, pairs);
-            else issue_pair<false>(p, ctl, tiles, tmem_base, pair, pairs);
+            if (p.four) issue_pair<true, BN>(p, ctl, tiles, tmem_base, pair, pairs);
+            else issue_pair<false, BN>(p, ctl, tiles, tmem_base, pair, pairs);
         }
     } else if (warp < 2 + EPI_WARPS) {
         bnn_pdl_wait();
@@ -440,10 +443,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1) k_m
             tile_at<WIDTH>(p, t, tm0, tn0);
             const int64_t m0 = tm0 + (int)rank * 128 + 32 * quad;
             const int rows = (int)(q.M - m0 < 32 ? q.M - m0 : 32);
-            const uint32_t acc = tmem_base + buf * ACC2 + ((uint32_t)(32 * quad) << 16);
+            const uint32_t acc = tmem_base + buf * second_acc<BN>() + ((uint32_t)(32 * quad) << 16);
             // the i-th piece of this warp: from above in the first accumulator, from below in the second, so that what they share comes first
             constexpr int EACH = OUT == OUT_MX ? BLOCK : CHUNK, PIECES = WIDTH / EACH, MINE = PIECES / PARTS;
-            constexpr int LAST_SHARED = SHARED / EACH <= PARTS ? 0 : SHARED / EACH / PARTS - 1;       // of this warp's pieces
+            static_assert(SHARED / EACH <= PARTS, "what is shared is among the warps' first pieces");
             static_assert(PIECES % PARTS == 0, "every warp has as many pieces");
             const auto column_of = [&](int i) { const int k = i * PARTS + part; return (buf ? k : PIECES - 1 - k) * EACH; };
             const bool adds = OUT != OUT_MX && !GATED && p.add != nullptr;
@@ -456,6 +459,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1) k_m
             // The residual is requested a piece ahead, the first one while the tile is being multiplied; with pre-activations to keep there are no registers for that.
             constexpr bool AHEAD = OUT == OUT_PLAIN;
             if (AHEAD) ask(0);
+            const auto hand_over = [&]() {
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cta0(smem_u32(&ctl->acc_empty));
+            };
+            if (BN == 128) hand_over();                          // the tile before, whose columns the next one writes, is done
             if (!warp_wait(ctl, p.wait_ns, &ctl->acc_full[buf], (count >> 1) & 1)) { fail(ctl, 3); break; }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             // Gated: the accumulators share columns of the up rows of the first and of the gate rows of the second.
@@ -473,12 +482,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1) k_m
                     tmem_ld_wait16(r);
                     if (GATED) tmem_ld_wait16(other);
                 }
-                if (i == LAST_SHARED) {
-                    // this warp has read its share of the columns that the next tile's MMAs write
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_cta0(smem_u32(&ctl->acc_empty));
-                }
+                if (BN == 256 && i == 0) hand_over();            // this warp has read its share of the columns that the next tile's MMAs write
                 const bool there = rows > 0 && (OUT == OUT_MX ? tn0 + c < p.q_limit : n > 0);
                 if constexpr (OUT == OUT_MX) {
                     if (!there) continue;
@@ -641,6 +645,18 @@ template <int EPI, bool MX> __global__ void __launch_bounds__(FEW_THREADS, 2) k_
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = ctl->tmem_base;
+    if ((warp == 0 || warp == FEW_THREADS / 32 - 1) && !f.drop_loads) {
+        // While the kernel before this one runs, the first weights are brought to L2.  (Only to L2, where its writes are seen: it may have made them.)
+        const int mine = warp == 0 ? 0 : 1, groups = f.four ? 2 : 1;
+        if (elected())
+            for (int kit = first + mine; kit < last && kit < first + f.stages; kit += 2)
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h) {
+                    asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(&f.maps.w[h]), "r"(kit * 128), "r"((int)n0) : "memory");
+                    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(&f.maps.ws[h]), "r"(0), "r"(kit * groups), "r"((int)(n0 >> 7)) : "memory");
+                }
+        __syncwarp();
+    }
     bnn_pdl_wait();
     bnn_pdl_launch_next();
 
@@ -744,13 +760,13 @@ template <int EPI, bool MX> __global__ void __launch_bounds__(FEW_THREADS, 2) k_
 
 // ---------------------------------------------------------------------------------------------------------
 // Opts in to the shared memory and asks how many pairs fit the device, once per device and kernel; 0 = cannot run.
-template <int EPI, int OUT> int pairs_of(int device, int sm_count) {
+template <int EPI, int OUT, int BN> int pairs_of(int device, int sm_count) {
     static std::mutex lock;
     static int cached[64];
     if (device < 0 || device >= 64) return 0;
     std::lock_guard<std::mutex> guard(lock);
     if (cached[device] == 0) {
-        auto kernel = k_mx_pair<EPI, OUT>;
+        auto kernel = k_mx_pair<EPI, OUT, BN>;
         int pairs = 0;
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PAIR_SMEM) == cudaSuccess) {
             cudaLaunchConfig_t cfg = {};
@@ -766,11 +782,11 @@ template <int EPI, int OUT> int pairs_of(int device, int sm_count) {
     }
     return cached[device] > 0 ? cached[device] : 0;
 }
-template <int EPI, int OUT> int launch_pair(bnn_ctx *ctx, const PairArgs &a) {
-    const int pairs = pairs_of<EPI, OUT>(ctx->device, ctx->sm_count);
+template <int EPI, int OUT, int BN> int launch_pair(bnn_ctx *ctx, const PairArgs &a) {
+    const int pairs = pairs_of<EPI, OUT, BN>(ctx->device, ctx->sm_count);
     if (pairs == 0) return BNN_ERR_CUDA;
     const unsigned n = a.tiles < (uint32_t)pairs ? a.tiles : (unsigned)pairs;
-    BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_mx_pair<EPI, OUT>, dim3(2 * n), dim3(PAIR_THREADS), PAIR_SMEM, ctx->stream, a));
+    BNN_CUDA_TRY(ctx, bnn_launch_dependent(k_mx_pair<EPI, OUT, BN>, dim3(2 * n), dim3(PAIR_THREADS), PAIR_SMEM, ctx->stream, a));
     return bnn_check_launch(ctx);
 }
 template <int EPI, bool MX> int launch_few(bnn_ctx *ctx, const FewArgs &f, unsigned tiles, unsigned split) {
@@ -846,7 +862,7 @@ void common_args(MxCommon &a, Output &q, bnn_ctx *ctx, const Call &c) {
         a.q_limit = bnn_mx_groups(c.q->cols) * BNN_MX_GROUP; a.q_four = c.q->format == BNN_MX_E2M1;
     }
 }
-int map_operands(bnn_ctx *ctx, MxMaps &m, const Call &c, int x_rows, int x_tiles, int w_tiles) {
+int map_operands(bnn_ctx *ctx, MxMaps &m, const Call &c, int x_rows, int x_tiles, int w_rows, int w_tiles) {
     if (c.x->cols == 0) return BNN_OK;
     const bool packed = is_four(c);
     const int groups = packed ? 2 : 1;
@@ -854,32 +870,41 @@ int map_operands(bnn_ctx *ctx, MxMaps &m, const Call &c, int x_rows, int x_tiles
     if (int st = map_scales(ctx, &m.xs, c.x, groups, x_tiles)) return st;
     for (int i = 0; i < 2; ++i) {
         if (!c.w[i]) continue;
-        if (int st = map_elements(ctx, &m.w[i], c.w[i], packed, 128)) return st;
+        if (int st = map_elements(ctx, &m.w[i], c.w[i], packed, w_rows)) return st;
         if (int st = map_scales(ctx, &m.ws[i], c.w[i], groups, w_tiles)) return st;
     }
     return BNN_OK;
 }
 
+int64_t pair_tiles(const Call &c, int64_t width) { return (c.x->rows + 255) / 256 * ((c.w[0]->rows + width - 1) / width); }
+bool half_width(const bnn_ctx *ctx, const Call &c) { return !c.w[1] && 2 * pair_tiles(c, 256) <= ctx->sm_count / 2; }
 int product_pair(bnn_ctx *ctx, const Call &c) {
     PairArgs a{};
     common_args(a, a.q, ctx, c);
-    const bool gated = c.epilogue == BNN_EPI_GATED;
-    const int64_t width = gated ? 128 : 256, tiles_m = (a.q.M + 255) / 256, tiles_n = (a.q.N + width - 1) / width;
-    if (tiles_m * tiles_n > 0x7fffffff) return BNN_ERR_INVALID_ARG;
-    a.tiles_m = (uint32_t)tiles_m; a.tiles_n = (uint32_t)tiles_n; a.tiles = (uint32_t)(tiles_m * tiles_n);
-    a.idesc = instruction(a.four, c.x->format, c.w[0]->format, 256, 256);
+    const bool gated = c.epilogue == BNN_EPI_GATED, half = half_width(ctx, c);
+    const int64_t width = gated || half ? 128 : 256, tiles = pair_tiles(c, width);
+    if (tiles > 0x7fffffff) return BNN_ERR_INVALID_ARG;
+    a.tiles_m = (uint32_t)((a.q.M + 255) / 256); a.tiles_n = (uint32_t)((a.q.N + width - 1) / width); a.tiles = (uint32_t)tiles;
+    a.idesc = instruction(a.four, c.x->format, c.w[0]->format, half ? 128 : 256, 256);
     const auto sectors = [](const void *at, int64_t ld, int64_t rows) { return (reinterpret_cast<uintptr_t>(at) | (rows > 1 ? (uint64_t)ld * 2 : 0)) % 32 == 0 ? 3 : width_of(at, ld, rows, 2); };
     a.q.vec_out = sectors(c.out, c.ldo, a.q.M); a.vec_add = sectors(c.add, c.ld_add, a.q.M);
     a.vec_bias = width_of(c.bias, 0, 1, 2); a.vec_pre = width_of(c.pre, c.ldp, 2 * a.q.M, 4);
-    if (int st = map_operands(ctx, a.maps, c, 128, 1, gated ? 1 : 2)) return st;
-    if (gated) return c.pre ? launch_pair<BNN_EPI_GATED, OUT_PRE>(ctx, a) : c.q ? launch_pair<BNN_EPI_GATED, OUT_MX>(ctx, a) : launch_pair<BNN_EPI_GATED, OUT_PLAIN>(ctx, a);
-    return c.pre ? launch_pair<BNN_EPI_LINEAR, OUT_PRE>(ctx, a) : c.q ? launch_pair<BNN_EPI_LINEAR, OUT_MX>(ctx, a) : launch_pair<BNN_EPI_LINEAR, OUT_PLAIN>(ctx, a);
+    if (int st = map_operands(ctx, a.maps, c, 128, 1, half ? 64 : 128, gated || half ? 1 : 2)) return st;
+#define BNN_LAUNCH(EPI, BN) (c.pre ? launch_pair<EPI, OUT_PRE, BN>(ctx, a) : c.q ? launch_pair<EPI, OUT_MX, BN>(ctx, a) : launch_pair<EPI, OUT_PLAIN, BN>(ctx, a))
+    return gated ? BNN_LAUNCH(BNN_EPI_GATED, 256) : half ? BNN_LAUNCH(BNN_EPI_LINEAR, 128) : BNN_LAUNCH(BNN_EPI_LINEAR, 256);
+#undef BNN_LAUNCH
 }
 
-// Which kernel, and how k_mx_few divides the work: the estimates of the 16-bit products, whose K steps move and multiply as many bytes.
+// Which kernel, and how k_mx_few divides the work, by estimates of both in microseconds, fitted to 1095 plans of seventy sizes (1 to 1000 rows, 256 x 256 to
+// 8192 x 8192 weights in every pair of formats, gated ones too; calls that repeat the same weights, from L2).  The plan chosen takes 3 % longer than the best in the mean.
+//   pair: 6.2 + 0.33 per K step and round of tiles; half-width tiles 4.4 + 0.29.
+//   few:  4.2 for every round of CTAs, + per K step of an SM's CTAs 0.07 + 0.0022 per token of a tile, at least 0.29 where an SM has one CTA (gated 1.42 times that);
+//         + 0.83 for every doubling of the split, + 0.036 per token of a CTA's share of the epilogue.
+// Both are the rate at which an SM draws operands from L2, about 64 bytes a clock: a step without its copies of scales or without three of its four MMAs takes as long.
 double pair_cost(const bnn_ctx *ctx, const Call &c) {
-    const int64_t width = c.w[1] ? 128 : 256, tiles = (c.x->rows + 255) / 256 * ((c.w[0]->rows + width - 1) / width), pairs = ctx->sm_count / 2;
-    return 5.0 + 0.30 * (double)steps_of(c) * (double)((tiles + pairs - 1) / pairs);
+    const bool half = half_width(ctx, c);
+    const int64_t tiles = pair_tiles(c, c.w[1] || half ? 128 : 256), pairs = ctx->sm_count / 2;
+    return (half ? 4.4 : 6.2) + (half ? 0.29 : 0.33) * (double)steps_of(c) * (double)((tiles + pairs - 1) / pairs);
 }
 constexpr int FEW_RESIDENT[2][4] = {{148, 148, 132, 120}, {296, 296, 284, 264}};      // bnn_product.cu
 struct FewPlan { int64_t tiles; int token_tiles, tokens, split, per_sm; double cost; };
@@ -905,9 +930,9 @@ FewPlan few_plan(const Call &c) {
             f.per_sm = ctas > FEW_RESIDENT[0][log] && f.tokens <= 64 ? 2 : 1;      // half of an SM's memory still holds four stages of 64 tokens
             const int64_t resident = FEW_RESIDENT[f.per_sm - 1][log], rounds = (ctas + resident - 1) / resident;
             const double load = (double)(rounds > 1 ? rounds * f.per_sm : (ctas + 147) / 148), cta_steps = (double)((steps + f.split - 1) / f.split);
-            double step = 0.12 + 0.0012 * f.tokens;
-            if (step < (f.per_sm == 2 ? 0.26 : 0.28)) step = f.per_sm == 2 ? 0.26 : 0.28;
-            f.cost = 3.0 * (double)rounds + load * cta_steps * step * halves + (f.split > 1 ? 2.0 : 1.0) + 0.041 * f.tokens * halves / f.split * load;
+            double step = 0.07 + 0.0022 * f.tokens;
+            if (f.per_sm == 1 && step < 0.29) step = 0.29;
+            f.cost = 4.2 * (double)rounds + load * cta_steps * step * (halves == 2 ? 1.42 : 1.0) + 0.83 * log - 0.7 + 0.036 * f.tokens * halves / f.split * load;
             if (f.cost < best.cost) best = f;
         }
     }
@@ -940,7 +965,7 @@ int product_few(bnn_ctx *ctx, const Call &c, const FewPlan &plan) {
     f.stages = f.stages > FEW_STAGES ? FEW_STAGES : f.stages;
     if (f.stages > steps) f.stages = steps;
     f.stages = f.stages < 2 ? 2 : f.stages & ~1;
-    if (int st = map_operands(ctx, f.maps, c, f.tokens, (int)x_tiles, 1)) return st;
+    if (int st = map_operands(ctx, f.maps, c, f.tokens, (int)x_tiles, 128, 1)) return st;
     const unsigned tiles = (unsigned)plan.tiles, split = (unsigned)plan.split;
     if (halves == 2) return c.q ? launch_few<BNN_EPI_GATED, true>(ctx, f, tiles, split) : launch_few<BNN_EPI_GATED, false>(ctx, f, tiles, split);
     return c.q ? launch_few<BNN_EPI_LINEAR, true>(ctx, f, tiles, split) : launch_few<BNN_EPI_LINEAR, false>(ctx, f, tiles, split);
