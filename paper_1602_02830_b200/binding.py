@@ -934,7 +934,7 @@ class Context:
             out = self._new(M, N, dtype, here)
             op, ldo = out.data_ptr(), N
         elif type(out) is MxMatrix:
-            op, ldo, qp = None, 0, self._mx_out(out, M, N, residual is not None or pre is not None)
+            op, ldo, qp = None, 0, self._mx_out(out, x, M, N, residual is not None or pre is not None)
         else:
             op, ldo = self._fit(out, M, N, dtype, "out")
         st = lib().bnn_mx_linear(self._h, layer.ref, ref, rp, ldr, op, ldo, pp, ldp, qp)
@@ -954,7 +954,7 @@ class Context:
             out = self._new(M, N, dtype, here)
             op, ldo = out.data_ptr(), N
         elif type(out) is MxMatrix:
-            op, ldo, qp = None, 0, self._mx_out(out, M, N, pre is not None)
+            op, ldo, qp = None, 0, self._mx_out(out, x, M, N, pre is not None)
         else:
             op, ldo = self._fit(out, M, N, dtype, "out")
         st = lib().bnn_mx_gated(self._h, layer.ref, ref, op, ldo, pp, ldp, qp)
@@ -964,9 +964,11 @@ class Context:
             self._used(x.values, x.scales, pre, *self._memory(out), *layer.tensors)
         return out
 
-    def _mx_out(self, out, M, N, more):
+    def _mx_out(self, out, x, M, N, more):
         if more:
             raise ValueError("out: microscaled results come without residual and pre")
+        if out.desc.values == x.desc.values and out.desc.values:
+            raise ValueError("out: must not be x, which is read until the end")
         return self._mx(out, M, N, "out")
 
     @staticmethod

@@ -1,5 +1,7 @@
 """Microscaled operators on the GPU against their 64-bit forms: quantisation bit by bit, norms with a microscaled result, products of every pair of
 formats on both kernels, microscaled results, gradients straight through the rounding, edges of masks, sizes, strides and streams."""
+import threading
+
 import pytest
 import torch
 
@@ -347,6 +349,97 @@ def test_straight_through_gradients(ctx, M, N, K, act):
     moved = float(up[i, j].double() - Wv[i, j].double())
     slope = (z[1] - z[0])[:, i].double() / moved                     # d z / d W[i, j]: the column of x
     assert torch.allclose(slope, xv[:, j].double(), rtol=0, atol=float(2 * mx.linear(xv.double(), Wv.double(), b, None, act, BF)["pre"][1][:, i].max() / abs(moved)))
+
+
+@pytest.mark.parametrize("M,N,K", [(5, 40, 70), (300, 264, 136)])
+def test_straight_through_gradients_of_gated(ctx, M, N, K):
+    mk = Maker(M + N)
+    x, Wg, Wu, dh = mk(M, K), mk(N, K, scale=K ** -0.5), mk(N, K, scale=K ** -0.5), mk(M, N)
+    xv, gv, uv = (torch.empty_like(t) for t in (x, Wg, Wu))
+    q, g, u = ctx.mx_quantize(x, "e4m3", values=xv), ctx.mx_quantize(Wg, "e2m1", values=gv), ctx.mx_quantize(Wu, "e2m1", values=uv)
+    pre = ctx.empty(2, M, N, dtype=FF)
+    ctx.mx_gated(ctx.make_mx_gated(g, u), q, pre=pre)
+    back = ctx.make_gated(gv, uv)
+    ctx.set_workspace(torch.empty(max(256, ctx.gated_workspace_bytes(back, xv, backward=True)), dtype=torch.uint8, device="cuda"))
+    want = ref.gated(xv, gv, uv, "silu", dh)
+    for key, t in zip(("dx", "dWg", "dWu"), ctx.gated_backward(back, dh, xv, pre)):
+        ref.check(t, *want[key], key)
+    ctx.set_workspace(None)
+
+
+def test_scales_of_rows_that_do_not_exist_may_be_anything(ctx):
+    """Scale bytes are kept for 128 rows at a time.  NaN (255) in those of rows that do not exist reaches nothing, of x and of the weights, on both kernels."""
+    mk = Maker(8)
+    for M, N in ((3, 40), (150, 200), (700, 1050)):
+        for xf, wf in PAIRS:
+            x, W, U = mk(M, 200), mk(N, 200), mk(N, 200)
+            got = []
+            for fill in (255, 0):
+                q, w, u = ctx.make_mx(M, 200, xf), ctx.make_mx(N, 200, wf), ctx.make_mx(N, 200, wf)
+                for t, v in ((q, x), (w, W), (u, U)):
+                    t.scales.fill_(fill)
+                    ctx.mx_quantize(v, out=t)
+                h = ctx.mx_gated(ctx.make_mx_gated(w, u), q, out=ctx.make_mx(M, N, "e4m3"))
+                got.append((ctx.mx_linear(ctx.make_mx_linear(w), q), ctx.mx_gated(ctx.make_mx_gated(w, u), q), ctx.mx_values(h)))
+            for a, b in zip(*got):
+                assert a.isfinite().all() and torch.equal(a, b)
+
+
+def test_offsets_beyond_32_bits(ctx):
+    """More than 2^31 elements: the last rows are as they would be alone."""
+    M, K = 36000, 66000
+    x = torch.empty(M, K, dtype=BF, device="cuda").normal_()
+    q = ctx.mx_quantize(x, "e4m3")
+    out = ctx.mx_values(q, BF)
+    assert torch.equal(out[-3:], mx.quantize(x[-3:].double(), "e4m3").to(BF))
+    norm = ctx.make_block_norm(32768, BF)
+    wide = x.view(-1)[:72000 * 32768].view(72000, 32768)
+    stream, n = ctx.block_norm_mx(norm, wide, format="e4m3")
+    small = ctx.block_norm_mx(norm, wide[-128:], format="e4m3")[1]            # 72000 rows: the last 64 are half a tile of scales
+    assert torch.equal(ctx.mx_values(n, BF)[-64:], ctx.mx_values(small, BF)[-64:]) and torch.equal(stream[-3:], wide[-3:])
+    del out, wide, stream, n
+    w = ctx.mx_quantize(Maker(1)(64000, 96), "e4m3")
+    q = ctx.mx_quantize(x[:, :96], "e4m3")
+    y, pre = torch.empty(M, 64000, dtype=BF, device="cuda"), torch.empty(M, 64000, device="cuda")
+    layer = ctx.make_mx_linear(w)
+    ctx.mx_linear(layer, q, out=y, pre=pre)
+    want = mx.linear(ctx.mx_values(q)[-5:].double(), ctx.mx_values(w).double(), None, None, "none", BF)
+    ref.check(y[-5:], *want["y"], "y"), ref.check(pre[-5:], *want["pre"], "pre")
+    del pre
+    h = ctx.mx_linear(layer, q, out=ctx.make_mx(M, 64000, "e2m1"))
+    v = ctx.mx_values(h, BF)
+    mx.accept(v[-5:], *want["raw"], "e2m1", "microscaled y")
+
+
+def test_contexts_of_two_threads(ctx):
+    """A context per host thread: both kernels' one-time preparations and launches from two threads at once."""
+    mk = Maker(2)
+    q, big, w = ctx.mx_quantize(mk(5, 512)), ctx.mx_quantize(mk(900, 512)), ctx.mx_quantize(mk(700, 512), "e2m1")
+    layer = ctx.make_mx_linear(w)
+    want = ctx.mx_linear(layer, q), ctx.mx_linear(layer, big)
+    torch.cuda.synchronize()
+    failures = []
+
+    def work(i):
+        try:
+            s = torch.cuda.Stream()
+            c = binding.Context(0, s)
+            with torch.cuda.stream(s):
+                for _ in range(200):
+                    got = c.mx_linear(layer, q), c.mx_linear(layer, big)
+                s.synchronize()
+                assert all(torch.equal(a, b) for a, b in zip(got, want))
+                c.device_status()
+            c.close()
+        except Exception as e:                    # raised in the test's own thread below
+            failures.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failures, failures
 
 
 def test_other_streams_and_graphs(ctx):

@@ -120,7 +120,8 @@ def test_binding_refuses_by_shape_and_type(host):
     q, w, w4, other = host.make_mx(4, 64, "e4m3"), host.make_mx(32, 64, "e4m3"), host.make_mx(32, 64, "e2m1"), host.make_mx(32, 96, "e4m3")
     norm, flat = host.make_block_norm(64, BF), host.make_block_norm(64, BF, pre=False)
     layer, glu = host.make_mx_linear(w), host.make_mx_gated(w, w)
-    q4 = host.make_mx(4, 64, "e2m1")
+    q4, q64, w64 = host.make_mx(4, 64, "e2m1"), host.make_mx(4, 64), host.make_mx(64, 64)
+    square, layer64 = host.make_mx_gated(w64, w64), host.make_mx_linear(w64)
     for call, match in [
         (lambda: host.make_mx(4, 64, "e5m2"), "format"), (lambda: host.make_mx(-1, 64), "rows, cols"),
         (lambda: host.mx_quantize(x.int()), "x:"), (lambda: host.mx_quantize(x, "e2m1", out=q), "format"), (lambda: host.mx_quantize(x, out=w), "out:"),
@@ -133,6 +134,7 @@ def test_binding_refuses_by_shape_and_type(host):
         (lambda: host.mx_linear(host.make_mx_linear(other), q), "x:"), (lambda: host.mx_linear(layer, q, out=host.make_mx(4, 31)), "out:"),
         (lambda: host.mx_linear(layer, q, x[:, :32], out=host.make_mx(4, 32)), "without residual"), (lambda: host.mx_linear(layer, q, pre=torch.zeros(4, 32, dtype=BF)), "pre:"),
         (lambda: host.mx_gated(glu, q, pre=torch.zeros(2, 4, 31)), "pre:"), (lambda: host.mx_gated(glu, q, pre=torch.zeros(2, 4, 32), out=host.make_mx(4, 32)), "without residual"),
+        (lambda: host.mx_gated(square, q64, out=q64), "must not be x"), (lambda: host.mx_linear(layer64, q64, out=q64), "must not be x"),
     ]:
         with pytest.raises(ValueError, match=match):
             call()
