@@ -27,7 +27,7 @@ template <int N> struct ClipArgs {
     int sums;
     float *norm;
     double max_norm, eps;
-    int writes_norm;
+    int writes_norm, in_place;   // every tensor of the launch is its own output
 };
 constexpr int FEW = 24, MANY = 1000;      // tensors of a launch; its arguments are 0.9 or 32 KB
 
@@ -178,10 +178,11 @@ template <int N> __global__ void __launch_bounds__(THREADS) k_clip_scale(const _
     const double all = norm + p.eps, share = p.max_norm / all;
     const float f = all == 0.0 || share >= 1.0 ? 1.0f : (float)share;      // a NaN stays one
     if (blockIdx.x == 0 && threadIdx.x == 0 && p.writes_norm) *p.norm = (float)norm;
+    if (f == 1.0f && p.in_place) return;                     // nothing to change
     for (uint32_t i = blockIdx.x; i < p.chunks; i += gridDim.x) {
         const uint32_t c = p.chunks - 1 - i;
         const Entry &e = p.e[entry_of(p, c)];
-        if (f == 1.0f && e.out == e.g) continue;             // nothing to change
+        if (f == 1.0f && e.out == e.g) continue;
         const int64_t base = (int64_t)(c - e.first) * CHUNK;
         if (e.dtype == BNN_F32) chunk_scale<float>(e, base, f);
         else if (e.dtype == BNN_F16) chunk_scale<__half>(e, base, f);
@@ -196,10 +197,12 @@ int64_t launches_of(int64_t count) { return count > 0 ? (count + MANY - 1) / MAN
 template <int N> int fill(ClipArgs<N> &a, const bnn_gradient *list, int64_t from, int64_t to) {
     uint64_t chunks = 0;
     a.count = 0;
+    a.in_place = 1;
     for (int64_t i = from; i < to; ++i) {
         if (list[i].n == 0) continue;
         Entry &e = a.e[a.count++];
         e.g = list[i].g; e.out = list[i].out; e.n = list[i].n; e.first = (uint32_t)chunks; e.dtype = list[i].dtype;
+        if (e.out != e.g) a.in_place = 0;
         chunks += (uint64_t)chunks_of(list[i]);
         if (chunks > 0x7fffffffu) return BNN_ERR_INVALID_ARG;
     }

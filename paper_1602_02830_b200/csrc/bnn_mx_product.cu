@@ -591,15 +591,42 @@ template <bool FOUR, bool GATED> __device__ __forceinline__ void issue_few(const
     warp_wait(ctl, DRAIN_NS, &ctl->acc_full, 0, false);       // the MMAs issued end before tensor memory is given back, also where the epilogue has given up
 }
 
-// Four neighbouring outputs of one token, microscaled: eight neighbouring lanes hold a block.  All lanes of the warp take part; `there`: the token exists.
-template <int EPI, typename T> __device__ __forceinline__ void finish_mx4(const MxCommon &p, const Output &q, int64_t m, int64_t n0, bool there, float (&a)[4], float (&b)[4]) {
+template <int ACT> __device__ __forceinline__ void act4(float (&v)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = act_value(ACT, v[j]);
+}
+// Four neighbouring outputs of one token from their sums; bias and what is added have been read.
+template <int EPI, typename T>
+__device__ __forceinline__ void finish_few(const MxCommon &p, const Output &q, int64_t m, int64_t n0, float (&a)[4], float (&b)[4], const float (&bias)[4], const float (&add)[4]) {
+    constexpr bool GATED = EPI == BNN_EPI_GATED;
+    const int n = (int)(q.N - n0 < 4 ? q.N - n0 : 4);
+    if (!GATED) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) a[j] += bias[j];
+    }
+    if (p.pre) {
+        write4(p.pre + m * p.ldp + n0, n, p.vec_pre, a);
+        if (GATED) write4(p.pre + (q.M + m) * p.ldp + n0, n, p.vec_pre, b);
+    }
+#define BNN_CALL(ACT) act4<ACT>(a)
+    BNN_EACH_ACT(BNN_CALL)
+#undef BNN_CALL
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a[j] = GATED ? a[j] * b[j] : a[j] + add[j];
+    write4(static_cast<T *>(q.out[0]) + m * q.ldo[0] + n0, n, q.vec_out, a);
+}
+// The same, microscaled: eight neighbouring lanes hold a block.  All lanes of the warp take part; `there`: the token exists.
+template <int EPI>
+__device__ __forceinline__ void finish_few_mx(const MxCommon &p, const Output &q, int64_t m, int64_t n0, bool there, float (&a)[4], float (&b)[4], const float (&bias)[4]) {
     const int n = (int)(q.N - n0 < 4 ? (q.N > n0 ? q.N - n0 : 0) : 4);
-    float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (EPI == BNN_EPI_LINEAR && p.bias && there) read4(static_cast<const T *>(p.bias) + n0, n, p.vec_bias, d);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a[j] += EPI == BNN_EPI_GATED ? 0.0f : bias[j];
+#define BNN_CALL(ACT) act4<ACT>(a)
+    BNN_EACH_ACT(BNN_CALL)
+#undef BNN_CALL
     uint32_t top = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        a[j] = act_value(p.act, a[j] + d[j]);
         if (EPI == BNN_EPI_GATED) a[j] *= b[j];
         a[j] = j < n ? a[j] : 0.0f;
         top = max(top, mx_magnitude(a[j]));
@@ -613,6 +640,14 @@ template <int EPI, typename T> __device__ __forceinline__ void finish_mx4(const 
     if (p.q_four) { mx_encode8<true>(e, w); *reinterpret_cast<uint16_t *>(p.q_values + m * (p.q_limit / 2) + n0 / 2) = (uint16_t)w[0]; }
     else { mx_encode8<false>(e, w); *reinterpret_cast<uint32_t *>(p.q_values + m * p.q_limit + n0) = w[0]; }
     if ((threadIdx.x & 7) == 0) p.q_scales[mx_scale_at(m, n0 >> 5, p.q_limit >> 7)] = (uint8_t)scale;
+}
+// Four 16-bit values as float32, n of them inside; zeros without a matrix.
+__device__ __forceinline__ void read_half4(const MxCommon &p, const void *base, int64_t at, int n, int vec, float (&v)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = 0.0f;
+    if (!base || n <= 0) return;
+    if (p.f16) read4(static_cast<const __half *>(base) + at, n, vec, v);
+    else read4(static_cast<const __nv_bfloat16 *>(base) + at, n, vec, v);
 }
 
 template <int EPI, bool MX> __global__ void __launch_bounds__(FEW_THREADS, 2) k_mx_few(const __grid_constant__ FewArgs f) {
@@ -698,13 +733,15 @@ template <int EPI, bool MX> __global__ void __launch_bounds__(FEW_THREADS, 2) k_
     const int log = split == 8 ? 3 : (int)split >> 1, out = 128 >> log, share = out * HALVES, pitch = f.tokens * share;
     float *parts = reinterpret_cast<float *>(tiles);
     const int valid = (int)(q.M - t0 < f.tokens ? q.M - t0 : f.tokens);
-    {                                                             // what this thread's first outputs will need from memory is brought to L2
+    // A thread finishes four outputs of token after token, the same four: their bias, and what is added to the first of them, are requested here.
+    static_assert(FEW_THREADS % 32 == 0, "a multiple of out / 4 for every split");
+    const int row = (int)threadIdx.x % (out / 4) * 4, n_mine = (int)(q.N - n0 - (int)rank * out - row);
+    const int64_t n_at = n0 + (int)rank * out + row;
+    float bias[4], add[4];
+    if (!GATED) {
+        read_half4(f, f.bias, n_at, n_mine < 4 ? n_mine : 4, f.vec_bias, bias);
         const int t = (int)threadIdx.x / (out / 4);
-        const int64_t n = n0 + (int)rank * out + ((int)threadIdx.x - t * (out / 4)) * 4;
-        if (!GATED && t < valid && n < q.N) {
-            if (f.add) asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint16_t *>(f.add) + (t0 + t) * f.ld_add + n));
-            if (f.bias) asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint16_t *>(f.bias) + n));
-        }
+        if (!MX) read_half4(f, f.add, (t0 + t) * f.ld_add + n_at, t < valid ? (n_mine < 4 ? n_mine : 4) : 0, f.vec_add, add);
     }
     bool done = false;
     if (warp >= 2 && warp < 10) {
@@ -742,19 +779,19 @@ template <int EPI, bool MX> __global__ void __launch_bounds__(FEW_THREADS, 2) k_
     }
     if (*reinterpret_cast<volatile uint32_t *>(&ctl->failed) != 0u) return;
     const int all = valid * (out / 4);
+    if (!MX && n_mine <= 0) return;
     for (int i = threadIdx.x; MX ? i - lane < all : i < all; i += FEW_THREADS) {      // microscaled: a warp stays together
         const bool there = i < all;
-        const int t = there ? i / (out / 4) : 0, row = there ? (i - t * (out / 4)) * 4 : 0;
-        const int64_t n = n0 + (int)rank * out + row;
-        if (!MX && n >= q.N) continue;
+        const int t = there ? i / (out / 4) : 0;
         float a[4], b[4];
         sum_parts(parts + t * share + row, (int)split, pitch, a);
         if (GATED) sum_parts(parts + t * share + out + row, (int)split, pitch, b);
-        if constexpr (MX) {
-            if (f.f16) finish_mx4<EPI, __half>(f, q, t0 + t, n, there, a, b);
-            else finish_mx4<EPI, __nv_bfloat16>(f, q, t0 + t, n, there, a, b);
-        } else if (f.f16) finish4<EPI, __half>(f, q, t0 + t, n, a, b);
-        else finish4<EPI, __nv_bfloat16>(f, q, t0 + t, n, a, b);
+        if constexpr (MX) finish_few_mx<EPI>(f, q, t0 + t, n_at, there, a, b, bias);
+        else {
+            if (!GATED && i != (int)threadIdx.x) read_half4(f, f.add, (t0 + t) * f.ld_add + n_at, n_mine < 4 ? n_mine : 4, f.vec_add, add);
+            if (f.f16) finish_few<EPI, __half>(f, q, t0 + t, n_at, a, b, bias, add);
+            else finish_few<EPI, __nv_bfloat16>(f, q, t0 + t, n_at, a, b, bias, add);
+        }
     }
 }
 
