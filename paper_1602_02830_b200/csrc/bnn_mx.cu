@@ -1,6 +1,8 @@
 // Microscaled matrices: quantisation of rows and the way back (formats and layout: bnn_mx.cuh).
 //
-// Bound: HBM.  One pass: an element is read once, its code and, where asked for, the value that the code stands for are written once.
+// Bound: HBM.  One pass: an element is read once, its code and, where asked for, the value that the code stands for are written once.  Measured: 8192 x 4096 bf16 to
+// e4m3 with represented values 28.0 us = 6.0 TB/s, without 20.0 us = 5.1 TB/s, to e2m1 19.7 us; 1000 x 4100 float16 (rows off the 16-byte rule) 5.5 us, lane by lane
+// instead of by words 12.8; one row 1.7 us.
 #include "bnn_mx.cuh"
 
 namespace {
@@ -13,7 +15,7 @@ struct MxArgs {
     int64_t chunks;         // of 256 columns
 };
 
-// A warp takes 256 columns of a row, ROWS rows one after another, all of which it requests before it computes.
+// A warp takes 256 columns of a row, ROWS rows one after another, all of which it requests before it computes.  (Four rows: as fast at 8192 x 4096, 48 x 2048 1.8 -> 2.4 us.)
 constexpr int WARPS = 8, ROWS = 2, CHUNK = 256;
 
 template <typename T, bool VEC, bool FOUR>

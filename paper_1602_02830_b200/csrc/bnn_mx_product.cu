@@ -5,6 +5,12 @@
 // them from shared memory as they lie in memory.  Two kinds: mxf4 (e2m1 x e2m1, packed, 64 of K an instruction) and mxf8f6f4 (bytes, 32 of K); the latter takes e2m1
 // beside e4m3 when its nibbles lie in the low eight bytes of every sixteen, which the tensor map does on the way (16U4_ALIGN16B).
 // One stage is a row of 128 bytes of shared memory: 256 of K packed, 128 otherwise.
+//
+// Bound: many rows, the tensor pipe and the part's power limit (8192 x 8192 x 8192 of random values: 182 us = 6.0 PFLOP/s in 4 bits, 363 us = 3.0 PFLOP/s in 8 bits, the same
+// with 4-bit weights 340 to 430 by box; 8192 x 4096 -> 8192 in 4 bits 101 us, with a residual 116; gated, 4096 rows, 4096 -> 8192 twice, microscaled result 176 us = 3.1 PFLOP/s).  Short
+// sums: the epilogue (4096 x 128 -> 4096 13.5 to 19 us, gelu 27 to 42).  Fewer rows: what an SM draws from L2, about 64 bytes a clock (512 x 4096 -> 4096 13.8 us, in 4 bits
+// 9.4); a token, 4096 -> 4096 with 4-bit weights, 7.1 us, of which 3.5 are launch, set-up and tail.
+// Nothing is rounded between the sums and the one conversion of a result: to 16 bits, or to an element of a microscaled result.
 #include "bnn_epilogue.cuh"
 #include "bnn_internal.cuh"
 #include "bnn_mx.cuh"
@@ -103,7 +109,8 @@ __device__ __forceinline__ unsigned long long gelu2(unsigned long long z) {
     pair_out(s, a, b);
     return pair_of(ra - a, rb - b);
 }
-// The activation of sixteen values.  Measured against one value an instruction (4096 x 4096 outputs, K = 128): gelu 36 us then.
+// The activation of sixteen values; both forms of GELU two values an instruction (4096 x 2048 -> 4096: gelu 35.0 us, one at a time 37.5; its tanh form 32.3 and 34.2).
+// SILU has little but its exponential and reciprocal, sixteen a clock and SM either way, and is faster without the pairs (gated 48.8 and 50.6).
 __device__ __forceinline__ void activate(int act, float (&v)[16]) {
 #define BNN_EACH_PAIR(EXPRESSION)                              \
     _Pragma("unroll") for (int j = 0; j < 16; j += 2) {        \
@@ -116,7 +123,7 @@ __device__ __forceinline__ void activate(int act, float (&v)[16]) {
         case BNN_ACT_GELU_TANH:
             BNN_EACH_PAIR(times_sigmoid(z, mul2(z, fma2(mul2(z, z), both(-GELU_2C * GELU_A * LOG2E), both(-GELU_2C * LOG2E)))));
             break;
-        case BNN_ACT_SILU: BNN_EACH_PAIR(times_sigmoid(z, mul2(z, both(-LOG2E)))); break;
+        case BNN_ACT_SILU: act16<BNN_ACT_SILU>(v); break;
         case BNN_ACT_SIGMOID: act16<BNN_ACT_SIGMOID>(v); break;
         case BNN_ACT_RELU: act16<BNN_ACT_RELU>(v); break;
         default: act16<BNN_ACT_HTANH>(v); break;
@@ -282,9 +289,13 @@ __device__ __forceinline__ void finish_mx(const MxCommon &p, const Output &q, in
 //                 every column)
 //   warp 1        MMA issuer (CTA 0): scales to tensor memory, then up to four instructions a stage
 //   the others    epilogue
-// Each of the two producers makes every K step, so the ring may have any number of stages: a stage is full with the bytes of all four.
+// Each of the two producers makes every K step, so the ring may have any number of stages: a stage is full with the bytes of all four.  (Six or eight stages instead of
+// five changed nothing at any size.)  Issuer and producers run warp-wide with one elected lane: a single lane of a divergent warp took about 1100 clocks a K step
+// of ten instructions, 8192 x 8192 x 8192 in 4 bits 287 us.  One issuing lane keeps the order of the additions fixed: the same call gives the same bits.
 // Tensor memory: two accumulators of 256 columns and 48 of scales are more than there is.  The accumulators overlap by 64 columns: the epilogue
-// takes the blocks that they share first, from above in the first one and from below in the second, and hands them over before it computes.
+// takes the columns that they share first, from above in the first one and from below in the second, and hands them over before it computes (handed over after the
+// first block instead: 8192 x 4096 -> 8192 in 4 bits 116 us).  A lane writes and adds whole 32-byte sectors of its own row; through shared memory, as rows that are not whole
+// sectors go, the same took 24 instead of 19 us at K = 128.  The residual's lines brought to L2 during the tile before made it slower (117 -> 124 us).
 constexpr int STAGES = 5, BAND = 8, EPI_WARPS = 16, PAIR_THREADS = (EPI_WARPS + 3) * 32;
 constexpr uint32_t STAGE = 35 * 1024, X_SCALES = 2 * ROWS128, W_SCALES = X_SCALES + 1024;       // x, weights, scales of x, scales of weights
 constexpr uint32_t ACC2 = 192, SCALES = 448, SCALE_SET = 32;      // columns: second accumulator, scales (two sets: 8 of x, 16 of weights)
