@@ -1025,6 +1025,7 @@ int product(bnn_ctx *ctx, const Call &c) {
     bnn_device_guard guard(ctx);
     if (!guard.ok) return BNN_ERR_CUDA;
     const FewPlan plan = few_plan(c);
+    if (c.x->cols == 0 && plan.tiles == 0) return BNN_ERR_INVALID_ARG;        // the empty sum is the few-row kernel's, up to 2^26 rows
     return c.x->cols == 0 || plan.cost < pair_cost(ctx, c) ? product_few(ctx, c, plan) : product_pair(ctx, c);
 }
 // x e2m1: weights e2m1; x e4m3: weights of either format.
