@@ -948,7 +948,8 @@ int product_pair(bnn_ctx *ctx, const Call &c) {
 //   pair: 6.2 + 0.33 per K step and round of tiles; half-width tiles 4.4 + 0.29.
 //   few:  4.2 for every round of CTAs, + per K step of an SM's CTAs 0.07 + 0.0022 per token of a tile, at least 0.29 where an SM has one CTA (gated 1.42 times that);
 //         + 0.83 for every doubling of the split, + 0.036 per token of a CTA's share of the epilogue.
-// Both are the rate at which an SM draws operands from L2, about 64 bytes a clock: a step without its copies of scales or without three of its four MMAs takes as long.
+// Mostly the arrival of operands, by what was left out in copies of the pair kernel: 512 x 512 x 8192 and 512 x 4096 x 4096 in 8 bits took 20.0 and 14.0 us whole, 20.7 and
+// 14.2 without the copies of scales, 20.3 and 13.8 without their loads, 17.6 and 11.8 with one of four MMAs; the rest is about 64 bytes a clock and SM from L2.
 double pair_cost(const bnn_ctx *ctx, const Call &c) {
     const bool half = half_width(ctx, c);
     const int64_t tiles = pair_tiles(c, c.w[1] || half ? 128 : 256), pairs = ctx->sm_count / 2;

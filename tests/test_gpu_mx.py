@@ -173,6 +173,8 @@ NORM = [  # M, D, type, kind, post, gates, shift, block, alpha, pad, lead
     (7, 2050, FF, "rms", False, 0, True, True, 1.0, 1, 1), (400, 512, FF, "layer", False, 0, False, True, 1.0, 0, 0), (2, 8200, BF, "layer", True, 1, True, True, 1.0, 0, 0),
     (310, 520, HF, "rms", False, 0, False, False, 1.0, 0, 0), (3, 32768, BF, "rms", True, 0, False, True, 1.0, 0, 0), (600, 16400, HF, "layer", False, 1, False, True, 1.0, 0, 0),
     (350, 4104, FF, "rms", True, 0, False, True, 1.0, 0, 0), (2, 20001, HF, "layer", True, 0, True, True, 1.0, 0, 0), (320, 33, BF, "layer", False, 0, False, True, 1.0, 2, 0),
+    (5, 16400, FF, "rms", True, 1, True, True, 0.5, 0, 0), (4, 20001, FF, "layer", True, 0, True, True, 1.0, 0, 0), (300, 16384, FF, "rms", False, 0, False, True, 1.0, 0, 0),
+    (310, 8448, BF, "rms", False, 0, False, True, 1.0, 0, 0), (300, 2048, HF, "rms", False, 0, False, True, 0.5, 0, 0), (400, 512, BF, "rms", False, 0, False, True, 1.0, 0, 0),
 ]
 
 
