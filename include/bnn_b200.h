@@ -510,7 +510,7 @@ BNN_API size_t bnn_mx_scale_bytes(int64_t rows, int64_t cols);
 BNN_API int bnn_mx_quantize(bnn_ctx *ctx, int dtype, const void *x, int64_t ldx, const bnn_mx_matrix *q, void *represented, int64_t ldv);
 /* The values q stands for, as dtype. */
 BNN_API int bnn_mx_values(bnn_ctx *ctx, const bnn_mx_matrix *q, int dtype, void *out, int64_t ldo);
-/* bnn_block_norm with the norm of the stream microscaled (M x D, from the unrounded row); pre must be 1.  represented: NULL, or M x D of the norm's type, the
+/* bnn_block_norm with the norm of the stream microscaled (M x D, from the row in float32 before its rounding); pre must be 1.  represented: NULL, or M x D of the norm's type, the
  * values that normed stands for.  bnn_block_norm_backward takes the same stats: the gradient goes straight through the rounding. */
 BNN_API int bnn_block_norm_mx(bnn_ctx *ctx, const bnn_block_norm_desc *norm, const void *x, int64_t ldx, const void *block, int64_t ldb, int64_t M,
                               void *stream, int64_t lds, const bnn_mx_matrix *normed, void *represented, int64_t ldv, float *stats);

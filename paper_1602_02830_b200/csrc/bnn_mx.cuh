@@ -135,45 +135,94 @@ template <typename T> __device__ __forceinline__ void mx_spread8(T *row, int64_t
     __syncwarp();
 }
 
-// Values that are float32 as they stand; or float32 roundings of others: rest(j, v) is then what v lacks.  A value whose rounding lies on the border of two
-// elements, or beside it, goes to the side on which the exact one lies.  (One in 2^20 values rounds to a border: 20 elements of an 8192 x 4096 norm were a step off.)
-struct MxExact { static constexpr bool rounded = false; __device__ float operator()(int, float) const { return 0.0f; } };
+// Values that are float32 as they stand; or float32 roundings of others: rest.held().lack(j, v) is then what v lacks.  Whether such a value is on this or that side of a border
+// (of two elements; of two shared exponents, where it is the block's largest) is decided by the exact one, which differs from v by MX_NEAR of it at most: whatever lies farther
+// from a border is on the same side as v.  What lies closer than rest.tie of it can't be told from the border and counts as on it.  (One in 2^20 values rounds to a border.)
+struct MxExact { static constexpr bool rounded = false; };
+constexpr float MX_NEAR = 1.0f / (1 << 22);
+
+// The element that a scaled value is converted to, as a value.
+template <bool FOUR> __device__ __forceinline__ float mx_element(float v) {
+    float e[8] = {v, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    uint32_t w[2];
+    mx_encode8<FOUR>(e, w);
+    mx_decode8<FOUR>(w, e);
+    return e[0];
+}
+
+// Eight values of a lane one of which may be beside a border: their elements, and their block's scale from its largest magnitude.  The block's four lanes come together where its
+// largest is beside a power of two.  Out of line and in a loop, arrays in memory: one in two thousand lanes gets here, and inlined it took registers from all of them.
+constexpr uint32_t MX_UNITS = 2;
+struct MxCodes { uint32_t w[2], scale; };
+__device__ __forceinline__ bool mx_beside_power(uint32_t top) { return ((top + MX_UNITS) ^ (top - MX_UNITS)) & 0xff800000u; }
+template <bool FOUR, typename H> __device__ __noinline__ MxCodes mx_decide(const float *v, uint32_t top, const H *rest) {
+    if (mx_beside_power(top) && top - 0x00800000u < 0x7e800000u) {
+        // The largest reaches the power of two if one of the block's exact values does.
+        const uint32_t power = (top + MX_UNITS) & 0x7f800000u;
+        const float border = __uint_as_float(power);
+        bool reached = false;
+#pragma unroll 1
+        for (int j = 0; j < 8; ++j) {
+            const float size = fabsf(v[j]);
+            if (__float_as_uint(size) + MX_UNITS >= power) reached |= (size - border) + copysignf(1.0f, v[j]) * rest->lack(j, v[j]) >= -rest->tie * border;
+        }
+        top = __any_sync(0xfu << (threadIdx.x & 28), reached) ? max(top, power) : power - 1;
+    }
+    const uint32_t scale = mx_scale<FOUR>(top);
+    const float down = mx_down(scale);
+    float e[8];
+#pragma unroll 1
+    for (int j = 0; j < 8; ++j) {
+        const float low = mx_element<FOUR>(v[j] * (down * (1.0f - MX_NEAR))), high = mx_element<FOUR>(v[j] * (down * (1.0f + MX_NEAR))), edge = 0.5f * (low + high);
+        e[j] = low;
+        if (low == high) continue;
+        const float d = copysignf(1.0f, v[j]) * ((v[j] * down - edge) + rest->lack(j, v[j]) * down);
+        e[j] = fabsf(d) <= rest->tie * fabsf(edge) ? edge : d > 0.0f ? high : low;           // (an edge is converted to the even one)
+    }
+    MxCodes out;
+    mx_encode8<FOUR>(e, out.w);
+    out.scale = scale;
+    return out;
+}
 
 // One row's columns c .. c + 7 (c a multiple of 8; zeros behind the last column) of every lane of a warp, lanes next to each other: four neighbouring lanes
 // hold a block, sixteen a group.  All lanes take part; those with c >= limit (the row's pitch in elements, a multiple of 128) write nothing.
 // On return v holds the values that the elements stand for, where they are asked back.
 template <bool FOUR, typename F> __device__ __forceinline__ void mx_write8(uint8_t *values, uint8_t *scales, int64_t row, int64_t c, int64_t limit, float (&v)[8], bool back, const F &rest) {
-    uint32_t top = 0;
+    const int lane = threadIdx.x & 31;
+    uint32_t top = F::rounded ? MX_UNITS : 0;                       // (a block of zeros is beside no power of two)
 #pragma unroll
     for (int j = 0; j < 8; j += 2) top = __vimax3_u32(top, mx_magnitude(v[j]), mx_magnitude(v[j + 1]));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const uint32_t scale = mx_scale<FOUR>(top);
-    const float down = mx_down(scale), up = mx_up(scale);
-#pragma unroll
-    for (int j = 0; j < 8; j += 2) pair_out(mul2(pair_of(v[j], v[j + 1]), both(down)), v[j], v[j + 1]);
+    uint32_t scale = mx_scale<FOUR>(top), w[2];
+    const float down = mx_down(scale);
     if constexpr (F::rounded) {
-        // The bits below an element's (20 of e4m3, 22 of e2m1), moved to the top: a border is the highest of them alone.  (Elements below the smallest normal
-        // one have their borders elsewhere; what is missed there is 2^-15 of the block's largest.)
-        constexpr uint32_t UNIT = FOUR ? 1u << 10 : 1u << 12;
-        uint32_t near = 0xffffffffu;
+        // Elements of the values moved by MX_NEAR towards zero and away from it are alike where no border is near, and so is the exponent of the largest one moved by MX_UNITS.
+        float in[8], away[8];
+        uint32_t w_away[2];
 #pragma unroll
-        for (int j = 0; j < 8; j += 2)
-            near = __vimin3_u32(near, __float_as_uint(v[j]) * UNIT + (0x80000000u + UNIT), __float_as_uint(v[j + 1]) * UNIT + (0x80000000u + UNIT));
-        if (__builtin_expect(near <= 2 * UNIT, 0)) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t bits = __float_as_uint(v[j]), at = bits * UNIT + (0x80000000u + UNIT);
-                if (at > 2 * UNIT) continue;
-                const uint32_t border = bits + 1 - at / UNIT;
-                const float edge = __uint_as_float(border), d = (v[j] - edge) + rest(j, v[j] * up) * down;
-                v[j] = d == 0.0f || !(fabsf(v[j]) > 0.0f) ? edge : __uint_as_float((d > 0.0f) == (v[j] > 0.0f) ? border + 1 : border - 1);
-            }
+        for (int j = 0; j < 8; j += 2) {
+            const unsigned long long t = pair_of(v[j], v[j + 1]);
+            pair_out(mul2(t, both(down * (1.0f - MX_NEAR))), in[j], in[j + 1]);
+            pair_out(mul2(t, both(down * (1.0f + MX_NEAR))), away[j], away[j + 1]);
         }
+        mx_encode8<FOUR>(in, w);
+        mx_encode8<FOUR>(away, w_away);
+        if (__builtin_expect((w[0] != w_away[0]) | (w[1] != w_away[1]) | mx_beside_power(top), 0)) {
+            const auto held = rest.held();
+            float mine[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) mine[j] = v[j];
+            const MxCodes codes = mx_decide<FOUR>(mine, top, &held);
+            w[0] = codes.w[0]; w[1] = codes.w[1]; scale = codes.scale;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) pair_out(mul2(pair_of(v[j], v[j + 1]), both(down)), v[j], v[j + 1]);
+        mx_encode8<FOUR>(v, w);
     }
-    uint32_t w[2];
-    mx_encode8<FOUR>(v, w);
-    const int lane = threadIdx.x & 31;
+    const float up = mx_up(scale);
     uint32_t four = scale << (8 * ((lane >> 2) & 3));           // the group's scales in the order of its blocks
     four |= __shfl_xor_sync(0xffffffffu, four, 4);
     four |= __shfl_xor_sync(0xffffffffu, four, 8);

@@ -660,7 +660,7 @@ template <bool MX> int block_norm(bnn_ctx *ctx, const bnn_block_norm_desc *norm,
     a.x = x; a.ldx = ldx; a.block = block; a.ldb = ldb; a.stream = stream; a.lds = lds; a.normed = normed; a.ldn = ldn; a.stats = stats;
     if (MX) {
         a.mx_values = static_cast<uint8_t *>(q->values); a.mx_scales = static_cast<uint8_t *>(q->scales);
-        a.inv_low = (float)(1.0 / (double)norm->D - (double)a.inv_d);
+        a.inv = 1.0 / (double)norm->D;
         a.mx_limit = (int)bnn_mx_groups(norm->D) * BNN_MX_GROUP; a.mx_four = q->format == BNN_MX_E2M1;
     }
     const bool vec = norm_vec(norm, M, a);

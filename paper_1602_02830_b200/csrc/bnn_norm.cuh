@@ -27,7 +27,7 @@ struct NormArgs {
     // microscaled output: elements, scales, pitch in elements; normed receives the represented values
     uint8_t *mx_values, *mx_scales;
     int mx_limit, mx_four;
-    float inv_low;                     // 1 / D is inv_d + inv_low
+    double inv;                        // 1 / D
 };
 
 // Eight columns of one row per thread and slot, as they are in memory.  VEC: neighbouring columns in 16-byte accesses; otherwise

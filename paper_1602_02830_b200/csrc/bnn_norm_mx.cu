@@ -1,10 +1,12 @@
 // Norms around a block with the stream's norm microscaled (bnn_mx.cuh); the mathematics is that of bnn_norm.cu.  Eight neighbouring columns a thread and slot
 // whatever the alignment, so that four lanes hold a block.
-// Elements have three or one bits behind the point: what decides an element is on which side of a border its value lies.  So the sums of the warps, the mean square
-// and the reciprocal root are kept in two float32 each (a value and what it lacks), and what a value's float32 rounding lacks is known where it lies beside a border.
-// Bound: HBM, and the issue slots beside it (41 instructions an element where everything is optional).  8192 x 4096 bf16: residual and norm 41.3 us = 5.7 TB/s, with represented
-// values 48.2 us = 6.3 TB/s (BARE; 48.4 and 53.6 with a predicate for every access and optional weights); with a block norm 55.7 us.  Elements off the 64-bit result: 3 of 33.5
-// million, 20 in float32 alone.
+// Elements have three or one bits behind the point: what decides an element is on which side of a border its value lies, and likewise the block's exponent.  So the row's squares are
+// added up in float64, the reciprocal root is kept as a float32 and what it lacks, and what a value's float32 rounding lacks is known where it lies beside a border.  In the RMS form
+// without shifts that decides every border by the row s in float32 (x + block of 16 bits: their exact sum, unless they are 2^16 apart).  A row with a block norm, a gate or alpha
+// beside 1 is rounded to float32 before, the layer form's row around its mean as well; a shift that cancels most of the value leaves more than the border's surroundings cover.
+// Bound: HBM, and the issue slots beside it.  8192 x 4096 bf16: residual and norm 44.0 us = 5.4 TB/s, with represented values 50.4 us = 6.0 TB/s (BARE); with a block norm 59.5 us; layer
+// norm 75, with block norm, shifts and represented values 98; 2560 columns, not whole teams, 39; float16 rows of 1011 34.  2048 x 16384: 47 us, float32 76.  With float32 sums
+// and without the look at both sides of a value: 41.4 and 48.3 us, and 9 of 33.5 million elements off the 64-bit result; none now (20 in float32 alone).
 #include "bnn_norm.cuh"
 #include "bnn_mx.cuh"
 
@@ -12,37 +14,27 @@ namespace {
 using namespace bnn_norm;
 
 struct Two { float high, low; };
-__device__ __forceinline__ Two two_sum(float a, float b) {       // a + b exactly (Knuth)
-    const float s = __fadd_rn(a, b), t = __fsub_rn(s, a);
-    return {s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t))};
-}
-__device__ __forceinline__ Two two_product(float a, float b) {
-    const float s = __fmul_rn(a, b);
-    return {s, fmaf(a, b, -s)};
-}
-// Mean over the row of the block's sum of `a`, with `add` (eps or 0); 1 / D is inv + inv_low.
-__device__ __forceinline__ Two block_mean(float a, float add, float inv, float inv_low, float *buf, int warps, int warp, int lane) {
-    a = warp_sum(a);
-    Two s{a, 0.0f};
+__device__ __forceinline__ Two two(double v) { const float high = (float)v; return {high, (float)(v - (double)high)}; }
+// Mean over the row of the block's sum of `a`, with `add` (eps or 0).
+__device__ __forceinline__ double block_mean(double a, double add, double inv, double *buf, int warps, int warp, int lane) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
     if (warps > 1) {
         if (lane == 0) buf[warp] = a;
         __syncthreads();
-        s = {buf[0], 0.0f};
-        for (int w = 1; w < warps; ++w) {
-            const Two t = two_sum(s.high, buf[w]);
-            s = {t.high, s.low + t.low};
-        }
+        a = buf[0];
+        for (int w = 1; w < warps; ++w) a += buf[w];
     }
-    const Two t = two_product(s.high, inv), u = two_sum(t.high, add);
-    return {u.high, u.low + (t.low + (s.high * inv_low + s.low * inv))};
+    return fma(a, inv, add);
 }
-__device__ __forceinline__ Two inverse_root(Two v) {
-    if (!(v.high > 1e-30f && v.high < 1e30f)) return {1.0f / sqrtf(v.high), 0.0f};
-    // r (1 + e / 2), e = 1 - v r^2
-    const float r = rsqrtf(v.high);
-    const Two s = two_product(r, r), t = two_product(v.high, s.high);
-    const float e = ((1.0f - t.high) - t.low) - v.high * s.low - v.low * s.high, low = 0.5f * r * e, high = __fadd_rn(r, low);
-    return {high, __fsub_rn(low, __fsub_rn(high, r))};
+// From float32's root by r (1 - e)^(-1/2), e = 1 - v r^2, to the second order: e is below 2^-21.
+__device__ __forceinline__ Two inverse_root(double v) {
+    const bool small = v < 1e-30, large = v > 1e30;
+    v *= small ? 0x1p96 : large ? 0x1p-96 : 1.0;
+    const float first = rsqrtf((float)v);
+    if (!(first > 0.0f && first < 1e30f)) return {first, 0.0f};        // zero, infinity, NaN
+    const double r = (double)first, e = fma(-(v * r), r, 1.0);
+    return two(fma(r * e, fma(0.375, e, 0.5), r) * (small ? 0x1p48 : large ? 0x1p-48 : 1.0));
 }
 // WHOLE: the team's slots are the row's columns exactly, nothing is asked.
 template <typename T, bool VEC, bool WHOLE = false> __device__ __forceinline__ Eight<T> take8(const T *row, int slot, int tid, int team, int D) {
@@ -67,28 +59,44 @@ template <typename T, bool VEC, bool WHOLE = false> __device__ __forceinline__ v
     else if constexpr (VEC) write8<T, true>(row, slot, tid, team, D, v);
     else mx_spread8(row, column<true>(slot, 0, tid & ~31, team), D, v, stage + (tid >> 5) * 256);
 }
-// What u = round(t r + c), t = round(s w), lacks: s w is t and its own rest, r two parts.
+// What u = round(t r + c), t = round(s w), lacks: s w is t and its own rest, r two parts.  The rest is good to 2^-44 of u with float64 sums of squares, of LAYER_TIE where the
+// row around its mean is a float32 rounding itself and its sums are float32.
+constexpr float RMS_TIE = 1.0f / (1ll << 44), LAYER_TIE = 1.0f / (1 << 23);
+struct NormHeld {
+    float s[8], w[8], c[8];
+    Two r;
+    float tie;
+    __device__ __forceinline__ float lack(int j, float u) const {
+        const float t = __fmul_rn(s[j], w[j]);
+        return fmaf(fmaf(s[j], w[j], -t), r.high, fmaf(t, r.low, fmaf(t, r.high, c[j] - u)));
+    }
+};
 struct NormRest {
     static constexpr bool rounded = true;
     const float (&s)[8];
     const float (&w)[8];
     const float (&c)[8];
     Two r;
-    __device__ __forceinline__ float operator()(int j, float u) const {
-        const float t = __fmul_rn(s[j], w[j]);
-        return fmaf(fmaf(s[j], w[j], -t), r.high, fmaf(t, r.low, fmaf(t, r.high, c[j] - u)));
+    float tie;
+    __device__ __forceinline__ NormHeld held() const {
+        NormHeld h;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { h.s[j] = s[j]; h.w[j] = w[j]; h.c[j] = c[j]; }
+        h.r = r; h.tie = tie;
+        return h;
     }
 };
 template <typename T, bool VEC> __device__ __forceinline__ void spread(const Eight<T> &e, float (&v)[8]) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = e[j];
 }
-// ANY; PLAIN: BNN_NORM_RMS without shifts, with a block and a stream; BARE: that without a norm of the block and a gate, with a weight, rows of whole teams.
-enum NormKind { ANY, PLAIN_ROWS, BARE };
+// LAYER, RMS: the two norms; PLAIN_ROWS: BNN_NORM_RMS without shifts, with a block and a stream; BARE: that without a norm of the block and a gate, with a weight, rows of whole
+// teams.  (The two norms in one kernel kept float32 and float64 sums beside each other: layer norm of 4096 x 4096 float32 68 us.)
+enum NormKind { LAYER, RMS, PLAIN_ROWS, BARE };
 template <typename T, int SLOTS, int THREADS, bool VEC, int KIND, bool FOUR>
 __global__ void __launch_bounds__(THREADS, THREADS <= 256 ? 3 : 1) k_block_norm_mx(const NormArgs p) {
-    constexpr bool PLAIN = KIND != ANY, WHOLE = KIND == BARE;
-    __shared__ float buf[4][32];
+    constexpr bool PLAIN = KIND == PLAIN_ROWS || KIND == BARE, WHOLE = KIND == BARE, layer = KIND == LAYER;
+    __shared__ double buf[4][32];
     __shared__ __align__(16) T stage[VEC ? 8 : THREADS * 8];
     bnn_pdl_wait();
     bnn_pdl_launch_next();
@@ -96,7 +104,7 @@ __global__ void __launch_bounds__(THREADS, THREADS <= 256 ? 3 : 1) k_block_norm_
     const int tid = threadIdx.x, team = blockDim.x, warps = team >> 5, warp = tid >> 5, lane = tid & 31;
     const T *pw = WHOLE ? nullptr : static_cast<const T *>(p.post_w), *pc = PLAIN ? nullptr : static_cast<const T *>(p.post_c);
     const T *nw = static_cast<const T *>(p.pre_w), *nc = PLAIN ? nullptr : static_cast<const T *>(p.pre_c);
-    const bool layer = !PLAIN && p.layer, blocks = PLAIN || p.block, post = !WHOLE && p.post;
+    const bool blocks = PLAIN || p.block, post = !WHOLE && p.post;
     Eight<T> rx[SLOTS], rb[SLOTS];
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
@@ -117,7 +125,7 @@ __global__ void __launch_bounds__(THREADS, THREADS <= 256 ? 3 : 1) k_block_norm_
                 for (int j = 0; j < 8; ++j) v += rb[i][j];
                 t += v;
             }
-            mean = block_mean(t, 0.0f, p.inv_d, p.inv_low, buf[0], warps, warp, lane).high;
+            mean = (float)block_mean(t, 0.0, p.inv, buf[0], warps, warp, lane);
         }
         float q = 0.0f;
 #pragma unroll
@@ -130,10 +138,11 @@ __global__ void __launch_bounds__(THREADS, THREADS <= 256 ? 3 : 1) k_block_norm_
             }
             q += v;
         }
-        r = inverse_root(block_mean(q, p.eps, p.inv_d, p.inv_low, buf[1], warps, warp, lane));
+        r = inverse_root(block_mean(q, p.eps, p.inv, buf[1], warps, warp, lane));
     }
     if (p.stats && tid == 0) { p.stats[4 * m] = mean; p.stats[4 * m + 1] = r.high; }
-    float s[SLOTS][8], q = 0.0f;
+    float s[SLOTS][8];
+    double q = 0.0;
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
         Eight<T> w, g, c;
@@ -141,22 +150,20 @@ __global__ void __launch_bounds__(THREADS, THREADS <= 256 ? 3 : 1) k_block_norm_
         if (blocks && pw) w = take8<T, VEC, WHOLE>(pw, i, tid, team, p.D);
         if (gate) g = take8<T, VEC, WHOLE>(gate, i, tid, team, p.D);
         if (blocks && pc) c = take8<T, VEC, WHOLE>(pc, i, tid, team, p.D);
-        float v = 0.0f;
+        double even = 0.0, odd = 0.0;                               // of the squares; a float32 sum of the values where a mean comes first
+        float sum = 0.0f;
         if constexpr (PLAIN) {
-            unsigned long long squares = both(0.0f);
 #pragma unroll
             for (int j = 0; j < 8; j += 2) {
                 unsigned long long add = pair_of(rb[i][j], rb[i][j + 1]);
                 if (!WHOLE) add = mul2(add, pair_of(w[j], w[j + 1]));
                 if (post) add = fma2(add, both(r.high), mul2(add, both(r.low)));
                 if (gate) add = mul2(add, pair_of(g[j], g[j + 1]));
-                const unsigned long long sum = fma2(both(p.alpha), pair_of(rx[i][j], rx[i][j + 1]), add);
-                squares = fma2(sum, sum, squares);
-                pair_out(sum, s[i][j], s[i][j + 1]);
+                const unsigned long long both_sums = fma2(both(p.alpha), pair_of(rx[i][j], rx[i][j + 1]), add);
+                pair_out(both_sums, s[i][j], s[i][j + 1]);
+                even = fma((double)s[i][j], (double)s[i][j], even);
+                odd = fma((double)s[i][j + 1], (double)s[i][j + 1], odd);
             }
-            float odd;
-            pair_out(squares, v, odd);
-            v += odd;
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -169,29 +176,31 @@ __global__ void __launch_bounds__(THREADS, THREADS <= 256 ? 3 : 1) k_block_norm_
                 }
                 s[i][j] = fmaf(p.alpha, rx[i][j], add);
                 if (layer && column<true>(i, j, tid, team) >= p.D) s[i][j] = 0.0f;      // the block's mean is taken off zeros there
-                v = layer ? v + s[i][j] : fmaf(s[i][j], s[i][j], v);
+                if (layer) sum += s[i][j];
+                else even = fma((double)s[i][j], (double)s[i][j], even);
             }
         }
-        q += v;
+        q += layer ? (double)sum : even + odd;
         if (PLAIN || p.stream) give8<T, VEC, WHOLE>(static_cast<T *>(p.stream) + m * p.lds, i, tid, team, p.D, s[i], stage);
     }
     // the stream's
     mean = 0.0f;
-    Two of = block_mean(q, layer ? 0.0f : p.eps, p.inv_d, p.inv_low, buf[2], warps, warp, lane);
+    double of = block_mean(q, layer ? 0.0 : (double)p.eps, p.inv, buf[2], warps, warp, lane);
     if (layer) {
-        mean = of.high;
-        q = 0.0f;
+        const Two m = two(of);
+        mean = m.high;
+        q = 0.0;
 #pragma unroll
         for (int i = 0; i < SLOTS; ++i) {
             float v = 0.0f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                s[i][j] = column<true>(i, j, tid, team) < p.D ? (s[i][j] - mean) - of.low : 0.0f;
+                s[i][j] = column<true>(i, j, tid, team) < p.D ? (s[i][j] - mean) - m.low : 0.0f;
                 v = fmaf(s[i][j], s[i][j], v);
             }
-            q += v;
+            q += (double)v;
         }
-        of = block_mean(q, p.eps, p.inv_d, p.inv_low, buf[3], warps, warp, lane);
+        of = block_mean(q, p.eps, p.inv, buf[3], warps, warp, lane);
     }
     r = inverse_root(of);
     if (p.stats && tid == 0) { p.stats[4 * m + 2] = mean; p.stats[4 * m + 3] = r.high; }
@@ -216,12 +225,13 @@ __global__ void __launch_bounds__(THREADS, THREADS <= 256 ? 3 : 1) k_block_norm_
             for (int j = 0; j < 8; ++j)
                 if (c0 + j >= p.D) u[j] = 0.0f;
         }
-        const NormRest rest{s[i], w, c, r};
+        const NormRest rest{s[i], w, c, r, layer ? LAYER_TIE : RMS_TIE};
         mx_write8<FOUR>(p.mx_values, p.mx_scales, m, c0, p.mx_limit, u, p.normed != nullptr, rest);
         if (p.normed) give8<T, VEC, WHOLE>(static_cast<T *>(p.normed) + m * p.ldn, i, tid, team, p.D, u, stage);
     }
 }
 
+template <int N> struct Int { static constexpr int value = N; };
 // Teams as in bnn_norm.cu.
 template <typename T, bool VEC, bool FOUR> int launch_forward_mx(bnn_ctx *ctx, const NormArgs &a) {
     const int groups = (a.D + 7) / 8;
@@ -230,15 +240,18 @@ template <typename T, bool VEC, bool FOUR> int launch_forward_mx(bnn_ctx *ctx, c
     const int team = ((groups + slots - 1) / slots + 31) & ~31;
     const dim3 grid((unsigned)a.M), block(team);
     const bool plain = VEC && !a.layer && !a.post_c && !a.pre_c && a.block && a.stream, bare = plain && !a.post && !a.gate && a.pre_w && a.D == slots * team * 8;
-#define BNN_FORWARD(SLOTS, THREADS) BNN_CUDA_TRY(ctx, bnn_launch_dependent(bare ? k_block_norm_mx<T, SLOTS, THREADS, VEC, VEC ? BARE : ANY, FOUR> : \
-                                                                           plain ? k_block_norm_mx<T, SLOTS, THREADS, VEC, VEC ? PLAIN_ROWS : ANY, FOUR> : \
-                                                                           k_block_norm_mx<T, SLOTS, THREADS, VEC, ANY, FOUR>, grid, block, 0, ctx->stream, a))
-    if (slots == 1) BNN_FORWARD(1, 1024);
-    else if (slots == 2) BNN_FORWARD(2, 256);
-    else if (team <= 256) BNN_FORWARD(4, 256);
-    else BNN_FORWARD(4, 1024);
-#undef BNN_FORWARD
-    return bnn_check_launch(ctx);
+#define BNN_KERNEL(KIND) k_block_norm_mx<T, SLOTS, THREADS, VEC, KIND, FOUR>
+    const auto run = [&](auto slots_of, auto threads_of) -> int {
+        constexpr int SLOTS = decltype(slots_of)::value, THREADS = decltype(threads_of)::value;
+        auto kernel = a.layer ? BNN_KERNEL(LAYER) : BNN_KERNEL(RMS);
+        if constexpr (VEC) kernel = bare ? BNN_KERNEL(BARE) : plain ? BNN_KERNEL(PLAIN_ROWS) : kernel;
+        BNN_CUDA_TRY(ctx, bnn_launch_dependent(kernel, grid, block, 0, ctx->stream, a));
+        return bnn_check_launch(ctx);
+    };
+#undef BNN_KERNEL
+    if (slots == 1) return run(Int<1>(), Int<1024>());
+    if (slots == 2) return run(Int<2>(), Int<256>());
+    return team <= 256 ? run(Int<4>(), Int<256>()) : run(Int<4>(), Int<1024>());
 }
 template <typename T> int launch(bnn_ctx *ctx, const NormArgs &a, bool vec) {
     if (a.mx_four) return vec ? launch_forward_mx<T, true, true>(ctx, a) : launch_forward_mx<T, false, true>(ctx, a);
