@@ -82,7 +82,8 @@ template <bool FOUR> __device__ __forceinline__ void mx_decode8(const uint32_t (
     uint32_t h[4];
     if constexpr (FOUR) {
         // The three bits of a magnitude are the lowest two exponent bits and the highest mantissa bit of a half 2^14 times smaller, subnormals included.
-        // (Taken apart by shifts: bytes packed by one instruction and taken apart by another came back with the upper two zero.)
+        // Taken apart by shifts: where one kernel both packs four bytes by mov.b32 {p, q, r, s} (mx_e2m1x8) and takes a word apart by its reverse, nvcc 12.9.86 makes one of the two and
+        // loses the upper bytes, also with an opaque step between them (a kernel of nothing else: 32 of 32 words).  Either of them alone is right.
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t b = w[0] >> (8 * i);
