@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import glob
 import os
+import re
 import shutil
 import subprocess
 
@@ -14,8 +15,10 @@ LIB = os.path.join(HERE, "libbnn_b200.so")
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17", "-shared",
     "-Xcompiler", "-fPIC", "-Xcompiler", "-ffp-contract=off", "-Xcompiler", "-fvisibility=hidden",
-    "--expt-relaxed-constexpr", "--threads", "0",
+    "--expt-relaxed-constexpr", "--threads", "0", "-Xptxas=-warn-spills",
 ]
+# Kernels that keep accumulators, scales and requests in flight in registers and are laid out for exactly those that a thread has: a build in which one of them spills is refused.
+UNSPILLED = ("k_mx_pair", "k_mx_few")
 
 
 def nvcc() -> str:
@@ -37,6 +40,12 @@ def is_stale() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def spilled(log: str) -> list[str]:
+    """Kernels of UNSPILLED that ptxas reports as spilling, each with what it reports."""
+    found = re.findall(r"spilled to local memory in function '(\S+)', (\d+) bytes spill stores, (\d+) bytes spill loads", log)
+    return [f"{name}: {stores} bytes stored, {loads} loaded" for name, stores, loads in found if any(k in name for k in UNSPILLED)]
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compile every .cu under csrc/ into libbnn_b200.so next to this file."""
     if not force and not is_stale():
@@ -48,6 +57,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("nvcc failed:\n" + r.stdout + r.stderr)
+    if spilled(r.stderr):
+        os.remove(tmp)
+        raise RuntimeError("registers are spilled in\n" + "\n".join(spilled(r.stderr)))
     os.replace(tmp, LIB)
     if verbose:
         print(r.stderr)

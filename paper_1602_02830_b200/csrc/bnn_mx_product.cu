@@ -179,8 +179,8 @@ __device__ __forceinline__ void read_added(uint32_t (&in)[8], const uint16_t *fi
     const int lane = threadIdx.x & 31;
     if (lane < rows) read_sector(first + lane * ld, in);
 }
-// (The functions that are not inlined take no arrays, which would have to be in memory, and none of these kernels may spill registers around them: with twelve
-// bytes spilled, a warp's first piece of the residual came from the columns of another.)
+// (The functions that are not inlined take no arrays, which would have to be in memory.  The kernels are laid out not to spill, and the build refuses them otherwise; builds
+// held to 64 and 72 registers, which spill 12 to 356 bytes around these calls, gave the same results.)
 __device__ __noinline__ void land16(const uint16_t *first, int64_t ld, int rows, int n, uint8_t *piece) {
     const int lane = threadIdx.x & 31, c = lane & 15;
     uint16_t v[16];                                              // two rows a pass, all on their way
