@@ -495,6 +495,7 @@ BNN_API int bnn_dropout(bnn_ctx *ctx, int dtype, const void *x, int64_t ldx, con
  *   values: rows of bnn_mx_ld(format, cols) bytes, base 32-byte aligned; element 2 i of an e2m1 row is the low half of byte i; zeros behind cols.
  *   scales: bnn_mx_scale_bytes(rows, cols) bytes, base 16-byte aligned, 512 for each 128 rows x 128 columns: row r, block b of such a tile at
  *   16 (r % 32) + 4 (r / 32) + b; tiles of the same rows next to each other.  Bytes of rows that do not exist are neither written nor looked at.
+ * A result in this form shares no memory with what the same call reads or writes beside it (refused).
  * Only the calls below write and read this form.  float32 statistics, sums and pre-activations as above. */
 enum { BNN_MX_E4M3 = 0, BNN_MX_E2M1 = 1 };
 typedef struct {

@@ -134,6 +134,7 @@ extern "C" int bnn_mx_quantize(bnn_ctx *ctx, int dtype, const void *x, int64_t l
     if (!size) return BNN_ERR_INVALID_ARG;
     if (int st = bnn_check_real(x, ldx, q->rows, q->cols, size)) return st;
     if (int st = bnn_check_real_opt(represented, ldv, q->rows, q->cols, size)) return st;
+    if (bnn_mx_touches(q, x, ldx, q->rows, q->cols, size) || bnn_mx_touches(q, represented, ldv, q->rows, q->cols, size)) return BNN_ERR_INVALID_ARG;
     MxArgs a{};
     a.x = x; a.ldx = ldx; a.out = represented; a.ldo = ldv;
     return run(ctx, dtype, a, q);
@@ -144,6 +145,7 @@ extern "C" int bnn_mx_values(bnn_ctx *ctx, const bnn_mx_matrix *q, int dtype, vo
     const int size = bnn_real_size(dtype);
     if (!size) return BNN_ERR_INVALID_ARG;
     if (int st = bnn_check_real(out, ldo, q->rows, q->cols, size)) return st;
+    if (bnn_mx_touches(q, out, ldo, q->rows, q->cols, size)) return BNN_ERR_INVALID_ARG;
     MxArgs a{};
     a.out = out; a.ldo = ldo;
     return run(ctx, dtype, a, q);

@@ -22,6 +22,24 @@ static inline int bnn_check_mx(const bnn_mx_matrix *q) {
     if (reinterpret_cast<uintptr_t>(q->values) % 32 || reinterpret_cast<uintptr_t>(q->scales) % 16) return BNN_ERR_ALIGNMENT;
     return BNN_OK;
 }
+// Whether a microscaled matrix shares memory with `bytes` bytes at p; with a row-major matrix; with another one.  Results are written while other parts of the inputs are still to be
+// read, so that a call whose result shares memory with an input is refused.
+static inline bool bnn_mx_touches(const bnn_mx_matrix *q, const void *p, uint64_t bytes) {
+    if (!p || !bytes || q->rows == 0 || q->cols == 0) return false;
+    const auto meet = [&](const void *a, uint64_t n) {
+        const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(p);
+        return x < y ? y - x < n : x - y < bytes;
+    };
+    return meet(q->values, (uint64_t)q->rows * (uint64_t)bnn_mx_pitch(q->format, q->cols)) || meet(q->scales, bnn_mx_scale_bytes(q->rows, q->cols));
+}
+static inline bool bnn_mx_touches(const bnn_mx_matrix *q, const void *p, int64_t ld, int64_t rows, int64_t cols, int size) {
+    return rows > 0 && cols > 0 && bnn_mx_touches(q, p, ((uint64_t)(rows - 1) * (uint64_t)(rows > 1 ? ld : 0) + (uint64_t)cols) * (uint64_t)size);
+}
+static inline bool bnn_mx_touches(const bnn_mx_matrix *q, const bnn_mx_matrix *other) {
+    if (other->rows == 0 || other->cols == 0) return false;
+    return bnn_mx_touches(q, other->values, (uint64_t)other->rows * (uint64_t)bnn_mx_pitch(other->format, other->cols)) ||
+           bnn_mx_touches(q, other->scales, bnn_mx_scale_bytes(other->rows, other->cols));
+}
 
 #ifdef __CUDACC__
 // Two float32 values in one instruction.

@@ -1034,11 +1034,12 @@ int check_operands(const bnn_mx_matrix *w, const bnn_mx_matrix *x) {
     if (w->cols != x->cols || (x->format == BNN_MX_E2M1 && w->format != BNN_MX_E2M1)) return BNN_ERR_INVALID_ARG;
     return BNN_OK;
 }
-int check_output(const bnn_mx_matrix *q, const void *y, const float *pre, int64_t rows, int64_t cols) {
+int check_output(const bnn_mx_matrix *q, const void *y, const float *pre, const bnn_mx_matrix *x, const bnn_mx_matrix *w, const bnn_mx_matrix *w2) {
     if (!q) return BNN_OK;
     if (y || pre) return BNN_ERR_INVALID_ARG;
     if (int st = bnn_check_mx(q)) return st;
-    return q->rows == rows && q->cols == cols ? BNN_OK : BNN_ERR_INVALID_ARG;
+    if (q->rows != x->rows || q->cols != w->rows) return BNN_ERR_INVALID_ARG;
+    return bnn_mx_touches(q, x) || bnn_mx_touches(q, w) || (w2 && bnn_mx_touches(q, w2)) ? BNN_ERR_INVALID_ARG : BNN_OK;
 }
 bool is_half(int dtype) { return dtype == BNN_F16 || dtype == BNN_BF16; }
 
@@ -1059,8 +1060,8 @@ extern "C" int bnn_mx_linear(bnn_ctx *ctx, const bnn_mx_linear_desc *layer, cons
     if (int st = check_operands(&layer->W, x)) return st;
     const int64_t M = x->rows, N = layer->W.rows;
     if (int st = bnn_check_real_opt(layer->bias, N, 1, N, 2)) return st;
-    if (int st = check_output(y_mx, y, pre, M, N)) return st;
-    if (y_mx && residual) return BNN_ERR_INVALID_ARG;
+    if (int st = check_output(y_mx, y, pre, x, &layer->W, nullptr)) return st;
+    if (y_mx && (residual || bnn_mx_touches(y_mx, layer->bias, 0, 1, N, 2))) return BNN_ERR_INVALID_ARG;
     if (!y_mx)
         if (int st = bnn_check_real(y, ldy, M, N, 2)) return st;
     if (int st = bnn_check_real_opt(residual, ldr, M, N, 2)) return st;
@@ -1080,7 +1081,7 @@ extern "C" int bnn_mx_gated(bnn_ctx *ctx, const bnn_mx_gated_desc *layer, const 
     if (int st = bnn_check_mx(x)) return st;
     if (int st = check_operands(&layer->Wg, x)) return st;
     const int64_t M = x->rows, N = layer->Wg.rows;
-    if (int st = check_output(h_mx, h, pre, M, N)) return st;
+    if (int st = check_output(h_mx, h, pre, x, &layer->Wg, &layer->Wu)) return st;
     if (!h_mx)
         if (int st = bnn_check_real(h, ldh, M, N, 2)) return st;
     if (int st = bnn_check_real_opt(pre, ldp, M > 0 && M < BNN_REAL_MAX / 2 ? 2 * M : M, N, 4)) return st;

@@ -651,6 +651,8 @@ template <bool MX> int block_norm(bnn_ctx *ctx, const bnn_block_norm_desc *norm,
     if (MX) {
         if (int st = bnn_check_mx(q)) return st;
         if (q->rows != M || q->cols != norm->D) return BNN_ERR_INVALID_ARG;
+        if (bnn_mx_touches(q, x, ldx, M, norm->D, size) || bnn_mx_touches(q, block, ldb, M, norm->D, size) || bnn_mx_touches(q, stream, lds, M, norm->D, size) ||
+            bnn_mx_touches(q, normed, ldn, M, norm->D, size)) return BNN_ERR_INVALID_ARG;
     }
     if (!ctx) return BNN_ERR_INVALID_ARG;
     if (M == 0) return BNN_OK;
