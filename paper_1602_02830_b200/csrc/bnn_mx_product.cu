@@ -89,12 +89,13 @@ __device__ __forceinline__ unsigned long long times_sigmoid(unsigned long long z
     pair_out(d, a, b);
     return mul2(z, pair_of(inverse_of(a), inverse_of(b)));
 }
-// gelu(z) = max(z, 0) - |z| Phi(-|z|), Phi as in normal_cdf (bnn_real.cuh).  Past |z| = 100 the second term is 0 and stays 0.
+// gelu(z) = max(z, 0) - |z| Phi(-|z|), Phi as in normal_cdf (bnn_real.cuh).  Above z = 100 the second term is 0 and stays 0; of minus infinity it is infinity times 0, a NaN as in
+// z Phi(z).
 __device__ __forceinline__ unsigned long long gelu2(unsigned long long z) {
     float a, b;
     pair_out(z, a, b);
     const float ra = a < 0.0f ? 0.0f : a, rb = b < 0.0f ? 0.0f : b;
-    const unsigned long long size = pair_of(fminf(fabsf(a), 100.0f), fminf(fabsf(b), 100.0f));
+    const unsigned long long size = pair_of(fabsf(fminf(a, 100.0f)), fabsf(fminf(b, 100.0f)));
     pair_out(mul2(mul2(z, z), both(-0.5f * LOG2E)), a, b);
     const unsigned long long e = pair_of(exp2_of(a), exp2_of(b));
     pair_out(fma2(size, both(0.26516503f), both(1.0f)), a, b);
@@ -467,7 +468,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1) k_m
                 const int c = column_of(i);
                 if (adds && p.vec_add == 3 && rows > 0 && q.N - tn0 - c >= CHUNK) read_added(in, add + c, p.ld_add, rows);
             };
-            // The residual is requested a piece ahead, the first one while the tile is being multiplied; with pre-activations to keep there are no registers for that.
+            // The residual is requested a piece ahead, the first one while the tile is being multiplied; not beside kept pre-activations (4096 x 2048 -> 4096, gelu: 55.0 us, ahead 58.6).
             constexpr bool AHEAD = OUT == OUT_PLAIN;
             if (AHEAD) ask(0);
             const auto hand_over = [&]() {
