@@ -136,7 +136,8 @@ BNN_API int bnn_set_conv_form(bnn_ctx *ctx, int form);
 BNN_API int bnn_set_wait_limit_ns(bnn_ctx *ctx, uint64_t ns);
 /* Test hook for the failure path above (host-side injection, nothing faults): while on = 1 the tensor-core kernels
  * launched through this context run in their single-SM form with a producer that requests no operands, so their
- * consumers' waits run into the limit.  Outputs of such calls are undefined.  on = 0 restores normal operation. */
+ * consumers' waits run into the limit.  Outputs of such calls are undefined.  on = 2: as 1, but where the products of few rows split their sums over a
+ * cluster, only its odd CTAs request nothing; no output of such a cluster is written.  on = 0 restores normal operation. */
 BNN_API int bnn_debug_drop_loads(bnn_ctx *ctx, int on);
 /* Test hook, host only (no context, no GPU): where stage number `stage` (0, 1, 2, ... in the order a CTA's producer fills
  * them) of a tensor-engine operand ring of `slots` slots lives.  The kernels guard every slot with TWO barrier pairs, used

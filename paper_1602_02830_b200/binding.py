@@ -345,7 +345,7 @@ class Context:
     def set_wait_limit_ns(self, ns: int):
         self._ck(lib().bnn_set_wait_limit_ns(self._h, ns), "bnn_set_wait_limit_ns")
 
-    def debug_drop_loads(self, on: bool):
+    def debug_drop_loads(self, on: "bool | int"):
         self._ck(lib().bnn_debug_drop_loads(self._h, int(on)), "bnn_debug_drop_loads")
 
     def measure_pipe_rates(self):

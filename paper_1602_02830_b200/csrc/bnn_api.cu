@@ -107,7 +107,7 @@ extern "C" int bnn_set_conv_form(bnn_ctx *ctx, int form) {
 }
 
 extern "C" int bnn_debug_drop_loads(bnn_ctx *ctx, int on) {
-    if (!ctx || (on != 0 && on != 1)) return BNN_ERR_INVALID_ARG;
+    if (!ctx || on < 0 || on > 2) return BNN_ERR_INVALID_ARG;
     ctx->drop_loads = on;
     return BNN_OK;
 }

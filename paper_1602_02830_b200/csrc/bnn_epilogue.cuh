@@ -31,11 +31,14 @@ struct Common {
     int act, f16;
     int vec_bias, vec_add, vec_pre;      // as vec_out; vec_pre 3 = 32-byte sectors
     unsigned long long wait_ns;
-    int drop_loads;                      // test hook: the producers request nothing, every consumer's wait runs out
+    int drop_loads;                      // test hook: the producers request nothing, every consumer's wait runs out (2: see loads_here)
 };
 // How long a kernel waits at its end for copies and MMAs that it has issued, whatever the limit of its other waits; and for copies that no
 // barrier of its own counts.
 constexpr unsigned long long DRAIN_NS = 1000000000ull, SETTLE_NS = 2000000ull;
+
+// Whether the producers of a CTA of a split sum request anything (the test hook: 2 = the odd CTAs of a cluster do not).
+__device__ __forceinline__ bool loads_here(int drop_loads, uint32_t split, uint32_t rank) { return drop_loads == 0 || (drop_loads == 2 && split > 1 && !(rank & 1)); }
 
 // Bounded wait on a phase parity; false once the limit has passed or another wait of the pair has given up (`look`: whether to ask).
 template <typename C> __device__ __forceinline__ bool wait(const C *ctl, unsigned long long limit, const uint64_t *barrier, uint32_t parity, bool look = true) {
@@ -339,6 +342,12 @@ __device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {
     uint32_t remote;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
     return remote;
+}
+// Between the two barriers of a split sum's cluster: a CTA that has given up tells the others, none of which then writes outputs that lack its share.
+template <typename C> __device__ __forceinline__ void tell_cluster(C *ctl, uint32_t split) {
+    const uint32_t code = *reinterpret_cast<volatile uint32_t *>(&ctl->failed);
+    if (code != 0u && threadIdx.x < split) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_cta(smem_u32(&ctl->failed), threadIdx.x)), "r"(code) : "memory");
+    __syncwarp();
 }
 // The sum of four neighbouring values over the ranks' parts, in the order of the ranks, `pitch` floats apart.
 __device__ __forceinline__ void sum_parts(const float *at, int split, int pitch, float (&v)[4]) {

@@ -692,7 +692,8 @@ template <int EPI, bool MX> __global__ void __launch_bounds__(FEW_THREADS, 2) k_
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = ctl->tmem_base;
-    if ((warp == 0 || warp == FEW_THREADS / 32 - 1) && !f.drop_loads) {
+    const bool loads = loads_here(f.drop_loads, split, rank);
+    if ((warp == 0 || warp == FEW_THREADS / 32 - 1) && loads) {
         // While the kernel before this one runs, the first weights are brought to L2.  (Only to L2, where its writes are seen: it may have made them.)
         const int mine = warp == 0 ? 0 : 1, groups = f.four ? 2 : 1;
         if (elected())
@@ -708,7 +709,7 @@ template <int EPI, bool MX> __global__ void __launch_bounds__(FEW_THREADS, 2) k_
     bnn_pdl_launch_next();
 
     if (warp == 0 || warp == FEW_THREADS / 32 - 1) {
-        if (!f.drop_loads) {
+        if (loads) {
             const int mine = warp == 0 ? 0 : 1, groups = f.four ? 2 : 1;
             int stage = mine % f.stages, lap = mine / f.stages;
             for (int kit = first + mine; kit < last; kit += 2) {
@@ -761,9 +762,11 @@ template <int EPI, bool MX> __global__ void __launch_bounds__(FEW_THREADS, 2) k_
         if (!done) few_fail(ctl, 23);
     }
     __syncwarp();
-    if (split > 1) cluster_sync_all();
-    else __syncthreads();
-    if (done && *reinterpret_cast<volatile uint32_t *>(&ctl->failed) == 0u) {
+    if (split > 1) {
+        cluster_sync_all();
+        tell_cluster(ctl, split);
+    } else __syncthreads();
+    if (__all_sync(0xffffffffu, done && *reinterpret_cast<volatile uint32_t *>(&ctl->failed) == 0u)) {       // the flag may come from another CTA now
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const int quad = warp & 3, row = 32 * quad + lane, owner = row / out;
 #pragma unroll

@@ -324,7 +324,7 @@ template <bool W_MN, bool T_MN, int EPI> __global__ void __launch_bounds__(FEW_T
     bnn_pdl_launch_next();
 
     if (warp == 0 || warp == FEW_THREADS / 32 - 1) {              // two producers take the K steps in turn, as in the pair kernel
-        if (lane == 0 && !p.drop_loads) {
+        if (lane == 0 && loads_here(p.drop_loads, split, rank)) {
             const int mine = warp == 0 ? 0 : 1;
             int stage = mine % f.stages, lap = mine / f.stages;
             for (int kit = first + mine; kit < last; kit += 2) {
@@ -392,9 +392,11 @@ template <bool W_MN, bool T_MN, int EPI> __global__ void __launch_bounds__(FEW_T
         if (!done) few_fail(ctl, 23);
     }
     __syncwarp();
-    if (split > 1) cluster_sync_all();
-    else __syncthreads();
-    if (done && *reinterpret_cast<volatile uint32_t *>(&ctl->failed) == 0u) {
+    if (split > 1) {
+        cluster_sync_all();
+        tell_cluster(ctl, split);
+    } else __syncthreads();
+    if (__all_sync(0xffffffffu, done && *reinterpret_cast<volatile uint32_t *>(&ctl->failed) == 0u)) {       // the flag may come from another CTA now
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const int quad = warp & 3, row = 32 * quad + lane, unit = GATED ? row & 63 : row, owner = unit / out;
         const int place = unit - owner * out + (GATED && row >= 64 ? out : 0);
