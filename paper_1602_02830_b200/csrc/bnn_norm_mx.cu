@@ -30,11 +30,11 @@ __device__ __forceinline__ double block_mean(double a, double add, double inv, d
 // From float32's root by r (1 - e)^(-1/2), e = 1 - v r^2, to the second order: e is below 2^-21.
 __device__ __forceinline__ Two inverse_root(double v) {
     const bool small = v < 1e-30, large = v > 1e30;
-    v *= small ? 0x1p96 : large ? 0x1p-96 : 1.0;
+    v *= small ? 0x1p192 : large ? 0x1p-160 : 1.0;                       // squares of any float32 are then in its range
     const float first = rsqrtf((float)v);
     if (!(first > 0.0f && first < 1e30f)) return {first, 0.0f};        // zero, infinity, NaN
     const double r = (double)first, e = fma(-(v * r), r, 1.0);
-    return two(fma(r * e, fma(0.375, e, 0.5), r) * (small ? 0x1p48 : large ? 0x1p-48 : 1.0));
+    return two(fma(r * e, fma(0.375, e, 0.5), r) * (small ? 0x1p96 : large ? 0x1p-80 : 1.0));
 }
 // WHOLE: the team's slots are the row's columns exactly, nothing is asked.
 template <typename T, bool VEC, bool WHOLE = false> __device__ __forceinline__ Eight<T> take8(const T *row, int slot, int tid, int team, int D) {

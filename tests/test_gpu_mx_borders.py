@@ -98,3 +98,29 @@ def test_values_on_a_border(ctx, fmt, D):
         got = mx.read(ctx.block_norm_mx(layer, x, format=fmt)[1])[0]
         want = mx.quantize(torch.sign(x.double()) * w.double(), fmt).cpu()
         assert torch.equal(got, want), (c, int((got != want).sum()))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("size", (1e-25, 1e-18, 1e-10, 1.0, 1e10, 1e18, 1e30, 1e35))
+def test_rows_of_any_size(ctx, fmt, size):
+    """float32 rows whose squares float32 does not hold: every element is that of the 64-bit result (one in 2^35 values is closer to a border than the kernel can tell)."""
+    g = torch.Generator(device="cuda").manual_seed(int(abs(torch.tensor(size).log10())) + 1)
+    x, w = torch.randn(40, 1032, device="cuda", generator=g) * size, 1 + torch.randn(1032, device="cuda", generator=g) / 5
+    for eps in (0.0, 2.0 ** -20):
+        layer = ctx.make_block_norm(1032, torch.float32, eps=eps, pre_weight=w)
+        v = x.double() / (x.double().pow(2).mean(1, keepdim=True) + eps).sqrt() * w.double()
+        assert torch.equal(mx.read(ctx.block_norm_mx(layer, x, format=fmt)[1])[0], mx.quantize(v, fmt).cpu()), eps
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("D", (64, 1000, 4096))
+def test_rows_that_are_not_finite_or_zero(ctx, fmt, D):
+    x = torch.randn(5, D, device="cuda")
+    x[0, 5], x[1, 40], x[2], x[3, D - 1] = float("inf"), float("nan"), 0.0, -float("inf")
+    w = torch.ones(D, device="cuda")
+    q = ctx.block_norm_mx(ctx.make_block_norm(D, torch.float32, eps=1e-6, pre_weight=w), x, format=fmt)[1]
+    v = x.double() / (x.double().pow(2).mean(1, keepdim=True) + float(torch.tensor(1e-6))).sqrt()
+    want = mx.quantize(v, fmt).cpu()
+    got = mx.read(q)[0]
+    assert torch.equal(got.isnan(), want.isnan()) and torch.equal(torch.nan_to_num(got, 0.0), torch.nan_to_num(want, 0.0))
+    assert got[0].isnan().sum() == 32 and got[1].isnan().all() and (got[2] == 0).all()
