@@ -4,9 +4,9 @@
 // added up in float64, the reciprocal root is kept as a float32 and what it lacks, and what a value's float32 rounding lacks is known where it lies beside a border.  In the RMS form
 // without shifts that decides every border by the row s in float32 (x + block of 16 bits: their exact sum, unless they are 2^16 apart).  A row with a block norm, a gate or alpha
 // beside 1 is rounded to float32 before, the layer form's row around its mean as well; a shift that cancels most of the value leaves more than the border's surroundings cover.
-// Bound: HBM, and the issue slots beside it.  8192 x 4096 bf16: residual and norm 44.0 us = 5.4 TB/s, with represented values 50.4 us = 6.0 TB/s (BARE); with a block norm 59.5 us; layer
-// norm 75, with block norm, shifts and represented values 98; 2560 columns, not whole teams, 39; float16 rows of 1011 34.  2048 x 16384: 47 us, float32 76.  With float32 sums
-// and without the look at both sides of a value: 41.4 and 48.3 us, and 9 of 33.5 million elements off the 64-bit result; none now (20 in float32 alone).
+// Bound: HBM, and the issue slots beside it.  8192 x 4096 bf16: residual and norm 41.7 us = 5.7 TB/s, with represented values 48.9 us = 6.2 TB/s (BARE); with a block norm 57.0 us; layer
+// norm 75, with block norm, shifts and represented values 98; 2560 columns, not whole teams, 37.6; float16 rows of 1011 31.5; float32 4096 x 4096 37.7, layer norm 50.  2048 x 16384: 47 us,
+// float32 75.  Elements off the 64-bit result: none of 33.5 million; 20 in float32 alone, 9 with float32 sums in a thread and the borders of normal elements only.
 #include "bnn_norm.cuh"
 #include "bnn_mx.cuh"
 
@@ -94,7 +94,8 @@ template <typename T, bool VEC> __device__ __forceinline__ void spread(const Eig
 // teams.  (The two norms in one kernel kept float32 and float64 sums beside each other: layer norm of 4096 x 4096 float32 68 us.)
 enum NormKind { LAYER, RMS, PLAIN_ROWS, BARE };
 template <typename T, int SLOTS, int THREADS, bool VEC, int KIND, bool FOUR>
-__global__ void __launch_bounds__(THREADS, THREADS <= 256 ? 3 : 1) k_block_norm_mx(const NormArgs p) {
+// (Four CTAs of 256 an SM, 64 registers: 44.0 -> 41.7 us; float32 rows and the layer norm lose by it, 37.7 -> 39.3 and 75.2 -> 76.9.)
+__global__ void __launch_bounds__(THREADS, THREADS > 256 ? 1 : sizeof(T) == 2 && KIND != LAYER ? 4 : 3) k_block_norm_mx(const NormArgs p) {
     constexpr bool PLAIN = KIND == PLAIN_ROWS || KIND == BARE, WHOLE = KIND == BARE, layer = KIND == LAYER;
     __shared__ double buf[4][32];
     __shared__ __align__(16) T stage[VEC ? 8 : THREADS * 8];
