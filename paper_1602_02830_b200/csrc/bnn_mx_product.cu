@@ -6,8 +6,8 @@
 // beside e4m3 when its nibbles lie in the low eight bytes of every sixteen, which the tensor map does on the way (16U4_ALIGN16B).
 // One stage is a row of 128 bytes of shared memory: 256 of K packed, 128 otherwise.
 //
-// Bound: many rows, the tensor pipe and the part's power limit (8192 x 8192 x 8192 of random values: 182 us = 6.0 PFLOP/s in 4 bits, 363 us = 3.0 PFLOP/s in 8 bits, the same
-// with 4-bit weights 340 to 430 by box; 8192 x 4096 -> 8192 in 4 bits 101 us, with a residual 116; gated, 4096 rows, 4096 -> 8192 twice, microscaled result 176 us = 3.1 PFLOP/s).  Short
+// Bound: many rows, the tensor pipe and the part's power limit (8192 x 8192 x 8192 of random values: 182 us = 6.0 PFLOP/s in 4 bits, 363 us = 3.0 PFLOP/s in 8 bits, 352 with 4-bit
+// weights, in bursts; 216, 435 and 404 after seconds on end at the power limit, 1250 to 1360 MHz; 8192 x 4096 -> 8192 in 4 bits 101 us, with a residual 116; gated, 4096 rows, 4096 -> 8192 twice, microscaled result 176 us = 3.1 PFLOP/s).  Short
 // sums: the epilogue (4096 x 128 -> 4096 13.5 to 19 us, gelu 27 to 42).  Fewer rows: mostly the operands' way from L2 (at pair_cost; 512 x 4096 -> 4096 13.8 us, in 4 bits
 // 9.4); a token, 4096 -> 4096 with 4-bit weights, 7.1 us, of which 3.5 are launch, set-up and tail.
 // Nothing is rounded between the sums and the one conversion of a result: to 16 bits, or to an element of a microscaled result.
