@@ -370,7 +370,7 @@ template <int EPI, int OUT, int BN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1) k_mx_pair(const __grid_constant__ PairArgs p) {
     constexpr bool GATED = EPI == BNN_EPI_GATED;
     constexpr int WIDTH = GATED ? BN / 2 : BN, PARTS = EPI_WARPS / 4;
-    static_assert(BN == 256 || (BN == 128 && !GATED), "gate and up rows of a tile are whole tiles of scales");
+    static_assert(BN == 256 || (BN == 128 && !GATED), "gate and up rows of a tile begin with a tile of scales each");
     extern __shared__ uint8_t smem_raw[];
     uint8_t *tiles = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     Control *ctl = reinterpret_cast<Control *>(tiles + STAGES * STAGE);
